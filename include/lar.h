@@ -514,6 +514,106 @@ enum { LAR_LPS_POISSON = 0, LAR_LPS_VARIABILITY = 1 };
 lar_status lar_estimate_lps(lar_ctx *ctx, const lar_lps_params *params, int32_t mode,
                             int32_t n_q, const int32_t *q_prefill, double *ttft_ms);
 
+/*
+ * Paged key/value cache and the attention of a token batch over it: the work that the
+ * terms c*D, d*C and e*A of the batch-time model stand for (KV-cache reads of the
+ * decoding sequences, attention of the prefill chunks; Sec. 4.1), so that a user can run
+ * it, and measure these coefficients, on the GPU that serves.
+ *
+ * A token batch is what the scheduler composes (lar_set_scheduler): per sequence one new
+ * token (decode) or a chunk of new tokens (prefill).  One handle plans a batch once
+ * (lar_kv_plan, lengths on the host); every layer of a model then calls lar_kv_append with
+ * its new K and V rows and lar_kv_attend with its queries, on that layer's own pages.
+ *
+ * Positions.  Sequence s has q_len[s] new tokens and ctx_len[s] tokens in the cache once
+ * they are appended; new token r is at position p = ctx_len[s] - q_len[s] + r.  A token
+ * with p < 0 (an empty slot of a batch of fixed size has ctx_len 0) is a padding row:
+ * nothing is written for it, it reads back as zeros, it attends to nothing (output 0,
+ * lse -infinity).  Tokens of the batch are numbered in sequence order: T in all.
+ *
+ * Pages.  k and v are dev [n_blocks][n_kv_heads][block_size][head_dim], the caller's, in
+ * cache_dtype.  Position p of sequence s is row p % block_size of the page
+ * table[s][p / block_size]; table is dev [n_seqs][table_cols] int32, its entries past a
+ * context are not read.  Sequences may share pages that no token of the batch is appended
+ * to.  A page outside 0 .. n_blocks-1 sets the sticky LAR_E_STATE (lar_kv_sync): nothing
+ * is written there, and what was to be read from it is undefined.
+ *
+ * LAR_KV_E4M3 holds a row of head_dim values x as e4m3 codes of x * 2^-k and one byte
+ * k + 127 in k_exp / v_exp, dev [n_blocks][n_kv_heads][block_size]: k is the least integer
+ * in [-100, 120] with max |x| <= 448 * 2^k over the finite x; codes are rounded to nearest
+ * even, infinities and NaN become NaN, and |x| is first held to 61440 (F16) or
+ * 1.875 * 2^127 (BF16) so that every code * 2^k is exact in dtype.
+ *
+ * Attention.  out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m), s_j = scale * q . k_j,
+ * over the keys j <= p, under a window W also j > p - W or j < sinks (the first tokens,
+ * which stay visible); query head h reads kv head h / (n_q_heads / n_kv_heads).  Scores,
+ * maxima and sums are held in 32 bits; the exponentials are rounded to dtype for the
+ * product with v.  Keys that a row does not see have no part in it, whatever they hold.
+ * lse = m + ln(sum_j exp(s_j - m)) joins parts of a context.
+ */
+typedef struct lar_kv lar_kv;
+
+enum { LAR_KV_F16 = 0, LAR_KV_BF16 = 1, LAR_KV_E4M3 = 2 };
+
+typedef struct {
+  int32_t n_q_heads;      /* a multiple of n_kv_heads, at most 64 per kv head           */
+  int32_t n_kv_heads;     /* 1 .. 1024                                                  */
+  int32_t head_dim;       /* 64 or 128                                                  */
+  int32_t dtype;          /* of q, k, v and out: LAR_KV_F16 or LAR_KV_BF16              */
+  int32_t cache_dtype;    /* of the pages: dtype or LAR_KV_E4M3                         */
+  int32_t block_size;     /* tokens of a page, a power of two, 1 .. 65536               */
+  int32_t max_seqs;       /* sequences of a batch at most, 1 .. 2^20                    */
+  int32_t max_tokens;     /* new tokens of a batch at most, 1 .. 2^26                   */
+  int32_t reserved;       /* must be 0                                                  */
+  void *stream;           /* hipStream_t to enqueue on; NULL = null stream              */
+} lar_kv_config;
+
+typedef struct {
+  void *k, *v;            /* dev, aligned to 16 bytes                                   */
+  uint8_t *k_exp, *v_exp; /* dev, LAR_KV_E4M3 only                                      */
+  int64_t n_blocks;       /* n_blocks * n_kv_heads * block_size < 2^32                  */
+} lar_kv_pages;
+
+/* Rows [token][head][head_dim]: strides in elements, head_dim contiguous, every row
+ * aligned to 16 bytes (a slice of a fused projection will do). */
+typedef struct {
+  void *data;
+  int64_t tok_stride, head_stride;
+} lar_kv_rows;
+
+/*
+ * lar_kv_create: a handle with its working memory (about 4 KiB * CUs * head_dim for
+ *   split attention, and the plan).  *out is NULL on failure.
+ * lar_kv_plan: the token batch of the calls that follow; q_len, ctx_len host [n_seqs],
+ *   copied.  window 0: none (sinks then have no effect).  Enqueues the plan's copy from
+ *   pinned memory; waits only if the copy before the previous one is still under way.
+ *   Clears a sticky error that was reported.  Not under stream capture; a captured call
+ *   belongs to the plan it was captured with.
+ * lar_kv_append: k, v rows [T][n_kv_heads][head_dim] into the pages.
+ * lar_kv_read: the rows of the batch's tokens from the pages into k, v.  A plan with
+ *   q_len == ctx_len reads whole contexts (swap-out of a preempted sequence).
+ * lar_kv_attend: q rows [T][n_q_heads][head_dim]; out dev [T][n_q_heads][head_dim]
+ *   contiguous; lse dev [T][n_q_heads] float32 or NULL; scale > 0.  The batch's own K and V
+ *   must have been appended.
+ * lar_kv_sync: synchronise the stream; the sticky device error, if any.
+ * Each call works on the handle's stream, allocates nothing (but create) and does not
+ * wait (but plan, as said, and sync).  A handle is not thread-safe; calls of one handle
+ * share its working memory, so they are ordered by its stream.
+ */
+lar_status lar_kv_create(lar_kv **out, const lar_kv_config *cfg);
+lar_status lar_kv_destroy(lar_kv *kv);
+const char *lar_kv_error_string(const lar_kv *kv);
+lar_status lar_kv_plan(lar_kv *kv, int32_t n_seqs, const int32_t *q_len, const int32_t *ctx_len,
+                       int32_t window, int32_t sinks);
+lar_status lar_kv_append(lar_kv *kv, const lar_kv_pages *pages, const lar_kv_rows *k,
+                         const lar_kv_rows *v, const int32_t *table, int32_t table_cols);
+lar_status lar_kv_read(lar_kv *kv, const lar_kv_pages *pages, const int32_t *table,
+                       int32_t table_cols, const lar_kv_rows *k, const lar_kv_rows *v);
+lar_status lar_kv_attend(lar_kv *kv, const lar_kv_pages *pages, const lar_kv_rows *q,
+                         const int32_t *table, int32_t table_cols, double scale, void *out,
+                         float *lse);
+lar_status lar_kv_sync(lar_kv *kv);
+
 /* Synchronise the stream; return the sticky device error, if any. */
 lar_status lar_sync(lar_ctx *ctx);
 

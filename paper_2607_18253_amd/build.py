@@ -1,8 +1,8 @@
 """Build the HIP library ``liblar.so`` in-tree for gfx950 with hipcc.
 
-Every floating-point operation in the kernels is a separate binary64
-round-to-nearest-even operation: -ffp-contract=off (no fused multiply-add), no
-fast-math.  Packed FP32 instructions are disabled for all device code.
+Every floating-point operation in the simulation's kernels is a separate binary64
+round-to-nearest-even operation: -ffp-contract=off (no fused multiply-add; the
+attention kernels write theirs out), no fast-math.  Packed FP32 instructions are disabled for all device code.
 """
 
 from __future__ import annotations
@@ -18,9 +18,11 @@ LIB = os.path.join(HERE, "liblar.so")
 SOURCES = [os.path.join(CSRC, "sfs_kernels.hip"), os.path.join(CSRC, "sfs_limits.hip"),
            os.path.join(CSRC, "sfs_lps.hip"),
            os.path.join(CSRC, "lar_api.cpp"), os.path.join(CSRC, "lar_noalloc.hip"),
-           os.path.join(CSRC, "lar_board.cpp")]
+           os.path.join(CSRC, "lar_board.cpp"), os.path.join(CSRC, "kv_pages.hip"),
+           os.path.join(CSRC, "kv_attend.hip"), os.path.join(CSRC, "kv_api.cpp")]
 HEADERS = [os.path.join(CSRC, "sfs_device.h"), os.path.join(CSRC, "sfs_launch.h"),
            os.path.join(CSRC, "sfs_limits.h"), os.path.join(CSRC, "sfs_route.h"), os.path.join(CSRC, "sfs_walk.h"),
+           os.path.join(CSRC, "kv_device.h"),
            os.path.join(ROOT, "include", "lar.h")]
 ARCH = "gfx950"
 

@@ -1,0 +1,463 @@
+// kv_api.cpp -- host side of the paged key/value cache (lar_kv_* in include/lar.h).
+//
+// A handle keeps the geometry, the plan of the current token batch and the working memory
+// of the attention; the pages belong to the caller.  lar_kv_plan checks the lengths, cuts
+// the attention into stretches of equal work and copies the plan to the device from one of
+// two pinned buffers; the other calls enqueue kernels, allocate nothing and do not wait.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+#include <cstring>
+#include <new>
+#include <string>
+#include <vector>
+
+#include "../../include/lar.h"
+#include "kv_device.h"
+
+using namespace lar;
+
+namespace {
+
+constexpr int kStages = 2;       // pinned copies of a plan: one may be on its way while the next is written
+constexpr int kNarrowPerCu = 8;  // waves of the narrow kernel that a CU holds
+constexpr int kWidePerCu = 1;    // workgroups of the wide kernel that a CU holds
+// Least key tiles of a wave or workgroup: fewer would cost more to join than they save.
+constexpr int kNarrowLeast = 2, kWideLeast = 4;
+
+size_t up(size_t x) { return (x + 255) & ~size_t(255); }
+
+// Byte offsets of a plan's arrays, the same on the host and on the device.
+struct Layout {
+  size_t tok = 0, narrow = 0, wide = 0, narrow_at = 0, wide_at = 0, join = 0, end = 0;
+  Layout() = default;
+  Layout(int64_t n_tok, int64_t n_narrow, int64_t n_wide, int64_t waves, int64_t groups, int64_t n_join) {
+    narrow = up(tok + sizeof(KvTok) * n_tok);
+    wide = up(narrow + sizeof(KvSeg) * n_narrow);
+    narrow_at = up(wide + sizeof(KvSeg) * n_wide);
+    wide_at = up(narrow_at + sizeof(int32_t) * (waves + 1));
+    join = up(wide_at + sizeof(int32_t) * (groups + 1));
+    end = up(join + sizeof(KvJoin) * n_join);
+  }
+};
+
+}  // namespace
+
+struct lar_kv {
+  lar_kv_config cfg{};
+  KvGeom g{};
+  hipStream_t stream = nullptr;
+  int cus = 0;
+  int waves = 0, groups = 0;  // of the narrow and the wide kernel at most
+  size_t cap = 0;             // bytes of a plan at most
+  Layout lay;                 // of the current plan
+  char* dev = nullptr;
+  char* pinned[kStages] = {};
+  hipEvent_t done[kStages] = {};
+  bool used[kStages] = {};
+  int stage = 0;
+  float *narrow_o = nullptr, *wide_o = nullptr;
+  float2 *narrow_ml = nullptr, *wide_ml = nullptr;
+  int32_t* err = nullptr;
+  // the plan
+  bool planned = false;
+  int32_t n_seq = 0, n_tok = 0, max_pages = 0, window = 0, sinks = 0;
+  int32_t n_narrow = 0, n_wide = 0, n_join = 0;
+  lar_status sticky = LAR_OK;
+  std::string msg;
+};
+
+namespace {
+
+lar_status fail(lar_kv* kv, lar_status code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  try {
+    kv->msg = buf;
+  } catch (...) {
+  }
+  return code;
+}
+
+#define KV_TRY(kv, expr)                                                           \
+  do {                                                                             \
+    hipError_t e_ = (expr);                                                        \
+    if (e_ != hipSuccess) return fail(kv, LAR_E_HIP, "%s: %s", #expr, hipGetErrorString(e_)); \
+  } while (0)
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// The key tiles (of K keys) that the tokens p0 .. p0 + n - 1 of a sequence see: tiles
+// [0, ns), then from fw on; their number.
+int key_tiles(int64_t p0, int n, int K, int window, int sinks, int* ns, int* fw) {
+  const int64_t last = p0 + n - 1;
+  *ns = *fw = 0;
+  if (last < 0) return 0;
+  const int64_t all = last / K + 1;
+  const int64_t lo = window ? std::max<int64_t>(0, std::max<int64_t>(p0, 0) - window + 1) : 0;
+  const int64_t first = lo / K;
+  const int64_t head = std::min<int64_t>(ceil_div(sinks, K), first);  // tiles of sinks before the window
+  *ns = (int)head;
+  *fw = (int)first;
+  return (int)(head + all - first);
+}
+
+// Query tiles of one kernel, in the order in which they are cut into stretches.
+struct Tile {
+  KvSeg s;
+  int tiles;
+};
+
+// Cuts the tiles' key tiles into stretches of equal number, one run of them for each of at
+// most `most` waves (or workgroups); a tile that is cut goes to the join.
+void cut(const std::vector<Tile>& tiles, int most, int least, bool wide, KvSeg* segs, int32_t* at, int32_t* n_run,
+         KvJoin* join, int32_t* n_join) {
+  int64_t total = 0;  // a tile without keys still has its result to write
+  for (const Tile& t : tiles) total += std::max(1, t.tiles);
+  int64_t runs = std::max<int64_t>(1, std::min<int64_t>(most, total / least));
+  *n_run = 0;
+  if (tiles.empty()) return;
+  int32_t n_seg = 0, slot = 0;
+  int64_t before = 0;  // key tiles before the current tile
+  int64_t run = 0;     // run w has key tiles [total * w / runs, total * (w + 1) / runs)
+  at[0] = 0;
+  for (const Tile& t : tiles) {
+    const int64_t n = std::max(1, t.tiles);
+    int64_t x = 0;
+    const int32_t slot0 = slot;
+    int parts = 0;
+    while (x < n) {
+      int64_t end = total * (run + 1) / runs;
+      while (end <= before + x) {
+        at[++run] = n_seg;
+        end = total * (run + 1) / runs;
+      }
+      const int64_t y = std::min(n, end - before);
+      KvSeg s = t.s;
+      s.t0 = (int32_t)x;
+      s.t1 = (int32_t)(t.tiles ? y : 0);
+      s.slot = x == 0 && y == n ? -1 : slot++;
+      segs[n_seg++] = s;
+      ++parts;
+      x = y;
+    }
+    if (parts > 1) {
+      KvJoin j{};
+      j.q0 = t.s.q0;
+      j.ntok = t.s.ntok;
+      j.p0 = t.s.p0;
+      j.head = t.s.head;
+      j.slot = slot0;
+      j.n = parts;
+      j.wide = wide;
+      join[(*n_join)++] = j;
+    }
+    before += n;
+  }
+  while (run < runs) at[++run] = n_seg;
+  *n_run = (int32_t)runs;
+}
+
+bool type16(int32_t t) { return t == LAR_KV_F16 || t == LAR_KV_BF16; }
+
+lar_status ready(lar_kv* kv) {
+  if (!kv) return LAR_E_ARG;
+  if (kv->sticky != LAR_OK) return kv->sticky;
+  if (!kv->planned) return fail(kv, LAR_E_STATE, "no token batch planned (call lar_kv_plan)");
+  return LAR_OK;
+}
+
+// The arguments that append, read and attend share.
+lar_status check(lar_kv* kv, const lar_kv_pages* pages, const int32_t* table, int32_t cols, KvPool* pool) {
+  if (lar_status st = ready(kv)) return st;
+  if (!pages || !pages->k || !pages->v) return fail(kv, LAR_E_ARG, "null pages");
+  if (!table) return fail(kv, LAR_E_ARG, "null block table");
+  if (kv->g.cache == kKvE4m3 && (!pages->k_exp || !pages->v_exp))
+    return fail(kv, LAR_E_ARG, "an e4m3 cache needs k_exp and v_exp");
+  if (((uintptr_t)pages->k | (uintptr_t)pages->v) & 15)
+    return fail(kv, LAR_E_ARG, "pages must be aligned to 16 bytes");
+  if (pages->n_blocks < 1 ||
+      pages->n_blocks > ((((int64_t)1 << 32) - 1) >> kv->g.sh) / kv->g.hkv)
+    return fail(kv, LAR_E_ARG, "n_blocks must be in 1 .. (2^32 - 1) / (block_size * n_kv_heads)");
+  if (cols < kv->max_pages)
+    return fail(kv, LAR_E_ARG, "block table has %d columns, the planned contexts need %d", cols, kv->max_pages);
+  *pool = KvPool{pages->k, pages->v, pages->k_exp, pages->v_exp, (uint32_t)pages->n_blocks};
+  return LAR_OK;
+}
+
+// Rows [T][heads][head_dim] with 16-byte rows.
+lar_status check_rows(lar_kv* kv, const lar_kv_rows* r, const char* name, KvRows* out) {
+  if (!r || !r->data) return fail(kv, LAR_E_ARG, "null %s", name);
+  if (((uintptr_t)r->data & 15) || (r->tok_stride & 7) || (r->head_stride & 7))
+    return fail(kv, LAR_E_ARG, "%s: every row must be aligned to 16 bytes", name);
+  *out = KvRows{r->data, r->tok_stride, r->head_stride};
+  return LAR_OK;
+}
+
+KvCopyArgs copy_args(const lar_kv* kv, const KvPool& pool, const int32_t* table, int32_t cols) {
+  KvCopyArgs a{};
+  a.g = kv->g;
+  a.pool = pool;
+  a.table = table;
+  a.cols = cols;
+  a.n_tok = kv->n_tok;
+  a.tok = (const KvTok*)(kv->dev + kv->lay.tok);
+  a.err = kv->err;
+  return a;
+}
+
+lar_status launched(lar_kv* kv, hipError_t e) {
+  return e == hipSuccess ? LAR_OK : fail(kv, LAR_E_HIP, "launch: %s", hipGetErrorString(e));
+}
+
+void release(lar_kv* kv) {
+  for (void* p : {(void*)kv->dev, (void*)kv->narrow_o, (void*)kv->wide_o, (void*)kv->narrow_ml,
+                  (void*)kv->wide_ml, (void*)kv->err})
+    if (p) (void)hipFree(p);
+  for (int i = 0; i < kStages; ++i) {
+    if (kv->pinned[i]) (void)hipHostFree(kv->pinned[i]);
+    if (kv->done[i]) (void)hipEventDestroy(kv->done[i]);
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+lar_status lar_kv_create(lar_kv** out, const lar_kv_config* cfg) {
+  if (!out) return LAR_E_ARG;
+  *out = nullptr;
+  if (!cfg) return LAR_E_ARG;
+  const int S = cfg->block_size;
+  if (cfg->n_kv_heads < 1 || cfg->n_kv_heads > 1024 || cfg->n_q_heads < 1 ||
+      cfg->n_q_heads % cfg->n_kv_heads || cfg->n_q_heads / cfg->n_kv_heads > 64 ||
+      (cfg->head_dim != 64 && cfg->head_dim != 128) || !type16(cfg->dtype) ||
+      (cfg->cache_dtype != cfg->dtype && cfg->cache_dtype != LAR_KV_E4M3) || S < 1 || S > 65536 ||
+      (S & (S - 1)) || cfg->max_seqs < 1 || cfg->max_seqs > 1 << 20 || cfg->max_tokens < 1 ||
+      cfg->max_tokens > 1 << 26 || cfg->reserved != 0)
+    return LAR_E_ARG;
+  lar_kv* kv = new (std::nothrow) lar_kv;
+  if (!kv) return LAR_E_HIP;
+  kv->cfg = *cfg;
+  kv->stream = static_cast<hipStream_t>(cfg->stream);
+  KvGeom& g = kv->g;
+  g.hq = cfg->n_q_heads;
+  g.hkv = cfg->n_kv_heads;
+  g.G = g.hq / g.hkv;
+  g.D = cfg->head_dim;
+  g.dtype = cfg->dtype;
+  g.cache = cfg->cache_dtype;
+  while ((1 << g.sh) < S) ++g.sh;
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess ||
+      hipDeviceGetAttribute(&kv->cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) {
+    delete kv;
+    return LAR_E_HIP;
+  }
+  kv->waves = kv->cus * kNarrowPerCu;
+  kv->groups = kv->cus * kWidePerCu;
+  // query tiles: a sequence of n tokens has ceil(n / tokens of a tile) of them per kv head
+  const int64_t nt = kNarrowRows / g.G, wt = kWideRows / g.G;
+  const int64_t narrow = std::min<int64_t>(cfg->max_seqs, cfg->max_tokens) * g.hkv;
+  const int64_t wide = (std::min<int64_t>(cfg->max_seqs, cfg->max_tokens / (nt + 1)) + cfg->max_tokens / wt) * g.hkv;
+  kv->cap = Layout(cfg->max_tokens, narrow + kv->waves, wide + kv->groups, kv->waves, kv->groups,
+                   std::min<int64_t>(narrow, kv->waves) + std::min<int64_t>(wide, kv->groups)).end;
+  // every wave or workgroup has two stretches at most that are parts of a tile
+  bool ok = hipMalloc((void**)&kv->dev, kv->cap) == hipSuccess &&
+            hipMalloc((void**)&kv->narrow_o, sizeof(float) * 2 * kv->waves * kNarrowRows * g.D) == hipSuccess &&
+            hipMalloc((void**)&kv->wide_o, sizeof(float) * 2 * kv->groups * kWideRows * g.D) == hipSuccess &&
+            hipMalloc((void**)&kv->narrow_ml, sizeof(float2) * 2 * kv->waves * kNarrowRows) == hipSuccess &&
+            hipMalloc((void**)&kv->wide_ml, sizeof(float2) * 2 * kv->groups * kWideRows) == hipSuccess &&
+            hipMalloc((void**)&kv->err, sizeof(int32_t)) == hipSuccess &&
+            hipMemset(kv->err, 0, sizeof(int32_t)) == hipSuccess;
+  for (int i = 0; ok && i < kStages; ++i)
+    ok = hipHostMalloc((void**)&kv->pinned[i], kv->cap, hipHostMallocDefault) == hipSuccess &&
+         hipEventCreateWithFlags(&kv->done[i], hipEventDisableTiming) == hipSuccess;
+  if (!ok) {
+    release(kv);
+    delete kv;
+    return LAR_E_HIP;
+  }
+  *out = kv;
+  return LAR_OK;
+}
+
+lar_status lar_kv_destroy(lar_kv* kv) {
+  if (!kv) return LAR_OK;
+  (void)hipStreamSynchronize(kv->stream);
+  release(kv);
+  delete kv;
+  return LAR_OK;
+}
+
+const char* lar_kv_error_string(const lar_kv* kv) { return kv ? kv->msg.c_str() : "null handle"; }
+
+lar_status lar_kv_plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t* ctx_len,
+                       int32_t window, int32_t sinks) {
+  if (!kv) return LAR_E_ARG;
+  if (n_seqs < 0 || n_seqs > kv->cfg.max_seqs)
+    return fail(kv, LAR_E_ARG, "%d sequences, at most %d", n_seqs, kv->cfg.max_seqs);
+  if (n_seqs && (!q_len || !ctx_len)) return fail(kv, LAR_E_ARG, "null lengths");
+  if (window < 0 || sinks < 0) return fail(kv, LAR_E_ARG, "negative window or sinks");
+  int64_t T = 0, pages = 0;
+  for (int s = 0; s < n_seqs; ++s) {
+    if (q_len[s] < 0 || ctx_len[s] < 0 || ctx_len[s] > 1 << 30)
+      return fail(kv, LAR_E_ARG, "sequence %d: %d new tokens, context %d", s, q_len[s], ctx_len[s]);
+    T += q_len[s];
+    if (q_len[s]) pages = std::max<int64_t>(pages, ceil_div(ctx_len[s], (int64_t)1 << kv->g.sh));
+  }
+  if (T > kv->cfg.max_tokens)
+    return fail(kv, LAR_E_ARG, "%lld new tokens, at most %d", (long long)T, kv->cfg.max_tokens);
+  // the copy that last left this buffer is done before it is written again
+  const int b = kv->stage;
+  if (kv->used[b]) KV_TRY(kv, hipEventSynchronize(kv->done[b]));
+  char* p = kv->pinned[b];
+  const KvGeom& g = kv->g;
+  KvTok* tok = (KvTok*)p;
+  int32_t n_narrow = 0, n_wide = 0, n_join = 0;
+  kv->planned = false;
+  try {
+    std::vector<Tile> narrow, wide;
+    const int nt = kNarrowRows / g.G, wt = kWideRows / g.G;
+    int64_t q0 = 0;
+    for (int s = 0; s < n_seqs; ++s) {
+      const int n = q_len[s];
+      const int64_t p0 = (int64_t)ctx_len[s] - n;
+      for (int r = 0; r < n; ++r) tok[q0 + r] = KvTok{s, (int32_t)(p0 + r)};
+      if (!n) continue;
+      const bool small = n <= nt;
+      const int per = small ? n : wt;
+      for (int h = 0; h < g.hkv; ++h)
+        for (int r = 0; r < n; r += per) {
+          Tile t{};
+          t.s.q0 = (int32_t)(q0 + r);
+          t.s.ntok = std::min(per, n - r);
+          t.s.p0 = (int32_t)(p0 + r);
+          t.s.head = h;
+          t.s.seq = s;
+          t.tiles = key_tiles(p0 + r, t.s.ntok, small ? kNarrowKeys : kWideKeys, window, sinks, &t.s.ns, &t.s.fw);
+          (small ? narrow : wide).push_back(t);
+        }
+      q0 += n;
+    }
+    const int64_t nn = (int64_t)narrow.size(), nw = (int64_t)wide.size();
+    const Layout L(T, nn ? nn + kv->waves : 0, nw ? nw + kv->groups : 0, kv->waves, kv->groups,
+                   std::min<int64_t>(nn, kv->waves) + std::min<int64_t>(nw, kv->groups));
+    if (L.end > kv->cap) return fail(kv, LAR_E_CAPACITY, "plan of %zu bytes, room for %zu", L.end, kv->cap);
+    kv->lay = L;
+    KvJoin* join = (KvJoin*)(p + L.join);
+    cut(narrow, kv->waves, kNarrowLeast, false, (KvSeg*)(p + L.narrow), (int32_t*)(p + L.narrow_at), &n_narrow, join,
+        &n_join);
+    cut(wide, kv->groups, kWideLeast, true, (KvSeg*)(p + L.wide), (int32_t*)(p + L.wide_at), &n_wide, join, &n_join);
+  } catch (const std::bad_alloc&) {
+    return fail(kv, LAR_E_CAPACITY, "out of host memory");
+  }
+  if (kv->sticky != LAR_OK) {  // an error that was reported ends with the batch it was in
+    KV_TRY(kv, hipMemsetAsync(kv->err, 0, sizeof(int32_t), kv->stream));
+    kv->sticky = LAR_OK;
+  }
+  if (T) {
+    KV_TRY(kv, hipMemcpyAsync(kv->dev, p, kv->lay.end, hipMemcpyHostToDevice, kv->stream));
+    KV_TRY(kv, hipEventRecord(kv->done[b], kv->stream));
+    kv->used[b] = true;
+    kv->stage = (b + 1) % kStages;
+  }
+  kv->n_seq = n_seqs;
+  kv->n_tok = (int32_t)T;
+  kv->max_pages = (int32_t)pages;
+  kv->window = window;
+  kv->sinks = window ? sinks : 0;
+  kv->n_narrow = n_narrow;
+  kv->n_wide = n_wide;
+  kv->n_join = n_join;
+  kv->planned = true;
+  return LAR_OK;
+}
+
+lar_status lar_kv_append(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_rows* k, const lar_kv_rows* v,
+                         const int32_t* table, int32_t table_cols) {
+  if (lar_status st = ready(kv)) return st;
+  if (!kv->n_tok) return LAR_OK;
+  KvPool pool;
+  KvRows kr, vr;
+  if (lar_status st = check(kv, pages, table, table_cols, &pool)) return st;
+  if (lar_status st = check_rows(kv, k, "k", &kr)) return st;
+  if (lar_status st = check_rows(kv, v, "v", &vr)) return st;
+  KvCopyArgs a = copy_args(kv, pool, table, table_cols);
+  a.k = kr;
+  a.v = vr;
+  return launched(kv, launch_kv_append(a, kv->stream));
+}
+
+lar_status lar_kv_read(lar_kv* kv, const lar_kv_pages* pages, const int32_t* table, int32_t table_cols,
+                       const lar_kv_rows* k, const lar_kv_rows* v) {
+  if (lar_status st = ready(kv)) return st;
+  if (!kv->n_tok) return LAR_OK;
+  KvPool pool;
+  KvRows kr, vr;
+  if (lar_status st = check(kv, pages, table, table_cols, &pool)) return st;
+  if (lar_status st = check_rows(kv, k, "k", &kr)) return st;
+  if (lar_status st = check_rows(kv, v, "v", &vr)) return st;
+  KvCopyArgs a = copy_args(kv, pool, table, table_cols);
+  a.k = kr;
+  a.v = vr;
+  return launched(kv, launch_kv_read(a, kv->stream));
+}
+
+lar_status lar_kv_attend(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_rows* q, const int32_t* table,
+                         int32_t table_cols, double scale, void* out, float* lse) {
+  if (lar_status st = ready(kv)) return st;
+  if (!kv->n_tok) return LAR_OK;
+  KvPool pool;
+  KvRows qr;
+  if (lar_status st = check(kv, pages, table, table_cols, &pool)) return st;
+  if (lar_status st = check_rows(kv, q, "q", &qr)) return st;
+  if (!(scale > 0.0) || !(scale < 1e30)) return fail(kv, LAR_E_ARG, "scale must be positive and finite");
+  if (!out || ((uintptr_t)out & 15)) return fail(kv, LAR_E_ARG, "out must be aligned to 16 bytes");
+  KvAttendArgs a{};
+  a.g = kv->g;
+  a.pool = pool;
+  a.q = qr;
+  a.table = table;
+  a.cols = table_cols;
+  a.scale = (float)(scale * 1.4426950408889634074);
+  a.window = kv->window;
+  a.sinks = kv->sinks;
+  a.out = out;
+  a.lse = lse;
+  a.narrow = (const KvSeg*)(kv->dev + kv->lay.narrow);
+  a.wide = (const KvSeg*)(kv->dev + kv->lay.wide);
+  a.narrow_at = (const int32_t*)(kv->dev + kv->lay.narrow_at);
+  a.wide_at = (const int32_t*)(kv->dev + kv->lay.wide_at);
+  a.n_narrow = kv->n_narrow;
+  a.n_wide = kv->n_wide;
+  a.join = (const KvJoin*)(kv->dev + kv->lay.join);
+  a.n_join = kv->n_join;
+  a.narrow_o = kv->narrow_o;
+  a.wide_o = kv->wide_o;
+  a.narrow_ml = kv->narrow_ml;
+  a.wide_ml = kv->wide_ml;
+  a.err = kv->err;
+  return launched(kv, launch_kv_attend(a, kv->stream));
+}
+
+lar_status lar_kv_sync(lar_kv* kv) {
+  if (!kv) return LAR_E_ARG;
+  if (kv->sticky != LAR_OK) return kv->sticky;
+  int32_t e = 0;
+  KV_TRY(kv, hipMemcpyAsync(&e, kv->err, sizeof e, hipMemcpyDeviceToHost, kv->stream));
+  KV_TRY(kv, hipStreamSynchronize(kv->stream));
+  if (e != LAR_OK) {
+    kv->sticky = e;
+    return fail(kv, e, "a block table names a page outside the pool");
+  }
+  return LAR_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,660 @@
+// kv_attend.hip -- attention of a token batch over the pages of a key/value cache.
+//
+// For new token r of a sequence, at position p, over the keys j it sees (j <= p, and under
+// a window W also j > p - W or j < sinks):
+//     s_j = scale * q . k_j,   out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),
+// in one pass over the keys with a running maximum m and sum, all in 32 bits.
+//
+// A query tile is up to 32 (narrow) or 256 (wide) rows of one sequence and one kv head,
+// row = token * G + head of the group, so that K and V are read once for the group.  Both
+// kernels compute S^T = K Q^T and O^T = V^T P^T with 32x32x16 matrix instructions: a
+// query row is a column, held by lanes n and n + 32, its maximum and sum are a lane's own
+// values, and the elements of P^T that a lane holds are those that it has to hand to the
+// second product, with its keys in the order  16 t + (j & 3) + 8 (j >> 2) + 4 h  that the
+// transposing LDS reads give V^T in.
+//
+//   k_kv_narrow  one wave per stretch of 32-key tiles: single tokens and short chunks.
+//                Bound by the bytes of K and V.  Waves share nothing, so there is no
+//                barrier; the next tile is on its way in registers while one is used.
+//   k_kv_wide    eight waves, 256 rows, 64-key tiles in LDS for all of them: chunks.
+//                Bound by the matrix instructions and the exponentials beside them.
+//   k_kv_join    the partial sums of the tiles whose keys were split over waves.
+//
+// P is rounded to the 16-bit type of V (nearest even) for the second product, an error of
+// the size of the output's own rounding; sums are taken of the unrounded values.
+#include "../../include/lar.h"
+#include "kv_device.h"
+
+namespace lar {
+namespace {
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(8))) short s16x8;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+typedef __attribute__((address_space(3))) char lds_char;
+
+constexpr float kLn2 = 0.693147180559945309f;
+// A row's maximum may fall behind by this much (log2 units) before its sums are rescaled:
+// exponentials up to 2^8 lose nothing in 32 bits, and stay in the range of 16-bit P.
+constexpr float kLag = 8.0f;
+
+template <bool BF> struct Elem;
+template <> struct Elem<true> {
+  using x8 = bf16x8;
+  static __device__ __forceinline__ f32x16 mma(s16x8 a, s16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ s16x8 pack(f32x8 x) {
+    return __builtin_bit_cast(s16x8, __builtin_convertvector(x, bf16x8));
+  }
+  static __device__ __forceinline__ uint32_t pair(uint32_t codes, float s, bool hi) {
+    return hi ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, s, true))
+              : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, s, false));
+  }
+  static __device__ __forceinline__ uint16_t one(float x) {
+    return __builtin_bit_cast(uint16_t, (__bf16)x);
+  }
+  static __device__ __forceinline__ float value(uint16_t x) {
+    return __uint_as_float((uint32_t)x << 16);
+  }
+  static constexpr uint32_t kExp = 0x7f80u;  // exponent bits: all ones where not finite
+};
+template <> struct Elem<false> {
+  using x8 = f16x8;
+  static __device__ __forceinline__ f32x16 mma(s16x8 a, s16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ s16x8 pack(f32x8 x) {
+    return __builtin_bit_cast(s16x8, __builtin_convertvector(x, f16x8));
+  }
+  static __device__ __forceinline__ uint32_t pair(uint32_t codes, float s, bool hi) {
+    return hi ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, s, true))
+              : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, s, false));
+  }
+  static __device__ __forceinline__ uint16_t one(float x) {
+    return __builtin_bit_cast(uint16_t, (_Float16)x);
+  }
+  static __device__ __forceinline__ float value(uint16_t x) {
+    return (float)__builtin_bit_cast(_Float16, x);
+  }
+  static constexpr uint32_t kExp = 0x7c00u;
+};
+
+// Whether one of the 8 16-bit values is an infinity or NaN.
+template <bool BF>
+__device__ __forceinline__ bool not_finite(const uint4& x) {
+  const uint32_t e = Elem<BF>::kExp, eh = e << 16;
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) bad |= (w[i] & e) == e || (w[i] & eh) == eh;
+  return bad;
+}
+
+// The larger, or the sum, of a lane's value and that of lane ^ 32.
+__device__ __forceinline__ float max_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float add_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Orders a wave's LDS accesses of different lanes: they run in program order.
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Key of element i of S^T's 32 keys in a lane of half h.
+__device__ __forceinline__ constexpr int key_of(int i, int h) {
+  return (i & 3) + 8 * (i >> 2) + 4 * h;
+}
+
+// LDS tiles: [key][D] 16-bit values in 16-byte chunks.  The K reads take one chunk of 32
+// rows, the V reads 64 bytes of 8 rows; the chunks are permuted so that each covers the
+// banks evenly.
+template <int D>
+__device__ __forceinline__ int k_chunk(int row, int c) {
+  return D == 128 ? c ^ (row & 15) : c ^ ((row >> 1) & 7);
+}
+template <int D>
+__device__ __forceinline__ int v_chunk(int row, int c) {
+  return D == 128 ? c ^ ((row & 3) << 2) : c ^ (((row >> 1) & 1) << 2);
+}
+
+// A query tile in a wave: this lane's row and what its keys are.
+struct Row {
+  int pos;    // position of the row's token; < 0: it sees nothing
+  int lo;     // keys > lo or < sinks
+  int sinks;
+  __device__ __forceinline__ bool sees(int j) const {
+    return j <= pos && (j > lo || j < sinks);
+  }
+};
+
+// The running sums of a wave's 32 rows.
+template <int D>
+struct Sums {
+  f32x16 o[D / 32];  // O^T: row n, value 32 b + key_of(i, h)
+  float m, l;        // maximum (log2 units); this half's part of the sum
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[b][i] = 0.0f;
+    m = -__builtin_inff();
+    l = 0.0f;
+  }
+};
+
+// S^T of 32 keys, `kt` their rows in LDS.
+template <bool BF, int D>
+__device__ __forceinline__ f32x16 scores(const char* kt, const s16x8 (&q)[D / 16], int n, int h) {
+  f32x16 s;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+  for (int t = 0; t < D / 16; ++t) {
+    const s16x8 k = *(const s16x8*)(kt + n * (D * 2) + k_chunk<D>(n, 2 * t + h) * 16);
+    s = Elem<BF>::mma(k, q[t], s);
+  }
+  return s;
+}
+
+// Takes the scores of NB blocks of 32 keys into the running maximum and sum, rescaling
+// the rows' sums where their maximum grew; p: the exponentials.
+template <int D, int NB>
+__device__ __forceinline__ void soften(f32x16 (&s)[NB], Sums<D>& a, float c) {
+  float mx = s[0][0];
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
+  mx = max_halves(mx) * c;
+  if (__any(mx > a.m + kLag)) {
+    const float m = fmaxf(mx, a.m);
+    const float f = m > a.m ? __builtin_amdgcn_exp2f(a.m - m) : 1.0f;  // 0 from a.m = -inf
+    a.m = m;
+    a.l *= f;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) a.o[b][i] *= f;
+  }
+  const float m = a.m == -__builtin_inff() ? 0.0f : a.m;
+  float l = 0.0f;
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c, -m));
+      l += s[b][i];
+    }
+  a.l += l;
+}
+
+// O^T += V^T P^T over 32 keys, `vt` their rows in LDS.
+template <bool BF, int D>
+__device__ __forceinline__ void weigh(const char* vt, const f32x16& p, Sums<D>& a, int lane) {
+  const int h = lane >> 5, i = lane & 15, g = lane >> 4;
+  const int row = 4 * h + (i >> 2);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    f32x8 x;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = p[8 * t + j];
+    const s16x8 pk = Elem<BF>::pack(x);
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) {
+      // 16 lanes read 4 keys x 16 values and get them by columns
+      const int c = 4 * b + 2 * (g & 1) + ((i & 3) >> 1);
+      const char* at = vt + (16 * t + row) * (D * 2) + v_chunk<D>(row, c) * 16 + (i & 1) * 8;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 8 * (D * 2)));
+      s16x8 v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[j] = lo[j];
+        v[4 + j] = hi[j];
+      }
+      a.o[b] = Elem<BF>::mma(v, pk, a.o[b]);
+    }
+  }
+}
+
+// V rows with infinities or NaN that only some rows of the tile see would reach the
+// others as 0 * inf: such a row r (of 32) is added here, for the lanes whose rows see it;
+// the caller then clears it in LDS.
+template <bool BF, int D>
+__device__ __forceinline__ void weigh_row(const char* vt, int r, bool seen, const f32x16& p, Sums<D>& a,
+                                       int lane) {
+  const int h = lane >> 5;
+  float x = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x = key_of(i, h) == r ? p[i] : x;
+  x = add_halves(x);
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int d = 32 * b + key_of(i, h);
+      const float v = Elem<BF>::value(*(const uint16_t*)(vt + r * (D * 2) + v_chunk<D>(r, d >> 3) * 16 + (d & 7) * 2));
+      a.o[b][i] = seen ? __builtin_fmaf(x, v, a.o[b][i]) : a.o[b][i];
+    }
+}
+
+// What a lane of a query tile is: its row's token and head, and what it sees.
+struct Lane {
+  int tok, qh;   // token of the batch, query head
+  bool real;     // the tile has this row
+  Row row;
+};
+
+__device__ __forceinline__ Lane lane_of(const KvAttendArgs& A, const KvSeg& s, int n) {
+  const int t = n / A.g.G;
+  Lane x;
+  x.real = t < s.ntok;
+  const int u = x.real ? t : s.ntok - 1;
+  x.tok = s.q0 + u;
+  x.qh = s.head * A.g.G + (x.real ? n - t * A.g.G : 0);
+  x.row.pos = s.p0 + u;
+  x.row.lo = A.window ? x.row.pos - A.window : -1;
+  x.row.sinks = A.sinks;
+  return x;
+}
+
+template <int D>
+__device__ __forceinline__ void load_q(const KvAttendArgs& A, const Lane& x, int h, s16x8 (&q)[D / 16]) {
+  const int16_t* p = (const int16_t*)A.q.p + (int64_t)x.tok * A.q.tok + (int64_t)x.qh * A.q.head;
+#pragma unroll
+  for (int t = 0; t < D / 16; ++t) {
+    s16x8 z = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (x.real) z = *(const s16x8*)(p + 16 * t + 8 * h);
+    q[t] = z;
+  }
+}
+
+// The result of a wave's rows, or their partial sums (`row0`: first row of the wave in the
+// slot, `rows` of a slot).
+template <bool BF, int D>
+__device__ __forceinline__ void finish(const KvAttendArgs& A, const Lane& x, const Sums<D>& a, int lane,
+                                       int slot, int row0, int rows, float* po, float2* pml) {
+  const int n = lane & 31, h = lane >> 5;
+  const float l = add_halves(a.l);
+  if (!x.real) return;
+  if (slot >= 0) {
+    float* o = po + ((int64_t)slot * rows + row0 + n) * D;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        f32x4 y = {a.o[b][i], a.o[b][i + 1], a.o[b][i + 2], a.o[b][i + 3]};
+        *(f32x4*)(o + 32 * b + key_of(i, h)) = y;
+      }
+    if (h == 0) pml[(int64_t)slot * rows + row0 + n] = make_float2(a.m, l);
+    return;
+  }
+  const bool none = x.row.pos < 0;
+  const float f = none ? 0.0f : 1.0f / l;
+  const int64_t at = (int64_t)x.tok * A.g.hq + x.qh;
+  uint16_t* out = (uint16_t*)A.out + at * D;
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      uint32_t w[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float y0 = none ? 0.0f : a.o[b][i + 2 * j] * f;
+        const float y1 = none ? 0.0f : a.o[b][i + 2 * j + 1] * f;
+        w[j] = Elem<BF>::one(y0) | (uint32_t)Elem<BF>::one(y1) << 16;
+      }
+      *(uint2*)(out + 32 * b + key_of(i, h)) = make_uint2(w[0], w[1]);
+    }
+  if (A.lse && h == 0) {
+    const float m = a.m == -__builtin_inff() ? 0.0f : a.m;
+    A.lse[at] = none ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+}
+
+// First key of tile t.
+template <int K>
+__device__ __forceinline__ int tile_key(const KvSeg& s, int t) {
+  return (t < s.ns ? t : s.fw + t - s.ns) * K;
+}
+
+// Rows of K and V on their way from the pages into LDS: `I` loads of 16 bytes for each.
+template <bool BF, bool F8, int D, int I, int LANES>
+struct Stage {
+  static constexpr int kChunks = F8 ? D / 16 : D / 8;  // 16-byte chunks of a row in memory
+  static constexpr int kStep = LANES / kChunks;        // rows of one load
+  uint4 k[I], v[I];
+  uint32_t ke[F8 ? I : 1], ve[F8 ? I : 1];
+
+  __device__ __forceinline__ void load(const KvPool& P, int i, uint32_t row, int c) {
+    const int64_t at = (int64_t)row * kChunks + c;
+    k[i] = ((const uint4*)P.k)[at];
+    v[i] = ((const uint4*)P.v)[at];
+    if (F8) {
+      ke[i] = P.ke[row];
+      ve[i] = P.ve[row];
+    }
+  }
+  // 16-bit chunks j (of 2 with 8-bit codes) of load i
+  static __device__ __forceinline__ uint4 widen(const uint4& x, uint32_t e, int j) {
+    if (!F8) return x;
+    const float s = __uint_as_float(e << 23);
+    const uint32_t a = j ? x.z : x.x, b = j ? x.w : x.y;
+    uint4 o;
+    o.x = Elem<BF>::pair(a, s, false);
+    o.y = Elem<BF>::pair(a, s, true);
+    o.z = Elem<BF>::pair(b, s, false);
+    o.w = Elem<BF>::pair(b, s, true);
+    return o;
+  }
+  // Puts load i, row r of the tile, into LDS; a V row from `end` on holds nothing that a
+  // row of the tile sees and is cleared.  Returns whether V has infinities or NaN there.
+  template <bool MASKED>
+  __device__ __forceinline__ bool put(char* kt, char* vt, int i, int r, int c, int end) const {
+    bool bad = false;
+#pragma unroll
+    for (int j = 0; j < (F8 ? 2 : 1); ++j) {
+      const int cc = F8 ? 2 * c + j : c;
+      const uint4 x = widen(k[i], ke[F8 ? i : 0], j);
+      uint4 y = widen(v[i], ve[F8 ? i : 0], j);
+      if (MASKED) {
+        if (r >= end) y = make_uint4(0, 0, 0, 0);
+        bad |= not_finite<BF>(y);
+      }
+      *(uint4*)(kt + r * (D * 2) + k_chunk<D>(r, cc) * 16) = x;
+      *(uint4*)(vt + r * (D * 2) + v_chunk<D>(r, cc) * 16) = y;
+    }
+    return bad;
+  }
+};
+
+// Row of the pool that holds key j (j inside the sequence's table) of a kv head; a page
+// outside the pool sets the sticky error and reads page 0.
+__device__ __forceinline__ uint32_t pool_row(const KvAttendArgs& A, int head, int32_t page, int j) {
+  if ((uint32_t)page >= A.pool.n_blocks) {
+    *A.err = LAR_E_STATE;
+    page = 0;
+  }
+  return (((uint32_t)page * (uint32_t)A.g.hkv + (uint32_t)head) << A.g.sh) +
+         (uint32_t)(j & ((1 << A.g.sh) - 1));
+}
+
+// ------------------------------------------------------------------ narrow tiles
+template <bool BF, bool F8, int D>
+__global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
+  __shared__ __align__(16) char lds[2 * kNarrowKeys * D * 2];
+  char *kt = lds, *vt = lds + kNarrowKeys * D * 2;
+  using St = Stage<BF, F8, D, kNarrowKeys * (F8 ? D / 16 : D / 8) / 64, 64>;
+  constexpr int I = kNarrowKeys / St::kStep;
+  const int lane = threadIdx.x, n = lane & 31, h = lane >> 5;
+  const int r0 = lane / St::kChunks, c = lane % St::kChunks;
+  const int e = A.narrow_at[blockIdx.x + 1];
+  for (int x = A.narrow_at[blockIdx.x]; x < e; ++x) {
+    const KvSeg s = A.narrow[x];
+    const Lane ln = lane_of(A, s, n);
+    s16x8 q[D / 16];
+    load_q<D>(A, ln, h, q);
+    Sums<D> a;
+    a.clear();
+    const int last = s.p0 + s.ntok - 1;  // position of the last token: keys 0 .. last
+    const int32_t* table = A.table + (int64_t)s.seq * A.cols;
+    const auto key = [&](int t) {
+      const int j = tile_key<kNarrowKeys>(s, t) + n;
+      return j < last ? j : last;
+    };
+    St st;
+    const auto fetch = [&](int32_t page, int j) {
+      const uint32_t row = pool_row(A, s.head, page, j);
+#pragma unroll
+      for (int i = 0; i < I; ++i)
+        st.load(A.pool, i, (uint32_t)__shfl((int)row, i * St::kStep + r0), c);
+    };
+    int32_t page = 0;
+    if (s.t0 < s.t1) {
+      fetch(table[key(s.t0) >> A.g.sh], key(s.t0));
+      if (s.t0 + 1 < s.t1) page = table[key(s.t0 + 1) >> A.g.sh];
+    }
+    for (int t = s.t0; t < s.t1; ++t) {
+      const int kb = tile_key<kNarrowKeys>(s, t);
+      // every row sees all of the tile's keys unless it reaches past the first row's
+      // position or before the last row's window
+      const bool masked = kb + kNarrowKeys - 1 > s.p0 ||
+                          (A.window && kb <= last - A.window && kb + kNarrowKeys > A.sinks);
+      uint32_t bad = 0;
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+          const uint64_t m = __ballot(st.template put<true>(kt, vt, i, i * St::kStep + r0, c, last + 1 - kb));
+          if (m)
+            for (int r = 0; r < St::kStep; ++r)
+              if (m >> (r * St::kChunks) & ((1ull << St::kChunks) - 1)) bad |= 1u << (i * St::kStep + r);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < I; ++i) st.template put<false>(kt, vt, i, i * St::kStep + r0, c, 0);
+      }
+      if (t + 1 < s.t1) {
+        fetch(page, key(t + 1));
+        if (t + 2 < s.t1) page = table[key(t + 2) >> A.g.sh];
+      }
+      wave_order();
+      f32x16 sc[1] = {scores<BF, D>(kt, q, n, h)};
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          sc[0][i] = ln.row.sees(kb + key_of(i, h)) ? sc[0][i] : -__builtin_inff();
+      }
+      soften<D, 1>(sc, a, A.scale);
+      if (masked && bad) {
+        for (uint32_t w = bad; w; w &= w - 1) {
+          const int r = __builtin_ctz(w);
+          weigh_row<BF, D>(vt, r, ln.row.sees(kb + r), sc[0], a, lane);
+          wave_order();
+          if (lane < D / 8) *(uint4*)(vt + r * (D * 2) + lane * 16) = make_uint4(0, 0, 0, 0);
+          wave_order();
+        }
+      }
+      weigh<BF, D>(vt, sc[0], a, lane);
+      wave_order();
+    }
+    finish<BF, D>(A, ln, a, lane, s.slot, 0, kNarrowRows, A.narrow_o, A.narrow_ml);
+  }
+}
+
+// ------------------------------------------------------------------ wide tiles
+template <bool BF, bool F8, int D>
+__global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) {
+  constexpr int kTile = kWideKeys * D * 2, kThreads = 64 * kWideWaves;
+  __shared__ __align__(16) char lds[4 * kTile];  // K and V, two tiles
+  __shared__ int flag[2];
+  using St = Stage<BF, F8, D, (kWideKeys * (F8 ? D / 16 : D / 8) + kThreads - 1) / kThreads, kThreads>;
+  constexpr int I = (kWideKeys + St::kStep - 1) / St::kStep;
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5, wave = tid >> 6;
+  const int r0 = tid / St::kChunks, c = tid % St::kChunks;
+  const bool loads = r0 < kWideKeys;  // narrow 8-bit rows need fewer threads
+  const int e = A.wide_at[blockIdx.x + 1];
+  for (int x = A.wide_at[blockIdx.x]; x < e; ++x) {
+    const KvSeg s = A.wide[x];
+    const Lane ln = lane_of(A, s, wave * 32 + n);
+    s16x8 q[D / 16];
+    load_q<D>(A, ln, h, q);
+    Sums<D> a;
+    a.clear();
+    const int last = s.p0 + s.ntok - 1;
+    // the last position of this wave's own rows: keys past it are not seen by any
+    const int wtok = (wave * 32 + 31) / A.g.G;
+    const int wlast = s.p0 + (wtok < s.ntok ? wtok : s.ntok - 1);
+    const bool wreal = wave * 32 < s.ntok * A.g.G;
+    const int32_t* table = A.table + (int64_t)s.seq * A.cols;
+    St st;
+    int32_t page[I];
+    const auto key = [&](int t, int i) {
+      const int j = tile_key<kWideKeys>(s, t) + i * St::kStep + r0;
+      return j < last ? j : last;
+    };
+    const auto look = [&](int t) {
+#pragma unroll
+      for (int i = 0; i < I; ++i)
+        if (loads) page[i] = table[key(t, i) >> A.g.sh];
+    };
+    const auto fetch = [&](int t) {
+#pragma unroll
+      for (int i = 0; i < I; ++i)
+        if (loads) st.load(A.pool, i, pool_row(A, s.head, page[i], key(t, i)), c);
+    };
+    const auto is_masked = [&](int kb) {
+      return kb + kWideKeys - 1 > s.p0 || (A.window && kb <= last - A.window && kb + kWideKeys > A.sinks);
+    };
+    const auto put = [&](int t, int b) {
+      const int kb = tile_key<kWideKeys>(s, t);
+      char *kt = lds + b * 2 * kTile, *vt = kt + kTile;
+      if (!loads) return;
+      if (is_masked(kb)) {
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+          bad |= st.template put<true>(kt, vt, i, i * St::kStep + r0, c, last + 1 - kb);
+        if (bad) flag[b] = t + 1;
+      } else {
+#pragma unroll
+        for (int i = 0; i < I; ++i) st.template put<false>(kt, vt, i, i * St::kStep + r0, c, 0);
+      }
+    };
+    if (tid < 2) flag[tid] = 0;
+    if (s.t0 < s.t1) {
+      look(s.t0);
+      fetch(s.t0);
+      if (s.t0 + 1 < s.t1) look(s.t0 + 1);
+    }
+    __syncthreads();  // the flags; and the last stretch's tiles are done with
+    if (s.t0 < s.t1) put(s.t0, s.t0 & 1);
+    __syncthreads();
+    for (int t = s.t0; t < s.t1; ++t) {
+      const int b = t & 1, kb = tile_key<kWideKeys>(s, t);
+      char *kt = lds + b * 2 * kTile, *vt = kt + kTile;
+      if (t + 1 < s.t1) {
+        fetch(t + 1);
+        if (t + 2 < s.t1) look(t + 2);
+      }
+      const bool masked = is_masked(kb);
+      const bool works = wreal && kb <= wlast;
+      f32x16 sc[2];
+      if (works) {
+        sc[0] = scores<BF, D>(kt, q, n, h);
+        sc[1] = scores<BF, D>(kt + 32 * D * 2, q, n, h);
+        if (masked) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              sc[u][i] = ln.row.sees(kb + 32 * u + key_of(i, h)) ? sc[u][i] : -__builtin_inff();
+        }
+        soften<D, 2>(sc, a, A.scale);
+      }
+      if (masked && flag[b] == t + 1) {  // the same for all waves
+        for (int r = 0; r < kWideKeys; ++r) {
+          char* row = vt + r * (D * 2);
+          if (!__any(lane < D / 8 && not_finite<BF>(*(const uint4*)(row + (lane % (D / 8)) * 16)))) continue;
+          if (works) weigh_row<BF, D>(vt + (r & 32) * (D * 2), r & 31, ln.row.sees(kb + r), sc[r >> 5], a, lane);
+        }
+        __syncthreads();
+        for (int r = wave; r < kWideKeys; r += kWideWaves) {
+          char* row = vt + r * (D * 2);
+          const bool mine = lane < D / 8;
+          if (__any(mine && not_finite<BF>(*(const uint4*)(row + (lane % (D / 8)) * 16))) && mine)
+            *(uint4*)(row + lane * 16) = make_uint4(0, 0, 0, 0);
+        }
+        __syncthreads();
+      }
+      if (works) {
+        weigh<BF, D>(vt, sc[0], a, lane);
+        weigh<BF, D>(vt + 32 * D * 2, sc[1], a, lane);
+      }
+      if (t + 1 < s.t1) put(t + 1, b ^ 1);
+      __syncthreads();
+    }
+    finish<BF, D>(A, ln, a, lane, s.slot, wave * 32, kWideRows, A.wide_o, A.wide_ml);
+  }
+}
+
+// ------------------------------------------------------------------ joining split tiles
+// One workgroup per 32 rows of a split tile; a thread has 4 values of a row, groups of
+// threads share out the slots.
+constexpr int kJoinThreads = 512;
+
+template <bool BF, int D>
+__global__ __launch_bounds__(kJoinThreads) void k_kv_join(KvAttendArgs A) {
+  const KvJoin j = A.join[blockIdx.x];
+  const int rows = j.wide ? kWideRows : kNarrowRows;
+  const int row0 = blockIdx.y * 32;
+  const int have = j.ntok * A.g.G - row0 < 32 ? j.ntok * A.g.G - row0 : 32;
+  if (have <= 0) return;
+  const float* po = j.wide ? A.wide_o : A.narrow_o;
+  const float2* pml = j.wide ? A.wide_ml : A.narrow_ml;
+  constexpr int kQuads = D / 4;
+  for (int u = threadIdx.x; u < have * kQuads; u += kJoinThreads) {
+    const int r = u / kQuads, d = (u % kQuads) * 4;
+    float m = -__builtin_inff();
+    for (int s = 0; s < j.n; ++s) m = fmaxf(m, pml[(int64_t)(j.slot + s) * rows + row0 + r].x);
+    const float mm = m == -__builtin_inff() ? 0.0f : m;
+    float l = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
+    for (int s = 0; s < j.n; ++s) {
+      const int64_t at = (int64_t)(j.slot + s) * rows + row0 + r;
+      const float2 ml = pml[at];
+      const float f = __builtin_amdgcn_exp2f(ml.x - mm);
+      l = __builtin_fmaf(f, ml.y, l);
+      const f32x4 y = *(const f32x4*)(po + at * D + d);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(f, y[i], o[i]);
+    }
+    const int t = (row0 + r) / A.g.G, g = row0 + r - t * A.g.G;
+    const bool none = j.p0 + t < 0;
+    const float inv = none ? 0.0f : 1.0f / l;
+    const int64_t at = (int64_t)(j.q0 + t) * A.g.hq + j.head * A.g.G + g;
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      w[i] = Elem<BF>::one(none ? 0.0f : o[2 * i] * inv) |
+             (uint32_t)Elem<BF>::one(none ? 0.0f : o[2 * i + 1] * inv) << 16;
+    *(uint2*)((uint16_t*)A.out + at * D + d) = make_uint2(w[0], w[1]);
+    if (A.lse && d == 0) A.lse[at] = none ? -__builtin_inff() : (mm + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+}
+
+template <bool BF, bool F8, int D>
+hipError_t run(const KvAttendArgs& a, hipStream_t stream) {
+  if (a.n_wide) k_kv_wide<BF, F8, D><<<a.n_wide, 64 * kWideWaves, 0, stream>>>(a);
+  if (a.n_narrow) k_kv_narrow<BF, F8, D><<<a.n_narrow, 64, 0, stream>>>(a);
+  if (a.n_join) k_kv_join<BF, D><<<dim3(a.n_join, a.n_wide ? kWideRows / 32 : 1), kJoinThreads, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <bool BF, bool F8>
+hipError_t run_d(const KvAttendArgs& a, hipStream_t stream) {
+  return a.g.D == 128 ? run<BF, F8, 128>(a, stream) : run<BF, F8, 64>(a, stream);
+}
+
+}  // namespace
+
+hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t stream) {
+  const bool f8 = a.g.cache == kKvE4m3;
+  if (a.g.dtype == kKvBf16) return f8 ? run_d<true, true>(a, stream) : run_d<true, false>(a, stream);
+  return f8 ? run_d<false, true>(a, stream) : run_d<false, false>(a, stream);
+}
+
+}  // namespace lar

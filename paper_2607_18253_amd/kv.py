@@ -1,0 +1,209 @@
+"""Python binding of the paged key/value cache (lar_kv_* in include/lar.h): a token batch's
+K and V rows into and out of the pages, and its attention over them.  Argument marshalling
+only, as in ``lar``; every step runs in the HIP kernels behind the C ABI.
+"""
+
+from __future__ import annotations
+
+import ctypes as C
+import math
+
+import numpy as np
+
+from .lar import LAR_OK, LarError, _dev, load_library
+
+KV_F16, KV_BF16, KV_E4M3 = 0, 1, 2
+
+
+class KvConfig(C.Structure):
+    _fields_ = [("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("cache_dtype", C.c_int32), ("block_size", C.c_int32),
+                ("max_seqs", C.c_int32), ("max_tokens", C.c_int32), ("reserved", C.c_int32),
+                ("stream", C.c_void_p)]
+
+
+class KvPagesArg(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p),
+                ("n_blocks", C.c_int64)]
+
+
+class KvRowsArg(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("tok_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class KvPages:
+    """The pages of one layer: GPU tensors k and v [n_blocks][n_kv_heads][block_size][head_dim]
+    (16-bit, or float8_e4m3fn with k_exp and v_exp uint8 [n_blocks][n_kv_heads][block_size]).
+    Make new ones with PagedKV.new_pages."""
+
+    __slots__ = ("k", "v", "k_exp", "v_exp", "_arg")
+
+    def __init__(self, k, v, k_exp=None, v_exp=None):
+        import torch
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
+            raise ValueError("k and v must be [n_blocks][n_kv_heads][block_size][head_dim] of one dtype")
+        e4m3 = k.dtype == torch.float8_e4m3fn
+        for e in (k_exp, v_exp):
+            if (e is not None) != e4m3 or (e4m3 and e.shape != k.shape[:3]):
+                raise ValueError("float8_e4m3fn pages, and only they, have k_exp and v_exp "
+                                 "[n_blocks][n_kv_heads][block_size]")
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self._arg = KvPagesArg(_dev(k, k.dtype, "k"), _dev(v, v.dtype, "v"),
+                               _dev(k_exp, torch.uint8, "k_exp"), _dev(v_exp, torch.uint8, "v_exp"),
+                               int(k.shape[0]))
+
+    def tensors(self):
+        return [t for t in (self.k, self.v, self.k_exp, self.v_exp) if t is not None]
+
+
+class PagedKV:
+    """A paged key/value cache's geometry and the plan of the current token batch; see
+    lar_kv_config and lar_kv_plan.  The pages of each layer are KvPages.
+
+    Work runs on ``stream`` (the current one when the handle is made).  A call made while
+    another stream is current is ordered after that stream's work, and that stream after
+    the call; a graph is captured on the handle's own stream (which then is not the
+    default one)."""
+
+    def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, *, block_size: int,
+                 dtype=None, cache_dtype=None, max_seqs: int, max_tokens: int, stream=None):
+        import torch
+        self._torch = torch
+        self._L = load_library()
+        self.stream = torch.cuda.current_stream() if stream is None else stream
+        self._sid = self.stream.cuda_stream
+        self.device = self.stream.device
+        self.dtype = torch.bfloat16 if dtype is None else dtype
+        self.cache_dtype = self.dtype if cache_dtype is None else cache_dtype
+        kinds = {torch.float16: KV_F16, torch.bfloat16: KV_BF16, torch.float8_e4m3fn: KV_E4M3}
+        if self.dtype not in kinds or self.cache_dtype not in kinds:
+            raise ValueError("dtype must be float16 or bfloat16, cache_dtype dtype or float8_e4m3fn")
+        self.n_q, self.n_kv, self.head_dim = int(n_q_heads), int(n_kv_heads), int(head_dim)
+        self.block_size = int(block_size)
+        cfg = KvConfig(self.n_q, self.n_kv, self.head_dim, kinds[self.dtype], kinds[self.cache_dtype],
+                       self.block_size, int(max_seqs), int(max_tokens), 0, C.c_void_p(self._sid))
+        h = C.c_void_p()
+        with torch.cuda.device(self.device):
+            st = self._L.lar_kv_create(C.byref(h), C.byref(cfg))
+        if st != LAR_OK:
+            raise LarError(st, "lar_kv_create failed")
+        self._h = h
+        self._n_seq = self._n_tok = 0
+
+    # ------------------------------------------------------------------ plumbing
+    def _check(self, st: int):
+        if st != LAR_OK:
+            raise LarError(st, self._L.lar_kv_error_string(self._h).decode())
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._L.lar_kv_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def _pages(self, pages):
+        k = pages.k
+        if k.dtype != self.cache_dtype or k.shape[1:] != (self.n_kv, self.block_size, self.head_dim):
+            raise ValueError(f"pages must be [n_blocks][{self.n_kv}][{self.block_size}][{self.head_dim}] "
+                             f"of {self.cache_dtype}")
+        return C.byref(pages._arg)
+
+    def _rows(self, t, heads, name):
+        if not t.is_cuda or t.dtype != self.dtype:
+            raise ValueError(f"{name} must be a GPU tensor of {self.dtype}")
+        if t.shape != (self._n_tok, heads, self.head_dim) or t.stride(2) != 1:
+            raise ValueError(f"{name} must be [{self._n_tok}][{heads}][{self.head_dim}] with "
+                             "contiguous rows")
+        return C.byref(KvRowsArg(t.data_ptr(), t.stride(0), t.stride(1)))
+
+    def _table(self, table):
+        if table.dim() != 2 or table.shape[0] < self._n_seq:
+            raise ValueError(f"table must have {self._n_seq} rows")
+        return _dev(table, self._torch.int32, "table"), table.shape[1]
+
+    def _call(self, f, tensors, *args):
+        """f(handle, *args) in order with the current stream."""
+        now = self._torch.cuda.current_stream(self.device)
+        if now.cuda_stream == self._sid:
+            self._check(f(self._h, *args))
+            return
+        if self._torch.cuda.is_current_stream_capturing():
+            raise ValueError("capture a graph on the handle's own stream")
+        self.stream.wait_stream(now)
+        try:
+            self._check(f(self._h, *args))
+        finally:
+            for t in tensors:
+                t.record_stream(self.stream)
+            now.wait_stream(self.stream)
+
+    # ------------------------------------------------------------------ calls
+    def new_pages(self, n_blocks: int) -> KvPages:
+        """Pages of one layer, not initialised."""
+        torch = self._torch
+        shape = (int(n_blocks), self.n_kv, self.block_size, self.head_dim)
+        kv = [torch.empty(shape, dtype=self.cache_dtype, device=self.device) for _ in range(2)]
+        if self.cache_dtype == torch.float8_e4m3fn:
+            kv += [torch.empty(shape[:3], dtype=torch.uint8, device=self.device) for _ in range(2)]
+        return KvPages(*kv)
+
+    def plan(self, q_len, ctx_len, window: int = 0, sinks: int = 0):
+        """The token batch of the calls that follow: new tokens per sequence and context
+        with them (host integers)."""
+        q = np.ascontiguousarray(q_len, np.int32)
+        c = np.ascontiguousarray(ctx_len, np.int32)
+        if q.ndim != 1 or q.shape != c.shape:
+            raise ValueError("q_len and ctx_len must be one-dimensional and of one length")
+        self._check(self._L.lar_kv_plan(self._h, len(q), q.ctypes.data, c.ctypes.data, int(window), int(sinks)))
+        self._n_seq, self._n_tok = len(q), int(q.sum())
+
+    def append(self, pages: KvPages, k, v, table):
+        """The batch's K and V rows [T][n_kv][head_dim] into the pages."""
+        p = self._pages(pages)
+        ka, va = self._rows(k, self.n_kv, "k"), self._rows(v, self.n_kv, "v")
+        self._call(self._L.lar_kv_append, (k, v, table, *pages.tensors()), p, ka, va, *self._table(table))
+
+    def read(self, pages: KvPages, table, k=None, v=None):
+        """The rows of the batch's tokens back from the pages: (k, v), each
+        [T][n_kv][head_dim] of dtype."""
+        torch = self._torch
+        shape = (self._n_tok, self.n_kv, self.head_dim)
+        if k is None:
+            k = torch.empty(shape, dtype=self.dtype, device=self.device)
+        if v is None:
+            v = torch.empty(shape, dtype=self.dtype, device=self.device)
+        p = self._pages(pages)
+        ka, va = self._rows(k, self.n_kv, "k"), self._rows(v, self.n_kv, "v")
+        self._call(self._L.lar_kv_read, (k, v, table, *pages.tensors()), p, *self._table(table), ka, va)
+        return k, v
+
+    def attend(self, pages: KvPages, q, table, scale=None, out=None, lse=None):
+        """Attention of the batch's queries [T][n_q][head_dim] over the pages; scale
+        defaults to head_dim ** -0.5.  Returns out [T][n_q][head_dim]; lse, when given, is
+        a float32 tensor [T][n_q] that takes the log of each row's sum."""
+        torch = self._torch
+        n = self._n_tok * self.n_q
+        if out is None:
+            out = torch.empty((self._n_tok, self.n_q, self.head_dim), dtype=self.dtype, device=self.device)
+        p, qa = self._pages(pages), self._rows(q, self.n_q, "q")
+        t = self._table(table)
+        held = (q, out, table, *pages.tensors()) if lse is None else (q, out, lse, table, *pages.tensors())
+        self._call(self._L.lar_kv_attend, held, p, qa, *t,
+                   1.0 / math.sqrt(self.head_dim) if scale is None else float(scale),
+                   _dev(out, self.dtype, "out", n * self.head_dim), _dev(lse, torch.float32, "lse", n))
+        return out
+
+    def sync(self):
+        """Synchronise; raises the sticky device error, if any."""
+        self._check(self._L.lar_kv_sync(self._h))

@@ -24,7 +24,9 @@ EXPORTED = ("lar_create", "lar_destroy", "lar_error_string", "lar_load_state", "
             "lar_stats", "lar_set_scheduler",
             "lar_ontime_utility", "lar_read_state", "lar_sync", "lar_trace_work", "lar_board_create",
             "lar_board_destroy", "lar_board_publish", "lar_board_collect",
-            "lar_whatif_noalloc", "lar_noalloc_error_string", "lar_estimate_lps")
+            "lar_whatif_noalloc", "lar_noalloc_error_string", "lar_estimate_lps",
+            "lar_kv_create", "lar_kv_destroy", "lar_kv_error_string", "lar_kv_plan", "lar_kv_append",
+            "lar_kv_read", "lar_kv_attend", "lar_kv_sync")
 LPS_POISSON, LPS_VARIABILITY = 0, 1
 
 
@@ -136,6 +138,23 @@ def load_library(path: str = LIB_PATH):
                                      vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     L.lar_noalloc_error_string.restype = C.c_char_p
     L.lar_noalloc_error_string.argtypes = []
+    # the paged key/value cache (kv.py): structures by reference
+    L.lar_kv_create.restype = i32
+    L.lar_kv_create.argtypes = [C.POINTER(vp), vp]
+    L.lar_kv_destroy.restype = i32
+    L.lar_kv_destroy.argtypes = [vp]
+    L.lar_kv_error_string.restype = C.c_char_p
+    L.lar_kv_error_string.argtypes = [vp]
+    L.lar_kv_plan.restype = i32
+    L.lar_kv_plan.argtypes = [vp, i32, vp, vp, i32, i32]
+    L.lar_kv_append.restype = i32
+    L.lar_kv_append.argtypes = [vp, vp, vp, vp, vp, i32]
+    L.lar_kv_read.restype = i32
+    L.lar_kv_read.argtypes = [vp, vp, vp, i32, vp, vp]
+    L.lar_kv_attend.restype = i32
+    L.lar_kv_attend.argtypes = [vp, vp, vp, vp, i32, dbl, vp, vp]
+    L.lar_kv_sync.restype = i32
+    L.lar_kv_sync.argtypes = [vp]
     _lib = L
     return L
 
