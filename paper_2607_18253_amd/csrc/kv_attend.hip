@@ -86,14 +86,20 @@ template <> struct Elem<false> {
   static constexpr uint32_t kExp = 0x7c00u;
 };
 
-// Whether one of the 8 16-bit values is an infinity or NaN.
+// Sets infinities and NaN among the 8 16-bit values to 0; whether there were any.
 template <bool BF>
-__device__ __forceinline__ bool not_finite(const uint4& x) {
-  const uint32_t e = Elem<BF>::kExp, eh = e << 16;
-  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+__device__ __forceinline__ bool clean(uint4& x) {
+  constexpr uint32_t e = Elem<BF>::kExp, eh = e << 16;
+  uint32_t w[4] = {x.x, x.y, x.z, x.w};
   bool bad = false;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) bad |= (w[i] & e) == e || (w[i] & eh) == eh;
+  for (int i = 0; i < 4; ++i) {
+    const bool lo = (w[i] & e) == e, hi = (w[i] & eh) == eh;
+    w[i] = lo ? w[i] & 0xffff0000u : w[i];
+    w[i] = hi ? w[i] & 0x0000ffffu : w[i];
+    bad |= lo || hi;
+  }
+  x = make_uint4(w[0], w[1], w[2], w[3]);
   return bad;
 }
 
@@ -119,17 +125,12 @@ __device__ __forceinline__ constexpr int key_of(int i, int h) {
   return (i & 3) + 8 * (i >> 2) + 4 * h;
 }
 
-// LDS tiles: [key][D] 16-bit values in 16-byte chunks.  The K reads take one chunk of 32
-// rows, the V reads 64 bytes of 8 rows; the chunks are permuted so that each covers the
-// banks evenly.
-template <int D>
-__device__ __forceinline__ int k_chunk(int row, int c) {
-  return D == 128 ? c ^ (row & 15) : c ^ ((row >> 1) & 7);
-}
-template <int D>
-__device__ __forceinline__ int v_chunk(int row, int c) {
-  return D == 128 ? c ^ ((row & 3) << 2) : c ^ (((row >> 1) & 1) << 2);
-}
+// LDS tiles: [key][D] 16-bit values, rows padded.  A K read takes 16 bytes at one place of
+// 32 rows: with 16 bytes of padding 16 rows cover the 64 banks.  A V read takes 64 bytes at
+// one place of 8 rows: rows 64 bytes apart, modulo the banks, cover them twice.
+template <int D> constexpr int kRowK = D * 2 + 16;
+template <int D> constexpr int kRowV = D * 2 + 64;
+template <int D, int K> constexpr int kTileBytes = K * (kRowK<D> + kRowV<D>);  // K, then V
 
 // A query tile in a wave: this lane's row and what its keys are.
 struct Row {
@@ -164,7 +165,7 @@ __device__ __forceinline__ f32x16 scores(const char* kt, const s16x8 (&q)[D / 16
   for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
   for (int t = 0; t < D / 16; ++t) {
-    const s16x8 k = *(const s16x8*)(kt + n * (D * 2) + k_chunk<D>(n, 2 * t + h) * 16);
+    const s16x8 k = *(const s16x8*)(kt + n * kRowK<D> + h * 16 + t * 32);
     s = Elem<BF>::mma(k, q[t], s);
   }
   return s;
@@ -216,10 +217,9 @@ __device__ __forceinline__ void weigh(const char* vt, const f32x16& p, Sums<D>& 
 #pragma unroll
     for (int b = 0; b < D / 32; ++b) {
       // 16 lanes read 4 keys x 16 values and get them by columns
-      const int c = 4 * b + 2 * (g & 1) + ((i & 3) >> 1);
-      const char* at = vt + (16 * t + row) * (D * 2) + v_chunk<D>(row, c) * 16 + (i & 1) * 8;
+      const char* at = vt + row * kRowV<D> + (g & 1) * 32 + (i & 3) * 8 + 16 * t * kRowV<D> + b * 64;
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 8 * (D * 2)));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 8 * kRowV<D>));
       s16x8 v;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -229,27 +229,6 @@ __device__ __forceinline__ void weigh(const char* vt, const f32x16& p, Sums<D>& 
       a.o[b] = Elem<BF>::mma(v, pk, a.o[b]);
     }
   }
-}
-
-// V rows with infinities or NaN that only some rows of the tile see would reach the
-// others as 0 * inf: such a row r (of 32) is added here, for the lanes whose rows see it;
-// the caller then clears it in LDS.
-template <bool BF, int D>
-__device__ __forceinline__ void weigh_row(const char* vt, int r, bool seen, const f32x16& p, Sums<D>& a,
-                                       int lane) {
-  const int h = lane >> 5;
-  float x = 0.0f;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) x = key_of(i, h) == r ? p[i] : x;
-  x = add_halves(x);
-#pragma unroll
-  for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int d = 32 * b + key_of(i, h);
-      const float v = Elem<BF>::value(*(const uint16_t*)(vt + r * (D * 2) + v_chunk<D>(r, d >> 3) * 16 + (d & 7) * 2));
-      a.o[b][i] = seen ? __builtin_fmaf(x, v, a.o[b][i]) : a.o[b][i];
-    }
 }
 
 // What a lane of a query tile is: its row's token and head, and what it sees.
@@ -338,21 +317,15 @@ struct Stage {
   static constexpr int kChunks = F8 ? D / 16 : D / 8;  // 16-byte chunks of a row in memory
   static constexpr int kStep = LANES / kChunks;        // rows of one load
   uint4 k[I], v[I];
-  uint32_t ke[F8 ? I : 1], ve[F8 ? I : 1];
 
   __device__ __forceinline__ void load(const KvPool& P, int i, uint32_t row, int c) {
     const int64_t at = (int64_t)row * kChunks + c;
     k[i] = ((const uint4*)P.k)[at];
     v[i] = ((const uint4*)P.v)[at];
-    if (F8) {
-      ke[i] = P.ke[row];
-      ve[i] = P.ve[row];
-    }
   }
-  // 16-bit chunks j (of 2 with 8-bit codes) of load i
-  static __device__ __forceinline__ uint4 widen(const uint4& x, uint32_t e, int j) {
+  // 16-bit chunk j (of 2 with 8-bit codes) of 16 bytes in memory; s: the row's scale
+  static __device__ __forceinline__ uint4 widen(const uint4& x, float s, int j) {
     if (!F8) return x;
-    const float s = __uint_as_float(e << 23);
     const uint32_t a = j ? x.z : x.x, b = j ? x.w : x.y;
     uint4 o;
     o.x = Elem<BF>::pair(a, s, false);
@@ -361,26 +334,30 @@ struct Stage {
     o.w = Elem<BF>::pair(b, s, true);
     return o;
   }
-  // Puts load i, row r of the tile, into LDS; a V row from `end` on holds nothing that a
-  // row of the tile sees and is cleared.  Returns whether V has infinities or NaN there.
+  // Puts load i, row r of the tile, into LDS.  Where rows of the tile see different keys a V
+  // row from `end` on, which none sees, is cleared, and so are infinities and NaN of the
+  // others: in the product they would reach rows that do not see them, as 0 * inf.  Returns
+  // whether there were any (spread() adds them).
   template <bool MASKED>
-  __device__ __forceinline__ bool put(char* kt, char* vt, int i, int r, int c, int end) const {
+  __device__ __forceinline__ bool put(char* kt, char* vt, int i, int r, int c, int end, float ks, float vs) const {
     bool bad = false;
 #pragma unroll
     for (int j = 0; j < (F8 ? 2 : 1); ++j) {
       const int cc = F8 ? 2 * c + j : c;
-      const uint4 x = widen(k[i], ke[F8 ? i : 0], j);
-      uint4 y = widen(v[i], ve[F8 ? i : 0], j);
+      const uint4 x = widen(k[i], ks, j);
+      uint4 y = widen(v[i], vs, j);
       if (MASKED) {
         if (r >= end) y = make_uint4(0, 0, 0, 0);
-        bad |= not_finite<BF>(y);
+        bad |= clean<BF>(y);
       }
-      *(uint4*)(kt + r * (D * 2) + k_chunk<D>(r, cc) * 16) = x;
-      *(uint4*)(vt + r * (D * 2) + v_chunk<D>(r, cc) * 16) = y;
+      *(uint4*)(kt + r * kRowK<D> + cc * 16) = x;
+      *(uint4*)(vt + r * kRowV<D> + cc * 16) = y;
     }
     return bad;
   }
 };
+
+__device__ __forceinline__ float scale_of(uint32_t exp) { return __uint_as_float((exp & 0xff) << 23); }
 
 // Row of the pool that holds key j (j inside the sequence's table) of a kv head; a page
 // outside the pool sets the sticky error and reads page 0.
@@ -393,11 +370,55 @@ __device__ __forceinline__ uint32_t pool_row(const KvAttendArgs& A, int head, in
          (uint32_t)(j & ((1 << A.g.sh) - 1));
 }
 
+// Whether some rows of a query tile may not see all the K keys from kb on: the tile reaches
+// past the first row's position or before the last row's window.
+__device__ __forceinline__ bool is_masked(const KvAttendArgs& A, const KvSeg& s, int kb, int K) {
+  return kb + K - 1 > s.p0 || (A.window && kb <= s.p0 + s.ntok - 1 - A.window && kb + K > A.sinks);
+}
+
+// Adds what clean() took out of V in the stretch's masked tiles to the rows that see it, in
+// the result or the partial sums that the wave has just written: w * inf is inf whatever the
+// weight w.  `row0`: the wave's first row in the query tile.
+template <bool BF, bool F8, int D, int K>
+__device__ __forceinline__ void spread(const KvAttendArgs& A, const KvSeg& s, int lane, int row0, int rows,
+                                       float* po) {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+  const int last = s.p0 + s.ntok - 1, G = A.g.G;
+  for (int t = s.t0; t < s.t1; ++t) {
+    const int kb = tile_key<K>(s, t);
+    if (!is_masked(A, s, kb, K)) continue;
+    for (int j = kb; j < kb + K && j <= last; ++j) {
+      const uint32_t row = pool_row(A, s.head, A.table[(int64_t)s.seq * A.cols + (j >> A.g.sh)], j);
+      for (int d = lane; d < D; d += 64) {
+        float v;
+        if (F8) {
+          const uint32_t c = ((const uint8_t*)A.pool.v)[(int64_t)row * D + d];
+          v = Elem<BF>::value((uint16_t)Elem<BF>::pair(c, scale_of(A.pool.ve[row]), false));
+        } else {
+          v = Elem<BF>::value(((const uint16_t*)A.pool.v)[(int64_t)row * D + d]);
+        }
+        if (__builtin_isfinite(v)) continue;
+        for (int n = row0; n < row0 + 32 && n < s.ntok * G; ++n) {
+          const int u = n / G, pos = s.p0 + u;
+          const Row r{pos, A.window ? pos - A.window : -1, A.sinks};
+          if (!r.sees(j)) continue;
+          if (s.slot >= 0) {
+            po[((int64_t)s.slot * rows + n) * D + d] += v;
+          } else {
+            uint16_t* o = (uint16_t*)A.out + ((int64_t)(s.q0 + u) * A.g.hq + s.head * G + n - u * G) * D + d;
+            *o = Elem<BF>::one(Elem<BF>::value(*o) + v);
+          }
+        }
+      }
+    }
+  }
+}
+
 // ------------------------------------------------------------------ narrow tiles
 template <bool BF, bool F8, int D>
 __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
-  __shared__ __align__(16) char lds[2 * kNarrowKeys * D * 2];
-  char *kt = lds, *vt = lds + kNarrowKeys * D * 2;
+  __shared__ __align__(16) char lds[kTileBytes<D, kNarrowKeys>];
+  char *kt = lds, *vt = lds + kNarrowKeys * kRowK<D>;
   using St = Stage<BF, F8, D, kNarrowKeys * (F8 ? D / 16 : D / 8) / 64, 64>;
   constexpr int I = kNarrowKeys / St::kStep;
   const int lane = threadIdx.x, n = lane & 31, h = lane >> 5;
@@ -417,35 +438,31 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
       return j < last ? j : last;
     };
     St st;
+    uint32_t ex = 0;  // exponents of this lane's row n: K, and V << 8
     const auto fetch = [&](int32_t page, int j) {
       const uint32_t row = pool_row(A, s.head, page, j);
 #pragma unroll
       for (int i = 0; i < I; ++i)
         st.load(A.pool, i, (uint32_t)__shfl((int)row, i * St::kStep + r0), c);
+      if (F8) ex = A.pool.ke[row] | (uint32_t)A.pool.ve[row] << 8;
     };
     int32_t page = 0;
     if (s.t0 < s.t1) {
       fetch(table[key(s.t0) >> A.g.sh], key(s.t0));
       if (s.t0 + 1 < s.t1) page = table[key(s.t0 + 1) >> A.g.sh];
     }
+    bool bad = false;
     for (int t = s.t0; t < s.t1; ++t) {
       const int kb = tile_key<kNarrowKeys>(s, t);
-      // every row sees all of the tile's keys unless it reaches past the first row's
-      // position or before the last row's window
-      const bool masked = kb + kNarrowKeys - 1 > s.p0 ||
-                          (A.window && kb <= last - A.window && kb + kNarrowKeys > A.sinks);
-      uint32_t bad = 0;
-      if (masked) {
+      const bool masked = is_masked(A, s, kb, kNarrowKeys);
 #pragma unroll
-        for (int i = 0; i < I; ++i) {
-          const uint64_t m = __ballot(st.template put<true>(kt, vt, i, i * St::kStep + r0, c, last + 1 - kb));
-          if (m)
-            for (int r = 0; r < St::kStep; ++r)
-              if (m >> (r * St::kChunks) & ((1ull << St::kChunks) - 1)) bad |= 1u << (i * St::kStep + r);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < I; ++i) st.template put<false>(kt, vt, i, i * St::kStep + r0, c, 0);
+      for (int i = 0; i < I; ++i) {
+        const int r = i * St::kStep + r0;
+        const uint32_t e = F8 ? (uint32_t)__shfl((int)ex, r) : 0;
+        if (masked)
+          bad |= st.template put<true>(kt, vt, i, r, c, last + 1 - kb, scale_of(e), scale_of(e >> 8));
+        else
+          st.template put<false>(kt, vt, i, r, c, 0, scale_of(e), scale_of(e >> 8));
       }
       if (t + 1 < s.t1) {
         fetch(page, key(t + 1));
@@ -459,28 +476,20 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
           sc[0][i] = ln.row.sees(kb + key_of(i, h)) ? sc[0][i] : -__builtin_inff();
       }
       soften<D, 1>(sc, a, A.scale);
-      if (masked && bad) {
-        for (uint32_t w = bad; w; w &= w - 1) {
-          const int r = __builtin_ctz(w);
-          weigh_row<BF, D>(vt, r, ln.row.sees(kb + r), sc[0], a, lane);
-          wave_order();
-          if (lane < D / 8) *(uint4*)(vt + r * (D * 2) + lane * 16) = make_uint4(0, 0, 0, 0);
-          wave_order();
-        }
-      }
       weigh<BF, D>(vt, sc[0], a, lane);
       wave_order();
     }
     finish<BF, D>(A, ln, a, lane, s.slot, 0, kNarrowRows, A.narrow_o, A.narrow_ml);
+    if (__any(bad)) spread<BF, F8, D, kNarrowKeys>(A, s, lane, 0, kNarrowRows, A.narrow_o);
   }
 }
 
 // ------------------------------------------------------------------ wide tiles
 template <bool BF, bool F8, int D>
 __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) {
-  constexpr int kTile = kWideKeys * D * 2, kThreads = 64 * kWideWaves;
-  __shared__ __align__(16) char lds[4 * kTile];  // K and V, two tiles
-  __shared__ int flag[2];
+  constexpr int kTile = kTileBytes<D, kWideKeys>, kThreads = 64 * kWideWaves;
+  __shared__ __align__(16) char lds[2 * kTile];
+  __shared__ int flag;
   using St = Stage<BF, F8, D, (kWideKeys * (F8 ? D / 16 : D / 8) + kThreads - 1) / kThreads, kThreads>;
   constexpr int I = (kWideKeys + St::kStep - 1) / St::kStep;
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5, wave = tid >> 6;
@@ -502,6 +511,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
     const int32_t* table = A.table + (int64_t)s.seq * A.cols;
     St st;
     int32_t page[I];
+    float ks[I], vs[I];
     const auto key = [&](int t, int i) {
       const int j = tile_key<kWideKeys>(s, t) + i * St::kStep + r0;
       return j < last ? j : last;
@@ -514,49 +524,52 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
     const auto fetch = [&](int t) {
 #pragma unroll
       for (int i = 0; i < I; ++i)
-        if (loads) st.load(A.pool, i, pool_row(A, s.head, page[i], key(t, i)), c);
-    };
-    const auto is_masked = [&](int kb) {
-      return kb + kWideKeys - 1 > s.p0 || (A.window && kb <= last - A.window && kb + kWideKeys > A.sinks);
+        if (loads) {
+          const uint32_t row = pool_row(A, s.head, page[i], key(t, i));
+          st.load(A.pool, i, row, c);
+          if (F8) {
+            ks[i] = scale_of(A.pool.ke[row]);
+            vs[i] = scale_of(A.pool.ve[row]);
+          }
+        }
     };
     const auto put = [&](int t, int b) {
       const int kb = tile_key<kWideKeys>(s, t);
-      char *kt = lds + b * 2 * kTile, *vt = kt + kTile;
+      char *kt = lds + b * kTile, *vt = kt + kWideKeys * kRowK<D>;
       if (!loads) return;
-      if (is_masked(kb)) {
+      if (is_masked(A, s, kb, kWideKeys)) {
         bool bad = false;
 #pragma unroll
         for (int i = 0; i < I; ++i)
-          bad |= st.template put<true>(kt, vt, i, i * St::kStep + r0, c, last + 1 - kb);
-        if (bad) flag[b] = t + 1;
+          bad |= st.template put<true>(kt, vt, i, i * St::kStep + r0, c, last + 1 - kb, ks[i], vs[i]);
+        if (bad) flag = 1;
       } else {
 #pragma unroll
-        for (int i = 0; i < I; ++i) st.template put<false>(kt, vt, i, i * St::kStep + r0, c, 0);
+        for (int i = 0; i < I; ++i) st.template put<false>(kt, vt, i, i * St::kStep + r0, c, 0, ks[i], vs[i]);
       }
     };
-    if (tid < 2) flag[tid] = 0;
+    __syncthreads();  // the last stretch's tiles and flag are done with
+    if (tid == 0) flag = 0;
     if (s.t0 < s.t1) {
       look(s.t0);
       fetch(s.t0);
       if (s.t0 + 1 < s.t1) look(s.t0 + 1);
     }
-    __syncthreads();  // the flags; and the last stretch's tiles are done with
+    __syncthreads();
     if (s.t0 < s.t1) put(s.t0, s.t0 & 1);
     __syncthreads();
     for (int t = s.t0; t < s.t1; ++t) {
       const int b = t & 1, kb = tile_key<kWideKeys>(s, t);
-      char *kt = lds + b * 2 * kTile, *vt = kt + kTile;
+      char *kt = lds + b * kTile, *vt = kt + kWideKeys * kRowK<D>;
       if (t + 1 < s.t1) {
         fetch(t + 1);
         if (t + 2 < s.t1) look(t + 2);
       }
-      const bool masked = is_masked(kb);
-      const bool works = wreal && kb <= wlast;
-      f32x16 sc[2];
-      if (works) {
+      if (wreal && kb <= wlast) {
+        f32x16 sc[2];
         sc[0] = scores<BF, D>(kt, q, n, h);
-        sc[1] = scores<BF, D>(kt + 32 * D * 2, q, n, h);
-        if (masked) {
+        sc[1] = scores<BF, D>(kt + 32 * kRowK<D>, q, n, h);
+        if (is_masked(A, s, kb, kWideKeys)) {
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -564,30 +577,14 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
               sc[u][i] = ln.row.sees(kb + 32 * u + key_of(i, h)) ? sc[u][i] : -__builtin_inff();
         }
         soften<D, 2>(sc, a, A.scale);
-      }
-      if (masked && flag[b] == t + 1) {  // the same for all waves
-        for (int r = 0; r < kWideKeys; ++r) {
-          char* row = vt + r * (D * 2);
-          if (!__any(lane < D / 8 && not_finite<BF>(*(const uint4*)(row + (lane % (D / 8)) * 16)))) continue;
-          if (works) weigh_row<BF, D>(vt + (r & 32) * (D * 2), r & 31, ln.row.sees(kb + r), sc[r >> 5], a, lane);
-        }
-        __syncthreads();
-        for (int r = wave; r < kWideKeys; r += kWideWaves) {
-          char* row = vt + r * (D * 2);
-          const bool mine = lane < D / 8;
-          if (__any(mine && not_finite<BF>(*(const uint4*)(row + (lane % (D / 8)) * 16))) && mine)
-            *(uint4*)(row + lane * 16) = make_uint4(0, 0, 0, 0);
-        }
-        __syncthreads();
-      }
-      if (works) {
         weigh<BF, D>(vt, sc[0], a, lane);
-        weigh<BF, D>(vt + 32 * D * 2, sc[1], a, lane);
+        weigh<BF, D>(vt + 32 * kRowV<D>, sc[1], a, lane);
       }
       if (t + 1 < s.t1) put(t + 1, b ^ 1);
       __syncthreads();
     }
     finish<BF, D>(A, ln, a, lane, s.slot, wave * 32, kWideRows, A.wide_o, A.wide_ml);
+    if (flag) spread<BF, F8, D, kWideKeys>(A, s, lane, wave * 32, kWideRows, A.wide_o);
   }
 }
 
