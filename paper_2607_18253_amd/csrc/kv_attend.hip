@@ -359,14 +359,12 @@ struct Stage {
 
 __device__ __forceinline__ float scale_of(uint32_t exp) { return __uint_as_float((exp & 0xff) << 23); }
 
-// Row of the pool that holds key j (j inside the sequence's table) of a kv head; a page
-// outside the pool sets the sticky error and reads page 0.
-__device__ __forceinline__ uint32_t pool_row(const KvAttendArgs& A, int head, int32_t page, int j) {
-  if ((uint32_t)page >= A.pool.n_blocks) {
-    *A.err = LAR_E_STATE;
-    page = 0;
-  }
-  return (((uint32_t)page * (uint32_t)A.g.hkv + (uint32_t)head) << A.g.sh) +
+// Row of the pool that holds key j (j inside the sequence's table) of a kv head; for a page
+// outside the pool sets `lost` and takes page 0.
+__device__ __forceinline__ uint32_t pool_row(const KvAttendArgs& A, int head, int32_t page, int j, bool& lost) {
+  const bool in = (uint32_t)page < A.pool.n_blocks;
+  lost |= !in;
+  return (((in ? (uint32_t)page : 0u) * (uint32_t)A.g.hkv + (uint32_t)head) << A.g.sh) +
          (uint32_t)(j & ((1 << A.g.sh) - 1));
 }
 
@@ -388,7 +386,8 @@ __device__ __forceinline__ void spread(const KvAttendArgs& A, const KvSeg& s, in
     const int kb = tile_key<K>(s, t);
     if (!is_masked(A, s, kb, K)) continue;
     for (int j = kb; j < kb + K && j <= last; ++j) {
-      const uint32_t row = pool_row(A, s.head, A.table[(int64_t)s.seq * A.cols + (j >> A.g.sh)], j);
+      bool lost = false;  // reported before
+      const uint32_t row = pool_row(A, s.head, A.table[(int64_t)s.seq * A.cols + (j >> A.g.sh)], j, lost);
       for (int d = lane; d < D; d += 64) {
         float v;
         if (F8) {
@@ -424,6 +423,7 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
   const int lane = threadIdx.x, n = lane & 31, h = lane >> 5;
   const int r0 = lane / St::kChunks, c = lane % St::kChunks;
   const int e = A.narrow_at[blockIdx.x + 1];
+  bool lost = false;  // a page outside the pool
   for (int x = A.narrow_at[blockIdx.x]; x < e; ++x) {
     const KvSeg s = A.narrow[x];
     const Lane ln = lane_of(A, s, n);
@@ -440,7 +440,7 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
     St st;
     uint32_t ex = 0;  // exponents of this lane's row n: K, and V << 8
     const auto fetch = [&](int32_t page, int j) {
-      const uint32_t row = pool_row(A, s.head, page, j);
+      const uint32_t row = pool_row(A, s.head, page, j, lost);
 #pragma unroll
       for (int i = 0; i < I; ++i)
         st.load(A.pool, i, (uint32_t)__shfl((int)row, i * St::kStep + r0), c);
@@ -482,6 +482,7 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
     finish<BF, D>(A, ln, a, lane, s.slot, 0, kNarrowRows, A.narrow_o, A.narrow_ml);
     if (__any(bad)) spread<BF, F8, D, kNarrowKeys>(A, s, lane, 0, kNarrowRows, A.narrow_o);
   }
+  if (lost) *A.err = LAR_E_STATE;
 }
 
 // ------------------------------------------------------------------ wide tiles
@@ -496,6 +497,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
   const int r0 = tid / St::kChunks, c = tid % St::kChunks;
   const bool loads = r0 < kWideKeys;  // narrow 8-bit rows need fewer threads
   const int e = A.wide_at[blockIdx.x + 1];
+  bool lost = false;  // a page outside the pool
   for (int x = A.wide_at[blockIdx.x]; x < e; ++x) {
     const KvSeg s = A.wide[x];
     const Lane ln = lane_of(A, s, wave * 32 + n);
@@ -525,7 +527,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
 #pragma unroll
       for (int i = 0; i < I; ++i)
         if (loads) {
-          const uint32_t row = pool_row(A, s.head, page[i], key(t, i));
+          const uint32_t row = pool_row(A, s.head, page[i], key(t, i), lost);
           st.load(A.pool, i, row, c);
           if (F8) {
             ks[i] = scale_of(A.pool.ke[row]);
@@ -557,6 +559,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
     }
     __syncthreads();
     if (s.t0 < s.t1) put(s.t0, s.t0 & 1);
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): or every tile would wait for its next loads with q's
     __syncthreads();
     for (int t = s.t0; t < s.t1; ++t) {
       const int b = t & 1, kb = tile_key<kWideKeys>(s, t);
@@ -586,6 +589,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
     finish<BF, D>(A, ln, a, lane, s.slot, wave * 32, kWideRows, A.wide_o, A.wide_ml);
     if (flag) spread<BF, F8, D, kWideKeys>(A, s, lane, wave * 32, kWideRows, A.wide_o);
   }
+  if (lost) *A.err = LAR_E_STATE;
 }
 
 // ------------------------------------------------------------------ joining split tiles
