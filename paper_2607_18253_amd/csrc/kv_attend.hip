@@ -103,6 +103,34 @@ __device__ __forceinline__ bool clean(uint4& x) {
   return bad;
 }
 
+// A value that is not known before this point, so that what is made of it is made here and
+// not kept in registers across the loops around.
+template <class T>
+__device__ __forceinline__ T here(T x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// The plan's arrays are not written while a kernel runs: scalar loads.
+template <class T>
+__device__ __forceinline__ T plan_at(const T* p, int i) {
+  constexpr int n = sizeof(T) / 4;
+  const auto* w = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(p + i);
+  int32_t x[n];
+#pragma unroll
+  for (int k = 0; k < n; ++k) x[k] = w[k];
+  T t;
+  __builtin_memcpy(&t, x, sizeof t);
+  return t;
+}
+
+// The run of stretches of this workgroup, of n.  Workgroups go to the 8 XCDs in turn; runs
+// that follow one another, which read the same keys or their neighbours, go to one XCD's L2.
+__device__ __forceinline__ int run_of(int n) {
+  const int x = blockIdx.x & 7, r = n & 7;
+  return x * (n >> 3) + (x < r ? x : r) + (blockIdx.x >> 3);
+}
+
 // The larger, or the sum, of a lane's value and that of lane ^ 32.
 __device__ __forceinline__ float max_halves(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -118,6 +146,13 @@ __device__ __forceinline__ void wave_order() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// A barrier of the workgroup for its LDS alone: loads from memory stay on their way.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
 // Key of element i of S^T's 32 keys in a lane of half h.
@@ -142,16 +177,31 @@ struct Row {
   }
 };
 
+// Takes the scores of keys from kb on that the row does not see to -infinity.
+template <int NB>
+__device__ __forceinline__ void hide(f32x16 (&s)[NB], const Row& r, int kb, int h) {
+  const int base = kb + 4 * h;  // the keys of a lane: base + constants
+  const int pos = r.pos - base, lo = r.lo - base, sinks = r.sinks - base;
+#pragma unroll
+  for (int u = 0; u < NB; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int j = 32 * u + key_of(i, 0);
+      s[u][i] = j <= pos && (j > lo || j < sinks) ? s[u][i] : -__builtin_inff();
+    }
+}
+
 // The running sums of a wave's 32 rows.
 template <int D>
 struct Sums {
   f32x16 o[D / 32];  // O^T: row n, value 32 b + key_of(i, h)
   float m, l;        // maximum (log2 units); this half's part of the sum
   __device__ __forceinline__ void clear() {
+    const float z = here(0.0f);
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[b][i] = 0.0f;
+      for (int i = 0; i < 16; ++i) o[b][i] = z;
     m = -__builtin_inff();
     l = 0.0f;
   }
@@ -171,16 +221,21 @@ __device__ __forceinline__ f32x16 scores(const char* kt, const s16x8 (&q)[D / 16
   return s;
 }
 
-// Takes the scores of NB blocks of 32 keys into the running maximum and sum, rescaling
-// the rows' sums where their maximum grew; p: the exponentials.
-template <int D, int NB>
-__device__ __forceinline__ void soften(f32x16 (&s)[NB], Sums<D>& a, float c) {
+// The largest of a row's scores in NB blocks of 32 keys.
+template <int NB>
+__device__ __forceinline__ float peak(const f32x16 (&s)[NB]) {
   float mx = s[0][0];
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
-  mx = max_halves(mx) * c;
+  return max_halves(mx);
+}
+
+// Takes a tile's largest scores (times the scale: log2 units) into the running maximum,
+// rescaling the rows' sums where it grew.
+template <int D>
+__device__ __forceinline__ void raise(Sums<D>& a, float mx) {
   if (__any(mx > a.m + kLag)) {
     const float m = fmaxf(mx, a.m);
     const float f = m > a.m ? __builtin_amdgcn_exp2f(a.m - m) : 1.0f;  // 0 from a.m = -inf
@@ -191,6 +246,11 @@ __device__ __forceinline__ void soften(f32x16 (&s)[NB], Sums<D>& a, float c) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) a.o[b][i] *= f;
   }
+}
+
+// Scores to their exponentials, into the running sum.
+template <int D, int NB>
+__device__ __forceinline__ void soften(f32x16 (&s)[NB], Sums<D>& a, float c) {
   const float m = a.m == -__builtin_inff() ? 0.0f : a.m;
   float l = 0.0f;
 #pragma unroll
@@ -203,32 +263,92 @@ __device__ __forceinline__ void soften(f32x16 (&s)[NB], Sums<D>& a, float c) {
   a.l += l;
 }
 
+// V^T fragment of 16 keys and 32 values, `vt` the keys' rows in LDS: 16 lanes read 4 keys x
+// 16 values and get them by columns.
+template <int D>
+__device__ __forceinline__ s16x8 v_part(const char* vt, int b, int lane) {
+  const int h = lane >> 5, i = lane & 15, g = lane >> 4;
+  const char* at = vt + (4 * h + (i >> 2)) * kRowV<D> + (g & 1) * 32 + (i & 3) * 8 + b * 64;
+  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at));
+  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 8 * kRowV<D>));
+  s16x8 v;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[j] = lo[j];
+    v[4 + j] = hi[j];
+  }
+  return v;
+}
+
+// The exponentials of 16 keys, rounded, in the order of v_part's keys.
+template <bool BF>
+__device__ __forceinline__ s16x8 p_part(const f32x16& p, int t) {
+  f32x8 x;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = p[8 * t + j];
+  return Elem<BF>::pack(x);
+}
+
 // O^T += V^T P^T over 32 keys, `vt` their rows in LDS.
 template <bool BF, int D>
 __device__ __forceinline__ void weigh(const char* vt, const f32x16& p, Sums<D>& a, int lane) {
-  const int h = lane >> 5, i = lane & 15, g = lane >> 4;
-  const int row = 4 * h + (i >> 2);
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    f32x8 x;
+    const s16x8 pk = p_part<BF>(p, t);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = p[8 * t + j];
-    const s16x8 pk = Elem<BF>::pack(x);
+    for (int b = 0; b < D / 32; ++b) a.o[b] = Elem<BF>::mma(v_part<D>(vt + 16 * t * kRowV<D>, b, lane), pk, a.o[b]);
+  }
+}
+
+// Exponentials of 32 keys with scores `s` and their product with V (rows `vt`), beside the
+// scores of the next 32 keys (rows `kt`) into `next`; returns the maximum of those.
+// Exponentials and maxima run in the shadow of the matrix instructions, in the order written.
+template <bool BF, int D>
+__device__ __forceinline__ float weigh_and_score(const char* vt, const char* kt, const s16x8 (&q)[D / 16],
+                                                 f32x16 (&s)[1], f32x16 (&next)[1], Sums<D>& a, float c, int lane) {
+  constexpr int kSteps = D / 16, kEach = 16 / kSteps;  // scores' steps, exponentials beside each
+  const int n = lane & 31, h = lane >> 5;
+  const char* kp = kt + n * kRowK<D> + h * 16;
+  const float m = a.m == -__builtin_inff() ? 0.0f : a.m;
+  s16x8 k[2] = {*(const s16x8*)kp, *(const s16x8*)(kp + 32)};
+  s16x8 pk[2];
+  f32x16 x;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+  float l = 0.0f;
+#pragma unroll
+  for (int t = 0; t < kSteps; ++t) {
+    x = Elem<BF>::mma(k[t & 1], q[t], x);
+    if (t + 2 < kSteps) k[t & 1] = *(const s16x8*)(kp + (t + 2) * 32);
+#pragma unroll
+    for (int e = t * kEach; e < (t + 1) * kEach; ++e) {
+      const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][e], c, -m));
+      s[0][e] = y;
+      l += y;
+      if ((e & 7) == 7) pk[e >> 3] = here(p_part<BF>(s[0], e >> 3));
+    }
+    l = here(l);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  a.l += l;
+  float mx = x[0];
+  s16x8 v[D / 32];
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b) v[b] = v_part<D>(vt, b, lane);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
 #pragma unroll
     for (int b = 0; b < D / 32; ++b) {
-      // 16 lanes read 4 keys x 16 values and get them by columns
-      const char* at = vt + row * kRowV<D> + (g & 1) * 32 + (i & 3) * 8 + 16 * t * kRowV<D> + b * 64;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 8 * kRowV<D>));
-      s16x8 v;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        v[j] = lo[j];
-        v[4 + j] = hi[j];
-      }
-      a.o[b] = Elem<BF>::mma(v, pk, a.o[b]);
+      a.o[b] = Elem<BF>::mma(v[b], pk[t], a.o[b]);
+      if (t < 1) v[b] = v_part<D>(vt + 16 * kRowV<D>, b, lane);
     }
+#pragma unroll
+    for (int i = 8 * t; i < 8 * t + 8; ++i) mx = fmaxf(mx, x[i]);
+    __builtin_amdgcn_sched_barrier(0);
   }
+  next[0] = x;
+  return max_halves(mx);
 }
 
 // What a lane of a query tile is: its row's token and head, and what it sees.
@@ -252,7 +372,7 @@ __device__ __forceinline__ Lane lane_of(const KvAttendArgs& A, const KvSeg& s, i
 }
 
 template <int D>
-__device__ __forceinline__ void load_q(const KvAttendArgs& A, const Lane& x, int h, s16x8 (&q)[D / 16]) {
+__device__ __forceinline__ Row load_q(const KvAttendArgs& A, const Lane& x, int h, s16x8 (&q)[D / 16]) {
   const int16_t* p = (const int16_t*)A.q.p + (int64_t)x.tok * A.q.tok + (int64_t)x.qh * A.q.head;
 #pragma unroll
   for (int t = 0; t < D / 16; ++t) {
@@ -260,14 +380,17 @@ __device__ __forceinline__ void load_q(const KvAttendArgs& A, const Lane& x, int
     if (x.real) z = *(const s16x8*)(p + 16 * t + 8 * h);
     q[t] = z;
   }
+  return x.row;
 }
 
 // The result of a wave's rows, or their partial sums (`row0`: first row of the wave in the
 // slot, `rows` of a slot).
 template <bool BF, int D>
-__device__ __forceinline__ void finish(const KvAttendArgs& A, const Lane& x, const Sums<D>& a, int lane,
-                                       int slot, int row0, int rows, float* po, float2* pml) {
-  const int n = lane & 31, h = lane >> 5;
+__device__ __forceinline__ void finish(const KvAttendArgs& A, const KvSeg& s, const Sums<D>& a, int lane,
+                                       int row0, int rows, float* po, float2* pml) {
+  lane = here(lane);
+  const int n = lane & 31, h = lane >> 5, slot = s.slot;
+  const Lane x = lane_of(A, s, row0 + n);
   const float l = add_halves(a.l);
   if (!x.real) return;
   if (slot >= 0) {
@@ -318,10 +441,11 @@ struct Stage {
   static constexpr int kStep = LANES / kChunks;        // rows of one load
   uint4 k[I], v[I];
 
-  __device__ __forceinline__ void load(const KvPool& P, int i, uint32_t row, int c) {
-    const int64_t at = (int64_t)row * kChunks + c;
-    k[i] = ((const uint4*)P.k)[at];
-    v[i] = ((const uint4*)P.v)[at];
+  __device__ __forceinline__ void load_k(const KvPool& P, int i, uint32_t row, int c) {
+    k[i] = ((const uint4*)P.k)[(int64_t)row * kChunks + c];
+  }
+  __device__ __forceinline__ void load_v(const KvPool& P, int i, uint32_t row, int c) {
+    v[i] = ((const uint4*)P.v)[(int64_t)row * kChunks + c];
   }
   // 16-bit chunk j (of 2 with 8-bit codes) of 16 bytes in memory; s: the row's scale
   static __device__ __forceinline__ uint4 widen(const uint4& x, float s, int j) {
@@ -334,24 +458,27 @@ struct Stage {
     o.w = Elem<BF>::pair(b, s, true);
     return o;
   }
-  // Puts load i, row r of the tile, into LDS.  Where rows of the tile see different keys a V
-  // row from `end` on, which none sees, is cleared, and so are infinities and NaN of the
-  // others: in the product they would reach rows that do not see them, as 0 * inf.  Returns
-  // whether there were any (spread() adds them).
+  // Puts load i, row r of the tile, into LDS.
+  __device__ __forceinline__ void put_k(char* kt, int i, int r, int c, float scale) const {
+#pragma unroll
+    for (int j = 0; j < (F8 ? 2 : 1); ++j)
+      *(uint4*)(kt + r * kRowK<D> + (F8 ? 2 * c + j : c) * 16) = widen(k[i], scale, j);
+  }
+  // The same.  Where rows of the query tile see different keys a V row from `end` on, which
+  // none sees, is cleared, and so are infinities and NaN of the others: in the product they
+  // would reach rows that do not see them, as 0 * inf.  Returns whether there were any
+  // (spread() adds them).
   template <bool MASKED>
-  __device__ __forceinline__ bool put(char* kt, char* vt, int i, int r, int c, int end, float ks, float vs) const {
+  __device__ __forceinline__ bool put_v(char* vt, int i, int r, int c, int end, float scale) const {
     bool bad = false;
 #pragma unroll
     for (int j = 0; j < (F8 ? 2 : 1); ++j) {
-      const int cc = F8 ? 2 * c + j : c;
-      const uint4 x = widen(k[i], ks, j);
-      uint4 y = widen(v[i], vs, j);
+      uint4 y = widen(v[i], scale, j);
       if (MASKED) {
         if (r >= end) y = make_uint4(0, 0, 0, 0);
         bad |= clean<BF>(y);
       }
-      *(uint4*)(kt + r * kRowK<D> + cc * 16) = x;
-      *(uint4*)(vt + r * kRowV<D> + cc * 16) = y;
+      *(uint4*)(vt + r * kRowV<D> + (F8 ? 2 * c + j : c) * 16) = y;
     }
     return bad;
   }
@@ -380,6 +507,7 @@ __device__ __forceinline__ bool is_masked(const KvAttendArgs& A, const KvSeg& s,
 template <bool BF, bool F8, int D, int K>
 __device__ __forceinline__ void spread(const KvAttendArgs& A, const KvSeg& s, int lane, int row0, int rows,
                                        float* po) {
+  lane = here(lane);
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
   const int last = s.p0 + s.ntok - 1, G = A.g.G;
   for (int t = s.t0; t < s.t1; ++t) {
@@ -422,13 +550,12 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
   constexpr int I = kNarrowKeys / St::kStep;
   const int lane = threadIdx.x, n = lane & 31, h = lane >> 5;
   const int r0 = lane / St::kChunks, c = lane % St::kChunks;
-  const int e = A.narrow_at[blockIdx.x + 1];
+  const int run = run_of(A.n_narrow), e = plan_at(A.narrow_at, run + 1);
   bool lost = false;  // a page outside the pool
-  for (int x = A.narrow_at[blockIdx.x]; x < e; ++x) {
-    const KvSeg s = A.narrow[x];
-    const Lane ln = lane_of(A, s, n);
+  for (int x = plan_at(A.narrow_at, run); x < e; ++x) {
+    const KvSeg s = plan_at(A.narrow, x);
     s16x8 q[D / 16];
-    load_q<D>(A, ln, h, q);
+    const Row row = load_q<D>(A, lane_of(A, s, n), h, q);
     Sums<D> a;
     a.clear();
     const int last = s.p0 + s.ntok - 1;  // position of the last token: keys 0 .. last
@@ -440,11 +567,14 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
     St st;
     uint32_t ex = 0;  // exponents of this lane's row n: K, and V << 8
     const auto fetch = [&](int32_t page, int j) {
-      const uint32_t row = pool_row(A, s.head, page, j, lost);
+      const uint32_t src = pool_row(A, s.head, page, j, lost);
 #pragma unroll
-      for (int i = 0; i < I; ++i)
-        st.load(A.pool, i, (uint32_t)__shfl((int)row, i * St::kStep + r0), c);
-      if (F8) ex = A.pool.ke[row] | (uint32_t)A.pool.ve[row] << 8;
+      for (int i = 0; i < I; ++i) {
+        const uint32_t at = (uint32_t)__shfl((int)src, i * St::kStep + r0);
+        st.load_k(A.pool, i, at, c);
+        st.load_v(A.pool, i, at, c);
+      }
+      if (F8) ex = A.pool.ke[src] | (uint32_t)A.pool.ve[src] << 8;
     };
     int32_t page = 0;
     if (s.t0 < s.t1) {
@@ -459,10 +589,11 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
       for (int i = 0; i < I; ++i) {
         const int r = i * St::kStep + r0;
         const uint32_t e = F8 ? (uint32_t)__shfl((int)ex, r) : 0;
+        st.put_k(kt, i, r, c, scale_of(e));
         if (masked)
-          bad |= st.template put<true>(kt, vt, i, r, c, last + 1 - kb, scale_of(e), scale_of(e >> 8));
+          bad |= st.template put_v<true>(vt, i, r, c, last + 1 - kb, scale_of(e >> 8));
         else
-          st.template put<false>(kt, vt, i, r, c, 0, scale_of(e), scale_of(e >> 8));
+          st.template put_v<false>(vt, i, r, c, 0, scale_of(e >> 8));
       }
       if (t + 1 < s.t1) {
         fetch(page, key(t + 1));
@@ -470,16 +601,13 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
       }
       wave_order();
       f32x16 sc[1] = {scores<BF, D>(kt, q, n, h)};
-      if (masked) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          sc[0][i] = ln.row.sees(kb + key_of(i, h)) ? sc[0][i] : -__builtin_inff();
-      }
+      if (masked) hide<1>(sc, row, kb, h);
+      raise<D>(a, peak<1>(sc) * A.scale);
       soften<D, 1>(sc, a, A.scale);
       weigh<BF, D>(vt, sc[0], a, lane);
       wave_order();
     }
-    finish<BF, D>(A, ln, a, lane, s.slot, 0, kNarrowRows, A.narrow_o, A.narrow_ml);
+    finish<BF, D>(A, s, a, lane, 0, kNarrowRows, A.narrow_o, A.narrow_ml);
     if (__any(bad)) spread<BF, F8, D, kNarrowKeys>(A, s, lane, 0, kNarrowRows, A.narrow_o);
   }
   if (lost) *A.err = LAR_E_STATE;
@@ -488,21 +616,21 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
 // ------------------------------------------------------------------ wide tiles
 template <bool BF, bool F8, int D>
 __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) {
-  constexpr int kTile = kTileBytes<D, kWideKeys>, kThreads = 64 * kWideWaves;
-  __shared__ __align__(16) char lds[2 * kTile];
+  constexpr int kTileK = kWideKeys * kRowK<D>, kTileV = kWideKeys * kRowV<D>, kThreads = 64 * kWideWaves;
+  __shared__ __align__(16) char ldk[3 * kTileK], ldv[2 * kTileV];
   __shared__ int flag;
   using St = Stage<BF, F8, D, (kWideKeys * (F8 ? D / 16 : D / 8) + kThreads - 1) / kThreads, kThreads>;
   constexpr int I = (kWideKeys + St::kStep - 1) / St::kStep;
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5, wave = tid >> 6;
   const int r0 = tid / St::kChunks, c = tid % St::kChunks;
-  const bool loads = r0 < kWideKeys;  // narrow 8-bit rows need fewer threads
-  const int e = A.wide_at[blockIdx.x + 1];
+  constexpr bool kAll = St::kStep <= kWideKeys;  // else 8-bit rows of 64 need half the threads
+  const bool loads = r0 < kWideKeys;
+  const int run = run_of(A.n_wide), e = plan_at(A.wide_at, run + 1);
   bool lost = false;  // a page outside the pool
-  for (int x = A.wide_at[blockIdx.x]; x < e; ++x) {
-    const KvSeg s = A.wide[x];
-    const Lane ln = lane_of(A, s, wave * 32 + n);
+  for (int x = plan_at(A.wide_at, run); x < e; ++x) {
+    const KvSeg s = plan_at(A.wide, x);
     s16x8 q[D / 16];
-    load_q<D>(A, ln, h, q);
+    const Row rw = load_q<D>(A, lane_of(A, s, wave * 32 + n), h, q);
     Sums<D> a;
     a.clear();
     const int last = s.p0 + s.ntok - 1;
@@ -512,81 +640,117 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
     const bool wreal = wave * 32 < s.ntok * A.g.G;
     const int32_t* table = A.table + (int64_t)s.seq * A.cols;
     St st;
-    int32_t page[I];
-    float ks[I], vs[I];
+    int32_t page[I];   // of the next tile whose K is fetched
+    uint32_t row[I];   // pool rows of the last tile whose K was fetched, the next V
+    uint32_t ks[I], vs[I];
+    // Loads are not skipped, so that what waits for one knows how many follow it: past the
+    // stretch's end they take the last tile, past the tile's rows the last key.
     const auto key = [&](int t, int i) {
-      const int j = tile_key<kWideKeys>(s, t) + i * St::kStep + r0;
+      const int j = tile_key<kWideKeys>(s, t < s.t1 ? t : s.t1 - 1) + (kAll ? i * St::kStep + r0 : r0 & (kWideKeys - 1));
       return j < last ? j : last;
     };
     const auto look = [&](int t) {
 #pragma unroll
-      for (int i = 0; i < I; ++i)
-        if (loads) page[i] = table[key(t, i) >> A.g.sh];
+      for (int i = 0; i < I; ++i) page[i] = table[key(t, i) >> A.g.sh];
     };
-    const auto fetch = [&](int t) {
+    const auto fetch_k = [&](int t, const uint32_t (&r)[I]) {
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+        st.load_k(A.pool, i, r[i], c);
+        if (F8) ks[i] = A.pool.ke[r[i]];
+      }
+    };
+    const auto fetch_v = [&]() {
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+        st.load_v(A.pool, i, row[i], c);
+        if (F8) vs[i] = A.pool.ve[row[i]];
+      }
+    };
+    const auto put_k = [&](int at) {
 #pragma unroll
       for (int i = 0; i < I; ++i)
-        if (loads) {
-          const uint32_t row = pool_row(A, s.head, page[i], key(t, i), lost);
-          st.load(A.pool, i, row, c);
-          if (F8) {
-            ks[i] = scale_of(A.pool.ke[row]);
-            vs[i] = scale_of(A.pool.ve[row]);
-          }
-        }
+        if (kAll || loads) st.put_k(ldk + at, i, i * St::kStep + r0, c, scale_of(ks[i]));
     };
-    const auto put = [&](int t, int b) {
-      const int kb = tile_key<kWideKeys>(s, t);
-      char *kt = lds + b * kTile, *vt = kt + kWideKeys * kRowK<D>;
-      if (!loads) return;
+    const auto put_v = [&](int t) {
+      const int kb = tile_key<kWideKeys>(s, t < s.t1 ? t : s.t1 - 1);
+      char* vt = ldv + (t & 1) * kTileV;
+      if (!kAll && !loads) return;
       if (is_masked(A, s, kb, kWideKeys)) {
         bool bad = false;
 #pragma unroll
         for (int i = 0; i < I; ++i)
-          bad |= st.template put<true>(kt, vt, i, i * St::kStep + r0, c, last + 1 - kb, ks[i], vs[i]);
+          bad |= st.template put_v<true>(vt, i, i * St::kStep + r0, c, last + 1 - kb, scale_of(vs[i]));
         if (bad) flag = 1;
       } else {
 #pragma unroll
-        for (int i = 0; i < I; ++i) st.template put<false>(kt, vt, i, i * St::kStep + r0, c, 0, ks[i], vs[i]);
+        for (int i = 0; i < I; ++i) st.template put_v<false>(vt, i, i * St::kStep + r0, c, 0, scale_of(vs[i]));
       }
+    };
+    const auto works = [&](int kb) { return wreal && kb <= wlast; };
+    // 32 keys from kb on, their scores in `sc`, their maximum taken: exponentials and the
+    // product with V, beside the scores of the 32 keys from nb on (past the wave's last key
+    // these are of any rows, and not used)
+    const auto half = [&](int kb, const char* vt, bool more, int nb, const char* kt, f32x16 (&sc)[1], f32x16 (&next)[1]) {
+      if (!works(kb)) return;
+      float mx = weigh_and_score<BF, D>(vt, kt, q, sc, next, a, A.scale, lane);
+      if (!more || !works(nb)) return;
+      if (is_masked(A, s, nb, 32)) {
+        hide<1>(next, rw, nb, h);
+        mx = peak<1>(next);
+      }
+      raise<D>(a, mx * A.scale);
     };
     __syncthreads();  // the last stretch's tiles and flag are done with
     if (tid == 0) flag = 0;
+    __syncthreads();
+    f32x16 sa[1], sb[1];
+    int kc = 0, kn = kTileK, kx = 2 * kTileK;  // K of this tile, the next and the one after
+    const auto rows = [&](int t, uint32_t (&r)[I]) {
+#pragma unroll
+      for (int i = 0; i < I; ++i) r[i] = pool_row(A, s.head, page[i], key(t, i), lost);
+    };
     if (s.t0 < s.t1) {
       look(s.t0);
-      fetch(s.t0);
-      if (s.t0 + 1 < s.t1) look(s.t0 + 1);
+      rows(s.t0, row);
+      fetch_k(s.t0, row);
+      fetch_v();
+      look(s.t0 + 1);
+      put_k(kc);
+      put_v(s.t0);
+      rows(s.t0 + 1, row);
+      fetch_k(s.t0 + 1, row);
+      look(s.t0 + 2);
+      put_k(kn);
     }
-    __syncthreads();
-    if (s.t0 < s.t1) put(s.t0, s.t0 & 1);
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): or every tile would wait for its next loads with q's
     __syncthreads();
-    for (int t = s.t0; t < s.t1; ++t) {
-      const int b = t & 1, kb = tile_key<kWideKeys>(s, t);
-      char *kt = lds + b * kTile, *vt = kt + kWideKeys * kRowK<D>;
-      if (t + 1 < s.t1) {
-        fetch(t + 1);
-        if (t + 2 < s.t1) look(t + 2);
-      }
-      if (wreal && kb <= wlast) {
-        f32x16 sc[2];
-        sc[0] = scores<BF, D>(kt, q, n, h);
-        sc[1] = scores<BF, D>(kt + 32 * kRowK<D>, q, n, h);
-        if (is_masked(A, s, kb, kWideKeys)) {
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              sc[u][i] = ln.row.sees(kb + 32 * u + key_of(i, h)) ? sc[u][i] : -__builtin_inff();
-        }
-        soften<D, 2>(sc, a, A.scale);
-        weigh<BF, D>(vt, sc[0], a, lane);
-        weigh<BF, D>(vt + 32 * kRowV<D>, sc[1], a, lane);
-      }
-      if (t + 1 < s.t1) put(t + 1, b ^ 1);
-      __syncthreads();
+    if (s.t0 < s.t1 && works(tile_key<kWideKeys>(s, s.t0))) {
+      sa[0] = scores<BF, D>(ldk, q, n, h);
+      if (is_masked(A, s, tile_key<kWideKeys>(s, s.t0), 32)) hide<1>(sa, rw, tile_key<kWideKeys>(s, s.t0), h);
+      raise<D>(a, peak<1>(sa) * A.scale);
     }
-    finish<BF, D>(A, ln, a, lane, s.slot, wave * 32, kWideRows, A.wide_o, A.wide_ml);
+    for (int t = s.t0; t < s.t1; ++t) {
+      uint32_t r[I];
+      rows(t + 2, r);
+      fetch_v();
+      fetch_k(t + 2, r);
+      look(t + 3);
+#pragma unroll
+      for (int i = 0; i < I; ++i) row[i] = r[i];
+      const char* vt = ldv + (t & 1) * kTileV;
+      const int kb = tile_key<kWideKeys>(s, t);
+      half(kb, vt, true, kb + 32, ldk + kc + 32 * kRowK<D>, sa, sb);
+      half(kb + 32, vt + 32 * kRowV<D>, t + 1 < s.t1, tile_key<kWideKeys>(s, t + 1), ldk + kn, sb, sa);
+      put_v(t + 1);
+      put_k(kx);
+      const int z = kc;
+      kc = kn;
+      kn = kx;
+      kx = z;
+      lds_barrier();
+    }
+    finish<BF, D>(A, s, a, lane, wave * 32, kWideRows, A.wide_o, A.wide_ml);
     if (flag) spread<BF, F8, D, kWideKeys>(A, s, lane, wave * 32, kWideRows, A.wide_o);
   }
   if (lost) *A.err = LAR_E_STATE;
@@ -599,7 +763,7 @@ constexpr int kJoinThreads = 512;
 
 template <bool BF, int D>
 __global__ __launch_bounds__(kJoinThreads) void k_kv_join(KvAttendArgs A) {
-  const KvJoin j = A.join[blockIdx.x];
+  const KvJoin j = plan_at(A.join, blockIdx.x);
   const int rows = j.wide ? kWideRows : kNarrowRows;
   const int row0 = blockIdx.y * 32;
   const int have = j.ntok * A.g.G - row0 < 32 ? j.ntok * A.g.G - row0 : 32;
