@@ -300,26 +300,35 @@ __device__ __forceinline__ void weigh(const char* vt, const f32x16& p, Sums<D>& 
   }
 }
 
+// K fragments that a wave has on their way from LDS ahead of their use.
+constexpr int kAhead = 4;
+
+template <int D>
+__device__ __forceinline__ s16x8 k_part(const char* kt, int t, int lane) {
+  return *(const s16x8*)(kt + (lane & 31) * kRowK<D> + (lane >> 5) * 16 + t * 32);
+}
+
 // Exponentials of 32 keys with scores `s` and their product with V (rows `vt`), beside the
-// scores of the next 32 keys (rows `kt`) into `next`; returns the maximum of those.
-// Exponentials and maxima run in the shadow of the matrix instructions, in the order written.
+// scores of the next 32 keys (rows `kt`, their first fragments in `k`) into `next`; returns
+// the maximum of those, and in `k` the first fragments of rows `kn`.  Exponentials and maxima
+// run in the shadow of the matrix instructions, LDS reads four of those ahead, in the order
+// written.
 template <bool BF, int D>
-__device__ __forceinline__ float weigh_and_score(const char* vt, const char* kt, const s16x8 (&q)[D / 16],
-                                                 f32x16 (&s)[1], f32x16 (&next)[1], Sums<D>& a, float c, int lane) {
-  constexpr int kSteps = D / 16, kEach = 16 / kSteps;  // scores' steps, exponentials beside each
-  const int n = lane & 31, h = lane >> 5;
-  const char* kp = kt + n * kRowK<D> + h * 16;
+__device__ __forceinline__ float weigh_and_score(const char* vt, const char* kt, const char* kn, s16x8 (&k)[kAhead],
+                                                 const s16x8 (&q)[D / 16], f32x16 (&s)[1], f32x16 (&next)[1],
+                                                 Sums<D>& a, float c, int lane) {
+  constexpr int kSteps = D / 16, kEach = 16 / kSteps, kB = D / 32;  // scores' steps, exponentials beside each
   const float m = a.m == -__builtin_inff() ? 0.0f : a.m;
-  s16x8 k[2] = {*(const s16x8*)kp, *(const s16x8*)(kp + 32)};
-  s16x8 pk[2];
+  s16x8 pk[2], v[kB];
   f32x16 x;
 #pragma unroll
   for (int i = 0; i < 16; ++i) x[i] = 0.0f;
   float l = 0.0f;
 #pragma unroll
   for (int t = 0; t < kSteps; ++t) {
-    x = Elem<BF>::mma(k[t & 1], q[t], x);
-    if (t + 2 < kSteps) k[t & 1] = *(const s16x8*)(kp + (t + 2) * 32);
+    x = Elem<BF>::mma(k[t % kAhead], q[t], x);
+    if (t + kAhead < kSteps) k[t % kAhead] = k_part<D>(kt, t + kAhead, lane);
+    if (t >= kSteps - kB) v[t - (kSteps - kB)] = v_part<D>(vt, t - (kSteps - kB), lane);
 #pragma unroll
     for (int e = t * kEach; e < (t + 1) * kEach; ++e) {
       const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][e], c, -m));
@@ -332,21 +341,21 @@ __device__ __forceinline__ float weigh_and_score(const char* vt, const char* kt,
   }
   a.l += l;
   float mx = x[0];
-  s16x8 v[D / 32];
 #pragma unroll
-  for (int b = 0; b < D / 32; ++b) v[b] = v_part<D>(vt, b, lane);
-  __builtin_amdgcn_sched_barrier(0);
+  for (int t = 0; t < 2; ++t)
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-#pragma unroll
-    for (int b = 0; b < D / 32; ++b) {
+    for (int b = 0; b < kB; ++b) {
       a.o[b] = Elem<BF>::mma(v[b], pk[t], a.o[b]);
-      if (t < 1) v[b] = v_part<D>(vt + 16 * kRowV<D>, b, lane);
-    }
+      if (t == 0)
+        v[b] = v_part<D>(vt + 16 * kRowV<D>, b, lane);
+      else {
 #pragma unroll
-    for (int i = 8 * t; i < 8 * t + 8; ++i) mx = fmaxf(mx, x[i]);
-    __builtin_amdgcn_sched_barrier(0);
-  }
+        for (int i = b * kAhead / kB; i < (b + 1) * kAhead / kB; ++i) k[i] = k_part<D>(kn, i, lane);
+#pragma unroll
+        for (int i = 16 * b / kB; i < 16 * (b + 1) / kB; ++i) mx = fmaxf(mx, x[i]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   next[0] = x;
   return max_halves(mx);
 }
@@ -441,11 +450,9 @@ struct Stage {
   static constexpr int kStep = LANES / kChunks;        // rows of one load
   uint4 k[I], v[I];
 
-  __device__ __forceinline__ void load_k(const KvPool& P, int i, uint32_t row, int c) {
-    k[i] = ((const uint4*)P.k)[(int64_t)row * kChunks + c];
-  }
-  __device__ __forceinline__ void load_v(const KvPool& P, int i, uint32_t row, int c) {
-    v[i] = ((const uint4*)P.v)[(int64_t)row * kChunks + c];
+  // from chunk c of row `row` of the pool, `base` the address of that chunk of row 0
+  static __device__ __forceinline__ uint4 load(const char* base, uint32_t row) {
+    return *(const uint4*)(base + (uint64_t)row * (kChunks * 16));
   }
   // 16-bit chunk j (of 2 with 8-bit codes) of 16 bytes in memory; s: the row's scale
   static __device__ __forceinline__ uint4 widen(const uint4& x, float s, int j) {
@@ -486,13 +493,17 @@ struct Stage {
 
 __device__ __forceinline__ float scale_of(uint32_t exp) { return __uint_as_float((exp & 0xff) << 23); }
 
-// Row of the pool that holds key j (j inside the sequence's table) of a kv head; for a page
-// outside the pool sets `lost` and takes page 0.
-__device__ __forceinline__ uint32_t pool_row(const KvAttendArgs& A, int head, int32_t page, int j, bool& lost) {
+// First row of a page in the pool; for a page outside it sets `lost` and takes page 0.
+__device__ __forceinline__ uint32_t page_at(const KvAttendArgs& A, int32_t page, bool& lost) {
   const bool in = (uint32_t)page < A.pool.n_blocks;
   lost |= !in;
-  return (((in ? (uint32_t)page : 0u) * (uint32_t)A.g.hkv + (uint32_t)head) << A.g.sh) +
-         (uint32_t)(j & ((1 << A.g.sh) - 1));
+  return (in ? (uint32_t)page : 0u) * ((uint32_t)A.g.hkv << A.g.sh);
+}
+
+// Row of key j in its page, of a kv head.  Keys past the last one that the table has are
+// read from the last page: rows of the pool, of which no use is made.
+__device__ __forceinline__ uint32_t in_page(const KvAttendArgs& A, int head, int j) {
+  return ((uint32_t)head << A.g.sh) + (uint32_t)(j & ((1 << A.g.sh) - 1));
 }
 
 // Whether some rows of a query tile may not see all the K keys from kb on: the tile reaches
@@ -515,7 +526,7 @@ __device__ __forceinline__ void spread(const KvAttendArgs& A, const KvSeg& s, in
     if (!is_masked(A, s, kb, K)) continue;
     for (int j = kb; j < kb + K && j <= last; ++j) {
       bool lost = false;  // reported before
-      const uint32_t row = pool_row(A, s.head, A.table[(int64_t)s.seq * A.cols + (j >> A.g.sh)], j, lost);
+      const uint32_t row = page_at(A, A.table[(int64_t)s.seq * A.cols + (j >> A.g.sh)], lost) + in_page(A, s.head, j);
       for (int d = lane; d < D; d += 64) {
         float v;
         if (F8) {
@@ -560,26 +571,28 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
     a.clear();
     const int last = s.p0 + s.ntok - 1;  // position of the last token: keys 0 .. last
     const int32_t* table = A.table + (int64_t)s.seq * A.cols;
-    const auto key = [&](int t) {
-      const int j = tile_key<kNarrowKeys>(s, t) + n;
-      return j < last ? j : last;
+    const int last_col = last >> A.g.sh;
+    const char *kp = (const char*)A.pool.k + c * 16, *vp = (const char*)A.pool.v + c * 16;
+    const auto look = [&](int t) {
+      const int col = (tile_key<kNarrowKeys>(s, t) + n) >> A.g.sh;
+      return table[col < last_col ? col : last_col];
     };
     St st;
     uint32_t ex = 0;  // exponents of this lane's row n: K, and V << 8
-    const auto fetch = [&](int32_t page, int j) {
-      const uint32_t src = pool_row(A, s.head, page, j, lost);
+    const auto fetch = [&](int32_t page, int t) {
+      const uint32_t src = page_at(A, page, lost) + in_page(A, s.head, tile_key<kNarrowKeys>(s, t) + n);
 #pragma unroll
       for (int i = 0; i < I; ++i) {
         const uint32_t at = (uint32_t)__shfl((int)src, i * St::kStep + r0);
-        st.load_k(A.pool, i, at, c);
-        st.load_v(A.pool, i, at, c);
+        st.k[i] = St::load(kp, at);
+        st.v[i] = St::load(vp, at);
       }
       if (F8) ex = A.pool.ke[src] | (uint32_t)A.pool.ve[src] << 8;
     };
     int32_t page = 0;
     if (s.t0 < s.t1) {
-      fetch(table[key(s.t0) >> A.g.sh], key(s.t0));
-      if (s.t0 + 1 < s.t1) page = table[key(s.t0 + 1) >> A.g.sh];
+      fetch(look(s.t0), s.t0);
+      if (s.t0 + 1 < s.t1) page = look(s.t0 + 1);
     }
     bool bad = false;
     for (int t = s.t0; t < s.t1; ++t) {
@@ -596,8 +609,8 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
           st.template put_v<false>(vt, i, r, c, 0, scale_of(e >> 8));
       }
       if (t + 1 < s.t1) {
-        fetch(page, key(t + 1));
-        if (t + 2 < s.t1) page = table[key(t + 2) >> A.g.sh];
+        fetch(page, t + 1);
+        if (t + 2 < s.t1) page = look(t + 2);
       }
       wave_order();
       f32x16 sc[1] = {scores<BF, D>(kt, q, n, h)};
@@ -643,27 +656,37 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
     int32_t page[I];   // of the next tile whose K is fetched
     uint32_t row[I];   // pool rows of the last tile whose K was fetched, the next V
     uint32_t ks[I], vs[I];
+    const int last_col = last >> A.g.sh, mask = (1 << A.g.sh) - 1;
+    const char *kp = (const char*)A.pool.k + c * 16, *vp = (const char*)A.pool.v + c * 16;
     // Loads are not skipped, so that what waits for one knows how many follow it: past the
-    // stretch's end they take the last tile, past the tile's rows the last key.
-    const auto key = [&](int t, int i) {
-      const int j = tile_key<kWideKeys>(s, t < s.t1 ? t : s.t1 - 1) + (kAll ? i * St::kStep + r0 : r0 & (kWideKeys - 1));
-      return j < last ? j : last;
-    };
+    // stretch's end they take its last tile.
+    const auto first = [&](int t) { return tile_key<kWideKeys>(s, t < s.t1 ? t : s.t1 - 1); };
+    const auto row_of = [&](int i) { return kAll ? i * St::kStep + r0 : r0 & (kWideKeys - 1); };
     const auto look = [&](int t) {
 #pragma unroll
-      for (int i = 0; i < I; ++i) page[i] = table[key(t, i) >> A.g.sh];
+      for (int i = 0; i < I; ++i) {
+        const int col = (first(t) + row_of(i)) >> A.g.sh;
+        page[i] = table[(uint32_t)(col < last_col ? col : last_col)];
+      }
     };
-    const auto fetch_k = [&](int t, const uint32_t (&r)[I]) {
+    // tiles start at multiples of 64: a key's row in its page is that of its row in the tile,
+    // and in pages of more than 64 tokens the tile's place in the page
+    const auto rows = [&](int t, uint32_t (&r)[I]) {
+#pragma unroll
+      for (int i = 0; i < I; ++i)
+        r[i] = page_at(A, page[i], lost) + (in_page(A, s.head, row_of(i)) + (uint32_t)(first(t) & mask));
+    };
+    const auto fetch_k = [&](const uint32_t (&r)[I]) {
 #pragma unroll
       for (int i = 0; i < I; ++i) {
-        st.load_k(A.pool, i, r[i], c);
+        st.k[i] = St::load(kp, r[i]);
         if (F8) ks[i] = A.pool.ke[r[i]];
       }
     };
     const auto fetch_v = [&]() {
 #pragma unroll
       for (int i = 0; i < I; ++i) {
-        st.load_v(A.pool, i, row[i], c);
+        st.v[i] = St::load(vp, row[i]);
         if (F8) vs[i] = A.pool.ve[row[i]];
       }
     };
@@ -673,7 +696,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
         if (kAll || loads) st.put_k(ldk + at, i, i * St::kStep + r0, c, scale_of(ks[i]));
     };
     const auto put_v = [&](int t) {
-      const int kb = tile_key<kWideKeys>(s, t < s.t1 ? t : s.t1 - 1);
+      const int kb = first(t);
       char* vt = ldv + (t & 1) * kTileV;
       if (!kAll && !loads) return;
       if (is_masked(A, s, kb, kWideKeys)) {
@@ -688,12 +711,14 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
       }
     };
     const auto works = [&](int kb) { return wreal && kb <= wlast; };
+    s16x8 kf[kAhead];
     // 32 keys from kb on, their scores in `sc`, their maximum taken: exponentials and the
     // product with V, beside the scores of the 32 keys from nb on (past the wave's last key
     // these are of any rows, and not used)
-    const auto half = [&](int kb, const char* vt, bool more, int nb, const char* kt, f32x16 (&sc)[1], f32x16 (&next)[1]) {
+    const auto half = [&](int kb, const char* vt, bool more, int nb, const char* kt, const char* kn,
+                          f32x16 (&sc)[1], f32x16 (&next)[1]) {
       if (!works(kb)) return;
-      float mx = weigh_and_score<BF, D>(vt, kt, q, sc, next, a, A.scale, lane);
+      float mx = weigh_and_score<BF, D>(vt, kt, kn, kf, q, sc, next, a, A.scale, lane);
       if (!more || !works(nb)) return;
       if (is_masked(A, s, nb, 32)) {
         hide<1>(next, rw, nb, h);
@@ -706,22 +731,25 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
     __syncthreads();
     f32x16 sa[1], sb[1];
     int kc = 0, kn = kTileK, kx = 2 * kTileK;  // K of this tile, the next and the one after
-    const auto rows = [&](int t, uint32_t (&r)[I]) {
-#pragma unroll
-      for (int i = 0; i < I; ++i) r[i] = pool_row(A, s.head, page[i], key(t, i), lost);
-    };
     if (s.t0 < s.t1) {
       look(s.t0);
       rows(s.t0, row);
-      fetch_k(s.t0, row);
+      fetch_k(row);
       fetch_v();
       look(s.t0 + 1);
       put_k(kc);
       put_v(s.t0);
       rows(s.t0 + 1, row);
-      fetch_k(s.t0 + 1, row);
+      fetch_k(row);
       look(s.t0 + 2);
       put_k(kn);
+      uint32_t r[I];
+      rows(s.t0 + 2, r);
+      fetch_v();
+      fetch_k(r);
+      look(s.t0 + 3);
+#pragma unroll
+      for (int i = 0; i < I; ++i) row[i] = r[i];
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): or every tile would wait for its next loads with q's
     __syncthreads();
@@ -729,21 +757,26 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
       sa[0] = scores<BF, D>(ldk, q, n, h);
       if (is_masked(A, s, tile_key<kWideKeys>(s, s.t0), 32)) hide<1>(sa, rw, tile_key<kWideKeys>(s, s.t0), h);
       raise<D>(a, peak<1>(sa) * A.scale);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) kf[i] = k_part<D>(ldk + 32 * kRowK<D>, i, lane);
     }
     for (int t = s.t0; t < s.t1; ++t) {
-      uint32_t r[I];
-      rows(t + 2, r);
-      fetch_v();
-      fetch_k(t + 2, r);
-      look(t + 3);
-#pragma unroll
-      for (int i = 0; i < I; ++i) row[i] = r[i];
-      const char* vt = ldv + (t & 1) * kTileV;
-      const int kb = tile_key<kWideKeys>(s, t);
-      half(kb, vt, true, kb + 32, ldk + kc + 32 * kRowK<D>, sa, sb);
-      half(kb + 32, vt + 32 * kRowV<D>, t + 1 < s.t1, tile_key<kWideKeys>(s, t + 1), ldk + kn, sb, sa);
+      // what was fetched beside the last tile goes into LDS beside this one, where all waves
+      // are past the tiles that were there
       put_v(t + 1);
       put_k(kx);
+      uint32_t next_row[I];
+      rows(t + 3, next_row);
+      fetch_v();
+      fetch_k(next_row);
+      look(t + 4);
+#pragma unroll
+      for (int i = 0; i < I; ++i) row[i] = next_row[i];
+      const char* vt = ldv + (t & 1) * kTileV;
+      const int kb = tile_key<kWideKeys>(s, t);
+      half(kb, vt, true, kb + 32, ldk + kc + 32 * kRowK<D>, ldk + kn, sa, sb);
+      half(kb + 32, vt + 32 * kRowV<D>, t + 1 < s.t1, tile_key<kWideKeys>(s, t + 1), ldk + kn,
+           ldk + kn + 32 * kRowK<D>, sb, sa);
       const int z = kc;
       kc = kn;
       kn = kx;
