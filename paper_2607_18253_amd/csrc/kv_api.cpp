@@ -11,6 +11,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <functional>
 #include <new>
 #include <string>
 #include <vector>
@@ -164,6 +165,105 @@ void cut(const std::vector<Tile>& tiles, int most, int least, bool wide, KvSeg* 
   *n_run = (int32_t)runs;
 }
 
+// The same for tiles that are many for the workgroups, or short: whole tiles where that
+// balances, parts of at most `limit` key tiles where it does not, the longest first to the
+// workgroup with the least work.  Costs are in key tiles, of about 2.4 us each.
+constexpr int kStart = 2;     // a stretch's queries, first keys and result
+constexpr int kPart = 1;      // partial sums instead of the result
+constexpr int kJoining = 3;   // the join
+// From this many key tiles per workgroup on parts cost nothing against them, and neighbours
+// that read the same keys at the same time are worth more than the best balance.
+constexpr int kLong = 128;
+
+void deal(const std::vector<Tile>& tiles, int groups, KvSeg* segs, int32_t* at, int32_t* n_run, KvJoin* join,
+          int32_t* n_join) {
+  int64_t total = 0;
+  for (const Tile& t : tiles) total += std::max(1, t.tiles);
+  if (tiles.empty() || total / groups >= kLong) {
+    cut(tiles, groups, kWideLeast, true, segs, at, n_run, join, n_join);
+    return;
+  }
+  struct Piece {
+    int32_t tile, part, cost;
+  };
+  const auto parts_of = [](const Tile& t, int64_t limit) { return (int32_t)std::max<int64_t>(1, ceil_div(t.tiles, limit)); };
+  const auto cost_of = [](const Tile& t, int32_t parts) {
+    return (int32_t)ceil_div(t.tiles, parts) + kStart + (parts > 1 ? kPart : 0);
+  };
+  std::vector<Piece> pieces, best;
+  std::vector<std::pair<int32_t, int32_t>> load;  // (work, workgroup), the least first
+  const auto more = std::greater<std::pair<int32_t, int32_t>>();
+  // hands the pieces out; returns the most that a workgroup has
+  const auto hand_out = [&](const std::vector<Piece>& p, int32_t* to) {
+    load.clear();
+    for (int g = 0; g < groups; ++g) load.emplace_back(0, g);
+    int32_t most = 0;
+    for (size_t i = 0; i < p.size(); ++i) {
+      std::pop_heap(load.begin(), load.end(), more);
+      load.back().first += p[i].cost;
+      most = std::max(most, load.back().first);
+      if (to) to[i] = load.back().second;
+      std::push_heap(load.begin(), load.end(), more);
+    }
+    return most;
+  };
+  int64_t limit = INT32_MAX, chosen = limit;
+  int32_t least = INT32_MAX;
+  for (int k = 0; k < 4; ++k) {
+    if (k) limit = std::max<int64_t>(kWideLeast, (total * 2 / groups) >> (k - 1));
+    pieces.clear();
+    int64_t parts = 0;
+    for (size_t i = 0; i < tiles.size(); ++i) {
+      const int32_t n = parts_of(tiles[i], limit);
+      if (n > 1) parts += n;
+      for (int32_t j = 0; j < n; ++j) pieces.push_back(Piece{(int32_t)i, j, cost_of(tiles[i], n)});
+    }
+    if (parts > 2 * groups) break;  // slots; and the smaller limits have more parts
+    std::stable_sort(pieces.begin(), pieces.end(), [](const Piece& x, const Piece& y) { return x.cost > y.cost; });
+    const int32_t most = hand_out(pieces, nullptr) + (parts ? kJoining : 0);
+    if (most < least) {
+      least = most;
+      chosen = limit;
+      best = pieces;
+    }
+    if (!parts && k) break;  // nothing was cut: no more to be had
+  }
+  std::vector<int32_t> to(best.size()), slot(tiles.size(), -1);
+  hand_out(best, to.data());
+  int32_t next = 0;
+  for (size_t i = 0; i < tiles.size(); ++i) {
+    const Tile& t = tiles[i];
+    const int32_t n = parts_of(t, chosen);
+    if (n < 2) continue;
+    slot[i] = next;
+    KvJoin j{};
+    j.q0 = t.s.q0;
+    j.ntok = t.s.ntok;
+    j.p0 = t.s.p0;
+    j.head = t.s.head;
+    j.slot = next;
+    j.n = n;
+    j.wide = 1;
+    join[(*n_join)++] = j;
+    next += n;
+  }
+  const int32_t runs = (int32_t)std::min<size_t>(groups, best.size());
+  std::vector<int32_t> fill(groups + 1, 0);
+  for (int32_t g : to) ++fill[g + 1];
+  for (int g = 0; g < groups; ++g) fill[g + 1] += fill[g];
+  for (int g = 0; g <= runs; ++g) at[g] = fill[g];
+  for (size_t i = 0; i < best.size(); ++i) {
+    const Tile& t = tiles[best[i].tile];
+    const int32_t n = parts_of(t, chosen);
+    KvSeg s = t.s;
+    s.t0 = (int32_t)((int64_t)t.tiles * best[i].part / n);
+    s.t1 = (int32_t)((int64_t)t.tiles * (best[i].part + 1) / n);
+    s.slot = n > 1 ? slot[best[i].tile] + best[i].part : -1;
+    segs[fill[to[i]]++] = s;
+  }
+  *n_run = runs;
+}
+
 bool type16(int32_t t) { return t == LAR_KV_F16 || t == LAR_KV_BF16; }
 
 lar_status ready(lar_kv* kv) {
@@ -266,7 +366,7 @@ lar_status lar_kv_create(lar_kv** out, const lar_kv_config* cfg) {
   const int64_t nt = kNarrowRows / g.G, wt = kWideRows / g.G;
   const int64_t narrow = std::min<int64_t>(cfg->max_seqs, cfg->max_tokens) * g.hkv;
   const int64_t wide = (std::min<int64_t>(cfg->max_seqs, cfg->max_tokens / (nt + 1)) + cfg->max_tokens / wt) * g.hkv;
-  kv->cap = Layout(cfg->max_tokens, narrow + kv->waves, wide + kv->groups, kv->waves, kv->groups,
+  kv->cap = Layout(cfg->max_tokens, narrow + kv->waves, wide + 2 * kv->groups, kv->waves, kv->groups,
                    std::min<int64_t>(narrow, kv->waves) + std::min<int64_t>(wide, kv->groups)).end;
   // every wave or workgroup has two stretches at most that are parts of a tile
   bool ok = hipMalloc((void**)&kv->dev, kv->cap) == hipSuccess &&
@@ -347,14 +447,14 @@ lar_status lar_kv_plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const i
       q0 += n;
     }
     const int64_t nn = (int64_t)narrow.size(), nw = (int64_t)wide.size();
-    const Layout L(T, nn ? nn + kv->waves : 0, nw ? nw + kv->groups : 0, kv->waves, kv->groups,
+    const Layout L(T, nn ? nn + kv->waves : 0, nw ? nw + 2 * kv->groups : 0, kv->waves, kv->groups,
                    std::min<int64_t>(nn, kv->waves) + std::min<int64_t>(nw, kv->groups));
     if (L.end > kv->cap) return fail(kv, LAR_E_CAPACITY, "plan of %zu bytes, room for %zu", L.end, kv->cap);
     kv->lay = L;
     KvJoin* join = (KvJoin*)(p + L.join);
     cut(narrow, kv->waves, kNarrowLeast, false, (KvSeg*)(p + L.narrow), (int32_t*)(p + L.narrow_at), &n_narrow, join,
         &n_join);
-    cut(wide, kv->groups, kWideLeast, true, (KvSeg*)(p + L.wide), (int32_t*)(p + L.wide_at), &n_wide, join, &n_join);
+    deal(wide, kv->groups, (KvSeg*)(p + L.wide), (int32_t*)(p + L.wide_at), &n_wide, join, &n_join);
   } catch (const std::bad_alloc&) {
     return fail(kv, LAR_E_CAPACITY, "out of host memory");
   }

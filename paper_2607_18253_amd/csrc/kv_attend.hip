@@ -790,12 +790,29 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
 }
 
 // ------------------------------------------------------------------ joining split tiles
-// One workgroup per 32 rows of a split tile; a thread has 4 values of a row, groups of
-// threads share out the slots.
-constexpr int kJoinThreads = 512;
+// One workgroup per 32 rows of a split tile.  A thread has 4 values of a row; where the rows
+// leave threads over, these share out the slots and are joined through LDS, in their order.
+// Bound by the latency of the slots' loads, of which each thread has four on their way.
+constexpr int kJoinThreads = 1024;
+
+struct Part {
+  float m, l;
+  f32x4 o;
+  // The sums of two parts of a row's keys.
+  __device__ __forceinline__ void join(const Part& p) {
+    const float top = fmaxf(m, p.m), t = top == -__builtin_inff() ? 0.0f : top;
+    const float f = __builtin_amdgcn_exp2f(m - t), g = __builtin_amdgcn_exp2f(p.m - t);
+    m = top;
+    l = __builtin_fmaf(p.l, g, l * f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(p.o[i], g, o[i] * f);
+  }
+};
 
 template <bool BF, int D>
 __global__ __launch_bounds__(kJoinThreads) void k_kv_join(KvAttendArgs A) {
+  constexpr int kQuads = D / 4;
+  __shared__ Part parts[kJoinThreads];
   const KvJoin j = plan_at(A.join, blockIdx.x);
   const int rows = j.wide ? kWideRows : kNarrowRows;
   const int row0 = blockIdx.y * 32;
@@ -803,34 +820,49 @@ __global__ __launch_bounds__(kJoinThreads) void k_kv_join(KvAttendArgs A) {
   if (have <= 0) return;
   const float* po = j.wide ? A.wide_o : A.narrow_o;
   const float2* pml = j.wide ? A.wide_ml : A.narrow_ml;
-  constexpr int kQuads = D / 4;
-  for (int u = threadIdx.x; u < have * kQuads; u += kJoinThreads) {
-    const int r = u / kQuads, d = (u % kQuads) * 4;
-    float m = -__builtin_inff();
-    for (int s = 0; s < j.n; ++s) m = fmaxf(m, pml[(int64_t)(j.slot + s) * rows + row0 + r].x);
-    const float mm = m == -__builtin_inff() ? 0.0f : m;
-    float l = 0.0f;
-    f32x4 o = {0, 0, 0, 0};
-    for (int s = 0; s < j.n; ++s) {
-      const int64_t at = (int64_t)(j.slot + s) * rows + row0 + r;
-      const float2 ml = pml[at];
-      const float f = __builtin_amdgcn_exp2f(ml.x - mm);
-      l = __builtin_fmaf(f, ml.y, l);
-      const f32x4 y = *(const f32x4*)(po + at * D + d);
+  const int n = have * kQuads;  // threads with values; 1024 at most
+  int share = kJoinThreads / n;  // threads on the same values
+  share = share < j.n ? share : j.n;
+  const int u = threadIdx.x % n, mine = threadIdx.x / n;
+  const int r = u / kQuads, d = (u % kQuads) * 4;
+  Part a{-__builtin_inff(), 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
+  if (mine < share) {
+    for (int s = mine; s < j.n; s += 4 * share) {
+      Part p[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(f, y[i], o[i]);
+      for (int k = 0; k < 4; ++k) {
+        const int x = s + k * share;
+        const int64_t at = (int64_t)(j.slot + (x < j.n ? x : s)) * rows + row0 + r;
+        const float2 ml = pml[at];
+        p[k].m = x < j.n ? ml.x : -__builtin_inff();
+        p[k].l = ml.y;
+        p[k].o = *(const f32x4*)(po + at * D + d);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (s + k * share < j.n) a.join(p[k]);
     }
-    const int t = (row0 + r) / A.g.G, g = row0 + r - t * A.g.G;
-    const bool none = j.p0 + t < 0;
-    const float inv = none ? 0.0f : 1.0f / l;
-    const int64_t at = (int64_t)(j.q0 + t) * A.g.hq + j.head * A.g.G + g;
-    uint32_t w[2];
+  }
+  if (share > 1) {
+    parts[threadIdx.x] = a;
+    __syncthreads();
+    if (mine == 0)
+      for (int k = 1; k < share; ++k) a.join(parts[k * n + u]);
+  }
+  if (mine != 0) return;
+  const int t = (row0 + r) / A.g.G, g = row0 + r - t * A.g.G;
+  const bool none = j.p0 + t < 0;
+  const float inv = none ? 0.0f : 1.0f / a.l;
+  const int64_t at = (int64_t)(j.q0 + t) * A.g.hq + j.head * A.g.G + g;
+  uint32_t w[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      w[i] = Elem<BF>::one(none ? 0.0f : o[2 * i] * inv) |
-             (uint32_t)Elem<BF>::one(none ? 0.0f : o[2 * i + 1] * inv) << 16;
-    *(uint2*)((uint16_t*)A.out + at * D + d) = make_uint2(w[0], w[1]);
-    if (A.lse && d == 0) A.lse[at] = none ? -__builtin_inff() : (mm + __builtin_amdgcn_logf(l)) * kLn2;
+  for (int i = 0; i < 2; ++i)
+    w[i] = Elem<BF>::one(none ? 0.0f : a.o[2 * i] * inv) |
+           (uint32_t)Elem<BF>::one(none ? 0.0f : a.o[2 * i + 1] * inv) << 16;
+  *(uint2*)((uint16_t*)A.out + at * D + d) = make_uint2(w[0], w[1]);
+  if (A.lse && d == 0) {
+    const float m = a.m == -__builtin_inff() ? 0.0f : a.m;
+    A.lse[at] = none ? -__builtin_inff() : (m + __builtin_amdgcn_logf(a.l)) * kLn2;
   }
 }
 

@@ -15,6 +15,13 @@ from .lar import LAR_OK, LarError, _dev, load_library
 KV_F16, KV_BF16, KV_E4M3 = 0, 1, 2
 
 
+def _raw_stream(index):
+    """hipStream_t of the current stream of a device (None where torch has no short way)."""
+    import torch
+    f = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return f(index) if f else torch.cuda.current_stream(index).cuda_stream
+
+
 class KvConfig(C.Structure):
     _fields_ = [("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
                 ("dtype", C.c_int32), ("cache_dtype", C.c_int32), ("block_size", C.c_int32),
@@ -36,7 +43,7 @@ class KvPages:
     (16-bit, or float8_e4m3fn with k_exp and v_exp uint8 [n_blocks][n_kv_heads][block_size]).
     Make new ones with PagedKV.new_pages."""
 
-    __slots__ = ("k", "v", "k_exp", "v_exp", "_arg")
+    __slots__ = ("k", "v", "k_exp", "v_exp", "_arg", "_ref", "_kind")
 
     def __init__(self, k, v, k_exp=None, v_exp=None):
         import torch
@@ -51,6 +58,8 @@ class KvPages:
         self._arg = KvPagesArg(_dev(k, k.dtype, "k"), _dev(v, v.dtype, "v"),
                                _dev(k_exp, torch.uint8, "k_exp"), _dev(v_exp, torch.uint8, "v_exp"),
                                int(k.shape[0]))
+        self._ref = C.byref(self._arg)
+        self._kind = (k.dtype, *k.shape[1:], k.device)
 
     def tensors(self):
         return [t for t in (self.k, self.v, self.k_exp, self.v_exp) if t is not None]
@@ -89,6 +98,10 @@ class PagedKV:
             raise LarError(st, "lar_kv_create failed")
         self._h = h
         self._n_seq = self._n_tok = 0
+        self._kind = (self.cache_dtype, self.n_kv, self.block_size, self.head_dim, self.device)
+        # the arguments of a call are read before it returns: one record each will do
+        self._args = {n: KvRowsArg() for n in ("q", "k", "v")}
+        self._refs = {n: C.byref(a) for n, a in self._args.items()}
 
     # ------------------------------------------------------------------ plumbing
     def _check(self, st: int):
@@ -113,19 +126,21 @@ class PagedKV:
         self.close()
 
     def _pages(self, pages):
-        k = pages.k
-        if k.dtype != self.cache_dtype or k.shape[1:] != (self.n_kv, self.block_size, self.head_dim):
+        if pages._kind != self._kind:
             raise ValueError(f"pages must be [n_blocks][{self.n_kv}][{self.block_size}][{self.head_dim}] "
-                             f"of {self.cache_dtype}")
-        return C.byref(pages._arg)
+                             f"of {self.cache_dtype} on {self.device}")
+        return pages._ref
 
     def _rows(self, t, heads, name):
-        if not t.is_cuda or t.dtype != self.dtype:
-            raise ValueError(f"{name} must be a GPU tensor of {self.dtype}")
+        if t.dtype is not self.dtype or t.device != self.device:
+            raise ValueError(f"{name} must be a tensor of {self.dtype} on {self.device}")
         if t.shape != (self._n_tok, heads, self.head_dim) or t.stride(2) != 1:
             raise ValueError(f"{name} must be [{self._n_tok}][{heads}][{self.head_dim}] with "
                              "contiguous rows")
-        return C.byref(KvRowsArg(t.data_ptr(), t.stride(0), t.stride(1)))
+        a = self._args[name]
+        a.data = t.data_ptr()
+        a.tok_stride, a.head_stride, _ = t.stride()
+        return self._refs[name]
 
     def _table(self, table):
         if table.dim() != 2 or table.shape[0] < self._n_seq:
@@ -134,12 +149,14 @@ class PagedKV:
 
     def _call(self, f, tensors, *args):
         """f(handle, *args) in order with the current stream."""
-        now = self._torch.cuda.current_stream(self.device)
-        if now.cuda_stream == self._sid:
-            self._check(f(self._h, *args))
+        if _raw_stream(self.device.index) == self._sid:
+            st = f(self._h, *args)
+            if st != LAR_OK:
+                self._check(st)
             return
         if self._torch.cuda.is_current_stream_capturing():
             raise ValueError("capture a graph on the handle's own stream")
+        now = self._torch.cuda.current_stream(self.device)
         self.stream.wait_stream(now)
         try:
             self._check(f(self._h, *args))
@@ -172,7 +189,8 @@ class PagedKV:
         """The batch's K and V rows [T][n_kv][head_dim] into the pages."""
         p = self._pages(pages)
         ka, va = self._rows(k, self.n_kv, "k"), self._rows(v, self.n_kv, "v")
-        self._call(self._L.lar_kv_append, (k, v, table, *pages.tensors()), p, ka, va, *self._table(table))
+        t, cols = self._table(table)
+        self._call(self._L.lar_kv_append, (k, v, table, *pages.tensors()), p, ka, va, t, cols)
 
     def read(self, pages: KvPages, table, k=None, v=None):
         """The rows of the batch's tokens back from the pages: (k, v), each
@@ -185,7 +203,8 @@ class PagedKV:
             v = torch.empty(shape, dtype=self.dtype, device=self.device)
         p = self._pages(pages)
         ka, va = self._rows(k, self.n_kv, "k"), self._rows(v, self.n_kv, "v")
-        self._call(self._L.lar_kv_read, (k, v, table, *pages.tensors()), p, *self._table(table), ka, va)
+        t, cols = self._table(table)
+        self._call(self._L.lar_kv_read, (k, v, table, *pages.tensors()), p, t, cols, ka, va)
         return k, v
 
     def attend(self, pages: KvPages, q, table, scale=None, out=None, lse=None):
@@ -197,9 +216,9 @@ class PagedKV:
         if out is None:
             out = torch.empty((self._n_tok, self.n_q, self.head_dim), dtype=self.dtype, device=self.device)
         p, qa = self._pages(pages), self._rows(q, self.n_q, "q")
-        t = self._table(table)
+        t, cols = self._table(table)
         held = (q, out, table, *pages.tensors()) if lse is None else (q, out, lse, table, *pages.tensors())
-        self._call(self._L.lar_kv_attend, held, p, qa, *t,
+        self._call(self._L.lar_kv_attend, held, p, qa, t, cols,
                    1.0 / math.sqrt(self.head_dim) if scale is None else float(scale),
                    _dev(out, self.dtype, "out", n * self.head_dim), _dev(lse, torch.float32, "lse", n))
         return out
