@@ -115,9 +115,21 @@ struct Tile {
   int tiles;
 };
 
-// Cuts the tiles' key tiles into stretches of equal number, one run of them for each of at
-// most `most` waves (or workgroups); a tile that is cut goes to the join.
-void cut(const std::vector<Tile>& tiles, int most, int least, bool wide, KvSeg* segs, int32_t* at, int32_t* n_run,
+KvJoin join_of(const KvSeg& s, int32_t slot, int32_t n, bool wide) {
+  KvJoin j{};
+  j.q0 = s.q0;
+  j.ntok = s.ntok;
+  j.p0 = s.p0;
+  j.head = s.head;
+  j.slot = slot;
+  j.n = n;
+  j.wide = wide;
+  return j;
+}
+
+// Narrow tiles: cuts their key tiles into stretches of equal number, one run of them for each
+// of at most `most` waves; a tile that is cut goes to the join.
+void cut(const std::vector<Tile>& tiles, int most, int least, KvSeg* segs, int32_t* at, int32_t* n_run,
          KvJoin* join, int32_t* n_join) {
   int64_t total = 0;  // a tile without keys still has its result to write
   for (const Tile& t : tiles) total += std::max(1, t.tiles);
@@ -148,39 +160,112 @@ void cut(const std::vector<Tile>& tiles, int most, int least, bool wide, KvSeg* 
       ++parts;
       x = y;
     }
-    if (parts > 1) {
-      KvJoin j{};
-      j.q0 = t.s.q0;
-      j.ntok = t.s.ntok;
-      j.p0 = t.s.p0;
-      j.head = t.s.head;
-      j.slot = slot0;
-      j.n = parts;
-      j.wide = wide;
-      join[(*n_join)++] = j;
-    }
+    if (parts > 1) join[(*n_join)++] = join_of(t.s, slot0, parts, false);
     before += n;
   }
   while (run < runs) at[++run] = n_seg;
   *n_run = (int32_t)runs;
 }
 
-// The same for tiles that are many for the workgroups, or short: whole tiles where that
+// Wide tiles.  Where they are short for the workgroups: whole tiles where that
 // balances, parts of at most `limit` key tiles where it does not, the longest first to the
 // workgroup with the least work.  Costs are in key tiles, of about 2.4 us each.
 constexpr int kStart = 2;     // a stretch's queries, first keys and result
 constexpr int kPart = 1;      // partial sums instead of the result
 constexpr int kJoining = 3;   // the join
-// From this many key tiles per workgroup on parts cost nothing against them, and neighbours
-// that read the same keys at the same time are worth more than the best balance.
+// From this many key tiles per workgroup on parts cost nothing against them, and workgroups
+// that read the same keys at the same time from one L2 are worth more.
 constexpr int kLong = 128;
+constexpr int kXcds = 8;  // workgroup runs are contiguous on an XCD (run_of in kv_attend.hip)
+
+// Long wide tiles: the workgroups of an XCD take neighbouring tiles whole, round by round, so
+// that they walk over the same keys together (a chunk of 7681 tokens at 131072: cut in order
+// 94 % of the L2's requests went on to memory and a call took 17.9 ms); what is left fills
+// them up to equal work, cut where it has to be.
+void march(const std::vector<Tile>& tiles, int groups, KvSeg* segs, int32_t* at, int32_t* n_run, KvJoin* join,
+           int32_t* n_join) {
+  struct Part {
+    int32_t run, tile, t0, t1;
+  };
+  std::vector<Part> parts;
+  std::vector<int64_t> load(groups, 0);
+  std::vector<int32_t> rest;
+  int64_t total = 0;
+  for (const Tile& t : tiles) total += std::max(1, t.tiles);
+  const int64_t target = ceil_div(total, groups);
+  int64_t before = 0;
+  size_t i = 0;
+  for (int x = 0, run0 = 0; x < kXcds; ++x) {
+    const int runs = groups / kXcds + (x < groups % kXcds ? 1 : 0);
+    // the tiles whose middle lies in this XCD's share
+    const size_t first = i;
+    while (i < tiles.size() &&
+           (x == kXcds - 1 || (2 * before + tiles[i].tiles) * groups < 2 * total * (run0 + runs))) {
+      before += std::max(1, tiles[i].tiles);
+      ++i;
+    }
+    size_t rounds = runs ? (i - first) / runs : 0;
+    for (; rounds; --rounds) {
+      int64_t most = 0;
+      for (int w = 0; w < runs; ++w) {
+        int64_t n = 0;
+        for (size_t k = 0; k < rounds; ++k) n += std::max(1, tiles[first + k * runs + w].tiles);
+        most = std::max(most, n);
+      }
+      if (most <= target) break;
+    }
+    for (size_t k = 0; k < rounds * runs; ++k) {
+      const int w = run0 + (int)(k % runs);
+      parts.push_back(Part{w, (int32_t)(first + k), 0, tiles[first + k].tiles});
+      load[w] += std::max(1, tiles[first + k].tiles);
+    }
+    for (size_t k = first + rounds * runs; k < i; ++k) rest.push_back((int32_t)k);
+    run0 += runs;
+  }
+  int w = 0;
+  for (int32_t k : rest) {
+    const int32_t n = std::max(1, tiles[k].tiles);
+    int32_t x = 0;
+    while (x < n) {
+      while (w < groups - 1 && load[w] >= target) ++w;
+      const int32_t y = w < groups - 1 ? (int32_t)std::min<int64_t>(n, x + target - load[w]) : n;
+      parts.push_back(Part{w, k, x, std::min(y, tiles[k].tiles)});
+      load[w] += y - x;
+      x = y;
+    }
+  }
+  std::vector<int32_t> fill(groups + 1, 0), made(tiles.size(), 0), slot(tiles.size(), -1);
+  for (const Part& q : parts) {
+    ++fill[q.run + 1];
+    ++made[q.tile];
+  }
+  for (int g = 0; g < groups; ++g) fill[g + 1] += fill[g];
+  for (int g = 0; g <= groups; ++g) at[g] = fill[g];
+  int32_t next = 0;
+  for (size_t k = 0; k < tiles.size(); ++k) {
+    if (made[k] < 2) continue;
+    slot[k] = next;
+    join[(*n_join)++] = join_of(tiles[k].s, next, made[k], true);
+    next += made[k];
+  }
+  for (const Part& q : parts) {  // parts of a tile come in the order of their keys
+    KvSeg s = tiles[q.tile].s;
+    s.t0 = q.t0;
+    s.t1 = q.t1;
+    s.slot = made[q.tile] > 1 ? slot[q.tile]++ : -1;
+    segs[fill[q.run]++] = s;
+  }
+  *n_run = groups;
+}
 
 void deal(const std::vector<Tile>& tiles, int groups, KvSeg* segs, int32_t* at, int32_t* n_run, KvJoin* join,
           int32_t* n_join) {
   int64_t total = 0;
   for (const Tile& t : tiles) total += std::max(1, t.tiles);
-  if (tiles.empty() || total / groups >= kLong) {
-    cut(tiles, groups, kWideLeast, true, segs, at, n_run, join, n_join);
+  *n_run = 0;
+  if (tiles.empty()) return;
+  if (total / groups >= kLong) {
+    march(tiles, groups, segs, at, n_run, join, n_join);
     return;
   }
   struct Piece {
@@ -236,15 +321,7 @@ void deal(const std::vector<Tile>& tiles, int groups, KvSeg* segs, int32_t* at, 
     const int32_t n = parts_of(t, chosen);
     if (n < 2) continue;
     slot[i] = next;
-    KvJoin j{};
-    j.q0 = t.s.q0;
-    j.ntok = t.s.ntok;
-    j.p0 = t.s.p0;
-    j.head = t.s.head;
-    j.slot = next;
-    j.n = n;
-    j.wide = 1;
-    join[(*n_join)++] = j;
+    join[(*n_join)++] = join_of(t.s, next, n, true);
     next += n;
   }
   const int32_t runs = (int32_t)std::min<size_t>(groups, best.size());
@@ -452,7 +529,7 @@ lar_status lar_kv_plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const i
     if (L.end > kv->cap) return fail(kv, LAR_E_CAPACITY, "plan of %zu bytes, room for %zu", L.end, kv->cap);
     kv->lay = L;
     KvJoin* join = (KvJoin*)(p + L.join);
-    cut(narrow, kv->waves, kNarrowLeast, false, (KvSeg*)(p + L.narrow), (int32_t*)(p + L.narrow_at), &n_narrow, join,
+    cut(narrow, kv->waves, kNarrowLeast, (KvSeg*)(p + L.narrow), (int32_t*)(p + L.narrow_at), &n_narrow, join,
         &n_join);
     deal(wide, kv->groups, (KvSeg*)(p + L.wide), (int32_t*)(p + L.wide_at), &n_wide, join, &n_join);
   } catch (const std::bad_alloc&) {
