@@ -62,6 +62,11 @@ template <> struct Elem<true> {
   static __device__ __forceinline__ float value(uint16_t x) {
     return __uint_as_float((uint32_t)x << 16);
   }
+  // c plus the two values of a pair
+  static __device__ __forceinline__ float add_pair(uint32_t x, float c) {
+    typedef __attribute__((ext_vector_type(2))) __bf16 x2;
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(x2, x), x2{(__bf16)1.0f, (__bf16)1.0f}, c, false);
+  }
   static constexpr uint32_t kExp = 0x7f80u;  // exponent bits: all ones where not finite
 };
 template <> struct Elem<false> {
@@ -82,6 +87,10 @@ template <> struct Elem<false> {
   }
   static __device__ __forceinline__ float value(uint16_t x) {
     return (float)__builtin_bit_cast(_Float16, x);
+  }
+  static __device__ __forceinline__ float add_pair(uint32_t x, float c) {
+    typedef __attribute__((ext_vector_type(2))) _Float16 x2;
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(x2, x), x2{(_Float16)1.0f, (_Float16)1.0f}, c, false);
   }
   static constexpr uint32_t kExp = 0x7c00u;
 };
@@ -450,9 +459,9 @@ struct Stage {
   static constexpr int kStep = LANES / kChunks;        // rows of one load
   uint4 k[I], v[I];
 
-  // from chunk c of row `row` of the pool, `base` the address of that chunk of row 0
-  static __device__ __forceinline__ uint4 load(const char* base, uint32_t row) {
-    return *(const uint4*)(base + (uint64_t)row * (kChunks * 16));
+  // 16 bytes, `at` bytes past the start of a row of the pool
+  static __device__ __forceinline__ uint4 load(const char* pool, uint32_t row, uint32_t at) {
+    return *(const uint4*)(pool + (uint64_t)row * (kChunks * 16) + at);
   }
   // 16-bit chunk j (of 2 with 8-bit codes) of 16 bytes in memory; s: the row's scale
   static __device__ __forceinline__ uint4 widen(const uint4& x, float s, int j) {
@@ -572,7 +581,6 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
     const int last = s.p0 + s.ntok - 1;  // position of the last token: keys 0 .. last
     const int32_t* table = A.table + (int64_t)s.seq * A.cols;
     const int last_col = last >> A.g.sh;
-    const char *kp = (const char*)A.pool.k + c * 16, *vp = (const char*)A.pool.v + c * 16;
     const auto look = [&](int t) {
       const int col = (tile_key<kNarrowKeys>(s, t) + n) >> A.g.sh;
       return table[col < last_col ? col : last_col];
@@ -584,8 +592,8 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
 #pragma unroll
       for (int i = 0; i < I; ++i) {
         const uint32_t at = (uint32_t)__shfl((int)src, i * St::kStep + r0);
-        st.k[i] = St::load(kp, at);
-        st.v[i] = St::load(vp, at);
+        st.k[i] = St::load((const char*)A.pool.k, at, c * 16);
+        st.v[i] = St::load((const char*)A.pool.v, at, c * 16);
       }
       if (F8) ex = A.pool.ke[src] | (uint32_t)A.pool.ve[src] << 8;
     };
@@ -627,14 +635,17 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
 }
 
 // ------------------------------------------------------------------ wide tiles
-template <bool BF, bool F8, int D>
+// PAGED: pages of 16 tokens and more.  The rows that a wave loads with one instruction (4, 8
+// or 16) then lie in one page, and their address is the wave's: the scalar unit's work.
+template <bool BF, bool F8, int D, bool PAGED>
 __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) {
   constexpr int kTileK = kWideKeys * kRowK<D>, kTileV = kWideKeys * kRowV<D>, kThreads = 64 * kWideWaves;
   __shared__ __align__(16) char ldk[3 * kTileK], ldv[2 * kTileV];
   __shared__ int flag;
   using St = Stage<BF, F8, D, (kWideKeys * (F8 ? D / 16 : D / 8) + kThreads - 1) / kThreads, kThreads>;
   constexpr int I = (kWideKeys + St::kStep - 1) / St::kStep;
-  const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r0 = tid / St::kChunks, c = tid % St::kChunks;
   constexpr bool kAll = St::kStep <= kWideKeys;  // else 8-bit rows of 64 need half the threads
   const bool loads = r0 < kWideKeys;
@@ -657,11 +668,16 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
     uint32_t row[I];   // pool rows of the last tile whose K was fetched, the next V
     uint32_t ks[I], vs[I];
     const int last_col = last >> A.g.sh, mask = (1 << A.g.sh) - 1;
-    const char *kp = (const char*)A.pool.k + c * 16, *vp = (const char*)A.pool.v + c * 16;
+    // where a thread's chunk lies from the row that its address is made of: its own, or the
+    // wave's first
+    const uint32_t at_row = PAGED ? lane / St::kChunks : 0, at_byte = at_row * (St::kChunks * 16) + c * 16;
     // Loads are not skipped, so that what waits for one knows how many follow it: past the
     // stretch's end they take its last tile.
     const auto first = [&](int t) { return tile_key<kWideKeys>(s, t < s.t1 ? t : s.t1 - 1); };
-    const auto row_of = [&](int i) { return kAll ? i * St::kStep + r0 : r0 & (kWideKeys - 1); };
+    const auto row_of = [&](int i) {
+      const int r = PAGED ? wave * (64 / St::kChunks) : r0;
+      return kAll ? i * St::kStep + r : r & (kWideKeys - 1);
+    };
     const auto look = [&](int t) {
 #pragma unroll
       for (int i = 0; i < I; ++i) {
@@ -674,20 +690,21 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
     const auto rows = [&](int t, uint32_t (&r)[I]) {
 #pragma unroll
       for (int i = 0; i < I; ++i)
-        r[i] = page_at(A, page[i], lost) + (in_page(A, s.head, row_of(i)) + (uint32_t)(first(t) & mask));
+        r[i] = page_at(A, PAGED ? __builtin_amdgcn_readfirstlane(page[i]) : page[i], lost) +
+               (in_page(A, s.head, row_of(i)) + (uint32_t)(first(t) & mask));
     };
     const auto fetch_k = [&](const uint32_t (&r)[I]) {
 #pragma unroll
       for (int i = 0; i < I; ++i) {
-        st.k[i] = St::load(kp, r[i]);
-        if (F8) ks[i] = A.pool.ke[r[i]];
+        st.k[i] = St::load((const char*)A.pool.k, r[i], at_byte);
+        if (F8) ks[i] = (A.pool.ke + r[i])[at_row];
       }
     };
     const auto fetch_v = [&]() {
 #pragma unroll
       for (int i = 0; i < I; ++i) {
-        st.v[i] = St::load(vp, row[i]);
-        if (F8) vs[i] = A.pool.ve[row[i]];
+        st.v[i] = St::load((const char*)A.pool.v, row[i], at_byte);
+        if (F8) vs[i] = (A.pool.ve + row[i])[at_row];
       }
     };
     const auto put_k = [&](int at) {
@@ -868,7 +885,10 @@ __global__ __launch_bounds__(kJoinThreads) void k_kv_join(KvAttendArgs A) {
 
 template <bool BF, bool F8, int D>
 hipError_t run(const KvAttendArgs& a, hipStream_t stream) {
-  if (a.n_wide) k_kv_wide<BF, F8, D><<<a.n_wide, 64 * kWideWaves, 0, stream>>>(a);
+  if (a.n_wide && a.g.sh >= 4)
+    k_kv_wide<BF, F8, D, true><<<a.n_wide, 64 * kWideWaves, 0, stream>>>(a);
+  else if (a.n_wide)
+    k_kv_wide<BF, F8, D, false><<<a.n_wide, 64 * kWideWaves, 0, stream>>>(a);
   if (a.n_narrow) k_kv_narrow<BF, F8, D><<<a.n_narrow, 64, 0, stream>>>(a);
   if (a.n_join) k_kv_join<BF, D><<<dim3(a.n_join, a.n_wide ? kWideRows / 32 : 1), kJoinThreads, 0, stream>>>(a);
   return hipGetLastError();
