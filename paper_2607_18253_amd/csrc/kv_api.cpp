@@ -66,7 +66,7 @@ struct lar_kv {
   // the plan
   bool planned = false;
   int32_t n_seq = 0, n_tok = 0, max_pages = 0, window = 0, sinks = 0;
-  int32_t n_narrow = 0, n_wide = 0, n_join = 0;
+  int32_t n_narrow = 0, n_wide = 0, n_join = 0, most_parts = 0;
   lar_status sticky = LAR_OK;
   std::string msg;
 };
@@ -115,22 +115,31 @@ struct Tile {
   int tiles;
 };
 
-KvJoin join_of(const KvSeg& s, int32_t slot, int32_t n, bool wide) {
-  KvJoin j{};
-  j.q0 = s.q0;
-  j.ntok = s.ntok;
-  j.p0 = s.p0;
-  j.head = s.head;
-  j.slot = slot;
-  j.n = n;
-  j.wide = wide;
-  return j;
-}
+// The join list of a plan.
+struct Joins {
+  KvJoin* list;
+  int32_t G, n = 0, most = 0;
+  void add(const KvSeg& s, int32_t slot, int32_t parts, bool wide) {
+    for (int32_t row0 = 0; row0 < s.ntok * G; row0 += 32) {
+      KvJoin j{};
+      j.q0 = s.q0;
+      j.ntok = s.ntok;
+      j.p0 = s.p0;
+      j.head = s.head;
+      j.slot = slot;
+      j.n = parts;
+      j.row0 = row0;
+      j.wide = wide;
+      list[n++] = j;
+    }
+    most = std::max(most, parts);
+  }
+};
 
 // Narrow tiles: cuts their key tiles into stretches of equal number, one run of them for each
 // of at most `most` waves; a tile that is cut goes to the join.
 void cut(const std::vector<Tile>& tiles, int most, int least, KvSeg* segs, int32_t* at, int32_t* n_run,
-         KvJoin* join, int32_t* n_join) {
+         Joins* join) {
   int64_t total = 0;  // a tile without keys still has its result to write
   for (const Tile& t : tiles) total += std::max(1, t.tiles);
   int64_t runs = std::max<int64_t>(1, std::min<int64_t>(most, total / least));
@@ -160,7 +169,7 @@ void cut(const std::vector<Tile>& tiles, int most, int least, KvSeg* segs, int32
       ++parts;
       x = y;
     }
-    if (parts > 1) join[(*n_join)++] = join_of(t.s, slot0, parts, false);
+    if (parts > 1) join->add(t.s, slot0, parts, false);
     before += n;
   }
   while (run < runs) at[++run] = n_seg;
@@ -182,8 +191,7 @@ constexpr int kXcds = 8;  // workgroup runs are contiguous on an XCD (run_of in 
 // that they walk over the same keys together (a chunk of 7681 tokens at 131072: cut in order
 // 94 % of the L2's requests went on to memory and a call took 17.9 ms); what is left fills
 // them up to equal work, cut where it has to be.
-void march(const std::vector<Tile>& tiles, int groups, KvSeg* segs, int32_t* at, int32_t* n_run, KvJoin* join,
-           int32_t* n_join) {
+void march(const std::vector<Tile>& tiles, int groups, KvSeg* segs, int32_t* at, int32_t* n_run, Joins* join) {
   struct Part {
     int32_t run, tile, t0, t1;
   };
@@ -245,7 +253,7 @@ void march(const std::vector<Tile>& tiles, int groups, KvSeg* segs, int32_t* at,
   for (size_t k = 0; k < tiles.size(); ++k) {
     if (made[k] < 2) continue;
     slot[k] = next;
-    join[(*n_join)++] = join_of(tiles[k].s, next, made[k], true);
+    join->add(tiles[k].s, next, made[k], true);
     next += made[k];
   }
   for (const Part& q : parts) {  // parts of a tile come in the order of their keys
@@ -258,14 +266,13 @@ void march(const std::vector<Tile>& tiles, int groups, KvSeg* segs, int32_t* at,
   *n_run = groups;
 }
 
-void deal(const std::vector<Tile>& tiles, int groups, KvSeg* segs, int32_t* at, int32_t* n_run, KvJoin* join,
-          int32_t* n_join) {
+void deal(const std::vector<Tile>& tiles, int groups, KvSeg* segs, int32_t* at, int32_t* n_run, Joins* join) {
   int64_t total = 0;
   for (const Tile& t : tiles) total += std::max(1, t.tiles);
   *n_run = 0;
   if (tiles.empty()) return;
   if (total / groups >= kLong) {
-    march(tiles, groups, segs, at, n_run, join, n_join);
+    march(tiles, groups, segs, at, n_run, join);
     return;
   }
   struct Piece {
@@ -321,7 +328,7 @@ void deal(const std::vector<Tile>& tiles, int groups, KvSeg* segs, int32_t* at, 
     const int32_t n = parts_of(t, chosen);
     if (n < 2) continue;
     slot[i] = next;
-    join[(*n_join)++] = join_of(t.s, next, n, true);
+    join->add(t.s, next, n, true);
     next += n;
   }
   const int32_t runs = (int32_t)std::min<size_t>(groups, best.size());
@@ -339,6 +346,33 @@ void deal(const std::vector<Tile>& tiles, int groups, KvSeg* segs, int32_t* at, 
     segs[fill[to[i]]++] = s;
   }
   *n_run = runs;
+}
+
+// How many of a device's workgroups the wide tiles of a batch get that has narrow ones too.
+// Wide tiles need time in proportion to their workgroups; narrow ones are bound by memory
+// from about 100 CUs on with 16-bit rows of 128 (255 decode tokens: 264 us with 768 waves,
+// 258 with 2048), later with shorter rows, so that most batches end sooner with both at work
+// (mixed batch of 3839 tokens: 387 us one after the other).
+int split(const std::vector<Tile>& narrow, const std::vector<Tile>& wide, int groups, const KvGeom& g) {
+  if (wide.empty()) return 0;
+  // microseconds: of a wide key tile and a stretch's start and end, of a narrow one in a wave
+  // alone; bytes of a narrow one
+  const double wt = g.D == 128 ? 2.1 : 1.35, ws = 8.0, nt = g.D == 128 ? 2.1 : 1.7;
+  const double nb = 2.0 * kNarrowKeys * g.D * (g.cache == kKvE4m3 ? 1 : 2), rate = 5.2e6;
+  int64_t w = 0, n = 0;
+  for (const Tile& t : wide) w += t.tiles;
+  for (const Tile& t : narrow) n += t.tiles;
+  int best = groups / 2;
+  double least = 1e300;
+  for (int k = kXcds; k <= groups - kXcds; k += kXcds) {
+    const double tw = w * wt / k + std::ceil((double)wide.size() / k) * ws;
+    const double tn = std::max(n * nt / ((groups - k) * kWideWaves), n * nb / rate);
+    if (std::max(tw, tn) < least) {
+      least = std::max(tw, tn);
+      best = k;
+    }
+  }
+  return best;
 }
 
 bool type16(int32_t t) { return t == LAR_KV_F16 || t == LAR_KV_BF16; }
@@ -443,8 +477,8 @@ lar_status lar_kv_create(lar_kv** out, const lar_kv_config* cfg) {
   const int64_t nt = kNarrowRows / g.G, wt = kWideRows / g.G;
   const int64_t narrow = std::min<int64_t>(cfg->max_seqs, cfg->max_tokens) * g.hkv;
   const int64_t wide = (std::min<int64_t>(cfg->max_seqs, cfg->max_tokens / (nt + 1)) + cfg->max_tokens / wt) * g.hkv;
-  kv->cap = Layout(cfg->max_tokens, narrow + kv->waves, wide + 2 * kv->groups, kv->waves, kv->groups,
-                   std::min<int64_t>(narrow, kv->waves) + std::min<int64_t>(wide, kv->groups)).end;
+  kv->cap = Layout(cfg->max_tokens, narrow + kv->waves, wide + narrow + 2 * kv->groups, kv->waves, kv->groups,
+                   std::min<int64_t>(narrow, kv->waves) + std::min<int64_t>(wide + narrow, kv->groups) * (kWideRows / 32)).end;
   // every wave or workgroup has two stretches at most that are parts of a tile
   bool ok = hipMalloc((void**)&kv->dev, kv->cap) == hipSuccess &&
             hipMalloc((void**)&kv->narrow_o, sizeof(float) * 2 * kv->waves * kNarrowRows * g.D) == hipSuccess &&
@@ -497,10 +531,10 @@ lar_status lar_kv_plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const i
   char* p = kv->pinned[b];
   const KvGeom& g = kv->g;
   KvTok* tok = (KvTok*)p;
-  int32_t n_narrow = 0, n_wide = 0, n_join = 0;
+  int32_t n_narrow = 0, n_wide = 0, n_join = 0, most_parts = 0;
   kv->planned = false;
   try {
-    std::vector<Tile> narrow, wide;
+    std::vector<Tile> narrow, wide, none;
     const int nt = kNarrowRows / g.G, wt = kWideRows / g.G;
     int64_t q0 = 0;
     for (int s = 0; s < n_seqs; ++s) {
@@ -519,19 +553,24 @@ lar_status lar_kv_plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const i
           t.s.head = h;
           t.s.seq = s;
           t.tiles = key_tiles(p0 + r, t.s.ntok, small ? kNarrowKeys : kWideKeys, window, sinks, &t.s.ns, &t.s.fw);
-          (small ? narrow : wide).push_back(t);
+          (t.tiles ? small ? narrow : wide : none).push_back(t);
         }
       q0 += n;
     }
+    // tiles without keys have only their zeros to write: either kernel will do, if they fit
+    for (const Tile& t : none) (t.s.ntok <= nt && wide.empty() ? narrow : wide).push_back(t);
     const int64_t nn = (int64_t)narrow.size(), nw = (int64_t)wide.size();
     const Layout L(T, nn ? nn + kv->waves : 0, nw ? nw + 2 * kv->groups : 0, kv->waves, kv->groups,
-                   std::min<int64_t>(nn, kv->waves) + std::min<int64_t>(nw, kv->groups));
+                   std::min<int64_t>(nn, kv->waves) + std::min<int64_t>(nw, kv->groups) * (kWideRows / 32));
     if (L.end > kv->cap) return fail(kv, LAR_E_CAPACITY, "plan of %zu bytes, room for %zu", L.end, kv->cap);
     kv->lay = L;
-    KvJoin* join = (KvJoin*)(p + L.join);
-    cut(narrow, kv->waves, kNarrowLeast, (KvSeg*)(p + L.narrow), (int32_t*)(p + L.narrow_at), &n_narrow, join,
-        &n_join);
-    deal(wide, kv->groups, (KvSeg*)(p + L.wide), (int32_t*)(p + L.wide_at), &n_wide, join, &n_join);
+    Joins join{(KvJoin*)(p + L.join), g.G};
+    const int groups = nn ? split(narrow, wide, kv->groups, g) : kv->groups;
+    cut(narrow, nw ? (kv->groups - groups) * kWideWaves : kv->waves, kNarrowLeast, (KvSeg*)(p + L.narrow),
+        (int32_t*)(p + L.narrow_at), &n_narrow, &join);
+    deal(wide, groups, (KvSeg*)(p + L.wide), (int32_t*)(p + L.wide_at), &n_wide, &join);
+    n_join = join.n;
+    most_parts = join.most;
   } catch (const std::bad_alloc&) {
     return fail(kv, LAR_E_CAPACITY, "out of host memory");
   }
@@ -553,6 +592,7 @@ lar_status lar_kv_plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const i
   kv->n_narrow = n_narrow;
   kv->n_wide = n_wide;
   kv->n_join = n_join;
+  kv->most_parts = most_parts;
   kv->planned = true;
   return LAR_OK;
 }
@@ -616,6 +656,7 @@ lar_status lar_kv_attend(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_row
   a.n_wide = kv->n_wide;
   a.join = (const KvJoin*)(kv->dev + kv->lay.join);
   a.n_join = kv->n_join;
+  a.most_parts = kv->most_parts;
   a.narrow_o = kv->narrow_o;
   a.wide_o = kv->wide_o;
   a.narrow_ml = kv->narrow_ml;

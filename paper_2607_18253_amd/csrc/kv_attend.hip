@@ -19,6 +19,7 @@
 //   k_kv_wide    eight waves, 256 rows, 64-key tiles in LDS for all of them: chunks.
 //                Bound by the matrix instructions and the exponentials beside them.
 //   k_kv_join    the partial sums of the tiles whose keys were split over waves.
+// A batch with both kinds of tiles is one launch of k_kv_wide.
 //
 // P is rounded to the 16-bit type of V (nearest even) for the second product, an error of
 // the size of the output's own rounding; sums are taken of the unrounded values.
@@ -133,11 +134,11 @@ __device__ __forceinline__ T plan_at(const T* p, int i) {
   return t;
 }
 
-// The run of stretches of this workgroup, of n.  Workgroups go to the 8 XCDs in turn; runs
-// that follow one another, which read the same keys or their neighbours, go to one XCD's L2.
-__device__ __forceinline__ int run_of(int n) {
-  const int x = blockIdx.x & 7, r = n & 7;
-  return x * (n >> 3) + (x < r ? x : r) + (blockIdx.x >> 3);
+// The run of stretches of workgroup `i` of n.  Workgroups go to the 8 XCDs in turn; runs that
+// follow one another, which read the same keys or their neighbours, go to one XCD's L2.
+__device__ __forceinline__ int run_of(int i, int n) {
+  const int x = i & 7, r = n & 7;
+  return x * (n >> 3) + (x < r ? x : r) + (i >> 3);
 }
 
 // The larger, or the sum, of a lane's value and that of lane ^ 32.
@@ -188,15 +189,21 @@ struct Row {
 
 // Takes the scores of keys from kb on that the row does not see to -infinity.
 template <int NB>
-__device__ __forceinline__ void hide(f32x16 (&s)[NB], const Row& r, int kb, int h) {
+__device__ __forceinline__ void hide(f32x16 (&s)[NB], const Row& r, int kb, int h, int window) {
   const int base = kb + 4 * h;  // the keys of a lane: base + constants
-  const int pos = r.pos - base, lo = r.lo - base, sinks = r.sinks - base;
+  const int pos = r.pos - base;
+#pragma unroll
+  for (int u = 0; u < NB; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[u][i] = 32 * u + key_of(i, 0) <= pos ? s[u][i] : -__builtin_inff();
+  if (!window) return;
+  const int lo = r.lo - base, sinks = r.sinks - base;
 #pragma unroll
   for (int u = 0; u < NB; ++u)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int j = 32 * u + key_of(i, 0);
-      s[u][i] = j <= pos && (j > lo || j < sinks) ? s[u][i] : -__builtin_inff();
+      s[u][i] = j > lo || j < sinks ? s[u][i] : -__builtin_inff();
     }
 }
 
@@ -401,32 +408,35 @@ __device__ __forceinline__ Row load_q(const KvAttendArgs& A, const Lane& x, int 
   return x.row;
 }
 
-// The result of a wave's rows, or their partial sums (`row0`: first row of the wave in the
-// slot, `rows` of a slot).
+// Where a split tile's partial sums are: 4 values of 32 rows side by side, by quads of values.
+template <int D>
+__device__ __forceinline__ int64_t part_at(int slot, int rows, int row, int quad) {
+  return ((((int64_t)slot * rows + row) / 32 * (D / 4) + quad) * 32 + row % 32) * 4;
+}
+
+// The result of a wave's 32 rows, through LDS (32 rows of `tmp`) so that whole rows are
+// written, or their partial sums (`row0`: first row of the wave in the slot, `rows` of one).
 template <bool BF, int D>
 __device__ __forceinline__ void finish(const KvAttendArgs& A, const KvSeg& s, const Sums<D>& a, int lane,
-                                       int row0, int rows, float* po, float2* pml) {
+                                       int row0, int rows, float* po, float2* pml, char* tmp) {
   lane = here(lane);
   const int n = lane & 31, h = lane >> 5, slot = s.slot;
   const Lane x = lane_of(A, s, row0 + n);
   const float l = add_halves(a.l);
-  if (!x.real) return;
   if (slot >= 0) {
-    float* o = po + ((int64_t)slot * rows + row0 + n) * D;
+    if (!x.real) return;
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
         f32x4 y = {a.o[b][i], a.o[b][i + 1], a.o[b][i + 2], a.o[b][i + 3]};
-        *(f32x4*)(o + 32 * b + key_of(i, h)) = y;
+        *(f32x4*)(po + part_at<D>(slot, rows, row0 + n, 8 * b + key_of(i, h) / 4)) = y;
       }
     if (h == 0) pml[(int64_t)slot * rows + row0 + n] = make_float2(a.m, l);
     return;
   }
   const bool none = x.row.pos < 0;
   const float f = none ? 0.0f : 1.0f / l;
-  const int64_t at = (int64_t)x.tok * A.g.hq + x.qh;
-  uint16_t* out = (uint16_t*)A.out + at * D;
 #pragma unroll
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
@@ -438,11 +448,18 @@ __device__ __forceinline__ void finish(const KvAttendArgs& A, const KvSeg& s, co
         const float y1 = none ? 0.0f : a.o[b][i + 2 * j + 1] * f;
         w[j] = Elem<BF>::one(y0) | (uint32_t)Elem<BF>::one(y1) << 16;
       }
-      *(uint2*)(out + 32 * b + key_of(i, h)) = make_uint2(w[0], w[1]);
+      *(uint2*)(tmp + n * kRowK<D> + (32 * b + key_of(i, h)) * 2) = make_uint2(w[0], w[1]);
     }
-  if (A.lse && h == 0) {
+  if (A.lse && x.real && h == 0) {
     const float m = a.m == -__builtin_inff() ? 0.0f : a.m;
-    A.lse[at] = none ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    A.lse[(int64_t)x.tok * A.g.hq + x.qh] = none ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+  wave_order();
+  const int have = s.ntok * A.g.G - row0;
+  for (int r = lane / (D / 8); r < 32 && r < have; r += 512 / D) {
+    const uint4 y = *(const uint4*)(tmp + r * kRowK<D> + lane % (D / 8) * 16);
+    const int t = (row0 + r) / A.g.G, g = row0 + r - t * A.g.G;
+    *(uint4*)((uint16_t*)A.out + ((int64_t)(s.q0 + t) * A.g.hq + s.head * A.g.G + g) * D + lane % (D / 8) * 8) = y;
   }
 }
 
@@ -458,6 +475,7 @@ struct Stage {
   static constexpr int kChunks = F8 ? D / 16 : D / 8;  // 16-byte chunks of a row in memory
   static constexpr int kStep = LANES / kChunks;        // rows of one load
   uint4 k[I], v[I];
+  uint32_t ks[F8 ? I : 1], vs[F8 ? I : 1];             // their exponents (wide tiles)
 
   // 16 bytes, `at` bytes past the start of a row of the pool
   static __device__ __forceinline__ uint4 load(const char* pool, uint32_t row, uint32_t at) {
@@ -515,10 +533,10 @@ __device__ __forceinline__ uint32_t in_page(const KvAttendArgs& A, int head, int
   return ((uint32_t)head << A.g.sh) + (uint32_t)(j & ((1 << A.g.sh) - 1));
 }
 
-// Whether some rows of a query tile may not see all the K keys from kb on: the tile reaches
-// past the first row's position or before the last row's window.
-__device__ __forceinline__ bool is_masked(const KvAttendArgs& A, const KvSeg& s, int kb, int K) {
-  return kb + K - 1 > s.p0 || (A.window && kb <= s.p0 + s.ntok - 1 - A.window && kb + K > A.sinks);
+// Whether some rows at positions p0 .. last may not see all the K keys from kb on: these
+// reach past the first row's position or before the last row's window.
+__device__ __forceinline__ bool is_masked(const KvAttendArgs& A, int p0, int last, int kb, int K) {
+  return kb + K - 1 > p0 || (A.window && kb <= last - A.window && kb + K > A.sinks);
 }
 
 // Adds what clean() took out of V in the stretch's masked tiles to the rows that see it, in
@@ -532,7 +550,7 @@ __device__ __forceinline__ void spread(const KvAttendArgs& A, const KvSeg& s, in
   const int last = s.p0 + s.ntok - 1, G = A.g.G;
   for (int t = s.t0; t < s.t1; ++t) {
     const int kb = tile_key<K>(s, t);
-    if (!is_masked(A, s, kb, K)) continue;
+    if (!is_masked(A, s.p0, last, kb, K)) continue;
     for (int j = kb; j < kb + K && j <= last; ++j) {
       bool lost = false;  // reported before
       const uint32_t row = page_at(A, A.table[(int64_t)s.seq * A.cols + (j >> A.g.sh)], lost) + in_page(A, s.head, j);
@@ -550,7 +568,7 @@ __device__ __forceinline__ void spread(const KvAttendArgs& A, const KvSeg& s, in
           const Row r{pos, A.window ? pos - A.window : -1, A.sinks};
           if (!r.sees(j)) continue;
           if (s.slot >= 0) {
-            po[((int64_t)s.slot * rows + n) * D + d] += v;
+            po[part_at<D>(s.slot, rows, n, d / 4) + d % 4] += v;
           } else {
             uint16_t* o = (uint16_t*)A.out + ((int64_t)(s.q0 + u) * A.g.hq + s.head * G + n - u * G) * D + d;
             *o = Elem<BF>::one(Elem<BF>::value(*o) + v);
@@ -562,15 +580,15 @@ __device__ __forceinline__ void spread(const KvAttendArgs& A, const KvSeg& s, in
 }
 
 // ------------------------------------------------------------------ narrow tiles
+// One wave's run of stretches; `lds`: its tile of 32 keys.
 template <bool BF, bool F8, int D>
-__global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
-  __shared__ __align__(16) char lds[kTileBytes<D, kNarrowKeys>];
+__device__ __forceinline__ void narrow(const KvAttendArgs& A, char* lds, int run, int lane) {
   char *kt = lds, *vt = lds + kNarrowKeys * kRowK<D>;
   using St = Stage<BF, F8, D, kNarrowKeys * (F8 ? D / 16 : D / 8) / 64, 64>;
   constexpr int I = kNarrowKeys / St::kStep;
-  const int lane = threadIdx.x, n = lane & 31, h = lane >> 5;
+  const int n = lane & 31, h = lane >> 5;
   const int r0 = lane / St::kChunks, c = lane % St::kChunks;
-  const int run = run_of(A.n_narrow), e = plan_at(A.narrow_at, run + 1);
+  const int e = plan_at(A.narrow_at, run + 1);
   bool lost = false;  // a page outside the pool
   for (int x = plan_at(A.narrow_at, run); x < e; ++x) {
     const KvSeg s = plan_at(A.narrow, x);
@@ -605,7 +623,7 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
     bool bad = false;
     for (int t = s.t0; t < s.t1; ++t) {
       const int kb = tile_key<kNarrowKeys>(s, t);
-      const bool masked = is_masked(A, s, kb, kNarrowKeys);
+      const bool masked = is_masked(A, s.p0, last, kb, kNarrowKeys);
 #pragma unroll
       for (int i = 0; i < I; ++i) {
         const int r = i * St::kStep + r0;
@@ -622,25 +640,38 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
       }
       wave_order();
       f32x16 sc[1] = {scores<BF, D>(kt, q, n, h)};
-      if (masked) hide<1>(sc, row, kb, h);
+      if (masked) hide<1>(sc, row, kb, h, A.window);
       raise<D>(a, peak<1>(sc) * A.scale);
       soften<D, 1>(sc, a, A.scale);
       weigh<BF, D>(vt, sc[0], a, lane);
       wave_order();
     }
-    finish<BF, D>(A, s, a, lane, 0, kNarrowRows, A.narrow_o, A.narrow_ml);
+    finish<BF, D>(A, s, a, lane, 0, kNarrowRows, A.narrow_o, A.narrow_ml, lds);
+    wave_order();
     if (__any(bad)) spread<BF, F8, D, kNarrowKeys>(A, s, lane, 0, kNarrowRows, A.narrow_o);
   }
   if (lost) *A.err = LAR_E_STATE;
 }
 
+template <bool BF, bool F8, int D>
+__global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
+  __shared__ __align__(16) char lds[kTileBytes<D, kNarrowKeys>];
+  narrow<BF, F8, D>(A, lds, run_of(blockIdx.x, A.n_narrow), threadIdx.x);
+}
+
 // ------------------------------------------------------------------ wide tiles
+// The workgroups past n_wide take narrow tiles, a run for each wave: the two kinds share the
+// device, one bound by matrix instructions and the other by memory.
+//
 // PAGED: pages of 16 tokens and more.  The rows that a wave loads with one instruction (4, 8
 // or 16) then lie in one page, and their address is the wave's: the scalar unit's work.
 template <bool BF, bool F8, int D, bool PAGED>
 __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) {
   constexpr int kTileK = kWideKeys * kRowK<D>, kTileV = kWideKeys * kRowV<D>, kThreads = 64 * kWideWaves;
-  __shared__ __align__(16) char ldk[3 * kTileK], ldv[2 * kTileV];
+  constexpr int kNarrow = kTileBytes<D, kNarrowKeys>, kWide = 3 * kTileK + 2 * kTileV;
+  __shared__ __align__(16) char lds[kWide > kWideWaves * kNarrow ? kWide : kWideWaves * kNarrow];
+  static_assert(kWideWaves * 32 * kRowK<D> <= kWide, "a result in LDS");
+  char *const ldk = lds, *const ldv = lds + 3 * kTileK;
   __shared__ int flag;
   using St = Stage<BF, F8, D, (kWideKeys * (F8 ? D / 16 : D / 8) + kThreads - 1) / kThreads, kThreads>;
   constexpr int I = (kWideKeys + St::kStep - 1) / St::kStep;
@@ -649,24 +680,32 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
   const int r0 = tid / St::kChunks, c = tid % St::kChunks;
   constexpr bool kAll = St::kStep <= kWideKeys;  // else 8-bit rows of 64 need half the threads
   const bool loads = r0 < kWideKeys;
-  const int run = run_of(A.n_wide), e = plan_at(A.wide_at, run + 1);
+  if ((int)blockIdx.x >= A.n_wide) {
+    const int run = run_of(blockIdx.x - A.n_wide, (A.n_narrow + kWideWaves - 1) / kWideWaves) * kWideWaves + wave;
+    if (run < A.n_narrow) narrow<BF, F8, D>(A, lds + wave * kNarrow, run, lane);
+    return;
+  }
+  const int run = run_of(blockIdx.x, A.n_wide), e = plan_at(A.wide_at, run + 1);
   bool lost = false;  // a page outside the pool
-  for (int x = plan_at(A.wide_at, run); x < e; ++x) {
-    const KvSeg s = plan_at(A.wide, x);
+  int x = plan_at(A.wide_at, run);
+  if (x >= e) return;
+  KvSeg after = plan_at(A.wide, x);
+  for (; x < e; ++x) {
+    const KvSeg s = after;
+    after = plan_at(A.wide, x + 1 < e ? x + 1 : x);
     s16x8 q[D / 16];
     const Row rw = load_q<D>(A, lane_of(A, s, wave * 32 + n), h, q);
     Sums<D> a;
     a.clear();
     const int last = s.p0 + s.ntok - 1;
-    // the last position of this wave's own rows: keys past it are not seen by any
-    const int wtok = (wave * 32 + 31) / A.g.G;
-    const int wlast = s.p0 + (wtok < s.ntok ? wtok : s.ntok - 1);
+    // positions of this wave's own rows: keys past the last are not seen by any
+    const int wtok = (wave * 32 + 31) / A.g.G, wtok0 = wave * 32 / A.g.G;
+    const int wlast = s.p0 + (wtok < s.ntok ? wtok : s.ntok - 1), wfirst = s.p0 + (wtok0 < s.ntok ? wtok0 : s.ntok - 1);
     const bool wreal = wave * 32 < s.ntok * A.g.G;
     const int32_t* table = A.table + (int64_t)s.seq * A.cols;
     St st;
     int32_t page[I];   // of the next tile whose K is fetched
     uint32_t row[I];   // pool rows of the last tile whose K was fetched, the next V
-    uint32_t ks[I], vs[I];
     const int last_col = last >> A.g.sh, mask = (1 << A.g.sh) - 1;
     // where a thread's chunk lies from the row that its address is made of: its own, or the
     // wave's first
@@ -678,53 +717,54 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
       const int r = PAGED ? wave * (64 / St::kChunks) : r0;
       return kAll ? i * St::kStep + r : r & (kWideKeys - 1);
     };
-    const auto look = [&](int t) {
+    const auto look = [&](int t, int32_t (&p)[I]) {
 #pragma unroll
       for (int i = 0; i < I; ++i) {
         const int col = (first(t) + row_of(i)) >> A.g.sh;
-        page[i] = table[(uint32_t)(col < last_col ? col : last_col)];
+        p[i] = table[(uint32_t)(col < last_col ? col : last_col)];
       }
     };
     // tiles start at multiples of 64: a key's row in its page is that of its row in the tile,
     // and in pages of more than 64 tokens the tile's place in the page
-    const auto rows = [&](int t, uint32_t (&r)[I]) {
+    const auto rows = [&](int t, const int32_t (&p)[I], uint32_t (&r)[I]) {
 #pragma unroll
       for (int i = 0; i < I; ++i)
-        r[i] = page_at(A, PAGED ? __builtin_amdgcn_readfirstlane(page[i]) : page[i], lost) +
+        r[i] = page_at(A, PAGED ? __builtin_amdgcn_readfirstlane(p[i]) : p[i], lost) +
                (in_page(A, s.head, row_of(i)) + (uint32_t)(first(t) & mask));
     };
-    const auto fetch_k = [&](const uint32_t (&r)[I]) {
+    const auto fetch_k = [&](St& x, const uint32_t (&r)[I]) {
 #pragma unroll
       for (int i = 0; i < I; ++i) {
-        st.k[i] = St::load((const char*)A.pool.k, r[i], at_byte);
-        if (F8) ks[i] = (A.pool.ke + r[i])[at_row];
+        x.k[i] = St::load((const char*)A.pool.k, r[i], at_byte);
+        if (F8) x.ks[i] = (A.pool.ke + r[i])[at_row];
       }
     };
-    const auto fetch_v = [&]() {
+    const auto fetch_v = [&](St& x, const uint32_t (&r)[I]) {
 #pragma unroll
       for (int i = 0; i < I; ++i) {
-        st.v[i] = St::load((const char*)A.pool.v, row[i], at_byte);
-        if (F8) vs[i] = (A.pool.ve + row[i])[at_row];
+        x.v[i] = St::load((const char*)A.pool.v, r[i], at_byte);
+        if (F8) x.vs[i] = (A.pool.ve + r[i])[at_row];
       }
     };
-    const auto put_k = [&](int at) {
+    const auto put_k = [&](const St& x, int at) {
 #pragma unroll
       for (int i = 0; i < I; ++i)
-        if (kAll || loads) st.put_k(ldk + at, i, i * St::kStep + r0, c, scale_of(ks[i]));
+        if (kAll || loads) x.put_k(ldk + at, i, i * St::kStep + r0, c, F8 ? scale_of(x.ks[i]) : 0.0f);
     };
-    const auto put_v = [&](int t) {
+    const auto put_v = [&](const St& x, int t) {
       const int kb = first(t);
       char* vt = ldv + (t & 1) * kTileV;
       if (!kAll && !loads) return;
-      if (is_masked(A, s, kb, kWideKeys)) {
+      if (is_masked(A, s.p0, last, kb, kWideKeys)) {
         bool bad = false;
 #pragma unroll
         for (int i = 0; i < I; ++i)
-          bad |= st.template put_v<true>(vt, i, i * St::kStep + r0, c, last + 1 - kb, scale_of(vs[i]));
+          bad |= x.template put_v<true>(vt, i, i * St::kStep + r0, c, last + 1 - kb, F8 ? scale_of(x.vs[i]) : 0.0f);
         if (bad) flag = 1;
       } else {
 #pragma unroll
-        for (int i = 0; i < I; ++i) st.template put_v<false>(vt, i, i * St::kStep + r0, c, 0, scale_of(vs[i]));
+        for (int i = 0; i < I; ++i)
+          x.template put_v<false>(vt, i, i * St::kStep + r0, c, 0, F8 ? scale_of(x.vs[i]) : 0.0f);
       }
     };
     const auto works = [&](int kb) { return wreal && kb <= wlast; };
@@ -737,42 +777,47 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
       if (!works(kb)) return;
       float mx = weigh_and_score<BF, D>(vt, kt, kn, kf, q, sc, next, a, A.scale, lane);
       if (!more || !works(nb)) return;
-      if (is_masked(A, s, nb, 32)) {
-        hide<1>(next, rw, nb, h);
+      if (is_masked(A, wfirst, wlast, nb, 32)) {
+        hide<1>(next, rw, nb, h, A.window);
         mx = peak<1>(next);
       }
       raise<D>(a, mx * A.scale);
     };
+    f32x16 sa[1], sb[1];
+    int kc = 0, kn = kTileK, kx = 2 * kTileK;  // K of this tile, the next and the one after
+    St s0, s1;
+    uint32_t r0s[I], r1s[I];
+    if (s.t0 < s.t1) {  // the first tiles, all on their way at once
+      int32_t p0[I], p1[I], p2[I];
+      look(s.t0, p0);
+      look(s.t0 + 1, p1);
+      look(s.t0 + 2, p2);
+      look(s.t0 + 3, page);
+      rows(s.t0, p0, r0s);
+      rows(s.t0 + 1, p1, r1s);
+      rows(s.t0 + 2, p2, row);
+      fetch_k(s0, r0s);
+      fetch_v(s0, r0s);
+      fetch_k(s1, r1s);
+    }
     __syncthreads();  // the last stretch's tiles and flag are done with
     if (tid == 0) flag = 0;
     __syncthreads();
-    f32x16 sa[1], sb[1];
-    int kc = 0, kn = kTileK, kx = 2 * kTileK;  // K of this tile, the next and the one after
     if (s.t0 < s.t1) {
-      look(s.t0);
-      rows(s.t0, row);
-      fetch_k(row);
-      fetch_v();
-      look(s.t0 + 1);
-      put_k(kc);
-      put_v(s.t0);
-      rows(s.t0 + 1, row);
-      fetch_k(row);
-      look(s.t0 + 2);
-      put_k(kn);
-      uint32_t r[I];
-      rows(s.t0 + 2, r);
-      fetch_v();
-      fetch_k(r);
-      look(s.t0 + 3);
-#pragma unroll
-      for (int i = 0; i < I; ++i) row[i] = r[i];
+      put_k(s0, kc);
+      put_v(s0, s.t0);
+      put_k(s1, kn);
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): or every tile would wait for its next loads with q's
-    __syncthreads();
+    if (s.t0 < s.t1) {
+      fetch_v(st, r1s);
+      fetch_k(st, row);
+    }
+    lds_barrier();
     if (s.t0 < s.t1 && works(tile_key<kWideKeys>(s, s.t0))) {
       sa[0] = scores<BF, D>(ldk, q, n, h);
-      if (is_masked(A, s, tile_key<kWideKeys>(s, s.t0), 32)) hide<1>(sa, rw, tile_key<kWideKeys>(s, s.t0), h);
+      const int kb = tile_key<kWideKeys>(s, s.t0);
+      if (is_masked(A, wfirst, wlast, kb, 32)) hide<1>(sa, rw, kb, h, A.window);
       raise<D>(a, peak<1>(sa) * A.scale);
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) kf[i] = k_part<D>(ldk + 32 * kRowK<D>, i, lane);
@@ -780,13 +825,13 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
     for (int t = s.t0; t < s.t1; ++t) {
       // what was fetched beside the last tile goes into LDS beside this one, where all waves
       // are past the tiles that were there
-      put_v(t + 1);
-      put_k(kx);
+      put_v(st, t + 1);
+      put_k(st, kx);
       uint32_t next_row[I];
-      rows(t + 3, next_row);
-      fetch_v();
-      fetch_k(next_row);
-      look(t + 4);
+      rows(t + 3, page, next_row);
+      fetch_v(st, row);
+      fetch_k(st, next_row);
+      look(t + 4, page);
 #pragma unroll
       for (int i = 0; i < I; ++i) row[i] = next_row[i];
       const char* vt = ldv + (t & 1) * kTileV;
@@ -800,7 +845,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
       kx = z;
       lds_barrier();
     }
-    finish<BF, D>(A, s, a, lane, wave * 32, kWideRows, A.wide_o, A.wide_ml);
+    finish<BF, D>(A, s, a, lane, wave * 32, kWideRows, A.wide_o, A.wide_ml, lds + wave * 32 * kRowK<D>);
     if (flag) spread<BF, F8, D, kWideKeys>(A, s, lane, wave * 32, kWideRows, A.wide_o);
   }
   if (lost) *A.err = LAR_E_STATE;
@@ -810,8 +855,6 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
 // One workgroup per 32 rows of a split tile.  A thread has 4 values of a row; where the rows
 // leave threads over, these share out the slots and are joined through LDS, in their order.
 // Bound by the latency of the slots' loads, of which each thread has four on their way.
-constexpr int kJoinThreads = 1024;
-
 struct Part {
   float m, l;
   f32x4 o;
@@ -826,71 +869,78 @@ struct Part {
   }
 };
 
-template <bool BF, int D>
-__global__ __launch_bounds__(kJoinThreads) void k_kv_join(KvAttendArgs A) {
+template <bool BF, int D, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_kv_join(KvAttendArgs A) {
   constexpr int kQuads = D / 4;
-  __shared__ Part parts[kJoinThreads];
+  __shared__ Part parts[THREADS];
   const KvJoin j = plan_at(A.join, blockIdx.x);
-  const int rows = j.wide ? kWideRows : kNarrowRows;
-  const int row0 = blockIdx.y * 32;
+  const int rows = j.wide ? kWideRows : kNarrowRows, row0 = j.row0;
   const int have = j.ntok * A.g.G - row0 < 32 ? j.ntok * A.g.G - row0 : 32;
-  if (have <= 0) return;
   const float* po = j.wide ? A.wide_o : A.narrow_o;
   const float2* pml = j.wide ? A.wide_ml : A.narrow_ml;
-  const int n = have * kQuads;  // threads with values; 1024 at most
-  int share = kJoinThreads / n;  // threads on the same values
-  share = share < j.n ? share : j.n;
-  const int u = threadIdx.x % n, mine = threadIdx.x / n;
-  const int r = u / kQuads, d = (u % kQuads) * 4;
-  Part a{-__builtin_inff(), 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
-  if (mine < share) {
-    for (int s = mine; s < j.n; s += 4 * share) {
-      Part p[4];
+  const int n = have * kQuads;  // quads of values
+  int share = THREADS / n;      // threads on the same one
+  share = share < 1 ? 1 : share < j.n ? share : j.n;
+  const int mine = n < THREADS ? threadIdx.x / n : 0;
+  for (int u = n < THREADS ? threadIdx.x % n : threadIdx.x; u < n; u += THREADS) {
+    const int r = u % have, d = (u / have) * 4;
+    Part a{-__builtin_inff(), 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
+    if (mine < share) {
+      for (int s = mine; s < j.n; s += 4 * share) {
+        Part p[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int x = s + k * share;
-        const int64_t at = (int64_t)(j.slot + (x < j.n ? x : s)) * rows + row0 + r;
-        const float2 ml = pml[at];
-        p[k].m = x < j.n ? ml.x : -__builtin_inff();
-        p[k].l = ml.y;
-        p[k].o = *(const f32x4*)(po + at * D + d);
+        for (int k = 0; k < 4; ++k) {
+          const int x = s + k * share < j.n ? s + k * share : s;
+          const float2 ml = pml[(int64_t)(j.slot + x) * rows + row0 + r];
+          p[k].m = ml.x;
+          p[k].l = ml.y;
+          p[k].o = *(const f32x4*)(po + part_at<D>(j.slot + x, rows, row0 + r, d / 4));
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (s + k * share < j.n) a.join(p[k]);
       }
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (s + k * share < j.n) a.join(p[k]);
     }
-  }
-  if (share > 1) {
-    parts[threadIdx.x] = a;
-    __syncthreads();
-    if (mine == 0)
-      for (int k = 1; k < share; ++k) a.join(parts[k * n + u]);
-  }
-  if (mine != 0) return;
-  const int t = (row0 + r) / A.g.G, g = row0 + r - t * A.g.G;
-  const bool none = j.p0 + t < 0;
-  const float inv = none ? 0.0f : 1.0f / a.l;
-  const int64_t at = (int64_t)(j.q0 + t) * A.g.hq + j.head * A.g.G + g;
-  uint32_t w[2];
+    if (share > 1) {  // then one round: every thread is here
+      parts[threadIdx.x] = a;
+      __syncthreads();
+      if (mine == 0)
+        for (int k = 1; k < share; ++k) a.join(parts[k * n + u]);
+    }
+    if (mine != 0) continue;
+    const int t = (row0 + r) / A.g.G, g = row0 + r - t * A.g.G;
+    const bool none = j.p0 + t < 0;
+    const float inv = none ? 0.0f : 1.0f / a.l;
+    const int64_t at = (int64_t)(j.q0 + t) * A.g.hq + j.head * A.g.G + g;
+    uint32_t w[2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-    w[i] = Elem<BF>::one(none ? 0.0f : a.o[2 * i] * inv) |
-           (uint32_t)Elem<BF>::one(none ? 0.0f : a.o[2 * i + 1] * inv) << 16;
-  *(uint2*)((uint16_t*)A.out + at * D + d) = make_uint2(w[0], w[1]);
-  if (A.lse && d == 0) {
-    const float m = a.m == -__builtin_inff() ? 0.0f : a.m;
-    A.lse[at] = none ? -__builtin_inff() : (m + __builtin_amdgcn_logf(a.l)) * kLn2;
+    for (int i = 0; i < 2; ++i)
+      w[i] = Elem<BF>::one(none ? 0.0f : a.o[2 * i] * inv) |
+             (uint32_t)Elem<BF>::one(none ? 0.0f : a.o[2 * i + 1] * inv) << 16;
+    *(uint2*)((uint16_t*)A.out + at * D + d) = make_uint2(w[0], w[1]);
+    if (A.lse && d == 0) {
+      const float m = a.m == -__builtin_inff() ? 0.0f : a.m;
+      A.lse[at] = none ? -__builtin_inff() : (m + __builtin_amdgcn_logf(a.l)) * kLn2;
+    }
   }
 }
 
 template <bool BF, bool F8, int D>
 hipError_t run(const KvAttendArgs& a, hipStream_t stream) {
-  if (a.n_wide && a.g.sh >= 4)
-    k_kv_wide<BF, F8, D, true><<<a.n_wide, 64 * kWideWaves, 0, stream>>>(a);
-  else if (a.n_wide)
-    k_kv_wide<BF, F8, D, false><<<a.n_wide, 64 * kWideWaves, 0, stream>>>(a);
-  if (a.n_narrow) k_kv_narrow<BF, F8, D><<<a.n_narrow, 64, 0, stream>>>(a);
-  if (a.n_join) k_kv_join<BF, D><<<dim3(a.n_join, a.n_wide ? kWideRows / 32 : 1), kJoinThreads, 0, stream>>>(a);
+  if (a.n_wide) {
+    const dim3 grid(a.n_wide + (a.n_narrow + kWideWaves - 1) / kWideWaves);
+    if (a.g.sh >= 4)
+      k_kv_wide<BF, F8, D, true><<<grid, 64 * kWideWaves, 0, stream>>>(a);
+    else
+      k_kv_wide<BF, F8, D, false><<<grid, 64 * kWideWaves, 0, stream>>>(a);
+  } else if (a.n_narrow) {
+    k_kv_narrow<BF, F8, D><<<a.n_narrow, 64, 0, stream>>>(a);
+  }
+  // many parts of few rows: more threads to share them out to
+  if (a.n_join && a.most_parts > 8)
+    k_kv_join<BF, D, 1024><<<a.n_join, 1024, 0, stream>>>(a);
+  else if (a.n_join)
+    k_kv_join<BF, D, 256><<<a.n_join, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
