@@ -540,9 +540,9 @@ lar_status lar_estimate_lps(lar_ctx *ctx, const lar_lps_params *params, int32_t 
  *
  * LAR_KV_E4M3 holds a row of head_dim values x as e4m3 codes of x * 2^-k and one byte
  * k + 127 in k_exp / v_exp, dev [n_blocks][n_kv_heads][block_size]: k is the least integer
- * in [-100, 120] with max |x| <= 448 * 2^k over the finite x; codes are rounded to nearest
- * even, infinities and NaN become NaN, and |x| is first held to 61440 (F16) or
- * 1.875 * 2^127 (BF16) so that every code * 2^k is exact in dtype.
+ * in [-100, 120] with max |x| <= 448 * 2^k over the finite x (-9 for a row of zeros);
+ * codes are rounded to nearest even, infinities and NaN become NaN, and |x| is first held
+ * to 61440 (F16) or 1.875 * 2^127 (BF16), so that every code * 2^k is exact in dtype.
  *
  * Attention.  out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m), s_j = scale * q . k_j,
  * over the keys j <= p, under a window W also j > p - W or j < sinks (the first tokens,
@@ -563,7 +563,8 @@ typedef struct {
   int32_t cache_dtype;    /* of the pages: dtype or LAR_KV_E4M3                         */
   int32_t block_size;     /* tokens of a page, a power of two, 1 .. 65536               */
   int32_t max_seqs;       /* sequences of a batch at most, 1 .. 2^20                    */
-  int32_t max_tokens;     /* new tokens of a batch at most, 1 .. 2^26                   */
+  int32_t max_tokens;     /* new tokens of a batch at most, 1 .. 2^26 and at most
+                           * 2^27 / n_kv_heads                                          */
   int32_t reserved;       /* must be 0                                                  */
   void *stream;           /* hipStream_t to enqueue on; NULL = null stream              */
 } lar_kv_config;

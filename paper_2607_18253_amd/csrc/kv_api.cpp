@@ -451,7 +451,8 @@ lar_status lar_kv_create(lar_kv** out, const lar_kv_config* cfg) {
       (cfg->head_dim != 64 && cfg->head_dim != 128) || !type16(cfg->dtype) ||
       (cfg->cache_dtype != cfg->dtype && cfg->cache_dtype != LAR_KV_E4M3) || S < 1 || S > 65536 ||
       (S & (S - 1)) || cfg->max_seqs < 1 || cfg->max_seqs > 1 << 20 || cfg->max_tokens < 1 ||
-      cfg->max_tokens > 1 << 26 || cfg->reserved != 0)
+      cfg->max_tokens > 1 << 26 || (int64_t)cfg->max_tokens * cfg->n_kv_heads > 1 << 27 ||
+      cfg->reserved != 0)
     return LAR_E_ARG;
   lar_kv* kv = new (std::nothrow) lar_kv;
   if (!kv) return LAR_E_HIP;

@@ -3,12 +3,13 @@
 //   k_kv_append  one thread per 16 bytes of a new token's K row and of its V row.  A
 //                16-bit cache takes the row as it is.  An 8-bit cache takes e4m3 codes of
 //                x * 2^-k, k the least integer that brings the row's largest finite
-//                magnitude to 448 at most (amax = m * 2^f, 1/2 <= m < 1: k = f - 9, one
-//                more where m > 7/8), so the scale is exact and the only rounding is that
-//                to 3 fraction bits, to nearest even; infinities and NaN become NaN.
+//                magnitude to 448 at most, so the scale is exact and the only rounding is
+//                that to 3 fraction bits, to nearest even; infinities and NaN become NaN.
 //   k_kv_read    the rows of the batch's tokens back as 16-bit values; code * 2^k needs
 //                4 significant bits, so this is exact.
-// Bound by the bytes of the rows.  The D/8 threads of a row sit in one wave.
+// Bound by the bytes of the rows.  The D/8 threads of a row sit in one wave; magnitudes are
+// compared as the bits of their 16-bit patterns, K's and V's in one word, over the row by
+// lane permutations, and the codes come from the conversion that takes a power of two along.
 #include "../../include/lar.h"
 #include "kv_device.h"
 
@@ -17,9 +18,15 @@ namespace {
 
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(2))) short s16x2;
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 
-// Row index of (page, head, row) in units of rows, or -1 with the sticky error for a page
-// outside the pool.
+// Patterns of infinity and of the largest magnitude that is held: its code times its scale
+// is the largest such value that the 16-bit type has.
+template <bool BF> constexpr uint32_t kInf = BF ? 0x7f80u : 0x7c00u;
+template <bool BF> constexpr uint32_t kHeld = BF ? 0x7f70u : 0x7b80u;  // 1.875 * 2^127, 61440
+
+// Row of (page, head, position) in the pool, or -1 with the sticky error for a page outside.
 __device__ __forceinline__ int64_t page_row(const KvGeom& g, const KvPool& pool, int32_t page,
                                             int head, int pos, int32_t* err) {
   if ((uint32_t)page >= pool.n_blocks) {
@@ -29,56 +36,77 @@ __device__ __forceinline__ int64_t page_row(const KvGeom& g, const KvPool& pool,
   return (((int64_t)page * g.hkv + head) << g.sh) + (pos & ((1 << g.sh) - 1));
 }
 
-template <bool BF>
-__device__ __forceinline__ float lo16(uint32_t w) {
-  if (BF) return __uint_as_float(w << 16);
-  return (float)__builtin_bit_cast(f16x2, w)[0];
-}
-template <bool BF>
-__device__ __forceinline__ float hi16(uint32_t w) {
-  if (BF) return __uint_as_float(w & 0xffff0000u);
-  return (float)__builtin_bit_cast(f16x2, w)[1];
+__device__ __forceinline__ uint32_t max16(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a),
+                                                                __builtin_bit_cast(u16x2, b)));
 }
 
-// e4m3 codes of the 8 values of this thread; the row lies in `lanes` (8 or 16) threads.
+// The largest pattern of 8 magnitudes.
+__device__ __forceinline__ uint32_t top(const uint4& x) {
+  const uint32_t m = max16(max16(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), max16(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
+  return max16(m, m >> 16) & 0xffffu;
+}
+
+// The larger of both halves of a word over the 8 or 16 lanes of a row.
+template <int LANES>
+__device__ __forceinline__ uint32_t top_of_row(uint32_t m) {
+  m = max16(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0xb1, 0xf, 0xf, false));   // lane ^ 1
+  m = max16(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x4e, 0xf, 0xf, false));   // lane ^ 2
+  m = max16(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x141, 0xf, 0xf, false));  // 7 - lane, of 8
+  if (LANES == 16) m = max16(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x140, 0xf, 0xf, false));
+  return m;
+}
+
+// Values that are not finite to NaN, and what is too large to what is held; the largest
+// finite pattern.
 template <bool BF>
-__device__ __forceinline__ uint2 quantise(const uint4& x, int lanes, int* exp_out) {
-  const float held = BF ? 0x1.ep+127f : 61440.0f;
-  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-  float f[8];
-  float amax = 0.0f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[2 * i] = lo16<BF>(w[i]);
-    f[2 * i + 1] = hi16<BF>(w[i]);
-  }
-#pragma unroll
+__device__ uint32_t hold(uint4& x) {
+  uint32_t w[4] = {x.x, x.y, x.z, x.w}, most = 0;
   for (int i = 0; i < 8; ++i) {
-    const float a = __builtin_fabsf(f[i]);
-    if (a < __builtin_inff()) {  // finite: held to what the 16-bit type takes back
-      f[i] = __builtin_copysignf(fminf(a, held), f[i]);
-      amax = fmaxf(amax, fminf(a, held));
+    const int sh = 16 * (i & 1);
+    uint32_t v = w[i >> 1] >> sh & 0xffffu, a = v & 0x7fffu;
+    if (a >= kInf<BF>) {
+      v |= 0x7fffu;
     } else {
-      f[i] = __builtin_nanf("");
+      a = a < kHeld<BF> ? a : kHeld<BF>;
+      v = (v & 0x8000u) | a;
+      most = most < a ? a : most;
     }
+    w[i >> 1] = (w[i >> 1] & ~(0xffffu << sh)) | v << sh;
   }
-  for (int m = 1; m < lanes; m <<= 1) amax = fmaxf(amax, __shfl_xor(amax, m));
-  int e;
-  const float mant = frexpf(amax, &e);
-  int k = e - 9 + (mant > 0.875f ? 1 : 0);
-  k = k < kKvExpMin ? kKvExpMin : k > kKvExpMax ? kKvExpMax : k;
-  *exp_out = k + 127;
-  const float s = __uint_as_float((uint32_t)(127 - k) << 23);
-  int lo = 0, hi = 0;
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[0] * s, f[1] * s, lo, false);
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[2] * s, f[3] * s, lo, true);
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[4] * s, f[5] * s, hi, false);
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[6] * s, f[7] * s, hi, true);
-  return make_uint2((uint32_t)lo, (uint32_t)hi);
+  x = make_uint4(w[0], w[1], w[2], w[3]);
+  return most;
+}
+
+// The least k with magnitude <= 448 * 2^k, within its bounds; a row of zeros has -9.
+template <bool BF>
+__device__ __forceinline__ int exponent(uint32_t pattern) {
+  const float f = BF ? __uint_as_float(pattern << 16) : (float)__builtin_bit_cast(f16x2, pattern)[0];
+  const uint32_t b = __float_as_uint(f);
+  if (b == 0) return -9;
+  const int k = (int)(b >> 23) - 135 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);  // 448 = 1.75 * 2^8
+  return k < kKvExpMin ? kKvExpMin : k > kKvExpMax ? kKvExpMax : k;
+}
+
+// e4m3 codes of x * 2^-k.
+template <bool BF>
+__device__ __forceinline__ uint2 codes(const uint4& x, int k) {
+  const float s = __uint_as_float((uint32_t)(k + 127) << 23);
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  s16x2 c[2] = {{0, 0}, {0, 0}};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (BF)
+      c[i >> 1] = i & 1 ? __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c[i >> 1], __builtin_bit_cast(bf16x2, w[i]), s, true)
+                        : __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c[i >> 1], __builtin_bit_cast(bf16x2, w[i]), s, false);
+    else
+      c[i >> 1] = i & 1 ? __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(c[i >> 1], __builtin_bit_cast(f16x2, w[i]), s, true)
+                        : __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(c[i >> 1], __builtin_bit_cast(f16x2, w[i]), s, false);
+  return make_uint2(__builtin_bit_cast(uint32_t, c[0]), __builtin_bit_cast(uint32_t, c[1]));
 }
 
 template <bool BF>
-__device__ __forceinline__ uint4 dequantise(uint2 c, uint32_t exp) {
+__device__ __forceinline__ uint4 values(uint2 c, uint32_t exp) {
   const float s = __uint_as_float(exp << 23);
   uint4 o;
   if (BF) {
@@ -95,94 +123,112 @@ __device__ __forceinline__ uint4 dequantise(uint2 c, uint32_t exp) {
   return o;
 }
 
-template <bool F8, bool BF>
+// A thread's place: token, head and 16-byte chunk (tokens * heads <= 2^27).
+struct Place {
+  uint32_t t, head, c;
+  const void *k, *v;
+  __device__ __forceinline__ Place(const KvCopyArgs& A, int lanes) {
+    const uint32_t x = blockIdx.x * 256 + threadIdx.x, r = x / lanes;
+    c = x % lanes;
+    t = r / (uint32_t)A.g.hkv;
+    head = r - t * (uint32_t)A.g.hkv;
+    k = (const uint16_t*)A.k.p + (int64_t)t * A.k.tok + (int64_t)head * A.k.head + c * 8;
+    v = (const uint16_t*)A.v.p + (int64_t)t * A.v.tok + (int64_t)head * A.v.head + c * 8;
+  }
+};
+
+template <bool F8, bool BF, int LANES>
 __global__ __launch_bounds__(256) void k_kv_append(KvCopyArgs A) {
-  const int lanes = A.g.D >> 3;
-  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t r = x / lanes;  // (token, head)
-  const int c = (int)(x - r * lanes);
-  const int64_t t = r / A.g.hkv;
-  const int head = (int)(r - t * A.g.hkv);
-  if (t >= A.n_tok) return;
-  const KvTok tok = A.tok[t];
+  const Place at(A, LANES);
+  if (at.t >= (uint32_t)A.n_tok) return;
+  const KvTok tok = A.tok[at.t];
   if (tok.pos < 0) return;
   const int32_t page = A.table[(int64_t)tok.seq * A.cols + (tok.pos >> A.g.sh)];
-  const uint4 k = *(const uint4*)((const uint16_t*)A.k.p + t * A.k.tok + head * A.k.head + c * 8);
-  const uint4 v = *(const uint4*)((const uint16_t*)A.v.p + t * A.v.tok + head * A.v.head + c * 8);
-  const int64_t row = page_row(A.g, A.pool, page, head, tok.pos, A.err);
+  uint4 k = *(const uint4*)at.k, v = *(const uint4*)at.v;
+  const int64_t row = page_row(A.g, A.pool, page, at.head, tok.pos, A.err);
   if (row < 0) return;
   if (F8) {
-    int ke, ve;
-    const uint2 kc = quantise<BF>(k, lanes, &ke), vc = quantise<BF>(v, lanes, &ve);
-    ((uint2*)A.pool.k)[row * lanes + c] = kc;
-    ((uint2*)A.pool.v)[row * lanes + c] = vc;
-    if (c == 0) {
-      ((uint8_t*)A.pool.ke)[row] = (uint8_t)ke;
-      ((uint8_t*)A.pool.ve)[row] = (uint8_t)ve;
+    uint32_t m = top_of_row<LANES>(top(k) | top(v) << 16);
+    if ((m & 0xffffu) > kHeld<BF> || m >> 16 > kHeld<BF>) {  // the row's threads go together
+      const uint32_t mk = hold<BF>(k), mv = hold<BF>(v);
+      m = top_of_row<LANES>(mk | mv << 16);
+    }
+    const int ke = exponent<BF>(m & 0xffffu), ve = exponent<BF>(m >> 16);
+    ((uint2*)A.pool.k)[row * LANES + at.c] = codes<BF>(k, ke);
+    ((uint2*)A.pool.v)[row * LANES + at.c] = codes<BF>(v, ve);
+    if (at.c == 0) {
+      ((uint8_t*)A.pool.ke)[row] = (uint8_t)(ke + 127);
+      ((uint8_t*)A.pool.ve)[row] = (uint8_t)(ve + 127);
     }
   } else {
-    ((uint4*)A.pool.k)[row * lanes + c] = k;
-    ((uint4*)A.pool.v)[row * lanes + c] = v;
+    ((uint4*)A.pool.k)[row * LANES + at.c] = k;
+    ((uint4*)A.pool.v)[row * LANES + at.c] = v;
   }
 }
 
-template <bool F8, bool BF>
+template <bool F8, bool BF, int LANES>
 __global__ __launch_bounds__(256) void k_kv_read(KvCopyArgs A) {
-  const int lanes = A.g.D >> 3;
-  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t r = x / lanes;
-  const int c = (int)(x - r * lanes);
-  const int64_t t = r / A.g.hkv;
-  const int head = (int)(r - t * A.g.hkv);
-  if (t >= A.n_tok) return;
-  const KvTok tok = A.tok[t];
+  const Place at(A, LANES);
+  if (at.t >= (uint32_t)A.n_tok) return;
+  const KvTok tok = A.tok[at.t];
   uint4 k = make_uint4(0, 0, 0, 0), v = k;
   if (tok.pos >= 0) {
     const int32_t page = A.table[(int64_t)tok.seq * A.cols + (tok.pos >> A.g.sh)];
-    const int64_t row = page_row(A.g, A.pool, page, head, tok.pos, A.err);
+    const int64_t row = page_row(A.g, A.pool, page, at.head, tok.pos, A.err);
     if (row >= 0) {
       if (F8) {
-        k = dequantise<BF>(((const uint2*)A.pool.k)[row * lanes + c], A.pool.ke[row]);
-        v = dequantise<BF>(((const uint2*)A.pool.v)[row * lanes + c], A.pool.ve[row]);
+        k = values<BF>(((const uint2*)A.pool.k)[row * LANES + at.c], A.pool.ke[row]);
+        v = values<BF>(((const uint2*)A.pool.v)[row * LANES + at.c], A.pool.ve[row]);
       } else {
-        k = ((const uint4*)A.pool.k)[row * lanes + c];
-        v = ((const uint4*)A.pool.v)[row * lanes + c];
+        k = ((const uint4*)A.pool.k)[row * LANES + at.c];
+        v = ((const uint4*)A.pool.v)[row * LANES + at.c];
       }
     }
   }
-  *(uint4*)((uint16_t*)A.k.p + t * A.k.tok + head * A.k.head + c * 8) = k;
-  *(uint4*)((uint16_t*)A.v.p + t * A.v.tok + head * A.v.head + c * 8) = v;
+  *(uint4*)at.k = k;
+  *(uint4*)at.v = v;
 }
 
-template <class Launch>
-hipError_t launch(const KvCopyArgs& a, Launch go) {
-  const int64_t n = (int64_t)a.n_tok * a.g.hkv * (a.g.D / 8);
-  go(dim3((unsigned)((n + 255) / 256)));
-  return hipGetLastError();
+template <int LANES>
+void append(const KvCopyArgs& a, unsigned n, hipStream_t stream) {
+  if (a.g.cache != kKvE4m3)
+    k_kv_append<false, false, LANES><<<n, 256, 0, stream>>>(a);
+  else if (a.g.dtype == kKvBf16)
+    k_kv_append<true, true, LANES><<<n, 256, 0, stream>>>(a);
+  else
+    k_kv_append<true, false, LANES><<<n, 256, 0, stream>>>(a);
+}
+
+template <int LANES>
+void read(const KvCopyArgs& a, unsigned n, hipStream_t stream) {
+  if (a.g.cache != kKvE4m3)
+    k_kv_read<false, false, LANES><<<n, 256, 0, stream>>>(a);
+  else if (a.g.dtype == kKvBf16)
+    k_kv_read<true, true, LANES><<<n, 256, 0, stream>>>(a);
+  else
+    k_kv_read<true, false, LANES><<<n, 256, 0, stream>>>(a);
+}
+
+unsigned blocks(const KvCopyArgs& a) {
+  return (unsigned)(((int64_t)a.n_tok * a.g.hkv * (a.g.D / 8) + 255) / 256);
 }
 
 }  // namespace
 
 hipError_t launch_kv_append(const KvCopyArgs& a, hipStream_t stream) {
-  return launch(a, [&](dim3 n) {
-    if (a.g.cache != kKvE4m3)
-      k_kv_append<false, false><<<n, 256, 0, stream>>>(a);
-    else if (a.g.dtype == kKvBf16)
-      k_kv_append<true, true><<<n, 256, 0, stream>>>(a);
-    else
-      k_kv_append<true, false><<<n, 256, 0, stream>>>(a);
-  });
+  if (a.g.D == 128)
+    append<16>(a, blocks(a), stream);
+  else
+    append<8>(a, blocks(a), stream);
+  return hipGetLastError();
 }
 
 hipError_t launch_kv_read(const KvCopyArgs& a, hipStream_t stream) {
-  return launch(a, [&](dim3 n) {
-    if (a.g.cache != kKvE4m3)
-      k_kv_read<false, false><<<n, 256, 0, stream>>>(a);
-    else if (a.g.dtype == kKvBf16)
-      k_kv_read<true, true><<<n, 256, 0, stream>>>(a);
-    else
-      k_kv_read<true, false><<<n, 256, 0, stream>>>(a);
-  });
+  if (a.g.D == 128)
+    read<16>(a, blocks(a), stream);
+  else
+    read<8>(a, blocks(a), stream);
+  return hipGetLastError();
 }
 
 }  // namespace lar
