@@ -26,8 +26,8 @@ namespace {
 constexpr int kStages = 2;       // pinned copies of a plan: one may be on its way while the next is written
 constexpr int kNarrowPerCu = 8;  // waves of the narrow kernel that a CU holds
 constexpr int kWidePerCu = 1;    // workgroups of the wide kernel that a CU holds
-// Least key tiles of a wave or workgroup: fewer would cost more to join than they save.
-constexpr int kNarrowLeast = 2, kWideLeast = 4;
+// Least key tiles of a workgroup's stretch: fewer would cost more to join than they save.
+constexpr int kWideLeast = 4;
 
 size_t up(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -135,6 +135,17 @@ struct Joins {
     most = std::max(most, parts);
   }
 };
+
+// Least key tiles of a wave's run.  A wave takes about 1.1 us for one; joining n parts of r
+// rows takes 0.26 us * n * r * D / 4096, since 1024 threads share their quads out.  A tile of
+// T key tiles in stretches of L then ends soonest with L = sqrt(T r D * 5.8e-5); measured at
+// T = 1179, r = 4 and 8, D = 128: 32 and 52 us with L = 2, 24 and 28 with 8, 31 and 33 with
+// 16; at T = 114, r = 4: 11.9 with 2, 12.9 with 1, 14.2 with 4.
+int narrow_least(const std::vector<Tile>& tiles, const KvGeom& g) {
+  double most = 0;
+  for (const Tile& t : tiles) most = std::max(most, (double)t.tiles * (t.s.ntok * g.G));
+  return std::max(2, (int)std::lround(std::sqrt(most * g.D * 5.8e-5)));
+}
 
 // Narrow tiles: cuts their key tiles into stretches of equal number, one run of them for each
 // of at most `most` waves; a tile that is cut goes to the join.
@@ -567,7 +578,7 @@ lar_status lar_kv_plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const i
     kv->lay = L;
     Joins join{(KvJoin*)(p + L.join), g.G};
     const int groups = nn ? split(narrow, wide, kv->groups, g) : kv->groups;
-    cut(narrow, nw ? (kv->groups - groups) * kWideWaves : kv->waves, kNarrowLeast, (KvSeg*)(p + L.narrow),
+    cut(narrow, nw ? (kv->groups - groups) * kWideWaves : kv->waves, narrow_least(narrow, g), (KvSeg*)(p + L.narrow),
         (int32_t*)(p + L.narrow_at), &n_narrow, &join);
     deal(wide, groups, (KvSeg*)(p + L.wide), (int32_t*)(p + L.wide_at), &n_wide, &join);
     n_join = join.n;
