@@ -1,0 +1,198 @@
+"""Batch-time coefficients of the attention, measured on the GPU that serves.
+
+The simulation times a token batch by T = a + b*P + c*D + d*C + e*A (lar_instance_params):
+P prefill tokens, D decoding sequences, C their context (KV-cache reads), A the prefill
+chunks' attention.  ``measure`` composes batches as the simulated scheduler does, under an
+instance's limits, runs each layer's append and attention on a paged key/value cache
+(``PagedKV``), times them, and ``fit`` turns the times into the attention's share of the
+coefficients -- d and e in full, and its part of a, b and c, to which the caller adds what
+the model's other layers take.  They go to ``LarContext.load_state`` as they are (ms).
+
+    python -m paper_2607_18253_amd.calibrate --layers 32 --cache e4m3
+"""
+
+from __future__ import annotations
+
+import argparse
+from dataclasses import dataclass
+
+import numpy as np
+
+from .kv import PagedKV
+
+NAMES = "abcde"
+
+
+@dataclass
+class Instance:
+    """Geometry and scheduler limits of a model instance (lar_kv_config, lar_sched_limits)."""
+    n_q_heads: int = 32
+    n_kv_heads: int = 8
+    head_dim: int = 128
+    layers: int = 32
+    token_budget: int = 4096
+    max_seqs: int = 256
+    chunk_cap: int = 512
+    kv_blocks: int = 18432
+    block_size: int = 16
+    max_ctx: int = 8192
+
+
+@dataclass
+class Batch:
+    """A token batch: new tokens and context (with them) per sequence, decodes first."""
+    q_len: np.ndarray
+    ctx_len: np.ndarray
+    n_dec: int
+
+    def features(self):
+        """(1, P, D, C, A) of lar_instance_params' batch time: contexts are those before the batch."""
+        q, before = self.q_len.astype(np.int64), self.ctx_len.astype(np.int64) - self.q_len
+        n = self.n_dec
+        chunk, at = q[n:], before[n:]
+        return (1, int(chunk.sum()), n, int(before[:n].sum()),
+                int((chunk * at + chunk * (chunk + 1) // 2).sum()))
+
+
+def compose(inst: Instance, rng, n_dec: int, prompts) -> Batch:
+    """A batch as the scheduler composes it: one token of each of n_dec decoding sequences,
+    then chunks of the prompts in order, at most chunk_cap each, while the budget, the
+    sequences and the pages last."""
+    S = inst.block_size
+    blocks, q, ctx = inst.kv_blocks, [], []
+    for _ in range(min(n_dec, inst.max_seqs, inst.token_budget)):
+        c = int(rng.integers(2, inst.max_ctx + 1))
+        if -(-c // S) > blocks:
+            break
+        blocks -= -(-c // S)
+        q.append(1)
+        ctx.append(c)
+    n, left = len(q), inst.token_budget - len(q)
+    for p in prompts:
+        done = int(rng.integers(0, p)) // inst.chunk_cap * inst.chunk_cap  # chunks of it before this one
+        chunk = min(p - done, inst.chunk_cap, left)
+        if chunk < 1 or len(q) == inst.max_seqs or -(-(done + chunk) // S) > blocks:
+            break
+        blocks -= -(-(done + chunk) // S)
+        left -= chunk
+        q.append(chunk)
+        ctx.append(done + chunk)
+    return Batch(np.array(q, np.int32), np.array(ctx, np.int32), n)
+
+
+def batches(inst: Instance, count: int, seed: int = 0):
+    """Batches over the range an instance runs: from a few sequences to full ones, decodes
+    alone, prefills alone and both."""
+    rng = np.random.default_rng(seed)
+    out = []
+    while len(out) < count:
+        kind = len(out) % 3
+        n_dec = 0 if kind == 1 else int(rng.integers(1, inst.max_seqs + 1))
+        room = (inst.token_budget - n_dec) // inst.chunk_cap + 1
+        n_pre = 0 if kind == 0 else int(rng.integers(1, room + 1))
+        prompts = np.clip(np.rint(rng.lognormal(6.5, 1.0, n_pre)), 16, inst.max_ctx - 1).astype(int)
+        b = compose(inst, rng, n_dec, prompts)
+        if len(b.q_len):
+            out.append(b)
+    return out
+
+
+def measure(inst: Instance, sample, *, e4m3: bool = False, dtype=None, seed: int = 0, repeat: int = 3):
+    """Milliseconds that all layers' append and attention of each batch take (the median of
+    `repeat` runs), on pages dealt out in random order."""
+    import torch
+    dtype = torch.bfloat16 if dtype is None else dtype
+    tokens = max(int(b.q_len.sum()) for b in sample)
+    kv = PagedKV(inst.n_q_heads, inst.n_kv_heads, inst.head_dim, block_size=inst.block_size, dtype=dtype,
+                 cache_dtype=torch.float8_e4m3fn if e4m3 else dtype, max_seqs=inst.max_seqs, max_tokens=tokens)
+    dev, S = kv.device, inst.block_size
+    g = torch.Generator(device=dev).manual_seed(seed)
+    rng = np.random.default_rng(seed)
+    pages = kv.new_pages(inst.kv_blocks)
+    for t in pages.tensors():   # contexts of earlier batches: any finite values will do
+        t.view(torch.uint8).fill_(0x38)
+    new = lambda heads: torch.randn((tokens, heads, inst.head_dim), device=dev, generator=g).to(dtype)
+    q, k, v = new(inst.n_q_heads), new(inst.n_kv_heads), new(inst.n_kv_heads)
+    out = torch.empty_like(q)
+    start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    times = []
+    with kv:
+        for b in sample:
+            need = -(-b.ctx_len // S)
+            table = np.zeros((len(need), int(need.max())), np.int32)
+            free = rng.permutation(inst.kv_blocks)[:int(need.sum())]
+            at = np.concatenate([[0], np.cumsum(need)])
+            for s, n in enumerate(need):
+                table[s, :n] = free[at[s]:at[s + 1]]
+            tab = torch.from_numpy(table).to(dev)
+            T = int(b.q_len.sum())
+            kv.plan(b.q_len, b.ctx_len)
+            got = []
+            for _ in range(repeat + 1):   # the first one warms up
+                start.record()
+                for _ in range(inst.layers):
+                    kv.append(pages, k[:T], v[:T], tab)
+                    kv.attend(pages, q[:T], tab, out=out[:T])
+                end.record()
+                end.synchronize()
+                got.append(start.elapsed_time(end))
+            times.append(sorted(got[1:])[repeat // 2])
+        kv.sync()
+    return np.array(times)
+
+
+def fit(features, ms):
+    """Coefficients a .. e >= 0 that take the features [n][5] to the times, least squares of
+    the relative errors; terms that no batch has, and those that would come out negative,
+    are 0."""
+    X, y = np.asarray(features, np.float64), np.asarray(ms, np.float64)
+    w = 1.0 / np.maximum(y, 1e-12)
+    size = np.abs(X).max(0)
+    use = list(np.nonzero(size)[0])
+    while use:
+        A = X[:, use] / size[use] * w[:, None]
+        c = np.linalg.lstsq(A, y * w, rcond=None)[0]
+        if (c >= 0).all():
+            out = np.zeros(X.shape[1])
+            out[use] = c / size[use]
+            return out
+        use.pop(int(np.argmin(c)))
+    return np.zeros(X.shape[1])
+
+
+def main(argv=None):
+    import torch
+    from .lar import LarContext
+    ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    for name, default in (("n_q_heads", 32), ("n_kv_heads", 8), ("head_dim", 128), ("layers", 32),
+                          ("token_budget", 4096), ("max_seqs", 256), ("chunk_cap", 512), ("kv_blocks", 18432),
+                          ("block_size", 16), ("max_ctx", 8192)):
+        ap.add_argument("--" + name.replace("_", "-"), type=int, default=default)
+    ap.add_argument("--cache", choices=("bf16", "e4m3"), default="bf16")
+    ap.add_argument("--batches", type=int, default=48)
+    a = vars(ap.parse_args(argv))
+    e4m3, count = a.pop("cache") == "e4m3", a.pop("batches")
+    inst = Instance(**a)
+    sample = batches(inst, count)
+    X = np.array([b.features() for b in sample])
+    ms = measure(inst, sample, e4m3=e4m3)
+    c = fit(X, ms)
+    for n, v in zip(NAMES, c):
+        print(f"{n} = {v:.6g} ms")
+    print(f"mean relative error over {len(ms)} batches: {np.mean(np.abs(X @ c - ms) / ms):.3f}")
+    # the simulation on them: one idle instance, prompts of several lengths
+    with LarContext(1, 1, max_seqs_cap=inst.max_seqs, queue_cap=16, max_prompt=inst.max_ctx) as ctx:
+        none = np.zeros(0, np.int32)
+        ctx.load_state(a=c[:1], b=c[1:2], c=c[2:3], d=c[3:4], e=c[4:5], budget=[inst.token_budget],
+                       max_seqs=[inst.max_seqs], col=[0], offsets=[0, 0], rem_prefill=none, rem_decode=none,
+                       context=none, clock_ms=[0.0])
+        prompts = [p for p in (128, 1024, 8191) if p < inst.max_ctx]
+        ttft, _ = ctx.estimate(torch.tensor(prompts, dtype=torch.int32, device="cuda"), 0.0)
+        ctx.sync()
+        for p, t in zip(prompts, ttft.flatten().tolist()):
+            print(f"attention's part of an idle instance's TTFT, {p}-token prompt: {t:.3f} ms")
+    return c
+
+
+if __name__ == "__main__":
+    main()

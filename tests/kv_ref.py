@@ -78,9 +78,8 @@ def attend_fast(q, k, v, mask, scale):
     """attend() with the rows at once, for finite inputs."""
     n, hq, d = q.shape
     G = hq // k.shape[1]
-    out, mag = torch.zeros(n, hq, d, dtype=torch.float64), torch.zeros(n, hq, d, dtype=torch.float64)
-    lse = torch.full((n, hq), -np.inf, dtype=torch.float64)
-    big = torch.zeros(n, hq, dtype=torch.float64)
+    out, mag = torch.zeros_like(q), torch.zeros_like(q)
+    lse, big = torch.full_like(q[..., 0], -np.inf), torch.zeros_like(q[..., 0])
     some = mask.any(1)
     for h in range(hq):
         kk, vv = k[:, h // G], v[:, h // G]

@@ -444,3 +444,65 @@ def test_batches_in_turn():
                 bo, _ = R.bounds(BF, mag, big, wz, 128, c[s], 8.0)
                 Batch.near(out[at:at + n[s]].double(), w, bo, (i, s))
             at += n[s]
+
+
+# ------------------------------------------------------------------ large plans, and the example
+def test_attend_long_chunk_marches():
+    """A chunk long enough that the workgroups of an XCD walk over the same keys: 32 tiles of
+    1094 key tiles and one of 1; the reference in 64 bits on the GPU, row by block of rows."""
+    hq, hkv, d, S, n, c = 4, 1, 64, 16, 2049, 70017
+    kv = PagedKV(hq, hkv, d, block_size=S, max_seqs=1, max_tokens=c)
+    g = torch.Generator(device=DEV).manual_seed(4)
+    k, v = (torch.randn((c, hkv, d), device=DEV, generator=g).to(BF) for _ in range(2))
+    q = (2 * torch.randn((n, hq, d), device=DEV, generator=g)).to(BF)
+    blocks = -(-c // S)
+    tab = torch.randperm(blocks, device=DEV, generator=g).int()[None].contiguous()
+    pages = kv.new_pages(blocks)
+    kv.plan([c], [c])
+    kv.append(pages, k, v, tab)
+    kv.plan([n], [c])
+    lse = torch.empty((n, hq), device=DEV)
+    out = kv.attend(pages, q, tab, lse=lse)
+    kv.sync()
+    kk, vv = k[:, 0].double(), v[:, 0].double()
+    for h in range(hq):
+        for a in range(0, n, 512):
+            b = min(n, a + 512)
+            mask = R.sees(b - a, c - n + b).to(DEV)
+            m = mask.shape[1]
+            want, wz, mag, big = R.attend_fast(q[a:b, h:h + 1].double(), kk[:m, None], vv[:m, None], mask, d ** -0.5)
+            bo, bz = R.bounds(BF, mag, big, wz, d, c, 6.0)
+            Batch.near(out[a:b, h:h + 1].double(), want.to(DEV), bo.to(DEV), (h, a))
+            Batch.near(lse[a:b, h:h + 1].double(), wz.to(DEV), bz.to(DEV), (h, a, "lse"))
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_attend_random_batches(seed):
+    """Random mixed batches: single tokens, short and long chunks, padding, windows, types."""
+    r = np.random.RandomState(100 + seed)
+    hkv = int(r.choice([1, 2, 3]))
+    G, d = int(r.choice([1, 3, 4, 8, 16])), int(r.choice([64, 128]))
+    dtype = [BF, F16][r.randint(2)]
+    cache = [dtype, E4][r.randint(2)]
+    n_seq = r.randint(1, 14)
+    q_len = [int(x) for x in np.where(r.rand(n_seq) < 0.5, 1, np.exp(r.uniform(0, 5.2, n_seq)))]
+    ctx = [int(x) for x in np.exp(r.uniform(0, 7.6, n_seq))]
+    ctx = [c if r.rand() < 0.15 else c + n for c, n in zip(ctx, q_len)]
+    window, sinks = (0, 0) if r.rand() < 0.5 else (int(np.exp(r.uniform(0, 6))), int(r.choice([0, 1, 4, 50])))
+    Batch(q_len, ctx, hq=hkv * G, hkv=hkv, d=d, S=int(r.choice([4, 16, 16, 32, 128])), dtype=dtype, cache=cache,
+          seed=seed).check(window, sinks)
+
+
+def test_calibration_runs_the_batches():
+    """The example: batches of a small instance through append and attention, its
+    coefficients fitted and handed to the simulation."""
+    from paper_2607_18253_amd import calibrate as K
+    inst = K.Instance(n_q_heads=8, n_kv_heads=2, head_dim=64, layers=2, token_budget=256, max_seqs=24, chunk_cap=64,
+                      kv_blocks=600, max_ctx=512)
+    some = K.batches(inst, 9, seed=2)
+    ms = K.measure(inst, some, e4m3=True)
+    assert ms.shape == (9,) and np.isfinite(ms).all() and (ms > 0).all()
+    c = K.fit([b.features() for b in some], ms)
+    assert np.isfinite(c).all() and (c >= 0).all() and c.any()
+    assert (K.main(["--layers", "2", "--kv-blocks", "2000", "--max-seqs", "32", "--token-budget", "512", "--max-ctx",
+                    "2048", "--chunk-cap", "128", "--batches", "12"]) >= 0).all()
