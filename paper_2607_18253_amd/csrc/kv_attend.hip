@@ -717,20 +717,21 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
       const int r = PAGED ? wave * (64 / St::kChunks) : r0;
       return kAll ? i * St::kStep + r : r & (kWideKeys - 1);
     };
-    const auto look = [&](int t, int32_t (&p)[I]) {
+    // the pages, and then the pool rows, of a tile whose first key is kb
+    const auto look = [&](int kb, int32_t (&p)[I]) {
 #pragma unroll
       for (int i = 0; i < I; ++i) {
-        const int col = (first(t) + row_of(i)) >> A.g.sh;
+        const int col = (kb + row_of(i)) >> A.g.sh;
         p[i] = table[(uint32_t)(col < last_col ? col : last_col)];
       }
     };
     // tiles start at multiples of 64: a key's row in its page is that of its row in the tile,
     // and in pages of more than 64 tokens the tile's place in the page
-    const auto rows = [&](int t, const int32_t (&p)[I], uint32_t (&r)[I]) {
+    const auto rows = [&](int kb, const int32_t (&p)[I], uint32_t (&r)[I]) {
 #pragma unroll
       for (int i = 0; i < I; ++i)
         r[i] = page_at(A, PAGED ? __builtin_amdgcn_readfirstlane(p[i]) : p[i], lost) +
-               (in_page(A, s.head, row_of(i)) + (uint32_t)(first(t) & mask));
+               (in_page(A, s.head, row_of(i)) + (uint32_t)(kb & mask));
     };
     const auto fetch_k = [&](St& x, const uint32_t (&r)[I]) {
 #pragma unroll
@@ -751,11 +752,11 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
       for (int i = 0; i < I; ++i)
         if (kAll || loads) x.put_k(ldk + at, i, i * St::kStep + r0, c, F8 ? scale_of(x.ks[i]) : 0.0f);
     };
-    const auto put_v = [&](const St& x, int t) {
-      const int kb = first(t);
+    // V of tile t, whose first key is kb; `plain`: every row sees all of it
+    const auto put_v = [&](const St& x, int t, int kb, bool plain) {
       char* vt = ldv + (t & 1) * kTileV;
       if (!kAll && !loads) return;
-      if (is_masked(A, s.p0, last, kb, kWideKeys)) {
+      if (!plain && is_masked(A, s.p0, last, kb, kWideKeys)) {
         bool bad = false;
 #pragma unroll
         for (int i = 0; i < I; ++i)
@@ -773,11 +774,11 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
     // product with V, beside the scores of the 32 keys from nb on (past the wave's last key
     // these are of any rows, and not used)
     const auto half = [&](int kb, const char* vt, bool more, int nb, const char* kt, const char* kn,
-                          f32x16 (&sc)[1], f32x16 (&next)[1]) {
-      if (!works(kb)) return;
+                          f32x16 (&sc)[1], f32x16 (&next)[1], bool plain) {
+      if (plain ? !wreal : !works(kb)) return;
       float mx = weigh_and_score<BF, D>(vt, kt, kn, kf, q, sc, next, a, A.scale, lane);
-      if (!more || !works(nb)) return;
-      if (is_masked(A, wfirst, wlast, nb, 32)) {
+      if (!plain && (!more || !works(nb))) return;
+      if (!plain && is_masked(A, wfirst, wlast, nb, 32)) {
         hide<1>(next, rw, nb, h, A.window);
         mx = peak<1>(next);
       }
@@ -789,13 +790,13 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
     uint32_t r0s[I], r1s[I];
     if (s.t0 < s.t1) {  // the first tiles, all on their way at once
       int32_t p0[I], p1[I], p2[I];
-      look(s.t0, p0);
-      look(s.t0 + 1, p1);
-      look(s.t0 + 2, p2);
-      look(s.t0 + 3, page);
-      rows(s.t0, p0, r0s);
-      rows(s.t0 + 1, p1, r1s);
-      rows(s.t0 + 2, p2, row);
+      look(first(s.t0), p0);
+      look(first(s.t0 + 1), p1);
+      look(first(s.t0 + 2), p2);
+      look(first(s.t0 + 3), page);
+      rows(first(s.t0), p0, r0s);
+      rows(first(s.t0 + 1), p1, r1s);
+      rows(first(s.t0 + 2), p2, row);
       fetch_k(s0, r0s);
       fetch_v(s0, r0s);
       fetch_k(s1, r1s);
@@ -805,7 +806,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
     __syncthreads();
     if (s.t0 < s.t1) {
       put_k(s0, kc);
-      put_v(s0, s.t0);
+      put_v(s0, s.t0, first(s.t0), false);
       put_k(s1, kn);
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): or every tile would wait for its next loads with q's
@@ -822,28 +823,44 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) kf[i] = k_part<D>(ldk + 32 * kRowK<D>, i, lane);
     }
-    for (int t = s.t0; t < s.t1; ++t) {
+    // Tile t; k0 .. k4: the first keys of it and of the four after it
+    const auto step = [&](int t, int k0, int k1, int k3, int k4, bool plain) {
       // what was fetched beside the last tile goes into LDS beside this one, where all waves
       // are past the tiles that were there
-      put_v(st, t + 1);
+      put_v(st, t + 1, k1, plain);
       put_k(st, kx);
       uint32_t next_row[I];
-      rows(t + 3, page, next_row);
+      rows(k3, page, next_row);
       fetch_v(st, row);
       fetch_k(st, next_row);
-      look(t + 4, page);
+      look(k4, page);
 #pragma unroll
       for (int i = 0; i < I; ++i) row[i] = next_row[i];
       const char* vt = ldv + (t & 1) * kTileV;
-      const int kb = tile_key<kWideKeys>(s, t);
-      half(kb, vt, true, kb + 32, ldk + kc + 32 * kRowK<D>, ldk + kn, sa, sb);
-      half(kb + 32, vt + 32 * kRowV<D>, t + 1 < s.t1, tile_key<kWideKeys>(s, t + 1), ldk + kn,
-           ldk + kn + 32 * kRowK<D>, sb, sa);
+      half(k0, vt, true, k0 + 32, ldk + kc + 32 * kRowK<D>, ldk + kn, sa, sb, plain);
+      half(k0 + 32, vt + 32 * kRowV<D>, plain || t + 1 < s.t1, k1, ldk + kn, ldk + kn + 32 * kRowK<D>, sb, sa, plain);
       const int z = kc;
       kc = kn;
       kn = kx;
       kx = z;
       lds_barrier();
+    };
+    // Plain tiles, which every row of the query tile sees whole, follow one another: from the
+    // first past the sinks and the last row's window's start up to the first row's position.
+    const int past = A.window && last >= A.window ? (last - A.window) / kWideKeys + 1 - s.fw + s.ns : 0;
+    const int plain0 = past > s.ns ? past : s.ns;
+    const int plain1 = s.p0 < 0 ? 0 : (s.p0 + 1) / kWideKeys - s.fw + s.ns;
+    int t = s.t0;
+    while (t < s.t1) {
+      // with the next one plain and four more to come, nothing is left to decide
+      const int stop = plain1 - 1 < s.t1 - 4 ? plain1 - 1 : s.t1 - 4;
+      if (t >= plain0)
+        for (int kb = tile_key<kWideKeys>(s, t); t < stop; ++t, kb += kWideKeys)
+          step(t, kb, kb + kWideKeys, kb + 3 * kWideKeys, kb + 4 * kWideKeys, true);
+      if (t < s.t1) {
+        step(t, first(t), first(t + 1), first(t + 3), first(t + 4), false);
+        ++t;
+      }
     }
     finish<BF, D>(A, s, a, lane, wave * 32, kWideRows, A.wide_o, A.wide_ml, lds + wave * 32 * kRowK<D>);
     if (flag) spread<BF, F8, D, kWideKeys>(A, s, lane, wave * 32, kWideRows, A.wide_o);
