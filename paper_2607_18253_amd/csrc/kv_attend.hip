@@ -463,6 +463,17 @@ __device__ __forceinline__ void finish(const KvAttendArgs& A, const KvSeg& s, co
   }
 }
 
+// The result of a query tile without keys, by `threads` threads: zeros.
+template <int D>
+__device__ __forceinline__ void blank(const KvAttendArgs& A, const KvSeg& s, int tid, int threads) {
+  for (int i = tid; i < s.ntok * A.g.G * (D / 8); i += threads) {
+    const int r = i / (D / 8), t = r / A.g.G;
+    const int64_t at = (int64_t)(s.q0 + t) * A.g.hq + s.head * A.g.G + r - t * A.g.G;
+    *(uint4*)((uint16_t*)A.out + at * D + i % (D / 8) * 8) = make_uint4(0, 0, 0, 0);
+    if (A.lse && i % (D / 8) == 0) A.lse[at] = -__builtin_inff();
+  }
+}
+
 // First key of tile t.
 template <int K>
 __device__ __forceinline__ int tile_key(const KvSeg& s, int t) {
@@ -688,134 +699,145 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
   const int run = run_of(blockIdx.x, A.n_wide), e = plan_at(A.wide_at, run + 1);
   bool lost = false;  // a page outside the pool
   int x = plan_at(A.wide_at, run);
-  if (x >= e) return;
-  KvSeg after = plan_at(A.wide, x);
-  for (; x < e; ++x) {
-    const KvSeg s = after;
-    after = plan_at(A.wide, x + 1 < e ? x + 1 : x);
-    s16x8 q[D / 16];
-    const Row rw = load_q<D>(A, lane_of(A, s, wave * 32 + n), h, q);
-    Sums<D> a;
-    a.clear();
-    const int last = s.p0 + s.ntok - 1;
+  // the current stretch, its queries, and its first keys on their way
+  KvSeg s;
+  s16x8 q[D / 16];
+  Row rw;
+  Sums<D> a;
+  int last, last_col, wfirst, wlast;
+  bool wreal;
+  const int32_t* table;
+  St st, s0, s1;
+  int32_t page[I];            // of the next tile whose K is fetched
+  uint32_t row[I], r1s[I];    // pool rows of the last tile whose K was fetched, the next V
+  const int mask = (1 << A.g.sh) - 1;
+  // where a thread's chunk lies from the row that its address is made of: its own, or the
+  // wave's first
+  const uint32_t at_row = PAGED ? lane / St::kChunks : 0, at_byte = at_row * (St::kChunks * 16) + c * 16;
+  // Loads are not skipped, so that what waits for one knows how many follow it: past the
+  // stretch's end they take its last tile.
+  const auto first = [&](int t) { return tile_key<kWideKeys>(s, t < s.t1 ? t : s.t1 - 1); };
+  const auto row_of = [&](int i) {
+    const int r = PAGED ? wave * (64 / St::kChunks) : r0;
+    return kAll ? i * St::kStep + r : r & (kWideKeys - 1);
+  };
+  // the pages, and then the pool rows, of a tile whose first key is kb
+  const auto look = [&](int kb, int32_t (&p)[I]) {
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      const int col = (kb + row_of(i)) >> A.g.sh;
+      p[i] = table[(uint32_t)(col < last_col ? col : last_col)];
+    }
+  };
+  // tiles start at multiples of 64: a key's row in its page is that of its row in the tile,
+  // and in pages of more than 64 tokens the tile's place in the page
+  const auto rows = [&](int kb, const int32_t (&p)[I], uint32_t (&r)[I]) {
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+      r[i] = page_at(A, PAGED ? __builtin_amdgcn_readfirstlane(p[i]) : p[i], lost) +
+             (in_page(A, s.head, row_of(i)) + (uint32_t)(kb & mask));
+  };
+  const auto fetch_k = [&](St& x, const uint32_t (&r)[I]) {
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      x.k[i] = St::load((const char*)A.pool.k, r[i], at_byte);
+      if (F8) x.ks[i] = (A.pool.ke + r[i])[at_row];
+    }
+  };
+  const auto fetch_v = [&](St& x, const uint32_t (&r)[I]) {
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      x.v[i] = St::load((const char*)A.pool.v, r[i], at_byte);
+      if (F8) x.vs[i] = (A.pool.ve + r[i])[at_row];
+    }
+  };
+  const auto put_k = [&](const St& x, int at) {
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+      if (kAll || loads) x.put_k(ldk + at, i, i * St::kStep + r0, c, F8 ? scale_of(x.ks[i]) : 0.0f);
+  };
+  // V of tile t, whose first key is kb; `plain`: every row sees all of it
+  const auto put_v = [&](const St& x, int t, int kb, bool plain) {
+    char* vt = ldv + (t & 1) * kTileV;
+    if (!kAll && !loads) return;
+    if (!plain && is_masked(A, s.p0, last, kb, kWideKeys)) {
+      bool bad = false;
+#pragma unroll
+      for (int i = 0; i < I; ++i)
+        bad |= x.template put_v<true>(vt, i, i * St::kStep + r0, c, last + 1 - kb, F8 ? scale_of(x.vs[i]) : 0.0f);
+      if (bad) flag = 1;
+    } else {
+#pragma unroll
+      for (int i = 0; i < I; ++i)
+        x.template put_v<false>(vt, i, i * St::kStep + r0, c, 0, F8 ? scale_of(x.vs[i]) : 0.0f);
+    }
+  };
+  const auto works = [&](int kb) { return wreal && kb <= wlast; };
+  s16x8 kf[kAhead];
+  // 32 keys from kb on, their scores in `sc`, their maximum taken: exponentials and the
+  // product with V, beside the scores of the 32 keys from nb on (past the wave's last key
+  // these are of any rows, and not used)
+  const auto half = [&](int kb, const char* vt, bool more, int nb, const char* kt, const char* kn,
+                        f32x16 (&sc)[1], f32x16 (&next)[1], bool plain) {
+    if (plain ? !wreal : !works(kb)) return;
+    float mx = weigh_and_score<BF, D>(vt, kt, kn, kf, q, sc, next, a, A.scale, lane);
+    if (!plain && (!more || !works(nb))) return;
+    if (!plain && is_masked(A, wfirst, wlast, nb, 32)) {
+      hide<1>(next, rw, nb, h, A.window);
+      mx = peak<1>(next);
+    }
+    raise<D>(a, mx * A.scale);
+  };
+  f32x16 sa[1], sb[1];
+  int kc = 0, kn = kTileK, kx = 2 * kTileK;  // K of this tile, the next and the one after
+  // Takes up the next stretch that has keys: its queries and first tiles, all on their way
+  // at once beside what the last one has left to do.
+  const auto next = [&]() {
+    for (; x < e; ++x) {
+      s = plan_at(A.wide, x);
+      if (s.t0 < s.t1) break;
+      blank<D>(A, s, tid, kThreads);
+    }
+    if (x++ >= e) return false;
+    rw = load_q<D>(A, lane_of(A, s, wave * 32 + n), h, q);
+    last = s.p0 + s.ntok - 1;
+    last_col = last >> A.g.sh;
     // positions of this wave's own rows: keys past the last are not seen by any
     const int wtok = (wave * 32 + 31) / A.g.G, wtok0 = wave * 32 / A.g.G;
-    const int wlast = s.p0 + (wtok < s.ntok ? wtok : s.ntok - 1), wfirst = s.p0 + (wtok0 < s.ntok ? wtok0 : s.ntok - 1);
-    const bool wreal = wave * 32 < s.ntok * A.g.G;
-    const int32_t* table = A.table + (int64_t)s.seq * A.cols;
-    St st;
-    int32_t page[I];   // of the next tile whose K is fetched
-    uint32_t row[I];   // pool rows of the last tile whose K was fetched, the next V
-    const int last_col = last >> A.g.sh, mask = (1 << A.g.sh) - 1;
-    // where a thread's chunk lies from the row that its address is made of: its own, or the
-    // wave's first
-    const uint32_t at_row = PAGED ? lane / St::kChunks : 0, at_byte = at_row * (St::kChunks * 16) + c * 16;
-    // Loads are not skipped, so that what waits for one knows how many follow it: past the
-    // stretch's end they take its last tile.
-    const auto first = [&](int t) { return tile_key<kWideKeys>(s, t < s.t1 ? t : s.t1 - 1); };
-    const auto row_of = [&](int i) {
-      const int r = PAGED ? wave * (64 / St::kChunks) : r0;
-      return kAll ? i * St::kStep + r : r & (kWideKeys - 1);
-    };
-    // the pages, and then the pool rows, of a tile whose first key is kb
-    const auto look = [&](int kb, int32_t (&p)[I]) {
-#pragma unroll
-      for (int i = 0; i < I; ++i) {
-        const int col = (kb + row_of(i)) >> A.g.sh;
-        p[i] = table[(uint32_t)(col < last_col ? col : last_col)];
-      }
-    };
-    // tiles start at multiples of 64: a key's row in its page is that of its row in the tile,
-    // and in pages of more than 64 tokens the tile's place in the page
-    const auto rows = [&](int kb, const int32_t (&p)[I], uint32_t (&r)[I]) {
-#pragma unroll
-      for (int i = 0; i < I; ++i)
-        r[i] = page_at(A, PAGED ? __builtin_amdgcn_readfirstlane(p[i]) : p[i], lost) +
-               (in_page(A, s.head, row_of(i)) + (uint32_t)(kb & mask));
-    };
-    const auto fetch_k = [&](St& x, const uint32_t (&r)[I]) {
-#pragma unroll
-      for (int i = 0; i < I; ++i) {
-        x.k[i] = St::load((const char*)A.pool.k, r[i], at_byte);
-        if (F8) x.ks[i] = (A.pool.ke + r[i])[at_row];
-      }
-    };
-    const auto fetch_v = [&](St& x, const uint32_t (&r)[I]) {
-#pragma unroll
-      for (int i = 0; i < I; ++i) {
-        x.v[i] = St::load((const char*)A.pool.v, r[i], at_byte);
-        if (F8) x.vs[i] = (A.pool.ve + r[i])[at_row];
-      }
-    };
-    const auto put_k = [&](const St& x, int at) {
-#pragma unroll
-      for (int i = 0; i < I; ++i)
-        if (kAll || loads) x.put_k(ldk + at, i, i * St::kStep + r0, c, F8 ? scale_of(x.ks[i]) : 0.0f);
-    };
-    // V of tile t, whose first key is kb; `plain`: every row sees all of it
-    const auto put_v = [&](const St& x, int t, int kb, bool plain) {
-      char* vt = ldv + (t & 1) * kTileV;
-      if (!kAll && !loads) return;
-      if (!plain && is_masked(A, s.p0, last, kb, kWideKeys)) {
-        bool bad = false;
-#pragma unroll
-        for (int i = 0; i < I; ++i)
-          bad |= x.template put_v<true>(vt, i, i * St::kStep + r0, c, last + 1 - kb, F8 ? scale_of(x.vs[i]) : 0.0f);
-        if (bad) flag = 1;
-      } else {
-#pragma unroll
-        for (int i = 0; i < I; ++i)
-          x.template put_v<false>(vt, i, i * St::kStep + r0, c, 0, F8 ? scale_of(x.vs[i]) : 0.0f);
-      }
-    };
-    const auto works = [&](int kb) { return wreal && kb <= wlast; };
-    s16x8 kf[kAhead];
-    // 32 keys from kb on, their scores in `sc`, their maximum taken: exponentials and the
-    // product with V, beside the scores of the 32 keys from nb on (past the wave's last key
-    // these are of any rows, and not used)
-    const auto half = [&](int kb, const char* vt, bool more, int nb, const char* kt, const char* kn,
-                          f32x16 (&sc)[1], f32x16 (&next)[1], bool plain) {
-      if (plain ? !wreal : !works(kb)) return;
-      float mx = weigh_and_score<BF, D>(vt, kt, kn, kf, q, sc, next, a, A.scale, lane);
-      if (!plain && (!more || !works(nb))) return;
-      if (!plain && is_masked(A, wfirst, wlast, nb, 32)) {
-        hide<1>(next, rw, nb, h, A.window);
-        mx = peak<1>(next);
-      }
-      raise<D>(a, mx * A.scale);
-    };
-    f32x16 sa[1], sb[1];
-    int kc = 0, kn = kTileK, kx = 2 * kTileK;  // K of this tile, the next and the one after
-    St s0, s1;
-    uint32_t r0s[I], r1s[I];
-    if (s.t0 < s.t1) {  // the first tiles, all on their way at once
-      int32_t p0[I], p1[I], p2[I];
-      look(first(s.t0), p0);
-      look(first(s.t0 + 1), p1);
-      look(first(s.t0 + 2), p2);
-      look(first(s.t0 + 3), page);
-      rows(first(s.t0), p0, r0s);
-      rows(first(s.t0 + 1), p1, r1s);
-      rows(first(s.t0 + 2), p2, row);
-      fetch_k(s0, r0s);
-      fetch_v(s0, r0s);
-      fetch_k(s1, r1s);
-    }
+    wlast = s.p0 + (wtok < s.ntok ? wtok : s.ntok - 1);
+    wfirst = s.p0 + (wtok0 < s.ntok ? wtok0 : s.ntok - 1);
+    wreal = wave * 32 < s.ntok * A.g.G;
+    table = A.table + (int64_t)s.seq * A.cols;
+    int32_t p0[I], p1[I], p2[I];
+    uint32_t r0s[I];
+    look(first(s.t0), p0);
+    look(first(s.t0 + 1), p1);
+    look(first(s.t0 + 2), p2);
+    look(first(s.t0 + 3), page);
+    rows(first(s.t0), p0, r0s);
+    rows(first(s.t0 + 1), p1, r1s);
+    rows(first(s.t0 + 2), p2, row);
+    fetch_k(s0, r0s);
+    fetch_v(s0, r0s);
+    fetch_k(s1, r1s);
+    return true;
+  };
+  bool more = next();
+  while (more) {
+    a.clear();
+    kc = 0;
+    kn = kTileK;
+    kx = 2 * kTileK;
     __syncthreads();  // the last stretch's tiles and flag are done with
     if (tid == 0) flag = 0;
     __syncthreads();
-    if (s.t0 < s.t1) {
-      put_k(s0, kc);
-      put_v(s0, s.t0, first(s.t0), false);
-      put_k(s1, kn);
-    }
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): or every tile would wait for its next loads with q's
-    if (s.t0 < s.t1) {
-      fetch_v(st, r1s);
-      fetch_k(st, row);
-    }
+    put_k(s0, kc);
+    put_v(s0, s.t0, first(s.t0), false);
+    put_k(s1, kn);
+    fetch_v(st, r1s);
+    fetch_k(st, row);
     lds_barrier();
-    if (s.t0 < s.t1 && works(tile_key<kWideKeys>(s, s.t0))) {
+    if (works(tile_key<kWideKeys>(s, s.t0))) {
       sa[0] = scores<BF, D>(ldk, q, n, h);
       const int kb = tile_key<kWideKeys>(s, s.t0);
       if (is_masked(A, wfirst, wlast, kb, 32)) hide<1>(sa, rw, kb, h, A.window);
@@ -862,8 +884,10 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
         ++t;
       }
     }
-    finish<BF, D>(A, s, a, lane, wave * 32, kWideRows, A.wide_o, A.wide_ml, lds + wave * 32 * kRowK<D>);
-    if (flag) spread<BF, F8, D, kWideKeys>(A, s, lane, wave * 32, kWideRows, A.wide_o);
+    const KvSeg done = s;
+    more = next();
+    finish<BF, D>(A, done, a, lane, wave * 32, kWideRows, A.wide_o, A.wide_ml, lds + wave * 32 * kRowK<D>);
+    if (flag) spread<BF, F8, D, kWideKeys>(A, done, lane, wave * 32, kWideRows, A.wide_o);
   }
   if (lost) *A.err = LAR_E_STATE;
 }
