@@ -59,7 +59,7 @@ struct lar_kv {
   bool used[kStages] = {};
   int stage = 0;
   float *narrow_o = nullptr, *wide_o = nullptr;
-  float2 *narrow_ml = nullptr, *wide_ml = nullptr;
+  float4 *narrow_ml = nullptr, *wide_ml = nullptr;
   int32_t* err = nullptr;
   // the plan
   bool planned = false;
@@ -498,8 +498,8 @@ lar_status lar_kv_create(lar_kv** out, const lar_kv_config* cfg) {
   bool ok = hipMalloc((void**)&kv->dev, kv->cap) == hipSuccess &&
             hipMalloc((void**)&kv->narrow_o, sizeof(float) * 2 * kv->waves * kNarrowRows * g.D) == hipSuccess &&
             hipMalloc((void**)&kv->wide_o, sizeof(float) * 2 * kv->groups * kWideRows * g.D) == hipSuccess &&
-            hipMalloc((void**)&kv->narrow_ml, sizeof(float2) * 2 * kv->waves * kNarrowRows) == hipSuccess &&
-            hipMalloc((void**)&kv->wide_ml, sizeof(float2) * 2 * kv->groups * kWideRows) == hipSuccess &&
+            hipMalloc((void**)&kv->narrow_ml, sizeof(float4) * 2 * kv->waves * kNarrowRows) == hipSuccess &&
+            hipMalloc((void**)&kv->wide_ml, sizeof(float4) * 2 * kv->groups * kWideRows) == hipSuccess &&
             hipMalloc((void**)&kv->err, sizeof(int32_t)) == hipSuccess &&
             hipMemset(kv->err, 0, sizeof(int32_t)) == hipSuccess;
   for (int i = 0; ok && i < kStages; ++i)

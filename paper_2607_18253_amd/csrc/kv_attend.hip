@@ -21,8 +21,12 @@
 //   k_kv_join    the partial sums of the tiles whose keys were split over waves.
 // A batch with both kinds of tiles is one launch of k_kv_wide.
 //
-// P is rounded to the 16-bit type of V (nearest even) for the second product, an error of
-// the size of the output's own rounding; sums are taken of the unrounded values.
+// For the second product P has to be of V's 16-bit type.  Single tokens on a 16-bit cache have
+// matrix instructions to spare: each weight is taken as two such values, 16 bits in all.
+// Else it is rounded once (nearest even), an error of the size of the output's own rounding,
+// and the result is divided by the sum of the rounded weights, so that nothing is lost of a
+// weight that outweighs the others; the log of the sum, where it is asked for, is that of the
+// unrounded ones.
 #include "../../include/lar.h"
 #include "kv_device.h"
 
@@ -53,6 +57,9 @@ template <> struct Elem<true> {
   static __device__ __forceinline__ s16x8 pack(f32x8 x) {
     return __builtin_bit_cast(s16x8, __builtin_convertvector(x, bf16x8));
   }
+  static __device__ __forceinline__ f32x8 unpack(s16x8 x) {
+    return __builtin_convertvector(__builtin_bit_cast(bf16x8, x), f32x8);
+  }
   static __device__ __forceinline__ uint32_t pair(uint32_t codes, float s, bool hi) {
     return hi ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, s, true))
               : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, s, false));
@@ -78,6 +85,9 @@ template <> struct Elem<false> {
   }
   static __device__ __forceinline__ s16x8 pack(f32x8 x) {
     return __builtin_bit_cast(s16x8, __builtin_convertvector(x, f16x8));
+  }
+  static __device__ __forceinline__ f32x8 unpack(s16x8 x) {
+    return __builtin_convertvector(__builtin_bit_cast(f16x8, x), f32x8);
   }
   static __device__ __forceinline__ uint32_t pair(uint32_t codes, float s, bool hi) {
     return hi ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, s, true))
@@ -211,7 +221,7 @@ __device__ __forceinline__ void hide(f32x16 (&s)[NB], const Row& r, int kb, int 
 template <int D>
 struct Sums {
   f32x16 o[D / 32];  // O^T: row n, value 32 b + key_of(i, h)
-  float m, l;        // maximum (log2 units); this half's part of the sum
+  float m, l, lr;    // maximum (log2 units); this half's part of the sum, and of what o has
   __device__ __forceinline__ void clear() {
     const float z = here(0.0f);
 #pragma unroll
@@ -219,7 +229,7 @@ struct Sums {
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[b][i] = z;
     m = -__builtin_inff();
-    l = 0.0f;
+    l = lr = 0.0f;
   }
 };
 
@@ -257,6 +267,7 @@ __device__ __forceinline__ void raise(Sums<D>& a, float mx) {
     const float f = m > a.m ? __builtin_amdgcn_exp2f(a.m - m) : 1.0f;  // 0 from a.m = -inf
     a.m = m;
     a.l *= f;
+    a.lr *= f;
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
 #pragma unroll
@@ -305,15 +316,36 @@ __device__ __forceinline__ s16x8 p_part(const f32x16& p, int t) {
   return Elem<BF>::pack(x);
 }
 
-// O^T += V^T P^T over 32 keys, `vt` their rows in LDS.
-template <bool BF, int D>
+// x plus the sum of 8 rounded weights.
+template <bool BF>
+__device__ __forceinline__ float add_rounded(s16x8 pk, float x) {
+  const uint4 w = __builtin_bit_cast(uint4, pk);
+  return Elem<BF>::add_pair(w.w, Elem<BF>::add_pair(w.z, Elem<BF>::add_pair(w.y, Elem<BF>::add_pair(w.x, x))));
+}
+
+// O^T += V^T P^T over 32 keys, `vt` their rows in LDS; TWO: P in two parts, the rounded
+// weights and what the rounding left.
+template <bool BF, int D, bool TWO>
 __device__ __forceinline__ void weigh(const char* vt, const f32x16& p, Sums<D>& a, int lane) {
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const s16x8 pk = p_part<BF>(p, t);
+    f32x8 x;
 #pragma unroll
-    for (int b = 0; b < D / 32; ++b) a.o[b] = Elem<BF>::mma(v_part<D>(vt + 16 * t * kRowV<D>, b, lane), pk, a.o[b]);
+    for (int j = 0; j < 8; ++j) x[j] = p[8 * t + j];
+    const s16x8 hi = Elem<BF>::pack(x);
+    s16x8 lo;
+    if (TWO)
+      lo = Elem<BF>::pack(x - Elem<BF>::unpack(hi));
+    else
+      a.lr = add_rounded<BF>(hi, a.lr);
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) {
+      const s16x8 v = v_part<D>(vt + 16 * t * kRowV<D>, b, lane);
+      a.o[b] = Elem<BF>::mma(v, hi, a.o[b]);
+      if (TWO) a.o[b] = Elem<BF>::mma(v, lo, a.o[b]);
+    }
   }
+  if (TWO) a.lr = a.l;
 }
 
 // K fragments that a wave has on their way from LDS ahead of their use.
@@ -329,7 +361,7 @@ __device__ __forceinline__ s16x8 k_part(const char* kt, int t, int lane) {
 // the maximum of those, and in `k` the first fragments of rows `kn`.  Exponentials and maxima
 // run in the shadow of the matrix instructions, LDS reads four of those ahead, in the order
 // written.
-template <bool BF, int D>
+template <bool BF, int D, bool LSE>
 __device__ __forceinline__ float weigh_and_score(const char* vt, const char* kt, const char* kn, s16x8 (&k)[kAhead],
                                                  const s16x8 (&q)[D / 16], f32x16 (&s)[1], f32x16 (&next)[1],
                                                  Sums<D>& a, float c, int lane) {
@@ -339,7 +371,7 @@ __device__ __forceinline__ float weigh_and_score(const char* vt, const char* kt,
   f32x16 x;
 #pragma unroll
   for (int i = 0; i < 16; ++i) x[i] = 0.0f;
-  float l = 0.0f;
+  float l = a.l, lr = a.lr;
 #pragma unroll
   for (int t = 0; t < kSteps; ++t) {
     x = Elem<BF>::mma(k[t % kAhead], q[t], x);
@@ -349,13 +381,18 @@ __device__ __forceinline__ float weigh_and_score(const char* vt, const char* kt,
     for (int e = t * kEach; e < (t + 1) * kEach; ++e) {
       const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][e], c, -m));
       s[0][e] = y;
-      l += y;
-      if ((e & 7) == 7) pk[e >> 3] = here(p_part<BF>(s[0], e >> 3));
+      if (LSE) l += y;
+      if ((e & 7) == 7) {
+        pk[e >> 3] = here(p_part<BF>(s[0], e >> 3));
+        lr = add_rounded<BF>(pk[e >> 3], lr);
+      }
     }
-    l = here(l);
+    if (LSE) l = here(l);
+    lr = here(lr);
     __builtin_amdgcn_sched_barrier(0);
   }
-  a.l += l;
+  a.l = l;
+  a.lr = lr;
   float mx = x[0];
 #pragma unroll
   for (int t = 0; t < 2; ++t)
@@ -418,11 +455,11 @@ __device__ __forceinline__ int64_t part_at(int slot, int rows, int row, int quad
 // written, or their partial sums (`row0`: first row of the wave in the slot, `rows` of one).
 template <bool BF, int D>
 __device__ __forceinline__ void finish(const KvAttendArgs& A, const KvSeg& s, const Sums<D>& a, int lane,
-                                       int row0, int rows, float* po, float2* pml, char* tmp) {
+                                       int row0, int rows, float* po, float4* pml, char* tmp) {
   lane = here(lane);
   const int n = lane & 31, h = lane >> 5, slot = s.slot;
   const Lane x = lane_of(A, s, row0 + n);
-  const float l = add_halves(a.l);
+  const float l = add_halves(a.l), lr = add_halves(a.lr);
   if (slot >= 0) {
     if (!x.real) return;
 #pragma unroll
@@ -432,11 +469,11 @@ __device__ __forceinline__ void finish(const KvAttendArgs& A, const KvSeg& s, co
         f32x4 y = {a.o[b][i], a.o[b][i + 1], a.o[b][i + 2], a.o[b][i + 3]};
         *(f32x4*)(po + part_at<D>(slot, rows, row0 + n, 8 * b + key_of(i, h) / 4)) = y;
       }
-    if (h == 0) pml[(int64_t)slot * rows + row0 + n] = make_float2(a.m, l);
+    if (h == 0) pml[(int64_t)slot * rows + row0 + n] = make_float4(a.m, l, lr, 0.0f);
     return;
   }
   const bool none = x.row.pos < 0;
-  const float f = none ? 0.0f : 1.0f / l;
+  const float f = none ? 0.0f : 1.0f / lr;
 #pragma unroll
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
@@ -654,7 +691,7 @@ __device__ __forceinline__ void narrow(const KvAttendArgs& A, char* lds, int run
       if (masked) hide<1>(sc, row, kb, h, A.window);
       raise<D>(a, peak<1>(sc) * A.scale);
       soften<D, 1>(sc, a, A.scale);
-      weigh<BF, D>(vt, sc[0], a, lane);
+      weigh<BF, D, !F8>(vt, sc[0], a, lane);
       wave_order();
     }
     finish<BF, D>(A, s, a, lane, 0, kNarrowRows, A.narrow_o, A.narrow_ml, lds);
@@ -676,7 +713,8 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
 //
 // PAGED: pages of 16 tokens and more.  The rows that a wave loads with one instruction (4, 8
 // or 16) then lie in one page, and their address is the wave's: the scalar unit's work.
-template <bool BF, bool F8, int D, bool PAGED>
+// LSE: the log of the sums is asked for.
+template <bool BF, bool F8, int D, bool PAGED, bool LSE>
 __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) {
   constexpr int kTileK = kWideKeys * kRowK<D>, kTileV = kWideKeys * kRowV<D>, kThreads = 64 * kWideWaves;
   constexpr int kNarrow = kTileBytes<D, kNarrowKeys>, kWide = 3 * kTileK + 2 * kTileV;
@@ -780,7 +818,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
   const auto half = [&](int kb, const char* vt, bool more, int nb, const char* kt, const char* kn,
                         f32x16 (&sc)[1], f32x16 (&next)[1], bool plain) {
     if (plain ? !wreal : !works(kb)) return;
-    float mx = weigh_and_score<BF, D>(vt, kt, kn, kf, q, sc, next, a, A.scale, lane);
+    float mx = weigh_and_score<BF, D, LSE>(vt, kt, kn, kf, q, sc, next, a, A.scale, lane);
     if (!plain && (!more || !works(nb))) return;
     if (!plain && is_masked(A, wfirst, wlast, nb, 32)) {
       hide<1>(next, rw, nb, h, A.window);
@@ -897,7 +935,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
 // leave threads over, these share out the slots and are joined through LDS, in their order.
 // Bound by the latency of the slots' loads, of which each thread has four on their way.
 struct Part {
-  float m, l;
+  float m, l, lr;
   f32x4 o;
   // The sums of two parts of a row's keys.
   __device__ __forceinline__ void join(const Part& p) {
@@ -905,6 +943,7 @@ struct Part {
     const float f = __builtin_amdgcn_exp2f(m - t), g = __builtin_amdgcn_exp2f(p.m - t);
     m = top;
     l = __builtin_fmaf(p.l, g, l * f);
+    lr = __builtin_fmaf(p.lr, g, lr * f);
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(p.o[i], g, o[i] * f);
   }
@@ -918,23 +957,24 @@ __global__ __launch_bounds__(THREADS) void k_kv_join(KvAttendArgs A) {
   const int rows = j.wide ? kWideRows : kNarrowRows, row0 = j.row0;
   const int have = j.ntok * A.g.G - row0 < 32 ? j.ntok * A.g.G - row0 : 32;
   const float* po = j.wide ? A.wide_o : A.narrow_o;
-  const float2* pml = j.wide ? A.wide_ml : A.narrow_ml;
+  const float4* pml = j.wide ? A.wide_ml : A.narrow_ml;
   const int n = have * kQuads;  // quads of values
   int share = THREADS / n;      // threads on the same one
   share = share < 1 ? 1 : share < j.n ? share : j.n;
   const int mine = n < THREADS ? threadIdx.x / n : 0;
   for (int u = n < THREADS ? threadIdx.x % n : threadIdx.x; u < n; u += THREADS) {
     const int r = u % have, d = (u / have) * 4;
-    Part a{-__builtin_inff(), 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
+    Part a{-__builtin_inff(), 0.0f, 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
     if (mine < share) {
       for (int s = mine; s < j.n; s += 4 * share) {
         Part p[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int x = s + k * share < j.n ? s + k * share : s;
-          const float2 ml = pml[(int64_t)(j.slot + x) * rows + row0 + r];
+          const float4 ml = pml[(int64_t)(j.slot + x) * rows + row0 + r];
           p[k].m = ml.x;
           p[k].l = ml.y;
+          p[k].lr = ml.z;
           p[k].o = *(const f32x4*)(po + part_at<D>(j.slot + x, rows, row0 + r, d / 4));
         }
 #pragma unroll
@@ -951,7 +991,7 @@ __global__ __launch_bounds__(THREADS) void k_kv_join(KvAttendArgs A) {
     if (mine != 0) continue;
     const int t = (row0 + r) / A.g.G, g = row0 + r - t * A.g.G;
     const bool none = j.p0 + t < 0;
-    const float inv = none ? 0.0f : 1.0f / a.l;
+    const float inv = none ? 0.0f : 1.0f / a.lr;
     const int64_t at = (int64_t)(j.q0 + t) * A.g.hq + j.head * A.g.G + g;
     uint32_t w[2];
 #pragma unroll
@@ -970,10 +1010,14 @@ template <bool BF, bool F8, int D>
 hipError_t run(const KvAttendArgs& a, hipStream_t stream) {
   if (a.n_wide) {
     const dim3 grid(a.n_wide + (a.n_narrow + kWideWaves - 1) / kWideWaves);
-    if (a.g.sh >= 4)
-      k_kv_wide<BF, F8, D, true><<<grid, 64 * kWideWaves, 0, stream>>>(a);
+    if (a.g.sh >= 4 && a.lse)
+      k_kv_wide<BF, F8, D, true, true><<<grid, 64 * kWideWaves, 0, stream>>>(a);
+    else if (a.g.sh >= 4)
+      k_kv_wide<BF, F8, D, true, false><<<grid, 64 * kWideWaves, 0, stream>>>(a);
+    else if (a.lse)
+      k_kv_wide<BF, F8, D, false, true><<<grid, 64 * kWideWaves, 0, stream>>>(a);
     else
-      k_kv_wide<BF, F8, D, false><<<grid, 64 * kWideWaves, 0, stream>>>(a);
+      k_kv_wide<BF, F8, D, false, false><<<grid, 64 * kWideWaves, 0, stream>>>(a);
   } else if (a.n_narrow) {
     k_kv_narrow<BF, F8, D><<<a.n_narrow, 64, 0, stream>>>(a);
   }
