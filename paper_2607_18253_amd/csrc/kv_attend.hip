@@ -711,10 +711,9 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
 // The workgroups past n_wide take narrow tiles, a run for each wave: the two kinds share the
 // device, one bound by matrix instructions and the other by memory.
 //
-// PAGED: pages of 16 tokens and more.  The rows that a wave loads with one instruction (4, 8
-// or 16) then lie in one page, and their address is the wave's: the scalar unit's work.
-// LSE: the log of the sums is asked for.
-template <bool BF, bool F8, int D, bool PAGED, bool LSE>
+// LSE: the log of the sums is asked for, which takes the sum of the unrounded weights too
+// (7681 tokens at 131072: 16.3 ms with it, 15.9 without; heads of 64: 10.0 and 9.5).
+template <bool BF, bool F8, int D, bool LSE>
 __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) {
   constexpr int kTileK = kWideKeys * kRowK<D>, kTileV = kWideKeys * kRowV<D>, kThreads = 64 * kWideWaves;
   constexpr int kNarrow = kTileBytes<D, kNarrowKeys>, kWide = 3 * kTileK + 2 * kTileV;
@@ -749,16 +748,10 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
   int32_t page[I];            // of the next tile whose K is fetched
   uint32_t row[I], r1s[I];    // pool rows of the last tile whose K was fetched, the next V
   const int mask = (1 << A.g.sh) - 1;
-  // where a thread's chunk lies from the row that its address is made of: its own, or the
-  // wave's first
-  const uint32_t at_row = PAGED ? lane / St::kChunks : 0, at_byte = at_row * (St::kChunks * 16) + c * 16;
   // Loads are not skipped, so that what waits for one knows how many follow it: past the
   // stretch's end they take its last tile.
   const auto first = [&](int t) { return tile_key<kWideKeys>(s, t < s.t1 ? t : s.t1 - 1); };
-  const auto row_of = [&](int i) {
-    const int r = PAGED ? wave * (64 / St::kChunks) : r0;
-    return kAll ? i * St::kStep + r : r & (kWideKeys - 1);
-  };
+  const auto row_of = [&](int i) { return kAll ? i * St::kStep + r0 : r0 & (kWideKeys - 1); };
   // the pages, and then the pool rows, of a tile whose first key is kb
   const auto look = [&](int kb, int32_t (&p)[I]) {
 #pragma unroll
@@ -772,21 +765,20 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
   const auto rows = [&](int kb, const int32_t (&p)[I], uint32_t (&r)[I]) {
 #pragma unroll
     for (int i = 0; i < I; ++i)
-      r[i] = page_at(A, PAGED ? __builtin_amdgcn_readfirstlane(p[i]) : p[i], lost) +
-             (in_page(A, s.head, row_of(i)) + (uint32_t)(kb & mask));
+      r[i] = page_at(A, p[i], lost) + (in_page(A, s.head, row_of(i)) + (uint32_t)(kb & mask));
   };
   const auto fetch_k = [&](St& x, const uint32_t (&r)[I]) {
 #pragma unroll
     for (int i = 0; i < I; ++i) {
-      x.k[i] = St::load((const char*)A.pool.k, r[i], at_byte);
-      if (F8) x.ks[i] = (A.pool.ke + r[i])[at_row];
+      x.k[i] = St::load((const char*)A.pool.k, r[i], c * 16);
+      if (F8) x.ks[i] = A.pool.ke[r[i]];
     }
   };
   const auto fetch_v = [&](St& x, const uint32_t (&r)[I]) {
 #pragma unroll
     for (int i = 0; i < I; ++i) {
-      x.v[i] = St::load((const char*)A.pool.v, r[i], at_byte);
-      if (F8) x.vs[i] = (A.pool.ve + r[i])[at_row];
+      x.v[i] = St::load((const char*)A.pool.v, r[i], c * 16);
+      if (F8) x.vs[i] = A.pool.ve[r[i]];
     }
   };
   const auto put_k = [&](const St& x, int at) {
@@ -1010,18 +1002,16 @@ template <bool BF, bool F8, int D>
 hipError_t run(const KvAttendArgs& a, hipStream_t stream) {
   if (a.n_wide) {
     const dim3 grid(a.n_wide + (a.n_narrow + kWideWaves - 1) / kWideWaves);
-    if (a.g.sh >= 4 && a.lse)
-      k_kv_wide<BF, F8, D, true, true><<<grid, 64 * kWideWaves, 0, stream>>>(a);
-    else if (a.g.sh >= 4)
-      k_kv_wide<BF, F8, D, true, false><<<grid, 64 * kWideWaves, 0, stream>>>(a);
-    else if (a.lse)
-      k_kv_wide<BF, F8, D, false, true><<<grid, 64 * kWideWaves, 0, stream>>>(a);
+    if (a.lse)
+      k_kv_wide<BF, F8, D, true><<<grid, 64 * kWideWaves, 0, stream>>>(a);
     else
-      k_kv_wide<BF, F8, D, false, false><<<grid, 64 * kWideWaves, 0, stream>>>(a);
+      k_kv_wide<BF, F8, D, false><<<grid, 64 * kWideWaves, 0, stream>>>(a);
   } else if (a.n_narrow) {
     k_kv_narrow<BF, F8, D><<<a.n_narrow, 64, 0, stream>>>(a);
   }
-  // many parts of few rows: more threads to share them out to
+  // Many parts of few rows: more threads to share them out to (one token over 3.6k and over
+  // 37.7k keys: 12.2 and 43 us with 1024 threads, 13.5 and 57 with 256); few parts of many
+  // tiles: smaller workgroups (255 decode tokens: 263 us with 256, 267 with 1024).
   if (a.n_join && a.most_parts > 8)
     k_kv_join<BF, D, 1024><<<a.n_join, 1024, 0, stream>>>(a);
   else if (a.n_join)

@@ -47,7 +47,7 @@ def test_bad_configurations_rejected_without_gpu(field, value):
 def test_cache_kernels_keep_their_registers(kernels):  # noqa: F811
     """The cache's kernels use no scratch memory, and the wide ones' workgroups fit a CU."""
     names = [n for n in kernels if "k_kv_" in n]
-    assert sum("k_kv_wide" in n for n in names) == 32 and sum("k_kv_narrow" in n for n in names) == 8
+    assert sum("k_kv_wide" in n for n in names) == 16 and sum("k_kv_narrow" in n for n in names) == 8
     for n in names:
         k = kernels[n]
         assert k[".private_segment_fixed_size"] == 0 and k[".vgpr_spill_count"] == 0, n
