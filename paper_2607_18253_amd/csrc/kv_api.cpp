@@ -531,15 +531,23 @@ lar_status lar_kv_plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const i
     return fail(kv, LAR_E_ARG, "%d sequences, at most %d", n_seqs, kv->cfg.max_seqs);
   if (n_seqs && (!q_len || !ctx_len)) return fail(kv, LAR_E_ARG, "null lengths");
   if (window < 0 || sinks < 0) return fail(kv, LAR_E_ARG, "negative window or sinks");
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (kv->stream) KV_TRY(kv, hipStreamIsCapturing(kv->stream, &capture));
+  if (capture != hipStreamCaptureStatusNone) return fail(kv, LAR_E_STATE, "no plan under stream capture");
   int64_t T = 0, pages = 0;
+  int32_t longest = 0;
   for (int s = 0; s < n_seqs; ++s) {
     if (q_len[s] < 0 || ctx_len[s] < 0 || ctx_len[s] > 1 << 30)
       return fail(kv, LAR_E_ARG, "sequence %d: %d new tokens, context %d", s, q_len[s], ctx_len[s]);
     T += q_len[s];
+    if (q_len[s]) longest = std::max(longest, ctx_len[s]);
     if (q_len[s]) pages = std::max<int64_t>(pages, ceil_div(ctx_len[s], (int64_t)1 << kv->g.sh));
   }
   if (T > kv->cfg.max_tokens)
     return fail(kv, LAR_E_ARG, "%lld new tokens, at most %d", (long long)T, kv->cfg.max_tokens);
+  // A window of every context hides nothing.  The kernels subtract a shorter one, and then a
+  // key of a context, from a position: all within 2^30, so within 32 bits.
+  if (window >= longest) window = 0;
   // the copy that last left this buffer is done before it is written again
   const int b = kv->stage;
   if (kv->used[b]) KV_TRY(kv, hipEventSynchronize(kv->done[b]));

@@ -196,6 +196,28 @@ def test_attend_window(window, sinks, cache, d):
           cache=cache).check(window, sinks)
 
 
+@pytest.mark.parametrize("window,sinks", [(1000, 0), (1001, 1), (999, 2 ** 31 - 1), (2 ** 30 + 7, 0),
+                                          (2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1)])
+@pytest.mark.parametrize("cache", [BF, E4])
+def test_attend_window_of_whole_contexts(window, sinks, cache):
+    """Windows and sinks as long as the longest context and longer, up to the largest number."""
+    Batch([1, 3, 70, 40, 5], [300, 1000, 400, 1000, 3], hq=8, hkv=2, d=64, S=16, dtype=BF, cache=cache).check(window, sinks)
+
+
+def test_no_plan_under_capture():
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        kv = PagedKV(8, 2, 64, block_size=16, max_seqs=1, max_tokens=4)
+        x = torch.zeros(4, device=DEV)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            refused(L.LAR_E_STATE, kv.plan, [1], [4])
+            x.fill_(1.0)
+        kv.plan([1], [4])
+        kv.sync()
+
+
 @pytest.mark.parametrize("cache", [BF, E4])
 def test_attend_padding_rows(cache):
     """Empty slots, and tokens before the first position: they see nothing."""
