@@ -16,10 +16,13 @@ KV_F16, KV_BF16, KV_E4M3 = 0, 1, 2
 
 
 def _raw_stream(index):
-    """hipStream_t of the current stream of a device (None where torch has no short way)."""
+    """hipStream_t of the current stream of a device; from the first call on, torch's short way
+    to it where it has one."""
+    global _raw_stream
     import torch
-    f = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return f(index) if f else torch.cuda.current_stream(index).cuda_stream
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                          lambda i: torch.cuda.current_stream(i).cuda_stream)
+    return _raw_stream(index)
 
 
 class KvConfig(C.Structure):
@@ -59,7 +62,7 @@ class KvPages:
                                _dev(k_exp, torch.uint8, "k_exp"), _dev(v_exp, torch.uint8, "v_exp"),
                                int(k.shape[0]))
         self._ref = C.byref(self._arg)
-        self._kind = (k.dtype, *k.shape[1:], k.device)
+        self._kind = (k.dtype, *k.shape[1:], k.get_device())
 
     def tensors(self):
         return [t for t in (self.k, self.v, self.k_exp, self.v_exp) if t is not None]
@@ -97,11 +100,14 @@ class PagedKV:
         if st != LAR_OK:
             raise LarError(st, "lar_kv_create failed")
         self._h = h
-        self._n_seq = self._n_tok = 0
-        self._kind = (self.cache_dtype, self.n_kv, self.block_size, self.head_dim, self.device)
+        self._int32, self._index = torch.int32, self.device.index
+        self._none = torch.empty(0, dtype=self.dtype, device=self.device)
+        self._scale = 1.0 / math.sqrt(self.head_dim)
+        self._batch(0, 0)
+        self._kind = (self.cache_dtype, self.n_kv, self.block_size, self.head_dim, self._index)
         # the arguments of a call are read before it returns: one record each will do
-        self._args = {n: KvRowsArg() for n in ("q", "k", "v")}
-        self._refs = {n: C.byref(a) for n, a in self._args.items()}
+        args = {n: KvRowsArg() for n in ("q", "k", "v")}
+        self._args = {n: (a, C.byref(a)) for n, a in args.items()}
 
     # ------------------------------------------------------------------ plumbing
     def _check(self, st: int):
@@ -131,25 +137,27 @@ class PagedKV:
                              f"of {self.cache_dtype} on {self.device}")
         return pages._ref
 
-    def _rows(self, t, heads, name):
-        if t.dtype is not self.dtype or t.device != self.device:
+    def _rows(self, t, shape, name):
+        if t.dtype is not self.dtype or t.get_device() != self._index:
             raise ValueError(f"{name} must be a tensor of {self.dtype} on {self.device}")
-        if t.shape != (self._n_tok, heads, self.head_dim) or t.stride(2) != 1:
-            raise ValueError(f"{name} must be [{self._n_tok}][{heads}][{self.head_dim}] with "
-                             "contiguous rows")
-        a = self._args[name]
+        if t.shape != shape:
+            raise ValueError(f"{name} must be [{shape[0]}][{shape[1]}][{shape[2]}]")
+        a, ref = self._args[name]
+        a.tok_stride, a.head_stride, last = t.stride()
+        if last != 1:
+            raise ValueError(f"{name} must have contiguous rows")
         a.data = t.data_ptr()
-        a.tok_stride, a.head_stride, _ = t.stride()
-        return self._refs[name]
+        return ref
 
     def _table(self, table):
-        if table.dim() != 2 or table.shape[0] < self._n_seq:
+        shape = table.shape
+        if len(shape) != 2 or shape[0] < self._n_seq:
             raise ValueError(f"table must have {self._n_seq} rows")
-        return _dev(table, self._torch.int32, "table"), table.shape[1]
+        return _dev(table, self._int32, "table"), shape[1]
 
-    def _call(self, f, tensors, *args):
+    def _call(self, f, pages, tensors, *args):
         """f(handle, *args) in order with the current stream."""
-        if _raw_stream(self.device.index) == self._sid:
+        if _raw_stream(self._index) == self._sid:
             st = f(self._h, *args)
             if st != LAR_OK:
                 self._check(st)
@@ -161,9 +169,15 @@ class PagedKV:
         try:
             self._check(f(self._h, *args))
         finally:
-            for t in tensors:
-                t.record_stream(self.stream)
+            for t in (*tensors, *pages.tensors()):
+                if t is not None:
+                    t.record_stream(self.stream)
             now.wait_stream(self.stream)
+
+    def _batch(self, n_seq, n_tok):
+        self._n_seq, self._n_tok = n_seq, n_tok
+        self._q_shape = (n_tok, self.n_q, self.head_dim)
+        self._kv_shape = (n_tok, self.n_kv, self.head_dim)
 
     # ------------------------------------------------------------------ calls
     def new_pages(self, n_blocks: int) -> KvPages:
@@ -183,44 +197,41 @@ class PagedKV:
         if q.ndim != 1 or q.shape != c.shape:
             raise ValueError("q_len and ctx_len must be one-dimensional and of one length")
         self._check(self._L.lar_kv_plan(self._h, len(q), q.ctypes.data, c.ctypes.data, int(window), int(sinks)))
-        self._n_seq, self._n_tok = len(q), int(q.sum())
+        self._batch(len(q), int(q.sum()))
 
     def append(self, pages: KvPages, k, v, table):
         """The batch's K and V rows [T][n_kv][head_dim] into the pages."""
-        p = self._pages(pages)
-        ka, va = self._rows(k, self.n_kv, "k"), self._rows(v, self.n_kv, "v")
         t, cols = self._table(table)
-        self._call(self._L.lar_kv_append, (k, v, table, *pages.tensors()), p, ka, va, t, cols)
+        self._call(self._L.lar_kv_append, pages, (k, v, table), self._pages(pages),
+                   self._rows(k, self._kv_shape, "k"), self._rows(v, self._kv_shape, "v"), t, cols)
 
     def read(self, pages: KvPages, table, k=None, v=None):
         """The rows of the batch's tokens back from the pages: (k, v), each
         [T][n_kv][head_dim] of dtype."""
-        torch = self._torch
-        shape = (self._n_tok, self.n_kv, self.head_dim)
         if k is None:
-            k = torch.empty(shape, dtype=self.dtype, device=self.device)
+            k = self._none.new_empty(self._kv_shape)
         if v is None:
-            v = torch.empty(shape, dtype=self.dtype, device=self.device)
-        p = self._pages(pages)
-        ka, va = self._rows(k, self.n_kv, "k"), self._rows(v, self.n_kv, "v")
+            v = self._none.new_empty(self._kv_shape)
         t, cols = self._table(table)
-        self._call(self._L.lar_kv_read, (k, v, table, *pages.tensors()), p, t, cols, ka, va)
+        self._call(self._L.lar_kv_read, pages, (k, v, table), self._pages(pages), t, cols,
+                   self._rows(k, self._kv_shape, "k"), self._rows(v, self._kv_shape, "v"))
         return k, v
 
     def attend(self, pages: KvPages, q, table, scale=None, out=None, lse=None):
         """Attention of the batch's queries [T][n_q][head_dim] over the pages; scale
         defaults to head_dim ** -0.5.  Returns out [T][n_q][head_dim]; lse, when given, is
         a float32 tensor [T][n_q] that takes the log of each row's sum."""
-        torch = self._torch
         n = self._n_tok * self.n_q
+        qa = self._rows(q, self._q_shape, "q")
         if out is None:
-            out = torch.empty((self._n_tok, self.n_q, self.head_dim), dtype=self.dtype, device=self.device)
-        p, qa = self._pages(pages), self._rows(q, self.n_q, "q")
+            out = self._none.new_empty(self._q_shape)
+            to = out.data_ptr()
+        else:
+            to = _dev(out, self.dtype, "out", n * self.head_dim)
         t, cols = self._table(table)
-        held = (q, out, table, *pages.tensors()) if lse is None else (q, out, lse, table, *pages.tensors())
-        self._call(self._L.lar_kv_attend, held, p, qa, t, cols,
-                   1.0 / math.sqrt(self.head_dim) if scale is None else float(scale),
-                   _dev(out, self.dtype, "out", n * self.head_dim), _dev(lse, torch.float32, "lse", n))
+        self._call(self._L.lar_kv_attend, pages, (q, out, lse, table), self._pages(pages), qa, t, cols,
+                   self._scale if scale is None else float(scale), to,
+                   None if lse is None else _dev(lse, self._torch.float32, "lse", n))
         return out
 
     def sync(self):
