@@ -24,8 +24,6 @@ using namespace lar;
 namespace {
 
 constexpr int kStages = 2;  // pinned copies of a plan: one may be on its way while the next is written
-// Least key tiles of a workgroup's stretch: fewer would cost more to join than they save.
-constexpr int kWideLeast = 4;
 
 size_t up(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -64,7 +62,7 @@ struct lar_kv {
   // the plan
   bool planned = false;
   int32_t n_seq = 0, n_tok = 0, max_pages = 0, window = 0, sinks = 0;
-  int32_t n_narrow = 0, n_wide = 0, n_join = 0, most_parts = 0;
+  int32_t n_narrow = 0, n_wide = 0, n_join = 0, join_rows = 0, most_parts = 0;
   lar_status sticky = LAR_OK;
   std::string msg;
 };
@@ -118,36 +116,55 @@ struct Tile {
   int tiles;
 };
 
-// The join list of a plan.
+// The split tiles of a plan, and the join list made of them: a workgroup for every `rows` rows.
+// Fewer rows leave more threads to share the slots out to, and more CUs to load them; too many
+// workgroups take longer to start than that saves.  8 instead of 32 where that makes at most
+// kJoins8 workgroups (40 tokens of 4 heads over 400 keys: 14 us, 19 with 32; a limit of 256 takes
+// 19), 2 where it makes at most kJoins2 and there are more than kManyParts slots (one token of 4
+// heads over 60k keys: 52 us, 55 with 8; over 1000 keys, 32 slots: 10.3 and 9.7).
+constexpr int kJoins8 = 512, kJoins2 = 64, kManyParts = 64;
 struct Joins {
-  KvJoin* list;
-  int32_t G, n = 0, most = 0;
+  int32_t G, most = 0;
+  std::vector<KvJoin> tiles;
   void add(const KvSeg& s, int32_t slot, int32_t parts, bool wide) {
-    for (int32_t row0 = 0; row0 < s.ntok * G; row0 += 32) {
-      KvJoin j{};
-      j.q0 = s.q0;
-      j.ntok = s.ntok;
-      j.p0 = s.p0;
-      j.head = s.head;
-      j.slot = slot;
-      j.n = parts;
-      j.row0 = row0;
-      j.wide = wide;
-      list[n++] = j;
-    }
+    KvJoin j{};
+    j.q0 = s.q0;
+    j.ntok = s.ntok;
+    j.p0 = s.p0;
+    j.head = s.head;
+    j.slot = slot;
+    j.n = parts;
+    j.wide = wide;
+    tiles.push_back(j);
     most = std::max(most, parts);
+  }
+  int64_t count(int rows) const {
+    int64_t n = 0;
+    for (const KvJoin& j : tiles) n += ceil_div((int64_t)j.ntok * G, rows);
+    return n;
+  }
+  int32_t write(KvJoin* list, int32_t* rows) const {
+    *rows = most > kManyParts && count(2) <= kJoins2 ? 2 : count(8) <= kJoins8 ? 8 : 32;
+    int32_t n = 0;
+    for (KvJoin j : tiles)
+      for (j.row0 = 0; j.row0 < j.ntok * G; j.row0 += *rows) list[n++] = j;
+    return n;
   }
 };
 
 // Least key tiles of a wave's run.  A wave takes about 1.1 us for one; joining n parts of r
-// rows takes 0.26 us * n * r * D / 4096, since 1024 threads share their quads out.  A tile of
-// T key tiles in stretches of L then ends soonest with L = sqrt(T r D * 5.8e-5); measured at
-// T = 1179, r = 4 and 8, D = 128: 32 and 52 us with L = 2, 24 and 28 with 8, 31 and 33 with
-// 16; at T = 114, r = 4: 11.9 with 2, 12.9 with 1, 14.2 with 4.
+// rows takes time in proportion to n * r * D, since a workgroup's threads share their quads
+// out.  A tile of T key tiles in stretches of L then ends soonest with L = sqrt(T r D * c), here
+// from measurements at T = 1179, r = 4 and 8, D = 128 (32 and 52 us with L = 2, 24 and 28 with 8,
+// 31 and 33 with 16) and T = 7 to 114, r = 4 (8.6 and 11 us with L = 1 and 2 at T = 7, 15.0 and 13.9
+// at T = 114).  From some hundred key tiles on their waves no longer have a SIMD for themselves,
+// and runs of one cost more than they save.
 int narrow_least(const std::vector<Tile>& tiles, const KvGeom& g) {
   double most = 0;
+  int64_t total = 0;
+  for (const Tile& t : tiles) total += t.tiles;
   for (const Tile& t : tiles) most = std::max(most, (double)t.tiles * (t.s.ntok * g.G));
-  return std::max(2, (int)std::lround(std::sqrt(most * g.D * 5.8e-5)));
+  return std::max(total > 512 ? 2 : 1, (int)std::lround(std::sqrt(most * g.D * 5.8e-5)));
 }
 
 // Narrow tiles: cuts their key tiles into stretches of equal number, one run of them for each
@@ -192,10 +209,13 @@ void cut(const std::vector<Tile>& tiles, int most, int least, KvSeg* segs, int32
 
 // Wide tiles.  Where they are short for the workgroups: whole tiles where that
 // balances, parts of at most `limit` key tiles where it does not, the longest first to the
-// workgroup with the least work.  Costs are in key tiles, of about 2.4 us each.
-constexpr int kStart = 2;     // a stretch's queries, first keys and result
-constexpr int kPart = 1;      // partial sums instead of the result
-constexpr int kJoining = 3;   // the join
+// workgroup with the least work.  Costs are in key tiles, of about 2 us each.
+constexpr int kStart = 2;  // a stretch's queries, first keys and result
+// The join: its launch, its slots' latency, and their rows' bytes, written and read at about
+// 3 TB/s (2.2 us, 0.07 a slot); a key tile of narrower heads takes less time than that counts for.
+double join_cost(int32_t most, int64_t rows, int D) {
+  return (1.25 + 0.04 * most + 1.6e-6 * (double)(rows * D)) * (D == 128 ? 1.0 : 1.5);
+}
 // From this many key tiles per workgroup on parts cost nothing against them, and workgroups
 // that read the same keys at the same time from one L2 are worth more.
 constexpr int kLong = 128;
@@ -280,7 +300,8 @@ void march(const std::vector<Tile>& tiles, int groups, KvSeg* segs, int32_t* at,
   *n_run = groups;
 }
 
-void deal(const std::vector<Tile>& tiles, int groups, KvSeg* segs, int32_t* at, int32_t* n_run, Joins* join) {
+void deal(const std::vector<Tile>& tiles, int groups, const KvGeom& g, KvSeg* segs, int32_t* at, int32_t* n_run,
+          Joins* join) {
   int64_t total = 0;
   for (const Tile& t : tiles) total += std::max(1, t.tiles);
   *n_run = 0;
@@ -293,9 +314,7 @@ void deal(const std::vector<Tile>& tiles, int groups, KvSeg* segs, int32_t* at, 
     int32_t tile, part, cost;
   };
   const auto parts_of = [](const Tile& t, int64_t limit) { return (int32_t)std::max<int64_t>(1, ceil_div(t.tiles, limit)); };
-  const auto cost_of = [](const Tile& t, int32_t parts) {
-    return (int32_t)ceil_div(t.tiles, parts) + kStart + (parts > 1 ? kPart : 0);
-  };
+  const auto cost_of = [](const Tile& t, int32_t parts) { return (int32_t)ceil_div(t.tiles, parts) + kStart; };
   std::vector<Piece> pieces, best;
   std::vector<std::pair<int32_t, int32_t>> load;  // (work, workgroup), the least first
   const auto more = std::greater<std::pair<int32_t, int32_t>>();
@@ -313,26 +332,33 @@ void deal(const std::vector<Tile>& tiles, int groups, KvSeg* segs, int32_t* at, 
     }
     return most;
   };
-  int64_t limit = INT32_MAX, chosen = limit;
-  int32_t least = INT32_MAX;
-  for (int k = 0; k < 4; ++k) {
-    if (k) limit = std::max<int64_t>(kWideLeast, (total * 2 / groups) >> (k - 1));
+  const int64_t even = std::max<int64_t>(1, total * 2 / groups);
+  int64_t chosen = INT32_MAX, before = 0;
+  double least = 1e300;
+  for (const int64_t limit : {(int64_t)INT32_MAX, even * 4, even * 2, even, even / 2, even / 4}) {
+    if (limit < 1) break;
     pieces.clear();
-    int64_t parts = 0;
+    int64_t parts = 0, rows = 0;
+    int32_t many = 0;
     for (size_t i = 0; i < tiles.size(); ++i) {
       const int32_t n = parts_of(tiles[i], limit);
-      if (n > 1) parts += n;
+      if (n > 1) {
+        parts += n;
+        rows += (int64_t)n * tiles[i].s.ntok * g.G;
+        many = std::max(many, n);
+      }
       for (int32_t j = 0; j < n; ++j) pieces.push_back(Piece{(int32_t)i, j, cost_of(tiles[i], n)});
     }
-    if (parts > 2 * groups) break;  // slots; and the smaller limits have more parts
+    if (parts > 2 * groups) break;             // slots; and the smaller limits have more parts
+    if (parts == before && !best.empty()) continue;  // nothing more was cut
+    before = parts;
     std::stable_sort(pieces.begin(), pieces.end(), [](const Piece& x, const Piece& y) { return x.cost > y.cost; });
-    const int32_t most = hand_out(pieces, nullptr) + (parts ? kJoining : 0);
+    const double most = hand_out(pieces, nullptr) + (parts ? join_cost(many, rows, g.D) : 0.0);
     if (most < least) {
       least = most;
       chosen = limit;
       best = pieces;
     }
-    if (!parts && k) break;  // nothing was cut: no more to be had
   }
   std::vector<int32_t> to(best.size()), slot(tiles.size(), -1);
   hand_out(best, to.data());
@@ -493,7 +519,7 @@ lar_status lar_kv_create(lar_kv** out, const lar_kv_config* cfg) {
   const int64_t narrow = std::min<int64_t>(cfg->max_seqs, cfg->max_tokens) * g.hkv;
   const int64_t wide = (std::min<int64_t>(cfg->max_seqs, cfg->max_tokens / (nt + 1)) + cfg->max_tokens / wt) * g.hkv;
   kv->cap = Layout(cfg->max_tokens, narrow + kv->waves, wide + narrow + 2 * kv->groups, kv->waves, kv->groups,
-                   std::min<int64_t>(narrow, kv->waves) + std::min<int64_t>(wide + narrow, kv->groups) * (kWideRows / 32)).end;
+                   std::min<int64_t>(narrow, kv->waves) + std::min<int64_t>(wide + narrow, kv->groups) * (kWideRows / 32) + kJoins8).end;
   // every wave or workgroup has two stretches at most that are parts of a tile
   bool ok = hipMalloc((void**)&kv->dev, kv->cap) == hipSuccess &&
             hipMalloc((void**)&kv->narrow_o, sizeof(float) * 2 * kv->waves * kNarrowRows * g.D) == hipSuccess &&
@@ -554,7 +580,7 @@ lar_status lar_kv_plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const i
   char* p = kv->pinned[b];
   const KvGeom& g = kv->g;
   KvTok* tok = (KvTok*)p;
-  int32_t n_narrow = 0, n_wide = 0, n_join = 0, most_parts = 0;
+  int32_t n_narrow = 0, n_wide = 0, n_join = 0, join_rows = 0, most_parts = 0;
   kv->planned = false;
   try {
     std::vector<Tile> narrow, wide, none;
@@ -584,15 +610,15 @@ lar_status lar_kv_plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const i
     for (const Tile& t : none) (t.s.ntok <= nt && wide.empty() ? narrow : wide).push_back(t);
     const int64_t nn = (int64_t)narrow.size(), nw = (int64_t)wide.size();
     const Layout L(T, nn ? nn + kv->waves : 0, nw ? nw + 2 * kv->groups : 0, kv->waves, kv->groups,
-                   std::min<int64_t>(nn, kv->waves) + std::min<int64_t>(nw, kv->groups) * (kWideRows / 32));
+                   std::min<int64_t>(nn, kv->waves) + std::min<int64_t>(nw, kv->groups) * (kWideRows / 32) + kJoins8);
     if (L.end > kv->cap) return fail(kv, LAR_E_CAPACITY, "plan of %zu bytes, room for %zu", L.end, kv->cap);
     kv->lay = L;
-    Joins join{(KvJoin*)(p + L.join), g.G};
+    Joins join{g.G};
     const int groups = nn ? split(narrow, wide, kv->groups, g) : kv->groups;
     cut(narrow, nw ? (kv->groups - groups) * kWideWaves : kv->waves, narrow_least(narrow, g), (KvSeg*)(p + L.narrow),
         (int32_t*)(p + L.narrow_at), &n_narrow, &join);
-    deal(wide, groups, (KvSeg*)(p + L.wide), (int32_t*)(p + L.wide_at), &n_wide, &join);
-    n_join = join.n;
+    deal(wide, groups, g, (KvSeg*)(p + L.wide), (int32_t*)(p + L.wide_at), &n_wide, &join);
+    n_join = join.write((KvJoin*)(p + L.join), &join_rows);
     most_parts = join.most;
   } catch (const std::bad_alloc&) {
     return fail(kv, LAR_E_CAPACITY, "out of host memory");
@@ -615,6 +641,7 @@ lar_status lar_kv_plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const i
   kv->n_narrow = n_narrow;
   kv->n_wide = n_wide;
   kv->n_join = n_join;
+  kv->join_rows = join_rows;
   kv->most_parts = most_parts;
   kv->planned = true;
   return LAR_OK;
@@ -679,6 +706,7 @@ lar_status lar_kv_attend(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_row
   a.n_wide = kv->n_wide;
   a.join = (const KvJoin*)(kv->dev + kv->lay.join);
   a.n_join = kv->n_join;
+  a.join_rows = kv->join_rows;
   a.most_parts = kv->most_parts;
   a.narrow_o = kv->narrow_o;
   a.wide_o = kv->wide_o;

@@ -457,10 +457,13 @@ __device__ __forceinline__ Row load_q(const KvAttendArgs& A, const Lane& x, int 
   return x.row;
 }
 
-// Where a split tile's partial sums are: 4 values of 32 rows side by side, by quads of values.
+// Where a split tile's partial sums are: by blocks of 32 rows, in each 4 values of its rows side
+// by side, by quads of values.  `rows`: what a slot has room for; a narrow tile's `real` rows
+// have no gaps between them (one token of one head over 60k keys: 24 -> 14 us).
 template <int D>
-__device__ __forceinline__ int64_t part_at(int slot, int rows, int row, int quad) {
-  return ((((int64_t)slot * rows + row) / 32 * (D / 4) + quad) * 32 + row % 32) * 4;
+__device__ __forceinline__ int64_t part_at(int slot, int rows, int real, int row, int quad) {
+  const int first = row & ~31, n = rows == kNarrowRows ? real : 32;
+  return ((int64_t)slot * rows + first) * D + (quad * n + row - first) * 4;
 }
 
 // The result of a wave's 32 rows, through LDS (32 rows of `tmp`) so that whole rows are
@@ -479,7 +482,7 @@ __device__ __forceinline__ void finish(const KvAttendArgs& A, const KvSeg& s, co
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
         f32x4 y = {a.o[b][i], a.o[b][i + 1], a.o[b][i + 2], a.o[b][i + 3]};
-        *(f32x4*)(po + part_at<D>(slot, rows, row0 + n, 8 * b + key_of(i, h) / 4)) = y;
+        *(f32x4*)(po + part_at<D>(slot, rows, s.ntok * A.g.G, row0 + n, 8 * b + key_of(i, h) / 4)) = y;
       }
     if (h == 0) pml[(int64_t)slot * rows + row0 + n] = make_float4(a.m, l, lr, 0.0f);
     return;
@@ -628,7 +631,7 @@ __device__ __forceinline__ void spread(const KvAttendArgs& A, const KvSeg& s, in
           const Row r{pos, A.window ? pos - A.window : -1, A.sinks};
           if (!r.sees(j)) continue;
           if (s.slot >= 0) {
-            po[part_at<D>(s.slot, rows, n, d / 4) + d % 4] += v;
+            po[part_at<D>(s.slot, rows, s.ntok * G, n, d / 4) + d % 4] += v;
           } else {
             uint16_t* o = (uint16_t*)A.out + ((int64_t)(s.q0 + u) * A.g.hq + s.head * G + n - u * G) * D + d;
             *o = Elem<BF>::one(Elem<BF>::value(*o) + v);
@@ -935,8 +938,8 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
 }
 
 // ------------------------------------------------------------------ joining split tiles
-// One workgroup per 32 rows of a split tile.  A thread has 4 values of a row; where the rows
-// leave threads over, these share out the slots and are joined through LDS, in their order.
+// One workgroup per join_rows rows of a split tile.  A thread has 4 values of a row; where the
+// rows leave threads over, these share out the slots and are joined through LDS, in a fixed order.
 // Bound by the latency of the slots' loads, of which each thread has four on their way.
 struct Part {
   float m, l, lr;
@@ -959,7 +962,7 @@ __global__ __launch_bounds__(THREADS) void k_kv_join(KvAttendArgs A) {
   __shared__ Part parts[THREADS];
   const KvJoin j = plan_at(A.join, blockIdx.x);
   const int rows = j.wide ? kWideRows : kNarrowRows, row0 = j.row0;
-  const int have = j.ntok * A.g.G - row0 < 32 ? j.ntok * A.g.G - row0 : 32;
+  const int have = j.ntok * A.g.G - row0 < A.join_rows ? j.ntok * A.g.G - row0 : A.join_rows;
   const float* po = j.wide ? A.wide_o : A.narrow_o;
   const float4* pml = j.wide ? A.wide_ml : A.narrow_ml;
   const int n = have * kQuads;  // quads of values
@@ -979,18 +982,22 @@ __global__ __launch_bounds__(THREADS) void k_kv_join(KvAttendArgs A) {
           p[k].m = ml.x;
           p[k].l = ml.y;
           p[k].lr = ml.z;
-          p[k].o = *(const f32x4*)(po + part_at<D>(j.slot + x, rows, row0 + r, d / 4));
+          p[k].o = *(const f32x4*)(po + part_at<D>(j.slot + x, rows, j.ntok * A.g.G, row0 + r, d / 4));
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k)
           if (s + k * share < j.n) a.join(p[k]);
       }
     }
-    if (share > 1) {  // then one round: every thread is here
-      parts[threadIdx.x] = a;
+    // Shares are joined by fours, then what they made (then one round: every thread is here).
+    if (share > 1) parts[threadIdx.x] = a;
+    for (int k = 1; k < share; k *= 4) {
       __syncthreads();
-      if (mine == 0)
-        for (int k = 1; k < share; ++k) a.join(parts[k * n + u]);
+      if (mine % (4 * k) == 0) {
+        const int end = mine + 4 * k < share ? mine + 4 * k : share;
+        for (int i = mine + k; i < end; i += k) a.join(parts[i * n + u]);
+        parts[threadIdx.x] = a;
+      }
     }
     if (mine != 0) continue;
     const int t = (row0 + r) / A.g.G, g = row0 + r - t * A.g.G;
@@ -1021,9 +1028,9 @@ hipError_t run(const KvAttendArgs& a, hipStream_t stream) {
   } else if (a.n_narrow) {
     k_kv_narrow<BF, F8, D><<<a.n_narrow, 64, 0, stream>>>(a);
   }
-  // Many parts of few rows: more threads to share them out to (one token over 3.6k and over
-  // 37.7k keys: 12.2 and 43 us with 1024 threads, 13.5 and 57 with 256); few parts of many
-  // tiles: smaller workgroups (255 decode tokens: 263 us with 256, 267 with 1024).
+  // Many parts: more threads to share them out to (40 tokens of 8 heads over 4000 keys, 16
+  // parts of each tile: 15.4 us with 1024 threads, 19.3 with 256); few parts of many tiles:
+  // smaller workgroups (255 decode tokens take 1.5 % more with 1024).
   if (a.n_join && a.most_parts > 8)
     k_kv_join<BF, D, 1024><<<a.n_join, 1024, 0, stream>>>(a);
   else if (a.n_join)

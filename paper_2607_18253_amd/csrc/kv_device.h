@@ -43,8 +43,8 @@ struct KvSeg {
   int32_t slot;
 };
 
-// 32 rows, from row0 on, of a query tile whose key tiles were split: its partial sums are in
-// slots [slot, slot + n).
+// join_rows rows, from row0 on, of a query tile whose key tiles were split: its partial sums
+// are in slots [slot, slot + n).
 struct KvJoin {
   int32_t q0, ntok, p0, head;
   int32_t slot, n;
@@ -81,7 +81,7 @@ struct KvAttendArgs {
   const int32_t *narrow_at, *wide_at;  // [n + 1] stretches of each wave / workgroup
   int32_t n_narrow, n_wide;            // waves, workgroups
   const KvJoin* join;
-  int32_t n_join, most_parts;  // most_parts: the most slots of one
+  int32_t n_join, join_rows, most_parts;  // most_parts: the most slots of one
   float *narrow_o, *wide_o;            // partial sums of a slot's rows
   float4 *narrow_ml, *wide_ml;         // [slot][rows]: maximum (log2 units) and sums
   int32_t* err;
