@@ -2,7 +2,8 @@
 
 Every floating-point operation in the simulation's kernels is a separate binary64
 round-to-nearest-even operation: -ffp-contract=off (no fused multiply-add; the
-attention kernels write theirs out), no fast-math.  Packed FP32 instructions are disabled for all device code.
+attention kernels write theirs out), no fast-math.  Packed FP32 instructions are disabled
+for all device code.
 """
 
 from __future__ import annotations
