@@ -272,6 +272,35 @@ def test_attend_masked_values_have_no_part(q_len, G, dtype, bad):
         at += n
 
 
+@pytest.mark.parametrize("n,G", [(3, 4), (2, 16), (40, 4), (9, 5)])
+@pytest.mark.parametrize("cache", [BF, E4])
+def test_attend_masked_values_of_split_contexts(n, G, cache):
+    """NaN in V and K of the last tokens, over contexts whose keys are split: the rows before
+    them stay clean through the joins, for few rows (narrow tiles) and many (wide)."""
+    first = n // 2
+
+    def edit(b, rows):
+        k, v = rows[0]
+        v[len(v) - n + first, 0, 5] = math.nan
+        v[-1, 1, 40] = math.nan
+        k[-1, 0, 3] = math.nan
+    b = Batch([n], [4001], hq=2 * G, hkv=2, d=64, S=16, dtype=BF, cache=cache, edit=edit)
+    out, lse = b.attend()
+    k, v = (x.clone() for x in b.held[0])
+    mask = R.sees(n, 4001)
+    k[-1, 0], v[~torch.isfinite(v)] = 0, 0                   # for rows that do not see them
+    want, wz, mag, big = R.attend_fast(b.q.double(), k, v, mask, 0.125)
+    bo, bz = R.bounds(BF, mag, big, wz, 64, 4001, float(v.abs().max()))
+    Batch.near(out[:first].double(), want[:first], bo[:first], "rows before the first NaN")
+    Batch.near(lse[:n - 1].double(), wz[:n - 1], bz[:n - 1], "lse")
+    if cache is not E4:                                      # an e4m3 row with a NaN keeps its other values
+        got = out[first:n - 1, :G].double()
+        assert torch.isnan(got[..., 5]).all()
+        keep = [i for i in range(64) if i != 5]
+        Batch.near(got[..., keep], want[first:n - 1, :G][..., keep], bo[first:n - 1, :G][..., keep], "other values")
+        assert torch.isnan(out[n - 1, :G]).all() and torch.isnan(out[n - 1, G:, 40]).all()
+
+
 def test_attend_repeats_bit_for_bit():
     b = Batch([1, 1, 90, 1], [3000, 20000, 5000, 4], hq=8, hkv=2, d=128, S=16, dtype=BF, cache=BF)
     x, z = b.attend()
