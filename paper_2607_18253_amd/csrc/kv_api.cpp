@@ -389,15 +389,17 @@ void deal(const std::vector<Tile>& tiles, int groups, const KvGeom& g, KvSeg* se
 }
 
 // How many of a device's workgroups the wide tiles of a batch get that has narrow ones too.
-// Wide tiles need time in proportion to their workgroups; narrow ones are bound by memory
-// from about 100 CUs on with 16-bit rows of 128 (255 decode tokens: 264 us with 768 waves,
-// 258 with 2048), later with shorter rows, so that most batches end sooner with both at work
-// (mixed batch of 3839 tokens: 387 us one after the other).
+// Both need time in proportion to their workgroups until the narrow ones, which are bound by
+// memory, reach its rate (with 16-bit rows of 128 from about 150 CUs on), so that most
+// batches end sooner with both at work (mixed batch of 3839 tokens: 387 us one after the other,
+// 293 together).  Where the two bounds of the narrow ones meet they take more than either: a sum
+// of sixth powers (mixed batch: 298 us with the larger of the two).
 int split(const std::vector<Tile>& narrow, const std::vector<Tile>& wide, int groups, const KvGeom& g) {
   if (wide.empty()) return 0;
-  // microseconds: of a wide key tile and a stretch's start and end, of a narrow one in a wave
-  // alone; bytes of a narrow one
-  const double wt = g.D == 128 ? 2.1 : 1.35, ws = 8.0, nt = g.D == 128 ? 2.1 : 1.7;
+  // microseconds: of a wide key tile and a stretch's start and end, of a narrow one among a
+  // CU's eight waves (255 tokens beside 7 chunks of 512 with heads of 64: 161 us, 182 with a time
+  // 1.6 times less; 40 tokens beside them: 92 and 103); bytes of a narrow one
+  const double wt = g.D == 128 ? 2.1 : 1.35, ws = 8.0, nt = g.D == 128 ? 3.4 : 2.7;
   const double nb = 2.0 * kNarrowKeys * g.D * (g.cache == kKvE4m3 ? 1 : 2), rate = 5.2e6;
   int64_t w = 0, n = 0;
   for (const Tile& t : wide) w += t.tiles;
@@ -406,7 +408,7 @@ int split(const std::vector<Tile>& narrow, const std::vector<Tile>& wide, int gr
   double least = 1e300;
   for (int k = kXcds; k <= groups - kXcds; k += kXcds) {
     const double tw = w * wt / k + std::ceil((double)wide.size() / k) * ws;
-    const double tn = std::max(n * nt / ((groups - k) * kWideWaves), n * nb / rate);
+    const double tn = std::pow(std::pow(n * nt / ((groups - k) * kWideWaves), 6) + std::pow(n * nb / rate, 6), 1.0 / 6);
     if (std::max(tw, tn) < least) {
       least = std::max(tw, tn);
       best = k;
