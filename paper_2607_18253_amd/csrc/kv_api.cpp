@@ -335,7 +335,7 @@ void deal(const std::vector<Tile>& tiles, int groups, const KvGeom& g, KvSeg* se
   const int64_t even = std::max<int64_t>(1, total * 2 / groups);
   int64_t chosen = INT32_MAX, before = 0;
   double least = 1e300;
-  for (const int64_t limit : {(int64_t)INT32_MAX, even * 4, even * 2, even, even / 2, even / 4}) {
+  for (const int64_t limit : {(int64_t)INT32_MAX, even * 4, even * 2, even * 3 / 2, even, even * 3 / 4, even / 2, even / 4}) {
     if (limit < 1) break;
     pieces.clear();
     int64_t parts = 0, rows = 0;
