@@ -727,7 +727,7 @@ __global__ __launch_bounds__(64, 2) void k_kv_narrow(KvAttendArgs A) {
 // device, one bound by matrix instructions and the other by memory.
 //
 // LSE: the log of the sums is asked for, which takes the sum of the unrounded weights too
-// (7681 tokens at 131072: 16.3 ms with it, 15.9 without; heads of 64: 10.0 and 9.5).
+// (7681 tokens at 131072: 16.1 ms with it, 15.0 without; heads of 64: 9.6 and 8.8).
 template <bool BF, bool F8, int D, bool LSE>
 __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) {
   constexpr int kTileK = kWideKeys * kRowK<D>, kTileV = kWideKeys * kRowV<D>, kThreads = 64 * kWideWaves;
