@@ -25,6 +25,14 @@ def _raw_stream(index):
     return _raw_stream(index)
 
 
+def _int32s(x, name):
+    """One-dimensional int32 array of integers, none of which is cut."""
+    a = np.asarray(x)
+    if a.ndim != 1 or (a.size and (a.dtype.kind not in "iu" or a.max() > 2 ** 31 - 1 or a.min() < -2 ** 31)):
+        raise ValueError(f"{name} must be one-dimensional 32-bit integers")
+    return np.ascontiguousarray(a, np.int32)
+
+
 class KvConfig(C.Structure):
     _fields_ = [("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
                 ("dtype", C.c_int32), ("cache_dtype", C.c_int32), ("block_size", C.c_int32),
@@ -192,10 +200,10 @@ class PagedKV:
     def plan(self, q_len, ctx_len, window: int = 0, sinks: int = 0):
         """The token batch of the calls that follow: new tokens per sequence and context
         with them (host integers)."""
-        q = np.ascontiguousarray(q_len, np.int32)
-        c = np.ascontiguousarray(ctx_len, np.int32)
-        if q.ndim != 1 or q.shape != c.shape:
-            raise ValueError("q_len and ctx_len must be one-dimensional and of one length")
+        q, c = _int32s(q_len, "q_len"), _int32s(ctx_len, "ctx_len")
+        if q.shape != c.shape:
+            raise ValueError("q_len and ctx_len must be of one length")
+        _int32s([window, sinks], "window and sinks")
         self._check(self._L.lar_kv_plan(self._h, len(q), q.ctypes.data, c.ctypes.data, int(window), int(sinks)))
         self._batch(len(q), int(q.sum()))
 

@@ -90,3 +90,13 @@ def test_fit_recovers_the_coefficients():
     assert (c >= 0).all() and abs(c[3] / 1e-6 - 1) < 0.02
     X[:, 4] = 0
     assert K.fit(X, X @ want)[4] == 0
+
+
+def test_lengths_are_not_cut():
+    """Lengths that 32 bits cannot hold, fractions and tables are refused, not rounded."""
+    from paper_2607_18253_amd.kv import _int32s
+    for ok in ([], [1, 2], np.array([3], np.int64), np.array([7, 2 ** 31 - 1], np.uint32), (4,)):
+        assert _int32s(ok, "x").dtype == np.int32 and _int32s(ok, "x").tolist() == [int(v) for v in ok]
+    for bad in ([2 ** 31], [2 ** 32 + 5], [-2 ** 31 - 1], [1.5], [2.0], [[1, 2]], 3, np.array([2 ** 40]), [2 ** 70]):
+        with pytest.raises(ValueError):
+            _int32s(bad, "x")
