@@ -548,7 +548,9 @@ lar_status lar_estimate_lps(lar_ctx *ctx, const lar_lps_params *params, int32_t 
  * over the keys j <= p, under a window W also j > p - W or j < sinks (the first tokens,
  * which stay visible); query head h reads kv head h / (n_q_heads / n_kv_heads).  Scores,
  * maxima and sums are held in 32 bits; the exponentials are rounded to dtype for the
- * product with v.  Keys that a row does not see have no part in it, whatever they hold.
+ * product with v (LAR_KV_F16: by 2^-36 of the row's largest at most where they are too
+ * small for all its bits).  Keys that a row does not see have no part in it, whatever they
+ * hold.
  * lse = m + ln(sum_j exp(s_j - m)) joins parts of a context.
  */
 typedef struct lar_kv lar_kv;

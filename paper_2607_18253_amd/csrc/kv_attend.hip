@@ -26,7 +26,9 @@
 // Else it is rounded once (nearest even), an error of the size of the output's own rounding,
 // and the result is divided by the sum of the rounded weights, so that nothing is lost of a
 // weight that outweighs the others; the log of the sum, where it is asked for, is that of the
-// unrounded ones.
+// unrounded ones.  f16 has no values below 2^-24, and from 2^-14 down fewer bits: a row's weights
+// are scaled so that its largest is 2^11 to 2^15, and what a weight loses at that end is 2^-36
+// of the largest at most, 2^-17 of the result for 2^19 keys.
 #include "../../include/lar.h"
 #include "kv_device.h"
 
@@ -43,10 +45,9 @@ typedef __attribute__((ext_vector_type(8))) float f32x8;
 typedef __attribute__((address_space(3))) char lds_char;
 
 constexpr float kLn2 = 0.693147180559945309f;
-// A row's maximum may fall behind by this much (log2 units) before its sums are rescaled:
-// exponentials up to 2^8 lose nothing in 32 bits, and stay in the range of 16-bit P.
-constexpr float kLag = 8.0f;
 
+// Per 16-bit type, in log2 units: a row's largest weight is 2^kTop when its sums are scaled, and
+// may grow by 2^kLag before they are rescaled.
 template <bool BF> struct Elem;
 template <> struct Elem<true> {
   using x8 = bf16x8;
@@ -76,6 +77,7 @@ template <> struct Elem<true> {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(x2, x), x2{(__bf16)1.0f, (__bf16)1.0f}, c, false);
   }
   static constexpr uint32_t kExp = 0x7f80u;  // exponent bits: all ones where not finite
+  static constexpr float kTop = 0.0f, kLag = 8.0f;
 };
 template <> struct Elem<false> {
   using x8 = f16x8;
@@ -104,6 +106,7 @@ template <> struct Elem<false> {
     return __builtin_amdgcn_fdot2(__builtin_bit_cast(x2, x), x2{(_Float16)1.0f, (_Float16)1.0f}, c, false);
   }
   static constexpr uint32_t kExp = 0x7c00u;
+  static constexpr float kTop = 11.0f, kLag = 4.0f;  // 2^15 at most: f16 ends at 2^16
 };
 
 // Sets infinities and NaN among the 8 16-bit values to 0; whether there were any.
@@ -221,7 +224,7 @@ __device__ __forceinline__ void hide(f32x16 (&s)[NB], const Row& r, int kb, int 
 template <int D>
 struct Sums {
   f32x16 o[D / 32];  // O^T: row n, value 32 b + key_of(i, h)
-  float m, l, lr;    // maximum (log2 units); this half's part of the sum, and of what o has
+  float m, l, lr;    // weights are 2^(score - m); this half's part of their sum, and of what o has
   __device__ __forceinline__ void clear() {
     const float z = here(0.0f);
 #pragma unroll
@@ -258,12 +261,12 @@ __device__ __forceinline__ float peak(const f32x16 (&s)[NB]) {
   return max_halves(mx);
 }
 
-// Takes a tile's largest scores (times the scale: log2 units) into the running maximum,
-// rescaling the rows' sums where it grew.
-template <int D>
+// Takes a tile's largest scores (times the scale: log2 units) into the running maximum less
+// kTop, rescaling the rows' sums where it grew.
+template <bool BF, int D>
 __device__ __forceinline__ void raise(Sums<D>& a, float mx) {
-  if (__any(mx > a.m + kLag)) {
-    const float m = fmaxf(mx, a.m);
+  if (__any(mx > a.m + (Elem<BF>::kTop + Elem<BF>::kLag))) {
+    const float m = fmaxf(mx - Elem<BF>::kTop, a.m);
     const float f = m > a.m ? __builtin_amdgcn_exp2f(a.m - m) : 1.0f;  // 0 from a.m = -inf
     a.m = m;
     a.l *= f;
@@ -704,7 +707,7 @@ __device__ __forceinline__ void narrow(const KvAttendArgs& A, char* lds, int run
       wave_order();
       f32x16 sc[1] = {scores<BF, D>(kt, q, n, h)};
       if (masked) hide<1>(sc, row, kb, h, A.window);
-      raise<D>(a, peak<1>(sc) * A.scale);
+      raise<BF, D>(a, peak<1>(sc) * A.scale);
       soften<D, 1>(sc, a, A.scale);
       weigh<BF, D, !F8>(vt, sc[0], a, lane);
       wave_order();
@@ -831,7 +834,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
       hide<1>(next, rw, nb, h, A.window);
       mx = peak<1>(next);
     }
-    raise<D>(a, mx * A.scale);
+    raise<BF, D>(a, mx * A.scale);
   };
   f32x16 sa[1], sb[1];
   int kc = 0, kn = kTileK, kx = 2 * kTileK;  // K of this tile, the next and the one after
@@ -886,7 +889,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
       sa[0] = scores<BF, D>(ldk, q, n, h);
       const int kb = tile_key<kWideKeys>(s, s.t0);
       if (is_masked(A, wfirst, wlast, kb, 32)) hide<1>(sa, rw, kb, h, A.window);
-      raise<D>(a, peak<1>(sa) * A.scale);
+      raise<BF, D>(a, peak<1>(sa) * A.scale);
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) kf[i] = k_part<D>(ldk + 32 * kRowK<D>, i, lane);
     }

@@ -83,7 +83,7 @@ struct KvAttendArgs {
   const KvJoin* join;
   int32_t n_join, join_rows, most_parts;  // most_parts: the most slots of one
   float *narrow_o, *wide_o;            // partial sums of a slot's rows
-  float4 *narrow_ml, *wide_ml;         // [slot][rows]: maximum (log2 units) and sums
+  float4 *narrow_ml, *wide_ml;         // [slot][rows]: scale of the weights (log2 units) and sums
   int32_t* err;
 };
 
