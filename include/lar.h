@@ -550,7 +550,8 @@ lar_status lar_estimate_lps(lar_ctx *ctx, const lar_lps_params *params, int32_t 
  * maxima and sums are held in 32 bits; the exponentials are rounded to dtype for the
  * product with v (LAR_KV_F16: by 2^-36 of the row's largest at most where they are too
  * small for all its bits).  Keys that a row does not see have no part in it, whatever they
- * hold.
+ * hold; an infinity in v makes the rows that see it infinite, or NaN where both signs meet
+ * and where, for a chunk, its weight is too small for dtype.
  * lse = m + ln(sum_j exp(s_j - m)) joins parts of a context.
  */
 typedef struct lar_kv lar_kv;

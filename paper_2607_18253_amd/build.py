@@ -23,7 +23,7 @@ SOURCES = [os.path.join(CSRC, "sfs_kernels.hip"), os.path.join(CSRC, "sfs_limits
            os.path.join(CSRC, "kv_attend.hip"), os.path.join(CSRC, "kv_api.cpp")]
 HEADERS = [os.path.join(CSRC, "sfs_device.h"), os.path.join(CSRC, "sfs_launch.h"),
            os.path.join(CSRC, "sfs_limits.h"), os.path.join(CSRC, "sfs_route.h"), os.path.join(CSRC, "sfs_walk.h"),
-           os.path.join(CSRC, "kv_device.h"),
+           os.path.join(CSRC, "kv_device.h"), os.path.join(CSRC, "kv_words.h"),
            os.path.join(ROOT, "include", "lar.h")]
 ARCH = "gfx950"
 

@@ -31,6 +31,7 @@
 // of the largest at most, 2^-17 of the result for 2^19 keys.
 #include "../../include/lar.h"
 #include "kv_device.h"
+#include "kv_words.h"
 
 namespace lar {
 namespace {
@@ -564,8 +565,8 @@ struct Stage {
     for (int j = 0; j < (F8 ? 2 : 1); ++j)
       *(uint4*)(kt + r * kRowK<D> + (F8 ? 2 * c + j : c) * 16) = widen(k[i], scale, j);
   }
-  // The same.  Where rows of the query tile see different keys a V row from `end` on, which
-  // none sees, is cleared, and so are infinities and NaN of the others: in the product they
+  // The same.  MASKED, where rows of the query tile see different keys: a V row from `end` on,
+  // which none sees, is cleared, and so are infinities and NaN of the others: in the product they
   // would reach rows that do not see them, as 0 * inf.  Returns whether there were any
   // (spread() adds them).
   template <bool MASKED>
@@ -605,10 +606,23 @@ __device__ __forceinline__ bool is_masked(const KvAttendArgs& A, int p0, int las
   return kb + K - 1 > p0 || (A.window && kb <= last - A.window && kb + K > A.sinks);
 }
 
-// Adds what clean() took out of V in the stretch's masked tiles to the rows that see it, in
-// the result or the partial sums that the wave has just written: w * inf is inf whatever the
-// weight w.  `row0`: the wave's first row in the query tile.
-template <bool BF, bool F8, int D, int K>
+// Whether V has infinities or NaN in the K keys from kb on, up to key `last` (16-bit rows).
+template <bool BF, int D, int K>
+__device__ __forceinline__ bool odd_tile(const KvAttendArgs& A, const KvSeg& s, int lane, int kb, int last) {
+  constexpr int kChunks = D / 8;  // 16-byte chunks of a row
+  uint32_t m = 0;
+  bool lost = false;  // reported before
+  for (int j = kb + lane / kChunks; j < kb + K && j <= last; j += 64 / kChunks) {
+    const uint32_t row = page_at(A, A.table[(int64_t)s.seq * A.cols + (j >> A.g.sh)], lost) + in_page(A, s.head, j);
+    m = max16(m, top_pair(*(const uint4*)((const char*)A.pool.v + (uint64_t)row * (D * 2) + lane % kChunks * 16)));
+  }
+  return __any(top_half(m) >= kInf<BF>);
+}
+
+// Adds what clean() took out of V to the rows that see it, in the result or the partial sums that
+// the wave has just written: w * inf is inf whatever the weight w.  That was in the stretch's
+// masked tiles, or in ANY.  `row0`: the wave's first row in the query tile.
+template <bool BF, bool F8, int D, int K, bool ANY>
 __device__ __forceinline__ void spread(const KvAttendArgs& A, const KvSeg& s, int lane, int row0, int rows,
                                        float* po) {
   lane = here(lane);
@@ -616,7 +630,7 @@ __device__ __forceinline__ void spread(const KvAttendArgs& A, const KvSeg& s, in
   const int last = s.p0 + s.ntok - 1, G = A.g.G;
   for (int t = s.t0; t < s.t1; ++t) {
     const int kb = tile_key<K>(s, t);
-    if (!is_masked(A, s.p0, last, kb, K)) continue;
+    if (ANY ? !odd_tile<BF, D, K>(A, s, lane, kb, last) : !is_masked(A, s.p0, last, kb, K)) continue;
     for (int j = kb; j < kb + K && j <= last; ++j) {
       bool lost = false;  // reported before
       const uint32_t row = page_at(A, A.table[(int64_t)s.seq * A.cols + (j >> A.g.sh)], lost) + in_page(A, s.head, j);
@@ -690,15 +704,24 @@ __device__ __forceinline__ void narrow(const KvAttendArgs& A, char* lds, int run
     for (int t = s.t0; t < s.t1; ++t) {
       const int kb = tile_key<kNarrowKeys>(s, t);
       const bool masked = is_masked(A, s.p0, last, kb, kNarrowKeys);
+      uint32_t e[I], m = 0;
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+        e[i] = F8 ? (uint32_t)__shfl((int)ex, i * St::kStep + r0) : 0;
+        st.put_k(kt, i, i * St::kStep + r0, c, scale_of(e[i]));
+        if (!F8) m = max16(m, top_pair(st.v[i]));
+      }
+      // With weights in two parts infinities and NaN are taken out of any tile: the second part may
+      // be 0 or have the other sign, and 0 * inf and inf - inf are NaN.  (Finding them takes 9
+      // instructions for 16 bytes, which wait for memory anyway.)
+      const bool odd = !F8 && __any(top_half(m) >= kInf<BF>);
 #pragma unroll
       for (int i = 0; i < I; ++i) {
         const int r = i * St::kStep + r0;
-        const uint32_t e = F8 ? (uint32_t)__shfl((int)ex, r) : 0;
-        st.put_k(kt, i, r, c, scale_of(e));
-        if (masked)
-          bad |= st.template put_v<true>(vt, i, r, c, last + 1 - kb, scale_of(e >> 8));
+        if (masked || odd)
+          bad |= st.template put_v<true>(vt, i, r, c, last + 1 - kb, scale_of(e[i] >> 8));
         else
-          st.template put_v<false>(vt, i, r, c, 0, scale_of(e >> 8));
+          st.template put_v<false>(vt, i, r, c, 0, scale_of(e[i] >> 8));
       }
       if (t + 1 < s.t1) {
         fetch(page, t + 1);
@@ -714,7 +737,7 @@ __device__ __forceinline__ void narrow(const KvAttendArgs& A, char* lds, int run
     }
     finish<BF, D>(A, s, a, lane, 0, kNarrowRows, A.narrow_o, A.narrow_ml, lds);
     wave_order();
-    if (__any(bad)) spread<BF, F8, D, kNarrowKeys>(A, s, lane, 0, kNarrowRows, A.narrow_o);
+    if (__any(bad)) spread<BF, F8, D, kNarrowKeys, !F8>(A, s, lane, 0, kNarrowRows, A.narrow_o);
   }
   if (lost) *A.err = LAR_E_STATE;
 }
@@ -935,7 +958,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
     const KvSeg done = s;
     more = next();
     finish<BF, D>(A, done, a, lane, wave * 32, kWideRows, A.wide_o, A.wide_ml, lds + wave * 32 * kRowK<D>);
-    if (flag) spread<BF, F8, D, kWideKeys>(A, done, lane, wave * 32, kWideRows, A.wide_o);
+    if (flag) spread<BF, F8, D, kWideKeys, false>(A, done, lane, wave * 32, kWideRows, A.wide_o);
   }
   if (lost) *A.err = LAR_E_STATE;
 }

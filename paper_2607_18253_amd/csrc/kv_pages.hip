@@ -12,6 +12,7 @@
 // lane permutations, and the codes come from the conversion that takes a power of two along.
 #include "../../include/lar.h"
 #include "kv_device.h"
+#include "kv_words.h"
 
 namespace lar {
 namespace {
@@ -19,11 +20,9 @@ namespace {
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 typedef __attribute__((ext_vector_type(2))) short s16x2;
-typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 
-// Patterns of infinity and of the largest magnitude that is held: its code times its scale
-// is the largest such value that the 16-bit type has.
-template <bool BF> constexpr uint32_t kInf = BF ? 0x7f80u : 0x7c00u;
+// Pattern of the largest magnitude that is held: its code times its scale is the largest such
+// value that the 16-bit type has.
 template <bool BF> constexpr uint32_t kHeld = BF ? 0x7f70u : 0x7b80u;  // 1.875 * 2^127, 61440
 
 // Row of (page, head, position) in the pool, or -1 with the sticky error for a page outside.
@@ -36,16 +35,8 @@ __device__ __forceinline__ int64_t page_row(const KvGeom& g, const KvPool& pool,
   return (((int64_t)page * g.hkv + head) << g.sh) + (pos & ((1 << g.sh) - 1));
 }
 
-__device__ __forceinline__ uint32_t max16(uint32_t a, uint32_t b) {
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a),
-                                                                __builtin_bit_cast(u16x2, b)));
-}
-
 // The largest pattern of 8 magnitudes.
-__device__ __forceinline__ uint32_t top(const uint4& x) {
-  const uint32_t m = max16(max16(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), max16(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
-  return max16(m, m >> 16) & 0xffffu;
-}
+__device__ __forceinline__ uint32_t top(const uint4& x) { return top_half(top_pair(x)); }
 
 // The larger of both halves of a word over the 8 or 16 lanes of a row.
 template <int LANES>
