@@ -7,6 +7,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -695,7 +696,8 @@ lar_status lar_kv_attend(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_row
   a.q = qr;
   a.table = table;
   a.cols = table_cols;
-  a.scale = (float)(scale * 1.4426950408889634074);
+  // Not 0, which would make hidden scores -infinity * 0; scores under the smallest one are as equal.
+  a.scale = std::max((float)(scale * 1.4426950408889634074), FLT_TRUE_MIN);
   a.window = kv->window;
   a.sinks = kv->sinks;
   a.out = out;

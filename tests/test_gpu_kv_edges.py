@@ -46,3 +46,11 @@ def test_visible_infinities(q_len, ctx, G, dtype, window, sinks):
             if lse:
                 Batch.near(z[at:at + n].double(), wz, bz, (s, "lse"))
             at += n
+
+
+@pytest.mark.parametrize("n", [1, 50])
+@pytest.mark.parametrize("scale", [1e-40, 1e-60, 5e-324])
+def test_smallest_scales(n, scale):
+    """Scales that 32 bits hold only just or not at all: every key that a row sees weighs the same."""
+    b = Batch([n], [77], hq=8, hkv=2, d=64, S=16, dtype=BF, cache=BF)
+    b.check(scale=scale)
