@@ -587,7 +587,9 @@ typedef struct {
 
 /*
  * lar_kv_create: a handle with its working memory (about 4 KiB * CUs * head_dim for
- *   split attention, and the plan).  *out is NULL on failure.
+ *   split attention, and the plan).  *out is NULL on failure.  The handle belongs to the
+ *   device that is current, of which the stream has to be; its calls work on that one
+ *   whichever is current then, and leave that as it is.
  * lar_kv_plan: the token batch of the calls that follow; q_len, ctx_len host [n_seqs],
  *   copied.  window 0: none (sinks then have no effect).  Enqueues the plan's copy from
  *   pinned memory; waits only if the copy before the previous one is still under way.

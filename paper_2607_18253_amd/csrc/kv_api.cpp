@@ -48,7 +48,7 @@ struct lar_kv {
   lar_kv_config cfg{};
   KvGeom g{};
   hipStream_t stream = nullptr;
-  int cus = 0;
+  int device = 0, cus = 0;
   int waves = 0, groups = 0;  // of the narrow and the wide kernel at most
   size_t cap = 0;             // bytes of a plan at most
   Layout lay;                 // of the current plan
@@ -88,6 +88,29 @@ lar_status fail(lar_kv* kv, lar_status code, const char* fmt, ...) {
     hipError_t e_ = (expr);                                                        \
     if (e_ != hipSuccess) return fail(kv, LAR_E_HIP, "%s: %s", #expr, hipGetErrorString(e_)); \
   } while (0)
+
+// The handle's device is the current one while this lives: the null stream, and calls without
+// a stream, go to the current device.
+class OnDevice {
+ public:
+  explicit OnDevice(const lar_kv* kv) {
+    int now = 0;
+    status_ = hipGetDevice(&now);
+    if (status_ != hipSuccess || now == kv->device) return;
+    status_ = hipSetDevice(kv->device);
+    if (status_ == hipSuccess) before_ = now;
+  }
+  ~OnDevice() {
+    if (before_ >= 0) (void)hipSetDevice(before_);
+  }
+  OnDevice(const OnDevice&) = delete;
+  OnDevice& operator=(const OnDevice&) = delete;
+  hipError_t status() const { return status_; }
+
+ private:
+  int before_ = -1;
+  hipError_t status_ = hipSuccess;
+};
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -466,7 +489,12 @@ KvCopyArgs copy_args(const lar_kv* kv, const KvPool& pool, const int32_t* table,
   return a;
 }
 
-lar_status launched(lar_kv* kv, hipError_t e) {
+// A launch on the handle's device and stream.
+template <class Args>
+lar_status launch(lar_kv* kv, hipError_t (*f)(const Args&, hipStream_t), const Args& a) {
+  const OnDevice device(kv);
+  KV_TRY(kv, device.status());
+  const hipError_t e = f(a, kv->stream);
   return e == hipSuccess ? LAR_OK : fail(kv, LAR_E_HIP, "launch: %s", hipGetErrorString(e));
 }
 
@@ -509,9 +537,8 @@ lar_status lar_kv_create(lar_kv** out, const lar_kv_config* cfg) {
   g.dtype = cfg->dtype;
   g.cache = cfg->cache_dtype;
   while ((1 << g.sh) < S) ++g.sh;
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess ||
-      hipDeviceGetAttribute(&kv->cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) {
+  if (hipGetDevice(&kv->device) != hipSuccess ||
+      hipDeviceGetAttribute(&kv->cus, hipDeviceAttributeMultiprocessorCount, kv->device) != hipSuccess) {
     delete kv;
     return LAR_E_HIP;
   }
@@ -545,8 +572,11 @@ lar_status lar_kv_create(lar_kv** out, const lar_kv_config* cfg) {
 
 lar_status lar_kv_destroy(lar_kv* kv) {
   if (!kv) return LAR_OK;
-  (void)hipStreamSynchronize(kv->stream);
-  release(kv);
+  {
+    const OnDevice device(kv);
+    (void)hipStreamSynchronize(kv->stream);
+    release(kv);
+  }
   delete kv;
   return LAR_OK;
 }
@@ -560,6 +590,8 @@ lar_status lar_kv_plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const i
     return fail(kv, LAR_E_ARG, "%d sequences, at most %d", n_seqs, kv->cfg.max_seqs);
   if (n_seqs && (!q_len || !ctx_len)) return fail(kv, LAR_E_ARG, "null lengths");
   if (window < 0 || sinks < 0) return fail(kv, LAR_E_ARG, "negative window or sinks");
+  const OnDevice device(kv);
+  KV_TRY(kv, device.status());
   hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
   if (kv->stream) KV_TRY(kv, hipStreamIsCapturing(kv->stream, &capture));
   if (capture != hipStreamCaptureStatusNone) return fail(kv, LAR_E_STATE, "no plan under stream capture");
@@ -662,7 +694,7 @@ lar_status lar_kv_append(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_row
   KvCopyArgs a = copy_args(kv, pool, table, table_cols);
   a.k = kr;
   a.v = vr;
-  return launched(kv, launch_kv_append(a, kv->stream));
+  return launch(kv, launch_kv_append, a);
 }
 
 lar_status lar_kv_read(lar_kv* kv, const lar_kv_pages* pages, const int32_t* table, int32_t table_cols,
@@ -677,7 +709,7 @@ lar_status lar_kv_read(lar_kv* kv, const lar_kv_pages* pages, const int32_t* tab
   KvCopyArgs a = copy_args(kv, pool, table, table_cols);
   a.k = kr;
   a.v = vr;
-  return launched(kv, launch_kv_read(a, kv->stream));
+  return launch(kv, launch_kv_read, a);
 }
 
 lar_status lar_kv_attend(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_rows* q, const int32_t* table,
@@ -717,12 +749,14 @@ lar_status lar_kv_attend(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_row
   a.narrow_ml = kv->narrow_ml;
   a.wide_ml = kv->wide_ml;
   a.err = kv->err;
-  return launched(kv, launch_kv_attend(a, kv->stream));
+  return launch(kv, launch_kv_attend, a);
 }
 
 lar_status lar_kv_sync(lar_kv* kv) {
   if (!kv) return LAR_E_ARG;
   if (kv->sticky != LAR_OK) return kv->sticky;
+  const OnDevice device(kv);
+  KV_TRY(kv, device.status());
   int32_t e = 0;
   KV_TRY(kv, hipMemcpyAsync(&e, kv->err, sizeof e, hipMemcpyDeviceToHost, kv->stream));
   KV_TRY(kv, hipStreamSynchronize(kv->stream));

@@ -80,10 +80,10 @@ class PagedKV:
     """A paged key/value cache's geometry and the plan of the current token batch; see
     lar_kv_config and lar_kv_plan.  The pages of each layer are KvPages.
 
-    Work runs on ``stream`` (the current one when the handle is made).  A call made while
-    another stream is current is ordered after that stream's work, and that stream after
-    the call; a graph is captured on the handle's own stream (which then is not the
-    default one)."""
+    Work runs on ``stream`` (the current one when the handle is made) and its device,
+    whichever device is current when a call is made.  A call made while another stream is
+    current is ordered after that stream's work, and that stream after the call; a graph is
+    captured on the handle's own stream (which then is not the default one)."""
 
     def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, *, block_size: int,
                  dtype=None, cache_dtype=None, max_seqs: int, max_tokens: int, stream=None):
@@ -170,9 +170,10 @@ class PagedKV:
             if st != LAR_OK:
                 self._check(st)
             return
-        if self._torch.cuda.is_current_stream_capturing():
-            raise ValueError("capture a graph on the handle's own stream")
-        now = self._torch.cuda.current_stream(self.device)
+        with self._torch.cuda.device(self.device):
+            if self._torch.cuda.is_current_stream_capturing():
+                raise ValueError("capture a graph on the handle's own stream")
+            now = self._torch.cuda.current_stream()
         self.stream.wait_stream(now)
         try:
             self._check(f(self._h, *args))
