@@ -33,6 +33,14 @@ def _int32s(x, name):
     return np.ascontiguousarray(a, np.int32)
 
 
+def _on(index, t, dtype, name, numel=None):
+    """_dev of a tensor on GPU `index`."""
+    p = _dev(t, dtype, name, numel)
+    if t is not None and t.get_device() != index:
+        raise ValueError(f"{name} must be on cuda:{index}")
+    return p
+
+
 class KvConfig(C.Structure):
     _fields_ = [("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
                 ("dtype", C.c_int32), ("cache_dtype", C.c_int32), ("block_size", C.c_int32),
@@ -66,11 +74,12 @@ class KvPages:
                 raise ValueError("float8_e4m3fn pages, and only they, have k_exp and v_exp "
                                  "[n_blocks][n_kv_heads][block_size]")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
-        self._arg = KvPagesArg(_dev(k, k.dtype, "k"), _dev(v, v.dtype, "v"),
-                               _dev(k_exp, torch.uint8, "k_exp"), _dev(v_exp, torch.uint8, "v_exp"),
+        index = k.get_device()
+        self._arg = KvPagesArg(_on(index, k, k.dtype, "k"), _on(index, v, v.dtype, "v"),
+                               _on(index, k_exp, torch.uint8, "k_exp"), _on(index, v_exp, torch.uint8, "v_exp"),
                                int(k.shape[0]))
         self._ref = C.byref(self._arg)
-        self._kind = (k.dtype, *k.shape[1:], k.get_device())
+        self._kind = (k.dtype, *k.shape[1:], index)
 
     def tensors(self):
         return [t for t in (self.k, self.v, self.k_exp, self.v_exp) if t is not None]
@@ -161,7 +170,7 @@ class PagedKV:
         shape = table.shape
         if len(shape) != 2 or shape[0] < self._n_seq:
             raise ValueError(f"table must have {self._n_seq} rows")
-        return _dev(table, self._int32, "table"), shape[1]
+        return _on(self._index, table, self._int32, "table"), shape[1]
 
     def _call(self, f, pages, tensors, *args):
         """f(handle, *args) in order with the current stream."""
@@ -236,11 +245,11 @@ class PagedKV:
             out = self._none.new_empty(self._q_shape)
             to = out.data_ptr()
         else:
-            to = _dev(out, self.dtype, "out", n * self.head_dim)
+            to = _on(self._index, out, self.dtype, "out", n * self.head_dim)
         t, cols = self._table(table)
         self._call(self._L.lar_kv_attend, pages, (q, out, lse, table), self._pages(pages), qa, t, cols,
                    self._scale if scale is None else float(scale), to,
-                   None if lse is None else _dev(lse, self._torch.float32, "lse", n))
+                   None if lse is None else _on(self._index, lse, self._torch.float32, "lse", n))
         return out
 
     def sync(self):

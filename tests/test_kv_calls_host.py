@@ -84,3 +84,84 @@ def test_calls_go_to_the_handles_device(lib, current):
         assert call() == 0
         assert lib.stub_device() == current
         assert lib.stub_calls(0) == 0 and lib.stub_calls(1) > 0
+
+
+# ------------------------------------------------------------------ the binding's checks
+class Tensor:
+    """As much of a contiguous GPU tensor as the binding looks at."""
+
+    is_cuda, requires_grad = True, False
+
+    def __init__(self, shape, dtype, device=0, at=4096, stride=None):
+        self.shape, self.dtype, self.device_index, self.at = tuple(shape), dtype, device, at
+        self.strides = stride or tuple(int(np.prod(self.shape[i + 1:])) for i in range(len(self.shape)))
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return int(np.prod(self.shape))
+
+    def stride(self):
+        return self.strides
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return self.at
+
+    def get_device(self):
+        return self.device_index
+
+
+@pytest.fixture
+def binding(monkeypatch):
+    """A PagedKV of 8 and 2 heads of 64 on device 0 with a batch of 3 tokens, whose library
+    notes its calls."""
+    import torch
+    from paper_2607_18253_amd import kv as K
+
+    class Library:
+        def __init__(self):
+            self.calls = []
+
+        def __getattr__(self, name):
+            return lambda *args: self.calls.append((name, args)) or 0
+
+    x = object.__new__(K.PagedKV)
+    x._torch, x._L, x._h, x._sid = torch, Library(), C.c_void_p(1), 0
+    x.dtype = x.cache_dtype = torch.bfloat16
+    x.n_q, x.n_kv, x.head_dim, x.block_size, x.device = 8, 2, 64, 16, torch.device("cuda:0")
+    x._int32, x._index, x._scale = torch.int32, 0, 0.125
+    x._kind = (torch.bfloat16, 2, 16, 64, 0)
+    x._args = {n: (a, C.byref(a)) for n, a in ((n, KvRowsArg()) for n in "qkv")}
+    x._batch(1, 3)
+    monkeypatch.setattr(K, "_raw_stream", lambda index: 0)
+    return x
+
+
+def test_tensors_of_another_device_are_refused(binding):
+    import torch
+    from paper_2607_18253_amd import KvPages
+    B = torch.bfloat16
+    pages = KvPages(*(Tensor((9, 2, 16, 64), B) for _ in range(2)))
+    q, out, new = Tensor((3, 8, 64), B), Tensor((3, 8, 64), B), Tensor((3, 2, 64), B)
+    tab, lse = Tensor((1, 4), torch.int32), Tensor((3, 8), torch.float32)
+    binding.attend(pages, q, tab, out=out, lse=lse)
+    binding.append(pages, new, new, tab)
+    binding.read(pages, tab, k=new, v=new)
+    assert len(binding._L.calls) == 3
+    far = lambda t: Tensor(t.shape, t.dtype, device=1)
+    for call in (lambda: binding.attend(pages, q, far(tab), out=out), lambda: binding.attend(pages, q, tab, out=far(out)),
+                 lambda: binding.attend(pages, q, tab, out=out, lse=far(lse)), lambda: binding.attend(pages, far(q), tab, out=out),
+                 lambda: binding.append(pages, new, new, far(tab)), lambda: binding.append(pages, new, far(new), tab),
+                 lambda: binding.read(pages, far(tab), k=new, v=new), lambda: binding.read(pages, tab, k=far(new), v=new)):
+        with pytest.raises(ValueError, match="cuda:0"):
+            call()
+    assert len(binding._L.calls) == 3
+    k, e = Tensor((9, 2, 16, 64), torch.float8_e4m3fn), Tensor((9, 2, 16), torch.uint8)
+    KvPages(k, k, e, e)
+    for args in ((k, far(k), e, e), (k, k, far(e), e), (k, k, e, far(e))):
+        with pytest.raises(ValueError, match="cuda:0"):
+            KvPages(*args)
