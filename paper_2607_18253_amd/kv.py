@@ -60,12 +60,20 @@ class KvRowsArg(C.Structure):
 class KvPages:
     """The pages of one layer: GPU tensors k and v [n_blocks][n_kv_heads][block_size][head_dim]
     (16-bit, or float8_e4m3fn with k_exp and v_exp uint8 [n_blocks][n_kv_heads][block_size]).
-    Make new ones with PagedKV.new_pages."""
+    Make new ones with PagedKV.new_pages.  Which tensors they are is fixed; where these are is
+    looked up by every call."""
 
-    __slots__ = ("k", "v", "k_exp", "v_exp", "_arg", "_ref", "_kind")
+    __slots__ = ("_tensors", "_at", "_arg", "_ref", "_kind")
+    k, v, k_exp, v_exp = (property(lambda self, i=i: self._tensors[i]) for i in range(4))
 
     def __init__(self, k, v, k_exp=None, v_exp=None):
+        self._tensors = (k, v, k_exp, v_exp)
+        self._look()
+
+    def _look(self):
+        """Checks the tensors and takes their places down."""
         import torch
+        k, v, k_exp, v_exp = self._tensors
         if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
             raise ValueError("k and v must be [n_blocks][n_kv_heads][block_size][head_dim] of one dtype")
         e4m3 = k.dtype == torch.float8_e4m3fn
@@ -73,16 +81,22 @@ class KvPages:
             if (e is not None) != e4m3 or (e4m3 and e.shape != k.shape[:3]):
                 raise ValueError("float8_e4m3fn pages, and only they, have k_exp and v_exp "
                                  "[n_blocks][n_kv_heads][block_size]")
-        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         index = k.get_device()
         self._arg = KvPagesArg(_on(index, k, k.dtype, "k"), _on(index, v, v.dtype, "v"),
                                _on(index, k_exp, torch.uint8, "k_exp"), _on(index, v_exp, torch.uint8, "v_exp"),
                                int(k.shape[0]))
         self._ref = C.byref(self._arg)
         self._kind = (k.dtype, *k.shape[1:], index)
+        self._at = [t.data_ptr() for t in self.tensors()]
 
     def tensors(self):
-        return [t for t in (self.k, self.v, self.k_exp, self.v_exp) if t is not None]
+        return [t for t in self._tensors if t is not None]
+
+    def _now(self):
+        """The pages as an argument, where the tensors are now."""
+        if [t.data_ptr() for t in self._tensors if t is not None] != self._at:
+            self._look()
+        return self._ref
 
 
 class PagedKV:
@@ -149,10 +163,11 @@ class PagedKV:
         self.close()
 
     def _pages(self, pages):
+        ref = pages._now()
         if pages._kind != self._kind:
             raise ValueError(f"pages must be [n_blocks][{self.n_kv}][{self.block_size}][{self.head_dim}] "
                              f"of {self.cache_dtype} on {self.device}")
-        return pages._ref
+        return ref
 
     def _rows(self, t, shape, name):
         if t.dtype is not self.dtype or t.get_device() != self._index:

@@ -165,3 +165,39 @@ def test_tensors_of_another_device_are_refused(binding):
     for args in ((k, far(k), e, e), (k, k, far(e), e), (k, k, e, far(e))):
         with pytest.raises(ValueError, match="cuda:0"):
             KvPages(*args)
+
+
+def test_pages_are_where_their_tensors_are(binding):
+    """Pages whose tensors were given other memory, and pages that cannot be given other tensors."""
+    import torch
+    from paper_2607_18253_amd import KvPages
+    B, E4 = torch.bfloat16, torch.float8_e4m3fn
+    q, out, tab = Tensor((3, 8, 64), B), Tensor((3, 8, 64), B), Tensor((1, 4), torch.int32)
+
+    def seen():
+        binding.attend(pages, q, tab, out=out)
+        a = binding._L.calls[-1][1][1]._obj
+        return a.k, a.v, a.k_exp, a.v_exp, a.n_blocks
+    for kind in (B, E4):
+        binding._kind = (kind, 2, 16, 64, 0)
+        t = [Tensor((9, 2, 16, 64), kind, at=1 << 20), Tensor((9, 2, 16, 64), kind, at=1 << 21)]
+        if kind is E4:
+            t += [Tensor((9, 2, 16), torch.uint8, at=1 << 22), Tensor((9, 2, 16), torch.uint8, at=1 << 23)]
+        pages = KvPages(*t)
+        assert seen()[:len(t)] == tuple(x.at for x in t)
+        for x in t:
+            x.at += 1 << 24
+            x.shape = (12, *x.shape[1:])
+            for y in t:
+                y.shape = x.shape[:len(y.shape)] if len(y.shape) == 3 else (12, 2, 16, 64)
+            assert seen() == (*(y.at for y in t), *[None] * (4 - len(t)), 12)
+        t[1].at += 1 << 24
+        t[0].shape = t[1].shape = (12, 2, 32, 64)      # of another block size now
+        if kind is E4:
+            t[2].shape = t[3].shape = (12, 2, 32)
+        with pytest.raises(ValueError, match="pages must be"):
+            seen()
+        for name in ("k", "v", "k_exp", "v_exp"):
+            with pytest.raises(AttributeError):
+                setattr(pages, name, t[0])
+            assert getattr(pages, name) is (t + [None, None])[("k", "v", "k_exp", "v_exp").index(name)]
