@@ -593,8 +593,10 @@ typedef struct {
  * lar_kv_plan: the token batch of the calls that follow; q_len, ctx_len host [n_seqs],
  *   copied.  window 0: none (sinks then have no effect).  Enqueues the plan's copy from
  *   pinned memory; waits only if the copy before the previous one is still under way.
- *   Clears a sticky error that was reported.  Not under stream capture; a captured call
- *   belongs to the plan it was captured with.
+ *   Clears a sticky error that was reported.  Not under stream capture.  A captured call
+ *   belongs to the handle and to the plan it was captured with: replayed, in the order of
+ *   the handle's stream, while another plan is the current one it does nothing and sets the
+ *   sticky LAR_E_STATE.  (A plan of the same lengths, window and sinks is the same plan.)
  * lar_kv_append: k, v rows [T][n_kv_heads][head_dim] into the pages.
  * lar_kv_read: the rows of the batch's tokens from the pages into k, v.  A plan with
  *   q_len == ctx_len reads whole contexts (swap-out of a preempted sequence).

@@ -28,9 +28,9 @@ constexpr int kStages = 2;  // pinned copies of a plan: one may be on its way wh
 
 size_t up(size_t x) { return (x + 255) & ~size_t(255); }
 
-// Byte offsets of a plan's arrays, the same on the host and on the device.
+// Byte offsets of a plan's arrays, the same on the host and on the device, after its number.
 struct Layout {
-  size_t tok = 0, narrow = 0, wide = 0, narrow_at = 0, wide_at = 0, join = 0, end = 0;
+  size_t tok = up(sizeof(uint64_t)), narrow = 0, wide = 0, narrow_at = 0, wide_at = 0, join = 0, end = 0;
   Layout() = default;
   Layout(int64_t n_tok, int64_t n_narrow, int64_t n_wide, int64_t waves, int64_t groups, int64_t n_join) {
     narrow = up(tok + sizeof(KvTok) * n_tok);
@@ -62,6 +62,7 @@ struct lar_kv {
   int32_t* err = nullptr;
   // the plan
   bool planned = false;
+  uint64_t plan = 0;  // its number
   int32_t n_seq = 0, n_tok = 0, max_pages = 0, window = 0, sinks = 0;
   int32_t n_narrow = 0, n_wide = 0, n_join = 0, join_rows = 0, most_parts = 0;
   lar_status sticky = LAR_OK;
@@ -110,6 +111,17 @@ class OnDevice {
  private:
   int before_ = -1;
   hipError_t status_ = hipSuccess;
+};
+
+// A plan's number, made of all that a plan follows from, so that equal batches have equal plans
+// with equal numbers.  Each step maps the numbers one to one: batches that differ in one sequence's
+// lengths have different ones, and others the same with a chance of 2^-64.
+struct PlanId {
+  uint64_t x = 0x243f6a8885a308d3u;  // fraction of pi
+  void add(uint32_t a, uint32_t b) {
+    x = (x ^ ((uint64_t)a << 32 | b)) * 0x9e3779b97f4a7c15u;  // odd
+    x ^= x >> 29;
+  }
 };
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -477,8 +489,11 @@ lar_status check_rows(lar_kv* kv, const lar_kv_rows* r, const char* name, KvRows
   return LAR_OK;
 }
 
+KvPlanId plan_id(const lar_kv* kv) { return KvPlanId{(const uint64_t*)kv->dev, kv->plan}; }
+
 KvCopyArgs copy_args(const lar_kv* kv, const KvPool& pool, const int32_t* table, int32_t cols) {
   KvCopyArgs a{};
+  a.plan = plan_id(kv);
   a.g = kv->g;
   a.pool = pool;
   a.table = table;
@@ -609,12 +624,16 @@ lar_status lar_kv_plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const i
   // A window of every context hides nothing.  The kernels subtract a shorter one, and then a
   // key of a context, from a position: all within 2^30, so within 32 bits.
   if (window >= longest) window = 0;
+  if (!window) sinks = 0;
+  PlanId id;
+  id.add((uint32_t)window, (uint32_t)sinks);
+  for (int s = 0; s < n_seqs; ++s) id.add((uint32_t)q_len[s], (uint32_t)ctx_len[s]);
   // the copy that last left this buffer is done before it is written again
   const int b = kv->stage;
   if (kv->used[b]) KV_TRY(kv, hipEventSynchronize(kv->done[b]));
   char* p = kv->pinned[b];
   const KvGeom& g = kv->g;
-  KvTok* tok = (KvTok*)p;
+  KvTok* tok = (KvTok*)(p + Layout().tok);
   int32_t n_narrow = 0, n_wide = 0, n_join = 0, join_rows = 0, most_parts = 0;
   kv->planned = false;
   try {
@@ -663,6 +682,7 @@ lar_status lar_kv_plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const i
     kv->sticky = LAR_OK;
   }
   if (T) {
+    memcpy(p, &id.x, sizeof id.x);
     KV_TRY(kv, hipMemcpyAsync(kv->dev, p, kv->lay.end, hipMemcpyHostToDevice, kv->stream));
     KV_TRY(kv, hipEventRecord(kv->done[b], kv->stream));
     kv->used[b] = true;
@@ -672,7 +692,8 @@ lar_status lar_kv_plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const i
   kv->n_tok = (int32_t)T;
   kv->max_pages = (int32_t)pages;
   kv->window = window;
-  kv->sinks = window ? sinks : 0;
+  kv->sinks = sinks;
+  kv->plan = id.x;
   kv->n_narrow = n_narrow;
   kv->n_wide = n_wide;
   kv->n_join = n_join;
@@ -723,6 +744,7 @@ lar_status lar_kv_attend(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_row
   if (!(scale > 0.0) || !(scale < 1e30)) return fail(kv, LAR_E_ARG, "scale must be positive and finite");
   if (!out || ((uintptr_t)out & 15)) return fail(kv, LAR_E_ARG, "out must be aligned to 16 bytes");
   KvAttendArgs a{};
+  a.plan = plan_id(kv);
   a.g = kv->g;
   a.pool = pool;
   a.q = qr;
@@ -760,9 +782,10 @@ lar_status lar_kv_sync(lar_kv* kv) {
   int32_t e = 0;
   KV_TRY(kv, hipMemcpyAsync(&e, kv->err, sizeof e, hipMemcpyDeviceToHost, kv->stream));
   KV_TRY(kv, hipStreamSynchronize(kv->stream));
-  if (e != LAR_OK) {
-    kv->sticky = e;
-    return fail(kv, e, "a block table names a page outside the pool");
+  if (e) {
+    kv->sticky = LAR_E_STATE;
+    return fail(kv, LAR_E_STATE, e == kKvLostPage ? "a block table names a page outside the pool"
+                                                  : "a captured call ran under another plan than its own");
   }
   return LAR_OK;
 }

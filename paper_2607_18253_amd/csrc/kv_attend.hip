@@ -148,6 +148,13 @@ __device__ __forceinline__ T plan_at(const T* p, int i) {
   return t;
 }
 
+// Whether the device has another plan now than the launch was made for.
+__device__ __forceinline__ bool other_plan(const KvAttendArgs& A) {
+  if (plan_at(A.plan.now, 0) == A.plan.id) return false;
+  *A.err = kKvOtherPlan;
+  return true;
+}
+
 // The run of stretches of workgroup `i` of n.  Workgroups go to the 8 XCDs in turn; runs that
 // follow one another, which read the same keys or their neighbours, go to one XCD's L2.
 __device__ __forceinline__ int run_of(int i, int n) {
@@ -670,7 +677,9 @@ __device__ __forceinline__ void narrow(const KvAttendArgs& A, char* lds, int run
   const int r0 = lane / St::kChunks, c = lane % St::kChunks;
   const int e = plan_at(A.narrow_at, run + 1);
   bool lost = false;  // a page outside the pool
-  for (int x = plan_at(A.narrow_at, run); x < e; ++x) {
+  int x = plan_at(A.narrow_at, run);
+  if (other_plan(A)) return;
+  for (; x < e; ++x) {
     const KvSeg s = plan_at(A.narrow, x);
     s16x8 q[D / 16];
     const Row row = load_q<D>(A, lane_of(A, s, n), h, q);
@@ -739,7 +748,7 @@ __device__ __forceinline__ void narrow(const KvAttendArgs& A, char* lds, int run
     wave_order();
     if (__any(bad)) spread<BF, F8, D, kNarrowKeys, !F8>(A, s, lane, 0, kNarrowRows, A.narrow_o);
   }
-  if (lost) *A.err = LAR_E_STATE;
+  if (lost) *A.err = kKvLostPage;
 }
 
 template <bool BF, bool F8, int D>
@@ -777,6 +786,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
   const int run = run_of(blockIdx.x, A.n_wide), e = plan_at(A.wide_at, run + 1);
   bool lost = false;  // a page outside the pool
   int x = plan_at(A.wide_at, run);
+  if (other_plan(A)) return;
   // the current stretch, its queries, and its first keys on their way
   KvSeg s;
   s16x8 q[D / 16];
@@ -960,7 +970,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
     finish<BF, D>(A, done, a, lane, wave * 32, kWideRows, A.wide_o, A.wide_ml, lds + wave * 32 * kRowK<D>);
     if (flag) spread<BF, F8, D, kWideKeys, false>(A, done, lane, wave * 32, kWideRows, A.wide_o);
   }
-  if (lost) *A.err = LAR_E_STATE;
+  if (lost) *A.err = kKvLostPage;
 }
 
 // ------------------------------------------------------------------ joining split tiles
@@ -987,6 +997,7 @@ __global__ __launch_bounds__(THREADS) void k_kv_join(KvAttendArgs A) {
   constexpr int kQuads = D / 4;
   __shared__ Part parts[THREADS];
   const KvJoin j = plan_at(A.join, blockIdx.x);
+  if (other_plan(A)) return;
   const int rows = j.wide ? kWideRows : kNarrowRows, row0 = j.row0;
   const int have = j.ntok * A.g.G - row0 < A.join_rows ? j.ntok * A.g.G - row0 : A.join_rows;
   const float* po = j.wide ? A.wide_o : A.narrow_o;

@@ -24,6 +24,9 @@ constexpr int kNarrowRows = 32, kWideWaves = 8, kWideRows = 32 * kWideWaves;
 // Exponents of the e4m3 rows' scales.
 constexpr int kKvExpMin = -100, kKvExpMax = 120;
 
+// What a kernel reports to the host.
+enum { kKvLostPage = 1, kKvOtherPlan = 2 };
+
 // A new token of the batch: its row of the block table and its position there (< 0: a
 // padding row).
 struct KvTok {
@@ -67,7 +70,16 @@ struct KvRows {
   int64_t tok, head;  // strides in elements
 };
 
+// The plan that a launch was made for.  The device's copy starts with the number of the current
+// one: a launch of a captured graph that finds another there touches nothing, since the offsets
+// and counts of its arguments belong to the plan that is gone.
+struct KvPlanId {
+  const uint64_t* now;
+  uint64_t id;
+};
+
 struct KvAttendArgs {
+  KvPlanId plan;
   KvGeom g;
   KvPool pool;
   KvRows q;
@@ -88,6 +100,7 @@ struct KvAttendArgs {
 };
 
 struct KvCopyArgs {
+  KvPlanId plan;
   KvGeom g;
   KvPool pool;        // written by an append
   KvRows k, v;        // rows of the batch, [T][hkv][D]

@@ -29,7 +29,7 @@ template <bool BF> constexpr uint32_t kHeld = BF ? 0x7f70u : 0x7b80u;  // 1.875 
 __device__ __forceinline__ int64_t page_row(const KvGeom& g, const KvPool& pool, int32_t page,
                                             int head, int pos, int32_t* err) {
   if ((uint32_t)page >= pool.n_blocks) {
-    *err = LAR_E_STATE;
+    *err = kKvLostPage;
     return -1;
   }
   return (((int64_t)page * g.hkv + head) << g.sh) + (pos & ((1 << g.sh) - 1));
@@ -37,6 +37,13 @@ __device__ __forceinline__ int64_t page_row(const KvGeom& g, const KvPool& pool,
 
 // The largest pattern of 8 magnitudes.
 __device__ __forceinline__ uint32_t top(const uint4& x) { return top_half(top_pair(x)); }
+
+// Whether the device has another plan now than the launch was made for.
+__device__ __forceinline__ bool other_plan(const KvCopyArgs& A) {
+  if (*A.plan.now == A.plan.id) return false;
+  *A.err = kKvOtherPlan;
+  return true;
+}
 
 // The larger of both halves of a word over the 8 or 16 lanes of a row.
 template <int LANES>
@@ -133,6 +140,7 @@ __global__ __launch_bounds__(256) void k_kv_append(KvCopyArgs A) {
   const Place at(A, LANES);
   if (at.t >= (uint32_t)A.n_tok) return;
   const KvTok tok = A.tok[at.t];
+  if (other_plan(A)) return;
   if (tok.pos < 0) return;
   const int32_t page = A.table[(int64_t)tok.seq * A.cols + (tok.pos >> A.g.sh)];
   uint4 k = *(const uint4*)at.k, v = *(const uint4*)at.v;
@@ -162,6 +170,7 @@ __global__ __launch_bounds__(256) void k_kv_read(KvCopyArgs A) {
   const Place at(A, LANES);
   if (at.t >= (uint32_t)A.n_tok) return;
   const KvTok tok = A.tok[at.t];
+  if (other_plan(A)) return;
   uint4 k = make_uint4(0, 0, 0, 0), v = k;
   if (tok.pos >= 0) {
     const int32_t page = A.table[(int64_t)tok.seq * A.cols + (tok.pos >> A.g.sh)];

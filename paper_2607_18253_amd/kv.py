@@ -106,7 +106,9 @@ class PagedKV:
     Work runs on ``stream`` (the current one when the handle is made) and its device,
     whichever device is current when a call is made.  A call made while another stream is
     current is ordered after that stream's work, and that stream after the call; a graph is
-    captured on the handle's own stream (which then is not the default one)."""
+    captured on the handle's own stream (which then is not the default one).  A captured
+    call belongs to the plan it was captured with: replayed while a batch of other lengths is
+    planned it does nothing, and ``sync`` raises."""
 
     def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, *, block_size: int,
                  dtype=None, cache_dtype=None, max_seqs: int, max_tokens: int, stream=None):

@@ -87,6 +87,25 @@ hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t) {
 extern "C" {
 void stub_use(int device) { current = device; }
 int stub_device() { return current; }
+// The number of the plan that the last launch was made for, and that of the device's plan.
+uint64_t stub_attend_plan() { return attend.plan.id; }
+uint64_t stub_copy_plan() { return copy.plan.id; }
+uint64_t stub_device_plan() { return *attend.plan.now; }
+// The plan that the last launches have on the device, as numbers; what a count is past `room` is
+// not written.  0: tokens (seq, pos), 1: narrow stretches, 2: wide ones, 3 and 4: where the runs
+// of each start, 5: joins, each in the order of its fields.
+int stub_plan(int what, int32_t* to, int room) {
+  const void* p = nullptr;
+  int n = 0;
+  if (what == 0) p = copy.tok, n = 2 * copy.n_tok;
+  if (what == 1) p = attend.narrow, n = attend.n_narrow ? attend.narrow_at[attend.n_narrow] * 10 : 0;
+  if (what == 2) p = attend.wide, n = attend.n_wide ? attend.wide_at[attend.n_wide] * 10 : 0;
+  if (what == 3) p = attend.narrow_at, n = attend.n_narrow ? attend.n_narrow + 1 : 0;
+  if (what == 4) p = attend.wide_at, n = attend.n_wide ? attend.n_wide + 1 : 0;
+  if (what == 5) p = attend.join, n = attend.n_join * 8;
+  if (n) std::memcpy(to, p, sizeof(int32_t) * (n < room ? n : room));
+  return n;
+}
 // Calls made while a device was current, since the last time.
 int stub_calls(int device) {
   const int n = calls[device];

@@ -86,6 +86,104 @@ def test_calls_go_to_the_handles_device(lib, current):
         assert lib.stub_calls(0) == 0 and lib.stub_calls(1) > 0
 
 
+def plan_arrays(lib):
+    """The device's plan: tokens, narrow and wide stretches, their runs' starts, joins."""
+    out = []
+    for what, fields in enumerate((2, 10, 10, 1, 1, 8)):
+        a = np.zeros(1 << 16, np.int32)
+        n = lib.stub_plan(what, a.ctypes.data_as(C.c_void_p), len(a))
+        assert n <= len(a)
+        out.append(a[:n].reshape(-1, fields))
+    return out
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_plan_as_the_kernels_read_it(lib, seed):
+    """Every array of the device's copy, from where the launches' arguments say it is: the tokens'
+    places, every key tile of every query tile once, slots and joins in their bounds."""
+    r = np.random.RandomState(seed)
+    lib.stub_use(0)
+    n = r.randint(1, 9)
+    q_len = np.where(r.rand(n) < 0.5, 1, np.exp(r.uniform(0, 4.8, n))).astype(int)
+    ctx = np.exp(r.uniform(0, 11 if seed % 2 else 7, n)).astype(int) + np.where(r.rand(n) < 0.8, q_len, 0)
+    window, sinks = (0, 0) if seed % 3 else (int(np.exp(r.uniform(0, 8))), int(r.choice([0, 1, 4, 200])))
+    x = Handle(lib, max_tokens=1024)
+    x.pages.n_blocks = 1 << 20
+    assert x.plan(q_len, ctx, window, sinks) == 0
+    big = 1 << 20   # columns enough
+    kv = C.byref(x.kv)
+    assert lib.lar_kv_append(x.h, C.byref(x.pages), kv, kv, 4096, big) == 0
+    assert lib.lar_kv_attend(x.h, C.byref(x.pages), C.byref(x.q), 4096, big, 0.125, 4096, None) == 0
+    tok, narrow, wide, narrow_at, wide_at, join = plan_arrays(lib)
+    want = [(s, c - m + i) for s, (m, c) in enumerate(zip(q_len, ctx)) for i in range(m)]
+    assert [tuple(t) for t in tok.tolist()] == want
+    seen = {}      # (first token, head) -> stretches
+    for kind, segs, at, rows, runs in (("narrow", narrow, narrow_at, 32, 2048), ("wide", wide, wide_at, 256, 256)):
+        if len(at):
+            assert at[0] == 0 and (np.diff(at[:, 0]) >= 0).all() and at[-1] == len(segs) and len(at) <= runs + 1
+        for q0, ntok, p0, head, seq, ns, fw, t0, t1, slot in segs.tolist():
+            assert 1 <= ntok <= rows // 4 and 0 <= head < 2 and slot < 2 * runs and 0 <= t0 <= t1
+            assert all(tuple(tok[q0 + i]) == (seq, p0 + i) for i in (0, ntok - 1))
+            seen.setdefault((q0, head), []).append((t0, t1, slot, kind, ntok, p0, ns, fw))
+    slots = []
+    covered = set()
+    W = window if window and window < max(ctx[q_len > 0], default=0) else 0
+    for (q0, head), parts in seen.items():
+        parts.sort()
+        kind, ntok, p0, ns, fw = parts[0][3:]
+        K = 32 if kind == "narrow" else 64
+        assert all(p[3:] == parts[0][3:] for p in parts)
+        assert parts[0][0] == 0 and all(a[1] == b[0] for a, b in zip(parts, parts[1:]))
+        tiles = [t if t < ns else fw + t - ns for t in range(parts[-1][1])]
+        keys = {j for t in tiles for j in range(t * K, t * K + K)}
+        assert len(keys) == K * len(tiles)
+        for i in range(ntok):
+            pos = p0 + i
+            lo = max(0, pos - W + 1) if W else 0
+            assert keys.issuperset(range(lo, pos + 1)) and keys.issuperset(range(min(sinks if W else 0, pos + 1)))
+            covered.add((q0 + i, head))
+        if len(parts) > 1:
+            mine = [j for j in join.tolist() if j[0] == q0 and j[3] == head]
+            assert [p[2] for p in parts] == list(range(mine[0][4], mine[0][4] + len(parts)))
+            assert all(j[1:6] == [ntok, p0, head, parts[0][2], len(parts)] and j[7] == (kind == "wide") for j in mine)
+            step = {b[6] - a[6] for a, b in zip(mine, mine[1:])} or {32 * 8}
+            assert mine[0][6] == 0 and len(step) == 1 and len(mine) == -(-ntok * 4 // step.pop())
+            slots += [(kind, p[2]) for p in parts]
+        else:
+            assert parts[0][2] == -1
+    assert len(slots) == len(set(slots)) and covered == {(t, h) for t in range(len(tok)) for h in range(2)}
+    assert x.close() == 0
+
+
+def test_launches_carry_their_plan(lib):
+    """What a kernel compares: the number of the plan a launch was made for and that at the head
+    of the device's copy.  Equal batches have equal numbers, all others different ones."""
+    for f in (lib.stub_attend_plan, lib.stub_copy_plan, lib.stub_device_plan):
+        f.restype = C.c_uint64
+    lib.stub_use(0)
+    x = Handle(lib)
+
+    def number(*plan):
+        assert x.plan(*plan) == 0 and x.append() == 0 and x.attend() == 0
+        assert lib.stub_attend_plan() == lib.stub_copy_plan() == lib.stub_device_plan()
+        return lib.stub_device_plan()
+    first = number([1, 5], [40, 100])
+    plans = [([1, 5], [40, 101]), ([5, 1], [100, 40]), ([1, 5], [40, 100], 8), ([1, 5], [40, 100], 8, 2), ([1], [40]),
+             ([1, 5, 0], [40, 100, 0]), ([0, 1, 5], [0, 40, 100]), ([1, 6], [40, 100]), ([1, 5], [100, 40]),
+             ([1, 1], [40, 40]), ([1, 1, 1], [40, 40, 40])]
+    r = np.random.RandomState(5)
+    for _ in range(3000):
+        n = r.randint(1, 9)
+        plans.append((r.randint(1, 8, n).tolist(), r.randint(1, 60, n).tolist()))
+    numbers = {}
+    for p in plans:
+        numbers.setdefault(number(*p), set()).add(str(p))
+    assert all(len(p) == 1 for p in numbers.values()) and first not in numbers
+    # windows of every context hide nothing, nor do sinks without a window
+    assert number([1, 5], [40, 100]) == number([1, 5], [40, 100], 0, 3) == number([1, 5], [40, 100], 100, 2) == first
+    assert x.close() == 0
+
+
 # ------------------------------------------------------------------ the binding's checks
 class Tensor:
     """As much of a contiguous GPU tensor as the binding looks at."""
