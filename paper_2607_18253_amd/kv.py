@@ -63,7 +63,7 @@ class KvPages:
     Make new ones with PagedKV.new_pages.  Which tensors they are is fixed; where these are is
     looked up by every call."""
 
-    __slots__ = ("_tensors", "_at", "_arg", "_ref", "_kind")
+    __slots__ = ("_tensors", "_ptr", "_at", "_arg", "_ref", "_kind")
     k, v, k_exp, v_exp = (property(lambda self, i=i: self._tensors[i]) for i in range(4))
 
     def __init__(self, k, v, k_exp=None, v_exp=None):
@@ -87,14 +87,17 @@ class KvPages:
                                int(k.shape[0]))
         self._ref = C.byref(self._arg)
         self._kind = (k.dtype, *k.shape[1:], index)
-        self._at = [t.data_ptr() for t in self.tensors()]
+        self._ptr = [None if t is None else t.data_ptr for t in self._tensors]
+        self._at = [p and p() for p in self._ptr]
 
     def tensors(self):
         return [t for t in self._tensors if t is not None]
 
     def _now(self):
         """The pages as an argument, where the tensors are now."""
-        if [t.data_ptr() for t in self._tensors if t is not None] != self._at:
+        k, v, ke, ve = self._ptr
+        at = self._at
+        if k() != at[0] or v() != at[1] or (ke is not None and (ke() != at[2] or ve() != at[3])):
             self._look()
         return self._ref
 
