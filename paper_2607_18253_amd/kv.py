@@ -33,6 +33,13 @@ def _int32s(x, name):
     return np.ascontiguousarray(a, np.int32)
 
 
+def _int32(x, name):
+    """A number as an int that 32 bits hold, nothing cut off."""
+    if not -2 ** 31 <= x < 2 ** 31 or int(x) != x:
+        raise ValueError(f"{name} must be a 32-bit integer")
+    return int(x)
+
+
 def _on(index, t, dtype, name, numel=None):
     """_dev of a tensor on GPU `index`."""
     p = _dev(t, dtype, name, numel)
@@ -126,10 +133,11 @@ class PagedKV:
         kinds = {torch.float16: KV_F16, torch.bfloat16: KV_BF16, torch.float8_e4m3fn: KV_E4M3}
         if self.dtype not in kinds or self.cache_dtype not in kinds:
             raise ValueError("dtype must be float16 or bfloat16, cache_dtype dtype or float8_e4m3fn")
-        self.n_q, self.n_kv, self.head_dim = int(n_q_heads), int(n_kv_heads), int(head_dim)
-        self.block_size = int(block_size)
+        self.n_q, self.n_kv = _int32(n_q_heads, "n_q_heads"), _int32(n_kv_heads, "n_kv_heads")
+        self.head_dim, self.block_size = _int32(head_dim, "head_dim"), _int32(block_size, "block_size")
         cfg = KvConfig(self.n_q, self.n_kv, self.head_dim, kinds[self.dtype], kinds[self.cache_dtype],
-                       self.block_size, int(max_seqs), int(max_tokens), 0, C.c_void_p(self._sid))
+                       self.block_size, _int32(max_seqs, "max_seqs"), _int32(max_tokens, "max_tokens"), 0,
+                       C.c_void_p(self._sid))
         h = C.c_void_p()
         with torch.cuda.device(self.device):
             st = self._L.lar_kv_create(C.byref(h), C.byref(cfg))

@@ -299,3 +299,25 @@ def test_pages_are_where_their_tensors_are(binding):
             with pytest.raises(AttributeError):
                 setattr(pages, name, t[0])
             assert getattr(pages, name) is (t + [None, None])[("k", "v", "k_exp", "v_exp").index(name)]
+
+
+@pytest.mark.parametrize("field", ["n_q_heads", "n_kv_heads", "head_dim", "block_size", "max_seqs", "max_tokens"])
+@pytest.mark.parametrize("bad", [2 ** 32 + 8, -2 ** 32 + 8, 2 ** 63, 8.5, float("nan")])
+def test_geometry_is_not_cut(monkeypatch, field, bad):
+    """Numbers that 32 bits do not hold, and fractions, make no handle of what is left of them."""
+    import torch
+    from paper_2607_18253_amd import kv as K
+
+    class Stream:
+        cuda_stream, device = 0, torch.device("cuda:0")
+
+    def made(*args):
+        raise RuntimeError("made")
+    monkeypatch.setattr(K, "load_library", lambda: type("L", (), {"lar_kv_create": made}))
+    monkeypatch.setattr(K, "KvConfig", made)
+    args = dict(n_q_heads=8, n_kv_heads=8, head_dim=64, block_size=16, max_seqs=8, max_tokens=8)
+    with pytest.raises(RuntimeError, match="made"):
+        K.PagedKV(**args, stream=Stream)
+    with pytest.raises((ValueError, OverflowError)) as e:
+        K.PagedKV(**dict(args, **{field: bad}), stream=Stream)
+    assert field in str(e.value)
