@@ -579,7 +579,8 @@ typedef struct {
 } lar_kv_pages;
 
 /* Rows [token][head][head_dim]: strides in elements, head_dim contiguous, every row
- * aligned to 16 bytes (a slice of a fused projection will do). */
+ * aligned to 16 bytes (a slice of a fused projection will do); the stride of a single token
+ * or head does not matter. */
 typedef struct {
   void *data;
   int64_t tok_stride, head_stride;

@@ -480,10 +480,11 @@ lar_status check(lar_kv* kv, const lar_kv_pages* pages, const int32_t* table, in
   return LAR_OK;
 }
 
-// Rows [T][heads][head_dim] with 16-byte rows.
-lar_status check_rows(lar_kv* kv, const lar_kv_rows* r, const char* name, KvRows* out) {
+// Rows [T][heads][head_dim] with 16-byte rows.  A stride between things of which there is one
+// does not matter.
+lar_status check_rows(lar_kv* kv, const lar_kv_rows* r, int heads, const char* name, KvRows* out) {
   if (!r || !r->data) return fail(kv, LAR_E_ARG, "null %s", name);
-  if (((uintptr_t)r->data & 15) || (r->tok_stride & 7) || (r->head_stride & 7))
+  if (((uintptr_t)r->data & 15) || (kv->n_tok > 1 && (r->tok_stride & 7)) || (heads > 1 && (r->head_stride & 7)))
     return fail(kv, LAR_E_ARG, "%s: every row must be aligned to 16 bytes", name);
   *out = KvRows{r->data, r->tok_stride, r->head_stride};
   return LAR_OK;
@@ -710,8 +711,8 @@ lar_status lar_kv_append(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_row
   KvPool pool;
   KvRows kr, vr;
   if (lar_status st = check(kv, pages, table, table_cols, &pool)) return st;
-  if (lar_status st = check_rows(kv, k, "k", &kr)) return st;
-  if (lar_status st = check_rows(kv, v, "v", &vr)) return st;
+  if (lar_status st = check_rows(kv, k, kv->g.hkv, "k", &kr)) return st;
+  if (lar_status st = check_rows(kv, v, kv->g.hkv, "v", &vr)) return st;
   KvCopyArgs a = copy_args(kv, pool, table, table_cols);
   a.k = kr;
   a.v = vr;
@@ -725,8 +726,8 @@ lar_status lar_kv_read(lar_kv* kv, const lar_kv_pages* pages, const int32_t* tab
   KvPool pool;
   KvRows kr, vr;
   if (lar_status st = check(kv, pages, table, table_cols, &pool)) return st;
-  if (lar_status st = check_rows(kv, k, "k", &kr)) return st;
-  if (lar_status st = check_rows(kv, v, "v", &vr)) return st;
+  if (lar_status st = check_rows(kv, k, kv->g.hkv, "k", &kr)) return st;
+  if (lar_status st = check_rows(kv, v, kv->g.hkv, "v", &vr)) return st;
   KvCopyArgs a = copy_args(kv, pool, table, table_cols);
   a.k = kr;
   a.v = vr;
@@ -740,7 +741,7 @@ lar_status lar_kv_attend(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_row
   KvPool pool;
   KvRows qr;
   if (lar_status st = check(kv, pages, table, table_cols, &pool)) return st;
-  if (lar_status st = check_rows(kv, q, "q", &qr)) return st;
+  if (lar_status st = check_rows(kv, q, kv->g.hq, "q", &qr)) return st;
   if (!(scale > 0.0) || !(scale < 1e30)) return fail(kv, LAR_E_ARG, "scale must be positive and finite");
   if (!out || ((uintptr_t)out & 15)) return fail(kv, LAR_E_ARG, "out must be aligned to 16 bytes");
   KvAttendArgs a{};

@@ -41,9 +41,9 @@ def lib(tmp_path_factory):
 class Handle:
     """A handle of 8 and 2 heads of 64, pages and rows that no kernel looks at."""
 
-    def __init__(self, lib, max_seqs=8, max_tokens=256):
+    def __init__(self, lib, max_seqs=8, max_tokens=256, hq=8, hkv=2):
         self.L, self.h = lib, C.c_void_p()
-        cfg = KvConfig(8, 2, 64, 1, 1, 16, max_seqs, max_tokens, 0, None)
+        cfg = KvConfig(hq, hkv, 64, 1, 1, 16, max_seqs, max_tokens, 0, None)
         assert lib.lar_kv_create(C.byref(self.h), C.byref(cfg)) == 0
         self.pages = KvPagesArg(4096, 8192, None, None, 64)
         self.q, self.kv = KvRowsArg(4096, 512, 64), KvRowsArg(4096, 128, 64)
@@ -182,6 +182,21 @@ def test_launches_carry_their_plan(lib):
     # windows of every context hide nothing, nor do sinks without a window
     assert number([1, 5], [40, 100]) == number([1, 5], [40, 100], 0, 3) == number([1, 5], [40, 100], 100, 2) == first
     assert x.close() == 0
+
+
+def test_strides_of_single_tokens_and_heads(lib):
+    """They reach no second row, so any will do; between several rows they keep these aligned."""
+    lib.stub_use(0)
+    x, one = Handle(lib), Handle(lib, hq=1, hkv=1)
+    odd_tok, odd_head = KvRowsArg(4096, 1029, 64), KvRowsArg(4096, 128, 3)
+    for h in (x, one):
+        assert h.plan([1], [40]) == 0
+        assert h.append(odd_tok) == 0 and h.read(odd_tok) == 0 and h.attend(odd_tok) == 0
+        assert h.plan([1, 1], [40, 40]) == 0
+        assert h.append(odd_tok) == -1 and h.read(odd_tok) == -1 and h.attend(odd_tok) == -1
+    assert one.append(odd_head) == 0 and one.read(odd_head) == 0 and one.attend(odd_head) == 0
+    assert x.append(odd_head) == -1 and x.read(odd_head) == -1 and x.attend(odd_head) == -1
+    assert x.close() == 0 and one.close() == 0
 
 
 # ------------------------------------------------------------------ the binding's checks
