@@ -599,8 +599,9 @@ typedef struct {
  *   the handle's stream, while another plan is the current one it does nothing and sets the
  *   sticky LAR_E_STATE.  (A plan of the same lengths, window and sinks is the same plan.)
  * lar_kv_append: k, v rows [T][n_kv_heads][head_dim] into the pages.
- * lar_kv_read: the rows of the batch's tokens from the pages into k, v.  A plan with
- *   q_len == ctx_len reads whole contexts (swap-out of a preempted sequence).
+ * lar_kv_read: the rows of the batch's tokens from the pages into k, v, of which no two may
+ *   share memory.  A plan with q_len == ctx_len reads whole contexts (swap-out of a
+ *   preempted sequence).
  * lar_kv_attend: q rows [T][n_q_heads][head_dim]; out dev [T][n_q_heads][head_dim]
  *   contiguous; lse dev [T][n_q_heads] float32 or NULL; scale > 0.  The batch's own K and V
  *   must have been appended.

@@ -490,6 +490,39 @@ lar_status check_rows(lar_kv* kv, const lar_kv_rows* r, int heads, const char* n
   return LAR_OK;
 }
 
+// Whether row (t, h) of some rows, at t * a + h * b, and row (t', h') of others with the same
+// strides, `delta` further on, have a value in common; rows of D values, T x H of them.  `self`: they
+// are the same rows, of which (t, h) = (t', h') does not count.
+bool meet(int64_t a, int64_t b, int64_t T, int64_t H, int64_t D, int64_t delta, bool self) {
+  for (int64_t h = self ? 0 : 1 - H; h < H; ++h) {
+    const __int128 v = (__int128)h * b + delta;  // plus t * a, t = 1 - T .. T - 1: how near to 0?
+    const __int128 best = a ? -v / a : 0;
+    for (int i = -1; i <= 1; ++i) {
+      const int64_t t = (int64_t)std::max<__int128>(1 - T, std::min<__int128>(T - 1, best + i));
+      if (self && h == 0 && t == 0) continue;
+      const __int128 gap = v + (__int128)t * a;
+      if (gap < D && gap > -D) return true;
+    }
+  }
+  return false;
+}
+
+// Rows that a call writes: none of them may share memory.
+lar_status check_apart(lar_kv* kv, const KvRows& k, const KvRows& v) {
+  const int64_t T = kv->n_tok, H = kv->g.hkv, D = kv->g.D;
+  const bool rows = (H == 1 || k.head >= D) && (T == 1 || k.tok >= (H > 1 ? (H - 1) * k.head : 0) + D);
+  const bool same = (H == 1 || k.head == v.head) && (T == 1 || k.tok == v.tok);
+  const auto* kp = (const char*)k.p;
+  const auto* vp = (const char*)v.p;
+  const auto end = [&](const KvRows& r) { return (T - 1) * r.tok + (H - 1) * r.head + D; };
+  const bool far = rows && same && (kp < vp ? (vp - kp) / 2 >= end(k) : (kp - vp) / 2 >= end(v));
+  if (far) return LAR_OK;  // as tensors of their own are
+  if (meet(k.tok, k.head, T, H, D, 0, true) || meet(v.tok, v.head, T, H, D, 0, true) || kp == vp ||
+      (same && meet(k.tok, k.head, T, H, D, (vp - kp) / 2, false)))
+    return fail(kv, LAR_E_ARG, "rows of k and v to be written share memory");
+  return LAR_OK;
+}
+
 KvPlanId plan_id(const lar_kv* kv) { return KvPlanId{(const uint64_t*)kv->dev, kv->plan}; }
 
 KvCopyArgs copy_args(const lar_kv* kv, const KvPool& pool, const int32_t* table, int32_t cols) {
@@ -729,6 +762,7 @@ lar_status lar_kv_read(lar_kv* kv, const lar_kv_pages* pages, const int32_t* tab
   if (lar_status st = check_rows(kv, k, kv->g.hkv, "k", &kr)) return st;
   if (lar_status st = check_rows(kv, v, kv->g.hkv, "v", &vr)) return st;
   KvCopyArgs a = copy_args(kv, pool, table, table_cols);
+  if (lar_status st = check_apart(kv, kr, vr)) return st;
   a.k = kr;
   a.v = vr;
   return launch(kv, launch_kv_read, a);

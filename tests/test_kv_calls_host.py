@@ -199,6 +199,38 @@ def test_strides_of_single_tokens_and_heads(lib):
     assert x.close() == 0 and one.close() == 0
 
 
+def test_rows_written_share_no_memory(lib):
+    """lar_kv_read's k and v: every pair of rows against an enumeration of their values."""
+    lib.stub_use(0)
+    r = np.random.RandomState(1)
+    base, bad = 1 << 20, 0
+    cases = [((2048, 128), (2048, 128), 64), ((0, 64), (128, 64), 1 << 14), ((128, 0), (128, 64), 1 << 14),
+             ((64, 64), (128, 64), 1 << 14), ((256, 64), (256, 64), 128), ((256, 64), (256, 64), 120), ((128, 64), (128, 64), 0),
+             ((64, 64 * 8), (64, 64 * 8), 1 << 14), ((128, 192), (128, 192), 1 << 14), ((-128, 64), (128, 64), 1 << 14),
+             ((128, 64), (128, 64), -1 << 14), ((128, -64), (128, 64), 1 << 14), ((1 << 40, 1 << 50), (1 << 40, 1 << 50), 64)]
+    for _ in range(400):
+        tok, head = (int(x) * 8 for x in r.randint(-40, 60, 2))
+        cases.append(((tok, head), (tok, head), int(r.randint(-60, 60)) * 8))
+    for hkv in (1, 2, 3):
+        x = Handle(lib, hq=hkv, hkv=hkv)
+        for T in (1, 4):
+            assert x.plan([T], [40]) == 0
+            for k, v, delta in cases:
+                def starts(s, at):
+                    return [at + t * s[0] + h * s[1] for t in range(T) for h in range(hkv)]
+                rows = sorted(starts(k, 0) + starts(v, delta))
+                share = any(b - a < 64 for a, b in zip(rows, rows[1:]))
+                same = (hkv == 1 or k[1] == v[1]) and (T == 1 or k[0] == v[0])
+                if not same and share and not any(b - a < 64 for s, o in ((k, 0), (v, 0))
+                                                  for a, b in zip(sorted(starts(s, o)), sorted(starts(s, o))[1:])):
+                    continue    # k and v of different strides woven into each other: the caller's
+                got = x.read(KvRowsArg(base, *k), KvRowsArg(base + 2 * delta, *v))
+                assert got == (-1 if share else 0), (hkv, T, k, v, delta)
+                bad += share
+        assert x.close() == 0
+    assert bad > 300
+
+
 # ------------------------------------------------------------------ the binding's checks
 class Tensor:
     """As much of a contiguous GPU tensor as the binding looks at."""
