@@ -10,7 +10,7 @@ import math
 
 import numpy as np
 
-from .lar import LAR_OK, LarError, _dev, load_library
+from .lar import LAR_E_STATE, LAR_OK, LarError, _dev, load_library
 
 KV_F16, KV_BF16, KV_E4M3 = 0, 1, 2
 
@@ -242,6 +242,10 @@ class PagedKV:
         if q.shape != c.shape:
             raise ValueError("q_len and ctx_len must be of one length")
         _int32s([window, sinks], "window and sinks")
+        if _raw_stream(self._index) != self._sid:   # else the library sees to it
+            with self._torch.cuda.device(self.device):
+                if self._torch.cuda.is_current_stream_capturing():
+                    raise LarError(LAR_E_STATE, "no plan under stream capture")
         self._check(self._L.lar_kv_plan(self._h, len(q), q.ctypes.data, c.ctypes.data, int(window), int(sinks)))
         self._batch(len(q), int(q.sum()))
 

@@ -3,6 +3,7 @@ device its calls go to and what they hand to the kernels.  No GPU."""
 
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 import shutil
@@ -368,3 +369,22 @@ def test_geometry_is_not_cut(monkeypatch, field, bad):
     with pytest.raises((ValueError, OverflowError)) as e:
         K.PagedKV(**dict(args, **{field: bad}), stream=Stream)
     assert field in str(e.value)
+
+
+def test_no_plan_while_another_stream_captures(binding, monkeypatch):
+    """It would not be part of the graph; the handle's own stream is the library's to check."""
+    import torch
+    from paper_2607_18253_amd import LarError
+    from paper_2607_18253_amd import kv as K
+    from paper_2607_18253_amd import lar as L
+    capturing = [True]
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    monkeypatch.setattr(torch.cuda, "device", lambda d: contextlib.nullcontext())
+    binding.plan([1, 2], [4, 4])
+    monkeypatch.setattr(K, "_raw_stream", lambda index: 7)
+    with pytest.raises(LarError) as e:
+        binding.plan([1], [4])
+    assert e.value.code == L.LAR_E_STATE and len(binding._L.calls) == 1 and binding._n_tok == 3
+    capturing[0] = False
+    binding.plan([1], [4])
+    assert len(binding._L.calls) == 2 and binding._n_tok == 1
