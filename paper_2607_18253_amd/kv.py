@@ -118,7 +118,8 @@ class PagedKV:
     current is ordered after that stream's work, and that stream after the call; a graph is
     captured on the handle's own stream (which then is not the default one).  A captured
     call belongs to the plan it was captured with: replayed while a batch of other lengths is
-    planned it does nothing, and ``sync`` raises."""
+    planned it does nothing, and ``sync`` raises.  There are no gradients: under autograd a
+    tensor that requires one is refused."""
 
     def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, *, block_size: int,
                  dtype=None, cache_dtype=None, max_seqs: int, max_tokens: int, stream=None):
@@ -185,6 +186,8 @@ class PagedKV:
     def _rows(self, t, shape, name):
         if t.dtype is not self.dtype or t.get_device() != self._index:
             raise ValueError(f"{name} must be a tensor of {self.dtype} on {self.device}")
+        if t.requires_grad:
+            self._no_gradient(name)
         if t.shape != shape:
             raise ValueError(f"{name} must be [{shape[0]}][{shape[1]}][{shape[2]}]")
         a, ref = self._args[name]
@@ -193,6 +196,10 @@ class PagedKV:
             raise ValueError(f"{name} must have contiguous rows")
         a.data = t.data_ptr()
         return ref
+
+    def _no_gradient(self, name):
+        if self._torch.is_grad_enabled():
+            raise ValueError(f"{name} requires a gradient, and these calls have none: detach it, or use torch.no_grad()")
 
     def _table(self, table):
         shape = table.shape
@@ -278,6 +285,8 @@ class PagedKV:
             to = out.data_ptr()
         else:
             to = _on(self._index, out, self.dtype, "out", n * self.head_dim)
+            if out.requires_grad:
+                self._no_gradient("out")
         t, cols = self._table(table)
         self._call(self._L.lar_kv_attend, pages, (q, out, lse, table), self._pages(pages), qa, t, cols,
                    self._scale if scale is None else float(scale), to,

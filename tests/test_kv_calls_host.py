@@ -388,3 +388,25 @@ def test_no_plan_while_another_stream_captures(binding, monkeypatch):
     capturing[0] = False
     binding.plan([1], [4])
     assert len(binding._L.calls) == 2 and binding._n_tok == 1
+
+
+def test_tensors_that_require_a_gradient_are_refused(binding):
+    """Under autograd, where the result would silently have none."""
+    import torch
+    from paper_2607_18253_amd import KvPages
+    B = torch.bfloat16
+    pages = KvPages(*(Tensor((9, 2, 16, 64), B) for _ in range(2)))
+    tab = Tensor((1, 4), torch.int32)
+    q, out, new, grad_q, grad_new = (Tensor((3, h, 64), B) for h in (8, 8, 2, 8, 2))
+    grad_q.requires_grad = grad_new.requires_grad = True
+    calls = [lambda: binding.attend(pages, grad_q, tab, out=out), lambda: binding.attend(pages, q, tab, out=grad_q),
+             lambda: binding.append(pages, grad_new, new, tab), lambda: binding.append(pages, new, grad_new, tab),
+             lambda: binding.read(pages, tab, k=new, v=grad_new)]
+    for call in calls:
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    assert not binding._L.calls
+    with torch.no_grad():
+        for call in calls:
+            call()
+    assert len(binding._L.calls) == len(calls)
