@@ -21,11 +21,13 @@ import numpy as np
 from .kv import PagedKV
 
 NAMES = "abcde"
+SHORTEST = 16  # prompt
 
 
 @dataclass
 class Instance:
-    """Geometry and scheduler limits of a model instance (lar_kv_config, lar_sched_limits)."""
+    """Geometry and scheduler limits of a model instance (lar_kv_config, lar_sched_limits); a
+    chunk_cap of 0 is none.  What runs on a GPU has a number of pages and a longest context."""
     n_q_heads: int = 32
     n_kv_heads: int = 8
     head_dim: int = 128
@@ -36,6 +38,17 @@ class Instance:
     kv_blocks: int = 18432
     block_size: int = 16
     max_ctx: int = 8192
+
+    def __post_init__(self):
+        if self.token_budget < 1 or self.max_seqs < 1 or self.chunk_cap < 0:
+            raise ValueError("token_budget and max_seqs must be positive, chunk_cap not negative")
+        if self.max_ctx < 2 or self.kv_blocks * self.block_size < min(self.max_ctx, SHORTEST):
+            raise ValueError(f"max_ctx must be at least 2, and the pages hold a context of {SHORTEST} tokens or of max_ctx")
+
+    @property
+    def chunk(self):
+        """The most tokens of a prompt in a batch."""
+        return self.chunk_cap or self.token_budget
 
 
 @dataclass
@@ -56,7 +69,7 @@ class Batch:
 
 def compose(inst: Instance, rng, n_dec: int, prompts) -> Batch:
     """A batch as the scheduler composes it: one token of each of n_dec decoding sequences,
-    then chunks of the prompts in order, at most chunk_cap each, while the budget, the
+    then chunks of the prompts in order, at most chunk_cap each where there is one, while the budget, the
     sequences and the pages last."""
     S = inst.block_size
     blocks, q, ctx = inst.kv_blocks, [], []
@@ -69,8 +82,8 @@ def compose(inst: Instance, rng, n_dec: int, prompts) -> Batch:
         ctx.append(c)
     n, left = len(q), inst.token_budget - len(q)
     for p in prompts:
-        done = int(rng.integers(0, p)) // inst.chunk_cap * inst.chunk_cap  # chunks of it before this one
-        chunk = min(p - done, inst.chunk_cap, left)
+        done = int(rng.integers(0, p)) // inst.chunk * inst.chunk  # chunks of it before this one
+        chunk = min(p - done, inst.chunk, left)
         if chunk < 1 or len(q) == inst.max_seqs or -(-(done + chunk) // S) > blocks:
             break
         blocks -= -(-(done + chunk) // S)
@@ -87,10 +100,10 @@ def batches(inst: Instance, count: int, seed: int = 0):
     out = []
     while len(out) < count:
         kind = len(out) % 3
-        n_dec = 0 if kind == 1 else int(rng.integers(1, inst.max_seqs + 1))
-        room = (inst.token_budget - n_dec) // inst.chunk_cap + 1
+        n_dec = 0 if kind == 1 else int(rng.integers(1, min(inst.max_seqs, inst.token_budget) + 1))
+        room = (inst.token_budget - n_dec) // inst.chunk + 1
         n_pre = 0 if kind == 0 else int(rng.integers(1, room + 1))
-        prompts = np.clip(np.rint(rng.lognormal(6.5, 1.0, n_pre)), 16, inst.max_ctx - 1).astype(int)
+        prompts = np.clip(np.rint(rng.lognormal(6.5, 1.0, n_pre)), SHORTEST, inst.max_ctx - 1).astype(int)
         b = compose(inst, rng, n_dec, prompts)
         if len(b.q_len):
             out.append(b)
