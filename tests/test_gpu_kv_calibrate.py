@@ -1,0 +1,59 @@
+"""What the calibration measures: the batches as a serving program runs them."""
+
+from __future__ import annotations
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_2607_18253_amd import PagedKV  # noqa: E402
+from paper_2607_18253_amd import calibrate as K  # noqa: E402
+
+REPEAT, LAYERS = 2, 3
+
+
+@pytest.fixture(params=[False, True], ids=["bf16", "e4m3"])
+def run(request, monkeypatch):
+    """(calls in order, pages) of a measurement of three batches."""
+    calls, seen = [], {}
+
+    class Noted(PagedKV):
+        def plan(self, *a, **k):
+            calls.append("plan")
+            return super().plan(*a, **k)
+
+        def append(self, pages, *a, **k):
+            calls.append(("append", pages.k.data_ptr()))
+            seen[pages.k.data_ptr()] = pages
+            return super().append(pages, *a, **k)
+
+        def attend(self, pages, *a, **k):
+            calls.append(("attend", pages.k.data_ptr()))
+            return super().attend(pages, *a, **k)
+
+    class Event(torch.cuda.Event):
+        def record(self, *a):
+            calls.append("record")
+            return super().record(*a)
+    monkeypatch.setattr(K, "PagedKV", Noted)
+    monkeypatch.setattr(torch.cuda, "Event", Event)
+    inst = K.Instance(n_q_heads=8, n_kv_heads=2, head_dim=64, layers=LAYERS, token_budget=256, max_seqs=24, chunk_cap=64,
+                      kv_blocks=600, max_ctx=512)
+    ms = K.measure(inst, K.batches(inst, 3, seed=2), e4m3=request.param, repeat=REPEAT)
+    assert (ms > 0).all()
+    return calls, list(seen.values())
+
+
+def values(t, exp):
+    x = t.float()
+    return x if exp is None else x * torch.exp2(exp.float() - 127)[..., None]
+
+
+def test_contexts_hold_values(run):
+    """Finite values of unit size, of which no two tokens' rows are alike, K and V not alike."""
+    for p in run[1]:
+        k, v = values(p.k, p.k_exp), values(p.v, p.v_exp)
+        assert torch.isfinite(k).all() and torch.isfinite(v).all()
+        assert 0.5 < k.std() < 2.0 and 0.5 < v.std() < 2.0 and abs(k.mean()) < 0.1
+        assert not torch.equal(k, v) and len(torch.unique(k.flatten(0, 2), dim=0)) > 0.9 * k.flatten(0, 2).shape[0]
