@@ -127,7 +127,8 @@ def fill(pages, generator):
 
 def measure(inst: Instance, sample, *, e4m3: bool = False, dtype=None, seed: int = 0, repeat: int = 3):
     """Milliseconds that all layers' append and attention of each batch take (the median of
-    `repeat` runs), on pages dealt out in random order."""
+    `repeat` runs), on pages dealt out in random order.  Needs memory for the pages of all
+    layers."""
     import torch
     dtype = torch.bfloat16 if dtype is None else dtype
     tokens = max(int(b.q_len.sum()) for b in sample)
@@ -136,8 +137,10 @@ def measure(inst: Instance, sample, *, e4m3: bool = False, dtype=None, seed: int
     dev, S = kv.device, inst.block_size
     g = torch.Generator(device=dev).manual_seed(seed)
     rng = np.random.default_rng(seed)
-    pages = kv.new_pages(inst.kv_blocks)
-    fill(pages, g)   # contexts of earlier batches
+    # each layer's own, as in a model: a batch's contexts are not in a cache from the layer before
+    layers = [kv.new_pages(inst.kv_blocks) for _ in range(inst.layers)]
+    for pages in layers:   # contexts of earlier batches
+        fill(pages, g)
     new = lambda heads: torch.randn((tokens, heads, inst.head_dim), device=dev, generator=g).to(dtype)
     q, k, v = new(inst.n_q_heads), new(inst.n_kv_heads), new(inst.n_kv_heads)
     out = torch.empty_like(q)
@@ -157,7 +160,7 @@ def measure(inst: Instance, sample, *, e4m3: bool = False, dtype=None, seed: int
             got = []
             for _ in range(repeat + 1):   # the first one warms up
                 start.record()
-                for _ in range(inst.layers):
+                for pages in layers:
                     kv.append(pages, k[:T], v[:T], tab)
                     kv.attend(pages, q[:T], tab, out=out[:T])
                 end.record()

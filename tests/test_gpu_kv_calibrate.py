@@ -57,3 +57,11 @@ def test_contexts_hold_values(run):
         assert torch.isfinite(k).all() and torch.isfinite(v).all()
         assert 0.5 < k.std() < 2.0 and 0.5 < v.std() < 2.0 and abs(k.mean()) < 0.1
         assert not torch.equal(k, v) and len(torch.unique(k.flatten(0, 2), dim=0)) > 0.9 * k.flatten(0, 2).shape[0]
+
+
+def test_layers_have_their_own_pages(run):
+    at = [c[1] for c in run[0] if c[0] == "attend"]
+    assert len(set(at)) == LAYERS == len(run[1])
+    assert all(len(set(at[i:i + LAYERS])) == LAYERS for i in range(0, len(at), LAYERS))
+    ends = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for p in run[1] for t in p.tensors())
+    assert all(a[1] <= b[0] for a, b in zip(ends, ends[1:]))
