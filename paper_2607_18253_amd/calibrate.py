@@ -3,7 +3,7 @@
 The simulation times a token batch by T = a + b*P + c*D + d*C + e*A (lar_instance_params):
 P prefill tokens, D decoding sequences, C their context (KV-cache reads), A the prefill
 chunks' attention.  ``measure`` composes batches as the simulated scheduler does, under an
-instance's limits, runs each layer's append and attention on a paged key/value cache
+instance's limits, plans each and runs each layer's append and attention on a paged key/value cache
 (``PagedKV``), times them, and ``fit`` turns the times into the attention's share of the
 coefficients -- d and e in full, and its part of a, b and c, to which the caller adds what
 the model's other layers take.  They go to ``LarContext.load_state`` as they are (ms).
@@ -126,7 +126,7 @@ def fill(pages, generator):
 
 
 def measure(inst: Instance, sample, *, e4m3: bool = False, dtype=None, seed: int = 0, repeat: int = 3):
-    """Milliseconds that all layers' append and attention of each batch take (the median of
+    """Milliseconds that the plan and all layers' append and attention of each batch take (the median of
     `repeat` runs), on pages dealt out in random order.  Needs memory for the pages of all
     layers."""
     import torch
@@ -156,10 +156,10 @@ def measure(inst: Instance, sample, *, e4m3: bool = False, dtype=None, seed: int
                 table[s, :n] = free[at[s]:at[s + 1]]
             tab = torch.from_numpy(table).to(dev)
             T = int(b.q_len.sum())
-            kv.plan(b.q_len, b.ctx_len)
             got = []
             for _ in range(repeat + 1):   # the first one warms up
                 start.record()
+                kv.plan(b.q_len, b.ctx_len)
                 for pages in layers:
                     kv.append(pages, k[:T], v[:T], tab)
                     kv.attend(pages, q[:T], tab, out=out[:T])

@@ -65,3 +65,10 @@ def test_layers_have_their_own_pages(run):
     assert all(len(set(at[i:i + LAYERS])) == LAYERS for i in range(0, len(at), LAYERS))
     ends = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for p in run[1] for t in p.tensors())
     assert all(a[1] <= b[0] for a, b in zip(ends, ends[1:]))
+
+
+def test_a_batch_is_timed_with_its_plan(run):
+    calls = [c if isinstance(c, str) else c[0] for c in run[0]]
+    one = ["record", "plan"] + ["append", "attend"] * LAYERS + ["record"]
+    timed = "|".join(calls)
+    assert timed.count("|".join(one)) == 3 * (REPEAT + 1)
