@@ -675,10 +675,10 @@ __device__ __forceinline__ void narrow(const KvAttendArgs& A, char* lds, int run
   constexpr int I = kNarrowKeys / St::kStep;
   const int n = lane & 31, h = lane >> 5;
   const int r0 = lane / St::kChunks, c = lane % St::kChunks;
-  const int e = plan_at(A.narrow_at, run + 1);
+  int e = plan_at(A.narrow_at, run + 1);
   bool lost = false;  // a page outside the pool
   int x = plan_at(A.narrow_at, run);
-  if (other_plan(A)) return;
+  if (other_plan(A)) e = x;  // nothing to do
   for (; x < e; ++x) {
     const KvSeg s = plan_at(A.narrow, x);
     s16x8 q[D / 16];
@@ -783,10 +783,11 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_kv_wide(KvAttendArgs A) 
     if (run < A.n_narrow) narrow<BF, F8, D>(A, lds + wave * kNarrow, run, lane);
     return;
   }
-  const int run = run_of(blockIdx.x, A.n_wide), e = plan_at(A.wide_at, run + 1);
+  const int run = run_of(blockIdx.x, A.n_wide);
+  int e = plan_at(A.wide_at, run + 1);
   bool lost = false;  // a page outside the pool
   int x = plan_at(A.wide_at, run);
-  if (other_plan(A)) return;
+  if (other_plan(A)) e = x;  // nothing to do
   // the current stretch, its queries, and its first keys on their way
   KvSeg s;
   s16x8 q[D / 16];

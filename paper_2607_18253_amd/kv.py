@@ -100,14 +100,6 @@ class KvPages:
     def tensors(self):
         return [t for t in self._tensors if t is not None]
 
-    def _now(self):
-        """The pages as an argument, where the tensors are now."""
-        k, v, ke, ve = self._ptr
-        at = self._at
-        if k() != at[0] or v() != at[1] or (ke is not None and (ke() != at[2] or ve() != at[3])):
-            self._look()
-        return self._ref
-
 
 class PagedKV:
     """A paged key/value cache's geometry and the plan of the current token batch; see
@@ -177,11 +169,14 @@ class PagedKV:
         self.close()
 
     def _pages(self, pages):
-        ref = pages._now()
+        k, v, ke, ve = pages._ptr
+        at = pages._at
+        if k() != at[0] or v() != at[1] or (ke is not None and (ke() != at[2] or ve() != at[3])):
+            pages._look()
         if pages._kind != self._kind:
             raise ValueError(f"pages must be [n_blocks][{self.n_kv}][{self.block_size}][{self.head_dim}] "
                              f"of {self.cache_dtype} on {self.device}")
-        return ref
+        return pages._ref
 
     def _rows(self, t, shape, name):
         if t.dtype is not self.dtype or t.get_device() != self._index:
@@ -205,7 +200,9 @@ class PagedKV:
         shape = table.shape
         if len(shape) != 2 or shape[0] < self._n_seq:
             raise ValueError(f"table must have {self._n_seq} rows")
-        return _on(self._index, table, self._int32, "table"), shape[1]
+        if table.dtype is not self._int32 or table.get_device() != self._index or not table.is_contiguous():
+            _on(self._index, table, self._int32, "table")
+        return table.data_ptr(), shape[1]
 
     def _call(self, f, pages, tensors, *args):
         """f(handle, *args) in order with the current stream."""
