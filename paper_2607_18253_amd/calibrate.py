@@ -214,7 +214,7 @@ def main(argv=None):
     with LarContext(1, 1, max_seqs_cap=inst.max_seqs, queue_cap=16, max_prompt=inst.max_ctx) as ctx:
         none = np.zeros(0, np.int32)
         ctx.load_state(a=c[:1], b=c[1:2], c=c[2:3], d=c[3:4], e=c[4:5], budget=[inst.token_budget],
-                       max_seqs=[inst.max_seqs], col=[0], offsets=[0, 0], rem_prefill=none, rem_decode=none,
+                       max_seqs=[min(inst.max_seqs, inst.token_budget)], col=[0], offsets=[0, 0], rem_prefill=none, rem_decode=none,
                        context=none, clock_ms=[0.0])
         prompts = [p for p in (128, 1024, 8191) if p < inst.max_ctx]
         ttft, _ = ctx.estimate(torch.tensor(prompts, dtype=torch.int32, device="cuda"), 0.0)

@@ -72,3 +72,10 @@ def test_a_batch_is_timed_with_its_plan(run):
     one = ["record", "plan"] + ["append", "attend"] * LAYERS + ["record"]
     timed = "|".join(calls)
     assert timed.count("|".join(one)) == 3 * (REPEAT + 1)
+
+
+def test_more_sequences_than_budget(capsys):
+    """The command on an instance whose batches cannot hold a token of every sequence."""
+    c = K.main(["--layers", "2", "--token-budget", "128", "--max-seqs", "256", "--kv-blocks", "2000", "--max-ctx", "2048",
+                "--batches", "9"])
+    assert (c >= 0).all() and "1024-token prompt" in capsys.readouterr().out
