@@ -30,7 +30,8 @@
 // weight that outweighs the others; the log of the sum, where it is asked for, is that of the
 // unrounded ones.  f16 has no values below 2^-24, and from 2^-14 down fewer bits: a row's weights
 // are scaled so that its largest is 2^11 to 2^15, and what a weight loses at that end is 2^-36
-// of the largest at most, 2^-17 of the result for 2^19 keys.
+// of the largest at most, 2^-17 of the result for 2^19 keys.  (With largest weights of 1 the
+// share of 32767 keys that weigh 2^-23 to 2^-26 of one came out wrong by up to all of it.)
 #include "../../include/lar.h"
 #include "kv_device.h"
 #include "kv_words.h"
