@@ -553,6 +553,27 @@ lar_status lar_estimate_lps(lar_ctx *ctx, const lar_lps_params *params, int32_t 
  * hold; an infinity in v makes the rows that see it infinite, or NaN where both signs meet
  * and where, for a chunk, its weight is too small for dtype.
  * lse = m + ln(sum_j exp(s_j - m)) joins parts of a context.
+ *
+ * Trees.  Drafted tokens of a sequence may form trees (lar_kv_plan_tree): each new token has a
+ * parent among those before it, or follows the context.  They are appended and read at their
+ * positions, like any new tokens.  A token's place is the number of the context's and the tree's
+ * tokens that it follows: max(0, ctx_len - q_len) and one for each ancestor.  It sees those keys
+ * and itself, under a window W the ones whose places are > its own - W or < sinks.  In a chain,
+ * where each token follows the one before, this is what any token sees.
+ *
+ * Weights.  lar_kv_weigh adds up what each row of the cache got of the attention of a batch, in
+ * weights, dev [n_blocks][n_kv_heads][block_size] float32, the caller's, for each layer:
+ *     weights_j = before_j + sum_r exp(s_rj - lse_r)
+ * over the batch's tokens r that see j and the heads of the group, with before_j = 0 for the
+ * batch's new tokens.  A row r whose lse is -infinity adds nothing.
+ *
+ * Budgets.  lar_kv_select names, for every sequence of the plan (also those without new tokens)
+ * and kv head, the rows of its context to keep: all ctx_len if these are within the budget, else
+ * the first `first`, the last `last`, and of the others those of the largest weights (of equal
+ * ones the lowest positions; NaN is above all numbers, -0 is 0), `budget` in all.
+ * lar_kv_keep moves the rows of such lists to the front of the context, or those of a tree's
+ * accepted path to where the tree starts.  Heads then hold rows of different tokens in one place:
+ * windows, and the first and last rows of later selections, go by the places.
  */
 typedef struct lar_kv lar_kv;
 
@@ -605,6 +626,26 @@ typedef struct {
  * lar_kv_attend: q rows [T][n_q_heads][head_dim]; out dev [T][n_q_heads][head_dim]
  *   contiguous; lse dev [T][n_q_heads] float32 or NULL; scale > 0.  The batch's own K and V
  *   must have been appended.
+ * lar_kv_plan_tree: lar_kv_plan with host parents [T], copied: of each new token the number
+ *   of its parent among its sequence's new tokens, or -1; a parent comes before its children
+ *   and is no padding row (whose own parents are not looked at).  A tree, that is a sequence whose
+ *   tokens do not all follow one another, has at most 1024 tokens, and the trees of a batch 16384
+ *   together (LAR_E_ARG, LAR_E_CAPACITY).
+ * lar_kv_weigh: q and scale as for lar_kv_attend, and lse what it gave.  before: the
+ *   weights so far, weights itself or memory apart from it; the rows of the sequences with
+ *   new tokens are written, all others stay as they are.  Two sequences with new tokens may not
+ *   share pages here.  Not for a plan with trees (LAR_E_STATE).
+ * lar_kv_select: first + last <= budget.  rows dev [n_seqs][n_kv_heads][budget]: the positions
+ *   to keep in ascending order, then -1.  n_blocks: of the weights.
+ * lar_kv_keep: rows dev [n_seqs][n_kv_heads][n_rows], or with per_head 0 [n_seqs][n_rows] for all
+ *   heads: positions in ascending order, the first -1 ends a list.  Row rows[i] goes to place i;
+ *   with `fresh` both count from the sequence's first new token.  K and V, the exponents of an
+ *   e4m3 cache and, if given, the weights go along.  The place is that of to_table, dev
+ *   [n_seqs][to_cols], or of table itself (NULL); a page of to_table is either the one that
+ *   table has in that column or one that table has in no sequence of the batch, and no page that
+ *   is written to belongs to two sequences.  What is at the places past a list stays.  Lists that
+ *   do not ascend or leave the context set the sticky LAR_E_STATE; nothing is moved for an entry
+ *   that does, and what the places of such a list hold is undefined.
  * lar_kv_sync: synchronise the stream; the sticky device error, if any.
  * Each call works on the handle's stream, allocates nothing (but create) and does not
  * wait (but plan, as said, and sync).  A handle is not thread-safe; calls of one handle
@@ -622,6 +663,16 @@ lar_status lar_kv_read(lar_kv *kv, const lar_kv_pages *pages, const int32_t *tab
 lar_status lar_kv_attend(lar_kv *kv, const lar_kv_pages *pages, const lar_kv_rows *q,
                          const int32_t *table, int32_t table_cols, double scale, void *out,
                          float *lse);
+lar_status lar_kv_plan_tree(lar_kv *kv, int32_t n_seqs, const int32_t *q_len, const int32_t *ctx_len,
+                            const int32_t *parents, int32_t window, int32_t sinks);
+lar_status lar_kv_weigh(lar_kv *kv, const lar_kv_pages *pages, const lar_kv_rows *q,
+                        const int32_t *table, int32_t table_cols, double scale, const float *lse,
+                        const float *before, float *weights);
+lar_status lar_kv_select(lar_kv *kv, const float *weights, int64_t n_blocks, const int32_t *table,
+                         int32_t table_cols, int32_t budget, int32_t first, int32_t last, int32_t *rows);
+lar_status lar_kv_keep(lar_kv *kv, const lar_kv_pages *pages, const int32_t *table, int32_t table_cols,
+                       const int32_t *to_table, int32_t to_cols, const int32_t *rows, int32_t n_rows,
+                       int32_t per_head, int32_t fresh, float *weights);
 lar_status lar_kv_sync(lar_kv *kv);
 
 /* Synchronise the stream; return the sticky device error, if any. */

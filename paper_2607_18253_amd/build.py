@@ -20,10 +20,14 @@ SOURCES = [os.path.join(CSRC, "sfs_kernels.hip"), os.path.join(CSRC, "sfs_limits
            os.path.join(CSRC, "sfs_lps.hip"),
            os.path.join(CSRC, "lar_api.cpp"), os.path.join(CSRC, "lar_noalloc.hip"),
            os.path.join(CSRC, "lar_board.cpp"), os.path.join(CSRC, "kv_pages.hip"),
-           os.path.join(CSRC, "kv_attend.hip"), os.path.join(CSRC, "kv_api.cpp")]
+           os.path.join(CSRC, "kv_attend.hip"), os.path.join(CSRC, "kv_tree.hip"),
+           os.path.join(CSRC, "kv_weigh.hip"), os.path.join(CSRC, "kv_select.hip"),
+           os.path.join(CSRC, "kv_keep.hip"), os.path.join(CSRC, "kv_api.cpp"),
+           os.path.join(CSRC, "kv_rows_api.cpp")]
 HEADERS = [os.path.join(CSRC, "sfs_device.h"), os.path.join(CSRC, "sfs_launch.h"),
            os.path.join(CSRC, "sfs_limits.h"), os.path.join(CSRC, "sfs_route.h"), os.path.join(CSRC, "sfs_walk.h"),
-           os.path.join(CSRC, "kv_device.h"), os.path.join(CSRC, "kv_words.h"),
+           os.path.join(CSRC, "kv_device.h"), os.path.join(CSRC, "kv_words.h"), os.path.join(CSRC, "kv_attend.h"),
+           os.path.join(CSRC, "kv_handle.h"),
            os.path.join(ROOT, "include", "lar.h")]
 ARCH = "gfx950"
 

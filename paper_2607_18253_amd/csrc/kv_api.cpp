@@ -9,8 +9,6 @@
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <cstring>
 #include <functional>
 #include <new>
@@ -18,100 +16,11 @@
 #include <vector>
 
 #include "../../include/lar.h"
-#include "kv_device.h"
+#include "kv_handle.h"
 
 using namespace lar;
 
 namespace {
-
-constexpr int kStages = 2;  // pinned copies of a plan: one may be on its way while the next is written
-
-size_t up(size_t x) { return (x + 255) & ~size_t(255); }
-
-// Byte offsets of a plan's arrays, the same on the host and on the device, after its number.
-struct Layout {
-  size_t tok = up(sizeof(uint64_t)), narrow = 0, wide = 0, narrow_at = 0, wide_at = 0, join = 0, end = 0;
-  Layout() = default;
-  Layout(int64_t n_tok, int64_t n_narrow, int64_t n_wide, int64_t waves, int64_t groups, int64_t n_join) {
-    narrow = up(tok + sizeof(KvTok) * n_tok);
-    wide = up(narrow + sizeof(KvSeg) * n_narrow);
-    narrow_at = up(wide + sizeof(KvSeg) * n_wide);
-    wide_at = up(narrow_at + sizeof(int32_t) * (waves + 1));
-    join = up(wide_at + sizeof(int32_t) * (groups + 1));
-    end = up(join + sizeof(KvJoin) * n_join);
-  }
-};
-
-}  // namespace
-
-struct lar_kv {
-  lar_kv_config cfg{};
-  KvGeom g{};
-  hipStream_t stream = nullptr;
-  int device = 0, cus = 0;
-  int waves = 0, groups = 0;  // of the narrow and the wide kernel at most
-  size_t cap = 0;             // bytes of a plan at most
-  Layout lay;                 // of the current plan
-  char* dev = nullptr;
-  char* pinned[kStages] = {};
-  hipEvent_t done[kStages] = {};
-  bool used[kStages] = {};
-  int stage = 0;
-  float *narrow_o = nullptr, *wide_o = nullptr;
-  float4 *narrow_ml = nullptr, *wide_ml = nullptr;
-  int32_t* err = nullptr;
-  // the plan
-  bool planned = false;
-  uint64_t plan = 0;  // its number
-  int32_t n_seq = 0, n_tok = 0, max_pages = 0, window = 0, sinks = 0;
-  int32_t n_narrow = 0, n_wide = 0, n_join = 0, join_rows = 0, most_parts = 0;
-  lar_status sticky = LAR_OK;
-  std::string msg;
-};
-
-namespace {
-
-lar_status fail(lar_kv* kv, lar_status code, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
-  va_end(ap);
-  try {
-    kv->msg = buf;
-  } catch (...) {
-  }
-  return code;
-}
-
-#define KV_TRY(kv, expr)                                                           \
-  do {                                                                             \
-    hipError_t e_ = (expr);                                                        \
-    if (e_ != hipSuccess) return fail(kv, LAR_E_HIP, "%s: %s", #expr, hipGetErrorString(e_)); \
-  } while (0)
-
-// The handle's device is the current one while this lives: the null stream, and calls without
-// a stream, go to the current device.
-class OnDevice {
- public:
-  explicit OnDevice(const lar_kv* kv) {
-    int now = 0;
-    status_ = hipGetDevice(&now);
-    if (status_ != hipSuccess || now == kv->device) return;
-    status_ = hipSetDevice(kv->device);
-    if (status_ == hipSuccess) before_ = now;
-  }
-  ~OnDevice() {
-    if (before_ >= 0) (void)hipSetDevice(before_);
-  }
-  OnDevice(const OnDevice&) = delete;
-  OnDevice& operator=(const OnDevice&) = delete;
-  hipError_t status() const { return status_; }
-
- private:
-  int before_ = -1;
-  hipError_t status_ = hipSuccess;
-};
 
 // A plan's number, made of all that a plan follows from, so that equal batches have equal plans
 // with equal numbers.  Each step maps the numbers one to one: batches that differ in one sequence's
@@ -124,16 +33,14 @@ struct PlanId {
   }
 };
 
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-// The key tiles (of K keys) that the tokens p0 .. p0 + n - 1 of a sequence see: tiles
-// [0, ns), then from fw on; their number.
-int key_tiles(int64_t p0, int n, int K, int window, int sinks, int* ns, int* fw) {
+// The key tiles (of K keys) that the tokens p0 .. p0 + n - 1 of a sequence see, whose windows end
+// with position `low` at least: tiles [0, ns), then from fw on; their number.
+int key_tiles(int64_t p0, int n, int K, int window, int sinks, int64_t low, int* ns, int* fw) {
   const int64_t last = p0 + n - 1;
   *ns = *fw = 0;
   if (last < 0) return 0;
   const int64_t all = last / K + 1;
-  const int64_t lo = window ? std::max<int64_t>(0, std::max<int64_t>(p0, 0) - window + 1) : 0;
+  const int64_t lo = window ? std::max<int64_t>(0, std::max<int64_t>(low, 0) - window + 1) : 0;
   const int64_t first = lo / K;
   const int64_t head = std::min<int64_t>(ceil_div(sinks, K), first);  // tiles of sinks before the window
   *ns = (int)head;
@@ -455,41 +362,6 @@ int split(const std::vector<Tile>& narrow, const std::vector<Tile>& wide, int gr
 
 bool type16(int32_t t) { return t == LAR_KV_F16 || t == LAR_KV_BF16; }
 
-lar_status ready(lar_kv* kv) {
-  if (!kv) return LAR_E_ARG;
-  if (kv->sticky != LAR_OK) return kv->sticky;
-  if (!kv->planned) return fail(kv, LAR_E_STATE, "no token batch planned (call lar_kv_plan)");
-  return LAR_OK;
-}
-
-// The arguments that append, read and attend share.
-lar_status check(lar_kv* kv, const lar_kv_pages* pages, const int32_t* table, int32_t cols, KvPool* pool) {
-  if (lar_status st = ready(kv)) return st;
-  if (!pages || !pages->k || !pages->v) return fail(kv, LAR_E_ARG, "null pages");
-  if (!table) return fail(kv, LAR_E_ARG, "null block table");
-  if (kv->g.cache == kKvE4m3 && (!pages->k_exp || !pages->v_exp))
-    return fail(kv, LAR_E_ARG, "an e4m3 cache needs k_exp and v_exp");
-  if (((uintptr_t)pages->k | (uintptr_t)pages->v) & 15)
-    return fail(kv, LAR_E_ARG, "pages must be aligned to 16 bytes");
-  if (pages->n_blocks < 1 ||
-      pages->n_blocks > ((((int64_t)1 << 32) - 1) >> kv->g.sh) / kv->g.hkv)
-    return fail(kv, LAR_E_ARG, "n_blocks must be in 1 .. (2^32 - 1) / (block_size * n_kv_heads)");
-  if (cols < kv->max_pages)
-    return fail(kv, LAR_E_ARG, "block table has %d columns, the planned contexts need %d", cols, kv->max_pages);
-  *pool = KvPool{pages->k, pages->v, pages->k_exp, pages->v_exp, (uint32_t)pages->n_blocks};
-  return LAR_OK;
-}
-
-// Rows [T][heads][head_dim] with 16-byte rows.  A stride between things of which there is one
-// does not matter.
-lar_status check_rows(lar_kv* kv, const lar_kv_rows* r, int heads, const char* name, KvRows* out) {
-  if (!r || !r->data) return fail(kv, LAR_E_ARG, "null %s", name);
-  if (((uintptr_t)r->data & 15) || (kv->n_tok > 1 && (r->tok_stride & 7)) || (heads > 1 && (r->head_stride & 7)))
-    return fail(kv, LAR_E_ARG, "%s: every row must be aligned to 16 bytes", name);
-  *out = KvRows{r->data, r->tok_stride, r->head_stride};
-  return LAR_OK;
-}
-
 // Whether row (t, h) of some rows, at t * a + h * b, and row (t', h') of others with the same
 // strides, `delta` further on, have a value in common; rows of D values, T x H of them.  `self`: they
 // are the same rows, of which (t, h) = (t', h') does not count.
@@ -523,8 +395,6 @@ lar_status check_apart(lar_kv* kv, const KvRows& k, const KvRows& v) {
   return LAR_OK;
 }
 
-KvPlanId plan_id(const lar_kv* kv) { return KvPlanId{(const uint64_t*)kv->dev, kv->plan}; }
-
 KvCopyArgs copy_args(const lar_kv* kv, const KvPool& pool, const int32_t* table, int32_t cols) {
   KvCopyArgs a{};
   a.plan = plan_id(kv);
@@ -538,23 +408,264 @@ KvCopyArgs copy_args(const lar_kv* kv, const KvPool& pool, const int32_t* table,
   return a;
 }
 
-// A launch on the handle's device and stream.
-template <class Args>
-lar_status launch(lar_kv* kv, hipError_t (*f)(const Args&, hipStream_t), const Args& a) {
-  const OnDevice device(kv);
-  KV_TRY(kv, device.status());
-  const hipError_t e = f(a, kv->stream);
-  return e == hipSuccess ? LAR_OK : fail(kv, LAR_E_HIP, "launch: %s", hipGetErrorString(e));
-}
-
 void release(lar_kv* kv) {
   for (void* p : {(void*)kv->dev, (void*)kv->narrow_o, (void*)kv->wide_o, (void*)kv->narrow_ml,
                   (void*)kv->wide_ml, (void*)kv->err})
     if (p) (void)hipFree(p);
-  for (int i = 0; i < kStages; ++i) {
+  for (int i = 0; i < kKvStages; ++i) {
     if (kv->pinned[i]) (void)hipHostFree(kv->pinned[i]);
     if (kv->done[i]) (void)hipEventDestroy(kv->done[i]);
   }
+}
+
+// First block of 32 keys that a token's bits are about, and words of its bits, in a tree of n tokens.
+int tree_block(int32_t ctx, int32_t n) { return std::max(0, ctx - n) >> 5; }
+int tree_words(int32_t ctx, int32_t n) { return ((ctx - 1) >> 5) - tree_block(ctx, n) + 1; }
+
+// Tokens of trees in a plan at most, the words of their records, and the query tiles: with four
+// waves or more a tree may have several.
+int64_t tree_tokens(const lar_kv_config& cfg) { return std::min(cfg.max_tokens, kTreeTokens); }
+int64_t tree_room(const lar_kv_config& cfg) { return tree_tokens(cfg) * (kMaxTree / 32 + 3); }
+int64_t tree_tiles(const lar_kv_config& cfg, const KvGeom& g) {
+  return (std::min<int64_t>(cfg.max_seqs, tree_tokens(cfg)) + tree_tokens(cfg) / (128 / g.G)) * g.hkv;
+}
+
+// The trees of a batch: which sequences have one, and each token's place.
+struct Trees {
+  std::vector<int32_t> words;  // of each sequence: words of a token's bits, 0: no tree
+  std::vector<int32_t> place;  // of each new token
+  int64_t room = 0;            // words of all records
+  int64_t tokens = 0;          // of all trees
+  int32_t most = 0;            // tokens of the largest
+};
+
+// Waves of a workgroup of the tree kernel, each with 32 rows of a query tile: as many as the largest
+// tree has rows for.
+constexpr int kTreeWavesPerCu = 8;
+int tree_waves(const Trees& t, const KvGeom& g) {
+  int w = 1;
+  while (w < 8 && 32 * w < t.most * g.G) w *= 2;
+  return w;
+}
+int tree_keys(int waves) { return waves == 1 ? 32 : 64; }
+
+int tree_least(const std::vector<Tile>&, const KvGeom&) { return 2; }
+
+// Takes the parents in; a sequence whose tokens follow one another has no tree.
+lar_status take_parents(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t* ctx_len, int64_t T,
+                        const int32_t* parents, Trees* t) {
+  t->words.assign(n_seqs, 0);
+  t->place.resize(T);
+  int64_t q0 = 0;
+  for (int s = 0; s < n_seqs; q0 += q_len[s], ++s) {
+    const int32_t n = q_len[s], *up = parents + q0;
+    int32_t* place = t->place.data() + q0;
+    const int64_t base = (int64_t)ctx_len[s] - n;
+    const int32_t r0 = (int32_t)std::max<int64_t>(0, -base);  // the first token that is no padding
+    bool chain = true;
+    for (int32_t r = 0; r < n && r < r0; ++r) place[r] = -1;
+    for (int32_t r = r0; r < n; ++r) {
+      if (up[r] != -1 && (up[r] < r0 || up[r] >= r))
+        return fail(kv, LAR_E_ARG, "sequence %d: new token %d has parent %d, which is no earlier one", s, r, up[r]);
+      place[r] = up[r] < 0 ? (int32_t)(base + r0) : place[up[r]] + 1;
+      chain &= up[r] == (r == r0 ? -1 : r - 1);
+    }
+    if (chain) continue;
+    if (n > kMaxTree) return fail(kv, LAR_E_ARG, "sequence %d: a tree of %d tokens, at most %d", s, n, kMaxTree);
+    t->words[s] = tree_words(ctx_len[s], n);
+    t->room += (int64_t)n * (t->words[s] + 1);
+    t->tokens += n;
+    t->most = std::max(t->most, n);
+  }
+  if (t->tokens > tree_tokens(kv->cfg) || t->room > tree_room(kv->cfg))
+    return fail(kv, LAR_E_CAPACITY, "trees of %lld tokens, at most %lld", (long long)t->tokens,
+                (long long)tree_tokens(kv->cfg));
+  return LAR_OK;
+}
+
+// A tree's records: each token's place, and which keys it sees: its parent's, or the context's, and
+// itself, less what a window takes away, which is more the further a token is from the root.
+void write_tree(const int32_t* parents, const int32_t* place, int32_t n, int32_t ctx, int words, int window, int sinks,
+                uint32_t* to) {
+  const int step = words + 1;
+  const int64_t base = (int64_t)ctx - n, first = 32 * (int64_t)tree_block(ctx, n);
+  for (int32_t r = 0; r < n; ++r, to += step) {
+    memset(to, 0, sizeof(uint32_t) * step);
+    if (base + r < 0) continue;  // a padding row
+    to[0] = (uint32_t)place[r];
+    const auto set = [&](int64_t j) { to[1 + (j - first) / 32] |= 1u << ((j - first) % 32); };
+    if (parents[r] >= 0)
+      memcpy(to + 1, to + 1 - (int64_t)(r - parents[r]) * step, sizeof(uint32_t) * words);
+    else
+      for (int64_t j = first; j < base; ++j) set(j);
+    set(base + r);
+    if (!window) continue;
+    for (int w = 0; w < words; ++w)
+      for (uint32_t x = to[1 + w]; x; x &= x - 1) {
+        const int64_t j = first + 32 * w + __builtin_ctz(x), p = j < base ? j : place[j - base];
+        if (p <= place[r] - window && p >= sinks) to[1 + w] &= ~(x & -x);
+      }
+  }
+}
+
+lar_status plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t* ctx_len, const int32_t* parents,
+                int32_t window, int32_t sinks) {
+  if (n_seqs < 0 || n_seqs > kv->cfg.max_seqs)
+    return fail(kv, LAR_E_ARG, "%d sequences, at most %d", n_seqs, kv->cfg.max_seqs);
+  if (n_seqs && (!q_len || !ctx_len)) return fail(kv, LAR_E_ARG, "null lengths");
+  if (window < 0 || sinks < 0) return fail(kv, LAR_E_ARG, "negative window or sinks");
+  const OnDevice device(kv);
+  KV_TRY(kv, device.status());
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (kv->stream) KV_TRY(kv, hipStreamIsCapturing(kv->stream, &capture));
+  if (capture != hipStreamCaptureStatusNone) return fail(kv, LAR_E_STATE, "no plan under stream capture");
+  int64_t T = 0, pages = 0, all_pages = 0;
+  int32_t longest = 0, all_longest = 0;
+  for (int s = 0; s < n_seqs; ++s) {
+    if (q_len[s] < 0 || ctx_len[s] < 0 || ctx_len[s] > 1 << 30)
+      return fail(kv, LAR_E_ARG, "sequence %d: %d new tokens, context %d", s, q_len[s], ctx_len[s]);
+    T += q_len[s];
+    all_longest = std::max(all_longest, ctx_len[s]);
+    if (q_len[s]) longest = std::max(longest, ctx_len[s]);
+    if (q_len[s]) pages = std::max<int64_t>(pages, ceil_div(ctx_len[s], (int64_t)1 << kv->g.sh));
+  }
+  all_pages = ceil_div(all_longest, (int64_t)1 << kv->g.sh);
+  if (T > kv->cfg.max_tokens)
+    return fail(kv, LAR_E_ARG, "%lld new tokens, at most %d", (long long)T, kv->cfg.max_tokens);
+  // A window of every context hides nothing.  The kernels subtract a shorter one, and then a
+  // key of a context, from a position: all within 2^30, so within 32 bits.
+  if (window >= longest) window = 0;
+  if (!window) sinks = 0;
+  Trees trees;
+  try {
+    if (parents)
+      if (lar_status st = take_parents(kv, n_seqs, q_len, ctx_len, T, parents, &trees)) return st;
+  } catch (const std::bad_alloc&) {
+    return fail(kv, LAR_E_CAPACITY, "out of host memory");
+  }
+  PlanId id;
+  id.add((uint32_t)window, (uint32_t)sinks);
+  for (int s = 0; s < n_seqs; ++s) id.add((uint32_t)q_len[s], (uint32_t)ctx_len[s]);
+  if (trees.most) {
+    int64_t q0 = 0;
+    for (int s = 0; s < n_seqs; q0 += q_len[s], ++s)
+      for (int r = 0; trees.words[s] && r < q_len[s]; ++r) id.add((uint32_t)s, (uint32_t)parents[q0 + r]);
+  }
+  // the copy that last left this buffer is done before it is written again
+  const int b = kv->stage;
+  if (kv->used[b]) KV_TRY(kv, hipEventSynchronize(kv->done[b]));
+  char* p = kv->pinned[b];
+  const KvGeom& g = kv->g;
+  KvTok* tok = (KvTok*)(p + KvLayout().tok);
+  int32_t n_narrow = 0, n_wide = 0, n_join = 0, join_rows = 0, most_parts = 0;
+  int32_t n_tree = 0, n_tree_waves = 0, n_tree_join = 0, tree_join_rows = 0, tree_most_parts = 0;
+  int64_t blocks = 0;
+  kv->planned = false;
+  try {
+    std::vector<Tile> narrow, wide, none, tree;
+    const int waves = tree_waves(trees, g), runs = kv->cus * kTreeWavesPerCu / waves;
+    const int nt = kNarrowRows / g.G, wt = kWideRows / g.G;
+    int64_t q0 = 0;
+    for (int s = 0; s < n_seqs; ++s) {
+      const int n = q_len[s];
+      const int64_t p0 = (int64_t)ctx_len[s] - n;
+      for (int r = 0; r < n; ++r) tok[q0 + r] = KvTok{s, (int32_t)(p0 + r)};
+      if (!n) continue;
+      const bool has = trees.most && trees.words[s], small = !has && n <= nt;
+      const int per = has ? 32 * waves / g.G : small ? n : wt;
+      for (int h = 0; h < g.hkv; ++h)
+        for (int r = 0; r < n; r += per) {
+          Tile t{};
+          t.s.q0 = (int32_t)(q0 + r);
+          t.s.ntok = std::min(per, n - r);
+          t.s.p0 = (int32_t)(p0 + r);
+          t.s.head = h;
+          t.s.seq = s;
+          int64_t low = p0 + r;
+          if (has && window) {  // the least place, and all of the tree
+            for (int i = 0; i < t.s.ntok; ++i) low = std::min<int64_t>(low, trees.place[q0 + r + i]);
+            low = std::min(low, p0 + window - 1);
+          }
+          const int K = has ? tree_keys(waves) : small ? kNarrowKeys : kWideKeys;
+          t.tiles = key_tiles(p0 + r, t.s.ntok, K, window, sinks, low, &t.s.ns, &t.s.fw);
+          (has ? tree : !t.tiles ? none : small ? narrow : wide).push_back(t);
+        }
+      q0 += n;
+    }
+    // tiles without keys have only their zeros to write: either kernel will do, if they fit
+    for (const Tile& t : none) (t.s.ntok <= nt && wide.empty() ? narrow : wide).push_back(t);
+    const int64_t nn = (int64_t)narrow.size(), nw = (int64_t)wide.size();
+    const KvLayout L(T, nn ? nn + kv->waves : 0, nw ? nw + 2 * kv->groups : 0, kv->waves, kv->groups,
+                   std::min<int64_t>(nn, kv->waves) + std::min<int64_t>(nw, kv->groups) * (kWideRows / 32) + kJoins8,
+                   n_seqs, trees.room, tree.empty() ? 0 : (int64_t)tree.size() + runs, tree.empty() ? 0 : runs,
+                   tree.empty() ? 0 : runs * waves + kJoins8);
+    if (L.end > kv->cap) return fail(kv, LAR_E_CAPACITY, "plan of %zu bytes, room for %zu", L.end, kv->cap);
+    kv->lay = L;
+    Joins join{g.G};
+    const int groups = nn ? split(narrow, wide, kv->groups, g) : kv->groups;
+    cut(narrow, nw ? (kv->groups - groups) * kWideWaves : kv->waves, narrow_least(narrow, g), (KvSeg*)(p + L.narrow),
+        (int32_t*)(p + L.narrow_at), &n_narrow, &join);
+    deal(wide, groups, g, (KvSeg*)(p + L.wide), (int32_t*)(p + L.wide_at), &n_wide, &join);
+    n_join = join.write((KvJoin*)(p + L.join), &join_rows);
+    most_parts = join.most;
+    if (!tree.empty()) {
+      Joins parts{g.G};
+      cut(tree, runs, tree_least(tree, g), (KvSeg*)(p + L.tree), (int32_t*)(p + L.tree_at), &n_tree, &parts);
+      for (KvJoin& j : parts.tiles) j.wide = waves > 1;
+      n_tree_join = parts.write((KvJoin*)(p + L.tree_join), &tree_join_rows);
+      tree_most_parts = parts.most;
+      n_tree_waves = waves;
+    }
+    KvSpan* span = (KvSpan*)(p + L.spans);
+    int64_t rec = 0;
+    q0 = 0;
+    for (int s = 0; s < n_seqs; q0 += q_len[s], ++s) {
+      KvSpan x{(int32_t)q0, q_len[s], ctx_len[s], -1, 0, (int32_t)std::min<int64_t>(blocks, INT32_MAX)};
+      if (q_len[s] > nt) blocks += ceil_div(ctx_len[s], kWeighKeys);
+      if (trees.most && trees.words[s]) {
+        x.tree = (int32_t)rec;
+        x.words = trees.words[s];
+        write_tree(parents + q0, trees.place.data() + q0, q_len[s], ctx_len[s], x.words, window, sinks,
+                   (uint32_t*)(p + L.trees) + rec);
+        rec += (int64_t)q_len[s] * (x.words + 1);
+      }
+      span[s] = x;
+    }
+  } catch (const std::bad_alloc&) {
+    return fail(kv, LAR_E_CAPACITY, "out of host memory");
+  }
+  if (kv->sticky != LAR_OK) {  // an error that was reported ends with the batch it was in
+    KV_TRY(kv, hipMemsetAsync(kv->err, 0, sizeof(int32_t), kv->stream));
+    kv->sticky = LAR_OK;
+  }
+  if (n_seqs) {
+    memcpy(p, &id.x, sizeof id.x);
+    KV_TRY(kv, hipMemcpyAsync(kv->dev, p, kv->lay.end, hipMemcpyHostToDevice, kv->stream));
+    KV_TRY(kv, hipEventRecord(kv->done[b], kv->stream));
+    kv->used[b] = true;
+    kv->stage = (b + 1) % kKvStages;
+  }
+  kv->n_seq = n_seqs;
+  kv->n_tok = (int32_t)T;
+  kv->max_pages = (int32_t)pages;
+  kv->all_pages = (int32_t)all_pages;
+  kv->longest = all_longest;
+  kv->n_tree = n_tree;
+  kv->tree_waves = n_tree_waves;
+  kv->n_tree_join = n_tree_join;
+  kv->tree_join_rows = tree_join_rows;
+  kv->tree_most_parts = tree_most_parts;
+  kv->blocks = blocks;
+  kv->window = window;
+  kv->sinks = sinks;
+  kv->plan = id.x;
+  kv->n_narrow = n_narrow;
+  kv->n_wide = n_wide;
+  kv->n_join = n_join;
+  kv->join_rows = join_rows;
+  kv->most_parts = most_parts;
+  kv->planned = true;
+  return LAR_OK;
 }
 
 }  // namespace
@@ -597,8 +708,10 @@ lar_status lar_kv_create(lar_kv** out, const lar_kv_config* cfg) {
   const int64_t nt = kNarrowRows / g.G, wt = kWideRows / g.G;
   const int64_t narrow = std::min<int64_t>(cfg->max_seqs, cfg->max_tokens) * g.hkv;
   const int64_t wide = (std::min<int64_t>(cfg->max_seqs, cfg->max_tokens / (nt + 1)) + cfg->max_tokens / wt) * g.hkv;
-  kv->cap = Layout(cfg->max_tokens, narrow + kv->waves, wide + narrow + 2 * kv->groups, kv->waves, kv->groups,
-                   std::min<int64_t>(narrow, kv->waves) + std::min<int64_t>(wide + narrow, kv->groups) * (kWideRows / 32) + kJoins8).end;
+  kv->cap = KvLayout(cfg->max_tokens, narrow + kv->waves, wide + narrow + 2 * kv->groups, kv->waves, kv->groups,
+                   std::min<int64_t>(narrow, kv->waves) + std::min<int64_t>(wide + narrow, kv->groups) * (kWideRows / 32) + kJoins8,
+                     cfg->max_seqs, tree_room(*cfg), tree_tiles(*cfg, g) + kv->cus * kTreeWavesPerCu,
+                     kv->cus * kTreeWavesPerCu, kv->cus * kTreeWavesPerCu + kJoins8).end;
   // every wave or workgroup has two stretches at most that are parts of a tile
   bool ok = hipMalloc((void**)&kv->dev, kv->cap) == hipSuccess &&
             hipMalloc((void**)&kv->narrow_o, sizeof(float) * 2 * kv->waves * kNarrowRows * g.D) == hipSuccess &&
@@ -607,7 +720,7 @@ lar_status lar_kv_create(lar_kv** out, const lar_kv_config* cfg) {
             hipMalloc((void**)&kv->wide_ml, sizeof(float4) * 2 * kv->groups * kWideRows) == hipSuccess &&
             hipMalloc((void**)&kv->err, sizeof(int32_t)) == hipSuccess &&
             hipMemset(kv->err, 0, sizeof(int32_t)) == hipSuccess;
-  for (int i = 0; ok && i < kStages; ++i)
+  for (int i = 0; ok && i < kKvStages; ++i)
     ok = hipHostMalloc((void**)&kv->pinned[i], kv->cap, hipHostMallocDefault) == hipSuccess &&
          hipEventCreateWithFlags(&kv->done[i], hipEventDisableTiming) == hipSuccess;
   if (!ok) {
@@ -635,106 +748,14 @@ const char* lar_kv_error_string(const lar_kv* kv) { return kv ? kv->msg.c_str() 
 lar_status lar_kv_plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t* ctx_len,
                        int32_t window, int32_t sinks) {
   if (!kv) return LAR_E_ARG;
-  if (n_seqs < 0 || n_seqs > kv->cfg.max_seqs)
-    return fail(kv, LAR_E_ARG, "%d sequences, at most %d", n_seqs, kv->cfg.max_seqs);
-  if (n_seqs && (!q_len || !ctx_len)) return fail(kv, LAR_E_ARG, "null lengths");
-  if (window < 0 || sinks < 0) return fail(kv, LAR_E_ARG, "negative window or sinks");
-  const OnDevice device(kv);
-  KV_TRY(kv, device.status());
-  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-  if (kv->stream) KV_TRY(kv, hipStreamIsCapturing(kv->stream, &capture));
-  if (capture != hipStreamCaptureStatusNone) return fail(kv, LAR_E_STATE, "no plan under stream capture");
-  int64_t T = 0, pages = 0;
-  int32_t longest = 0;
-  for (int s = 0; s < n_seqs; ++s) {
-    if (q_len[s] < 0 || ctx_len[s] < 0 || ctx_len[s] > 1 << 30)
-      return fail(kv, LAR_E_ARG, "sequence %d: %d new tokens, context %d", s, q_len[s], ctx_len[s]);
-    T += q_len[s];
-    if (q_len[s]) longest = std::max(longest, ctx_len[s]);
-    if (q_len[s]) pages = std::max<int64_t>(pages, ceil_div(ctx_len[s], (int64_t)1 << kv->g.sh));
-  }
-  if (T > kv->cfg.max_tokens)
-    return fail(kv, LAR_E_ARG, "%lld new tokens, at most %d", (long long)T, kv->cfg.max_tokens);
-  // A window of every context hides nothing.  The kernels subtract a shorter one, and then a
-  // key of a context, from a position: all within 2^30, so within 32 bits.
-  if (window >= longest) window = 0;
-  if (!window) sinks = 0;
-  PlanId id;
-  id.add((uint32_t)window, (uint32_t)sinks);
-  for (int s = 0; s < n_seqs; ++s) id.add((uint32_t)q_len[s], (uint32_t)ctx_len[s]);
-  // the copy that last left this buffer is done before it is written again
-  const int b = kv->stage;
-  if (kv->used[b]) KV_TRY(kv, hipEventSynchronize(kv->done[b]));
-  char* p = kv->pinned[b];
-  const KvGeom& g = kv->g;
-  KvTok* tok = (KvTok*)(p + Layout().tok);
-  int32_t n_narrow = 0, n_wide = 0, n_join = 0, join_rows = 0, most_parts = 0;
-  kv->planned = false;
-  try {
-    std::vector<Tile> narrow, wide, none;
-    const int nt = kNarrowRows / g.G, wt = kWideRows / g.G;
-    int64_t q0 = 0;
-    for (int s = 0; s < n_seqs; ++s) {
-      const int n = q_len[s];
-      const int64_t p0 = (int64_t)ctx_len[s] - n;
-      for (int r = 0; r < n; ++r) tok[q0 + r] = KvTok{s, (int32_t)(p0 + r)};
-      if (!n) continue;
-      const bool small = n <= nt;
-      const int per = small ? n : wt;
-      for (int h = 0; h < g.hkv; ++h)
-        for (int r = 0; r < n; r += per) {
-          Tile t{};
-          t.s.q0 = (int32_t)(q0 + r);
-          t.s.ntok = std::min(per, n - r);
-          t.s.p0 = (int32_t)(p0 + r);
-          t.s.head = h;
-          t.s.seq = s;
-          t.tiles = key_tiles(p0 + r, t.s.ntok, small ? kNarrowKeys : kWideKeys, window, sinks, &t.s.ns, &t.s.fw);
-          (t.tiles ? small ? narrow : wide : none).push_back(t);
-        }
-      q0 += n;
-    }
-    // tiles without keys have only their zeros to write: either kernel will do, if they fit
-    for (const Tile& t : none) (t.s.ntok <= nt && wide.empty() ? narrow : wide).push_back(t);
-    const int64_t nn = (int64_t)narrow.size(), nw = (int64_t)wide.size();
-    const Layout L(T, nn ? nn + kv->waves : 0, nw ? nw + 2 * kv->groups : 0, kv->waves, kv->groups,
-                   std::min<int64_t>(nn, kv->waves) + std::min<int64_t>(nw, kv->groups) * (kWideRows / 32) + kJoins8);
-    if (L.end > kv->cap) return fail(kv, LAR_E_CAPACITY, "plan of %zu bytes, room for %zu", L.end, kv->cap);
-    kv->lay = L;
-    Joins join{g.G};
-    const int groups = nn ? split(narrow, wide, kv->groups, g) : kv->groups;
-    cut(narrow, nw ? (kv->groups - groups) * kWideWaves : kv->waves, narrow_least(narrow, g), (KvSeg*)(p + L.narrow),
-        (int32_t*)(p + L.narrow_at), &n_narrow, &join);
-    deal(wide, groups, g, (KvSeg*)(p + L.wide), (int32_t*)(p + L.wide_at), &n_wide, &join);
-    n_join = join.write((KvJoin*)(p + L.join), &join_rows);
-    most_parts = join.most;
-  } catch (const std::bad_alloc&) {
-    return fail(kv, LAR_E_CAPACITY, "out of host memory");
-  }
-  if (kv->sticky != LAR_OK) {  // an error that was reported ends with the batch it was in
-    KV_TRY(kv, hipMemsetAsync(kv->err, 0, sizeof(int32_t), kv->stream));
-    kv->sticky = LAR_OK;
-  }
-  if (T) {
-    memcpy(p, &id.x, sizeof id.x);
-    KV_TRY(kv, hipMemcpyAsync(kv->dev, p, kv->lay.end, hipMemcpyHostToDevice, kv->stream));
-    KV_TRY(kv, hipEventRecord(kv->done[b], kv->stream));
-    kv->used[b] = true;
-    kv->stage = (b + 1) % kStages;
-  }
-  kv->n_seq = n_seqs;
-  kv->n_tok = (int32_t)T;
-  kv->max_pages = (int32_t)pages;
-  kv->window = window;
-  kv->sinks = sinks;
-  kv->plan = id.x;
-  kv->n_narrow = n_narrow;
-  kv->n_wide = n_wide;
-  kv->n_join = n_join;
-  kv->join_rows = join_rows;
-  kv->most_parts = most_parts;
-  kv->planned = true;
-  return LAR_OK;
+  return plan(kv, n_seqs, q_len, ctx_len, nullptr, window, sinks);
+}
+
+lar_status lar_kv_plan_tree(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t* ctx_len,
+                            const int32_t* parents, int32_t window, int32_t sinks) {
+  if (!kv) return LAR_E_ARG;
+  if (n_seqs > 0 && !parents) return fail(kv, LAR_E_ARG, "null parents");
+  return plan(kv, n_seqs, q_len, ctx_len, parents, window, sinks);
 }
 
 lar_status lar_kv_append(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_rows* k, const lar_kv_rows* v,
@@ -806,6 +827,17 @@ lar_status lar_kv_attend(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_row
   a.narrow_ml = kv->narrow_ml;
   a.wide_ml = kv->wide_ml;
   a.err = kv->err;
+  a.wide_rows = kWideRows;
+  a.spans = (const KvSpan*)(kv->dev + kv->lay.spans);
+  a.trees = (const uint32_t*)(kv->dev + kv->lay.trees);
+  a.tree = (const KvSeg*)(kv->dev + kv->lay.tree);
+  a.tree_at = (const int32_t*)(kv->dev + kv->lay.tree_at);
+  a.n_tree = kv->n_tree;
+  a.tree_waves = kv->tree_waves;
+  a.tree_join = (const KvJoin*)(kv->dev + kv->lay.tree_join);
+  a.n_tree_join = kv->n_tree_join;
+  a.tree_join_rows = kv->tree_join_rows;
+  a.tree_most_parts = kv->tree_most_parts;
   return launch(kv, launch_kv_attend, a);
 }
 
@@ -819,8 +851,10 @@ lar_status lar_kv_sync(lar_kv* kv) {
   KV_TRY(kv, hipStreamSynchronize(kv->stream));
   if (e) {
     kv->sticky = LAR_E_STATE;
-    return fail(kv, LAR_E_STATE, e == kKvLostPage ? "a block table names a page outside the pool"
-                                                  : "a captured call ran under another plan than its own");
+    return fail(kv, LAR_E_STATE, "%s",
+                e == kKvLostPage   ? "a block table names a page outside the pool"
+                : e == kKvBadRows ? "rows to keep are not in ascending order, or not in the context"
+                                  : "a captured call ran under another plan than its own");
   }
   return LAR_OK;
 }

@@ -1,6 +1,6 @@
-// kv_device.h -- what the host (kv_api.cpp) and the kernels (kv_pages.hip, kv_attend.hip)
-// of the paged key/value cache share: the geometry, the plan of a token batch and the
-// launches.
+// kv_device.h -- what the host (kv_api.cpp, kv_rows_api.cpp) and the kernels (kv_pages.hip,
+// kv_attend.hip, kv_tree.hip, kv_weigh.hip, kv_select.hip, kv_keep.hip) of the paged key/value
+// cache share: the geometry, the plan of a token batch and the launches.
 //
 // Cache of one layer: pages of S = 2^sh tokens, [page][kv head][S][D] for K and for V, as
 // 16-bit values or as e4m3 codes with one byte per (page, kv head, row): the exponent k of
@@ -24,14 +24,28 @@ constexpr int kNarrowRows = 32, kWideWaves = 8, kWideRows = 32 * kWideWaves;
 // Exponents of the e4m3 rows' scales.
 constexpr int kKvExpMin = -100, kKvExpMax = 120;
 
+// Tokens of a tree, and of a batch's trees, at most.
+constexpr int kMaxTree = 1024, kTreeTokens = 16384;
+
 // What a kernel reports to the host.
-enum { kKvLostPage = 1, kKvOtherPlan = 2 };
+enum { kKvLostPage = 1, kKvOtherPlan = 2, kKvBadRows = 3 };
 
 // A new token of the batch: its row of the block table and its position there (< 0: a
 // padding row).
 struct KvTok {
   int32_t seq, pos;
 };
+
+// A sequence of the batch: its first new token, its new tokens and its context with them.  A tree's
+// tokens have a record each, from word `tree` of the plan's on (-1: no tree): the token's place
+// among those that it follows, then `words` words of bits, which keys it sees of the blocks of 32
+// from the one that the first new token is in on.
+struct KvSpan {
+  int32_t q0, q_len, ctx;
+  int32_t tree, words;
+  int32_t blocks;  // blocks of kWeighKeys keys of the sequences before it that take wide tiles
+};
+constexpr int kWeighKeys = 128;
 
 // A stretch of key tiles of one query tile, the work of one wave or workgroup.  Tiles
 // are counted over what the tile's rows can see: ns tiles of first tokens (sinks), then
@@ -97,6 +111,16 @@ struct KvAttendArgs {
   float *narrow_o, *wide_o;            // partial sums of a slot's rows
   float4 *narrow_ml, *wide_ml;         // [slot][rows]: scale of the weights (log2 units) and sums
   int32_t* err;
+  int32_t wide_rows;                   // rows of a slot of wide_o
+  // The query tiles of sequences with trees, of 32 * tree_waves rows; they have the slots of the
+  // narrow ones once these are joined.
+  const KvSpan* spans;                 // [n_seqs]
+  const uint32_t* trees;               // records
+  const KvSeg* tree;
+  const int32_t* tree_at;              // [n_tree + 1] stretches of each workgroup
+  int32_t n_tree, tree_waves;
+  const KvJoin* tree_join;
+  int32_t n_tree_join, tree_join_rows, tree_most_parts;
 };
 
 struct KvCopyArgs {
@@ -110,9 +134,63 @@ struct KvCopyArgs {
   int32_t* err;
 };
 
+// The sums of the attention's weights.  The narrow tiles of the plan have their keys to themselves;
+// the others' keys go by blocks, n_wide of them.
+struct KvWeighArgs {
+  KvPlanId plan;
+  KvGeom g;
+  KvPool pool;
+  KvRows q;
+  const int32_t* table;
+  int32_t cols;
+  float scale;        // of the scores, times log2(e)
+  int32_t window, sinks;
+  const float* lse;   // [T][hq]
+  const float* before;
+  float* after;       // [n_blocks][hkv][S]
+  const KvSeg* narrow;
+  const int32_t* narrow_at;
+  int32_t n_narrow, n_wide;
+  const KvSpan* spans;
+  int32_t n_seq;
+  int32_t* err;
+};
+
+struct KvSelectArgs {
+  KvPlanId plan;
+  KvGeom g;
+  const float* weights;  // [n_blocks][hkv][S]
+  uint32_t n_blocks;
+  const int32_t* table;
+  int32_t cols, n_seq;
+  const KvSpan* spans;
+  int32_t budget, first, last;
+  int32_t* rows;         // [n_seq][hkv][budget]
+  int32_t* err;
+};
+
+struct KvKeepArgs {
+  KvPlanId plan;
+  KvGeom g;
+  KvPool pool;           // written
+  float* weights;        // of the rows, or null
+  const int32_t *table, *to;
+  int32_t cols, to_cols, n_seq;
+  const KvSpan* spans;
+  const int32_t* rows;   // [n_seq][heads][n_rows], heads hkv or 1
+  int32_t heads, n_rows;
+  int32_t fresh;         // rows count from the first new token
+  int32_t* err;
+};
+
 hipError_t launch_kv_append(const KvCopyArgs& a, hipStream_t stream);
 hipError_t launch_kv_read(const KvCopyArgs& a, hipStream_t stream);
 hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t stream);
+hipError_t launch_kv_join(const KvAttendArgs& a, hipStream_t stream);
+hipError_t launch_kv_tree(const KvAttendArgs& a, hipStream_t stream);
+hipError_t launch_kv_weigh(const KvWeighArgs& a, hipStream_t stream);
+hipError_t launch_kv_select(const KvSelectArgs& a, hipStream_t stream);
+hipError_t launch_kv_keep(const KvKeepArgs& a, hipStream_t stream);
 
 }  // namespace lar
 

@@ -1,0 +1,139 @@
+// kv_keep.hip -- rows of a key/value cache to the places that they keep.
+//
+// Row base + rows[i] of a sequence and kv head goes to place base + i: base is 0, or the first new
+// token's position for a tree's path.  The rows ascend, so a row never goes up: of the rows that are
+// moved one after the other none is written over before it is read, and of those that are moved at
+// the same time all are read before one is written.  A workgroup walks over the list of one sequence
+// and head in that order, with its share of the columns of K, or of V, or with the rows' exponents
+// and weights.  Bound by the rows' bytes, read and written.
+#include "../../include/lar.h"
+#include "kv_device.h"
+
+namespace lar {
+namespace {
+
+struct Move {
+  uint32_t from, to;  // rows of the pool
+  bool on;
+};
+
+// What row i of the list is to do.
+struct List {
+  const KvKeepArgs& A;
+  const int32_t *rows, *table, *to;
+  int head, base, skip, limit;  // skip: padding rows before the first new token
+  bool bad = false, lost = false;
+  __device__ __forceinline__ List(const KvKeepArgs& a, int seq, int h) : A(a), head(h) {
+    const KvSpan s = A.spans[seq];
+    base = A.fresh ? s.ctx - s.q_len : 0;
+    skip = base < 0 ? -base : 0;
+    limit = A.fresh ? s.q_len : s.ctx;
+    rows = A.rows + ((int64_t)seq * A.heads + (A.heads > 1 ? h : 0)) * A.n_rows;
+    table = A.table + (int64_t)seq * A.cols;
+    to = A.to + (int64_t)seq * A.to_cols;
+  }
+  __device__ __forceinline__ uint32_t row(int32_t page, int pos) {
+    if ((uint32_t)page >= A.pool.n_blocks) {
+      lost = true;
+      return ~0u;
+    }
+    return (((uint32_t)page * (uint32_t)A.g.hkv + head) << A.g.sh) + (uint32_t)(pos & ((1 << A.g.sh) - 1));
+  }
+  __device__ __forceinline__ Move move(int i) {
+    Move m{0, 0, false};
+    if (i >= A.n_rows) return m;
+    const int r = rows[i], before = i ? rows[i - 1] : skip - 1;
+    if (r == -1) return m;                           // the list has ended
+    if (r >= limit || r < skip + i || r <= before || (i && before < 0)) {
+      bad = true;
+      return m;
+    }
+    const int src = base + r, dst = base + skip + i;
+    m.from = row(table[src >> A.g.sh], src);
+    m.to = row(to[dst >> A.g.sh], dst);
+    m.on = m.from != ~0u && m.to != ~0u && m.from != m.to;
+    return m;
+  }
+};
+
+// What was loaded has arrived before what follows: a barrier alone waits for no loads.
+template <int U>
+__device__ __forceinline__ void read(uint4 (&x)[U]) {
+#pragma unroll
+  for (int u = 0; u < U; ++u) asm volatile("" : "+v"(x[u].x), "+v"(x[u].y), "+v"(x[u].z), "+v"(x[u].w));
+}
+
+// The columns of 16 bytes from `col` on, `cols` of them, of the list's rows.
+template <int THREADS, int U>
+__device__ __forceinline__ void move_rows(List& list, char* pool, int row_bytes, int col, int cols) {
+  const int c = col + threadIdx.x % cols, r = threadIdx.x / cols, step = THREADS / cols;
+  for (int i0 = 0; i0 < list.A.n_rows; i0 += step * U) {
+    if (i0 && list.rows[i0] == -1) break;            // the same for all
+    uint4 x[U] = {};
+    Move m[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) m[u] = list.move(i0 + u * step + r);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (m[u].on) x[u] = *(const uint4*)(pool + (uint64_t)m[u].from * row_bytes + c * 16);
+    read(x);
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (m[u].on) *(uint4*)(pool + (uint64_t)m[u].to * row_bytes + c * 16) = x[u];
+  }
+}
+
+template <int THREADS>
+__device__ __forceinline__ void move_marks(List& list) {
+  const KvKeepArgs& A = list.A;
+  const bool f8 = A.g.cache == kKvE4m3;
+  uint8_t *ke = (uint8_t*)A.pool.ke, *ve = (uint8_t*)A.pool.ve;
+  for (int i0 = 0; i0 < A.n_rows; i0 += THREADS) {
+    if (i0 && list.rows[i0] == -1) break;
+    const Move m = list.move(i0 + threadIdx.x);
+    uint8_t a = 0, b = 0;
+    float w = 0.0f;
+    if (m.on) {
+      if (f8) a = ke[m.from], b = ve[m.from];
+      if (A.weights) w = A.weights[m.from];
+    }
+    uint4 x[1] = {make_uint4(a, b, __float_as_uint(w), 0)};
+    read(x);
+    __syncthreads();
+    if (m.on) {
+      if (f8) ke[m.to] = (uint8_t)x[0].x, ve[m.to] = (uint8_t)x[0].y;
+      if (A.weights) A.weights[m.to] = __uint_as_float(x[0].z);
+    }
+  }
+}
+
+// Jobs of a sequence and head: the shares of K, those of V, the marks.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_kv_keep(KvKeepArgs A, int shares, int jobs) {
+  const int job = blockIdx.x % jobs, x = blockIdx.x / jobs;
+  if (*A.plan.now != A.plan.id) {
+    if (threadIdx.x == 0) *A.err = kKvOtherPlan;
+    return;
+  }
+  List list(A, x / A.g.hkv, x % A.g.hkv);
+  if (job < 2 * shares) {
+    const int bytes = A.g.D * (A.g.cache == kKvE4m3 ? 1 : 2), cols = bytes / 16 / shares;
+    move_rows<THREADS, 4>(list, (char*)(job < shares ? A.pool.k : A.pool.v), bytes, job % shares * cols, cols);
+  } else {
+    move_marks<THREADS>(list);
+  }
+  if (list.lost) *A.err = kKvLostPage;
+  if (list.bad) *A.err = kKvBadRows;
+}
+
+}  // namespace
+
+hipError_t launch_kv_keep(const KvKeepArgs& a, hipStream_t stream) {
+  const bool marks = a.g.cache == kKvE4m3 || a.weights;
+  const int shares = 1, jobs = 2 * shares + marks;
+  k_kv_keep<256><<<a.n_seq * a.g.hkv * jobs, 256, 0, stream>>>(a, shares, jobs);
+  return hipGetLastError();
+}
+
+}  // namespace lar

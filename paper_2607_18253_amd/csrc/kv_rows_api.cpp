@@ -1,0 +1,141 @@
+// kv_rows_api.cpp -- host side of what decides over the rows of a paged key/value cache: the weights
+// that they got, which of them stay, and where they go (lar_kv_weigh, _select and _keep in
+// include/lar.h).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cfloat>
+
+#include "../../include/lar.h"
+#include "kv_handle.h"
+
+using namespace lar;
+
+namespace {
+
+// Bytes of a layer's weights.
+uint64_t weight_bytes(const lar_kv* kv, int64_t n_blocks) {
+  return ((uint64_t)n_blocks * kv->g.hkv << kv->g.sh) * sizeof(float);
+}
+
+// Workgroups of a launch, one or more for each sequence and kv head.
+lar_status check_grid(lar_kv* kv, int64_t n) {
+  return n < (int64_t)1 << 31 ? LAR_OK : fail(kv, LAR_E_CAPACITY, "a batch of %lld workgroups", (long long)n);
+}
+
+lar_status check_table(lar_kv* kv, const int32_t* table, int32_t cols, int64_t need, const char* name) {
+  if (!table) return fail(kv, LAR_E_ARG, "null %s", name);
+  if (cols < need) return fail(kv, LAR_E_ARG, "%s has %d columns, the planned contexts need %lld", name, cols, (long long)need);
+  return LAR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+lar_status lar_kv_weigh(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_rows* q, const int32_t* table,
+                        int32_t table_cols, double scale, const float* lse, const float* before, float* weights) {
+  if (lar_status st = ready(kv)) return st;
+  if (kv->n_tree) return fail(kv, LAR_E_STATE, "the planned batch has trees, whose tokens are not weighed");
+  if (!kv->n_tok) return LAR_OK;
+  KvPool pool;
+  KvRows qr;
+  if (lar_status st = check(kv, pages, table, table_cols, &pool)) return st;
+  if (lar_status st = check_rows(kv, q, kv->g.hq, "q", &qr)) return st;
+  if (!(scale > 0.0) || !(scale < 1e30)) return fail(kv, LAR_E_ARG, "scale must be positive and finite");
+  if (!lse || !before || !weights) return fail(kv, LAR_E_ARG, "null lse, before or weights");
+  const uint64_t bytes = weight_bytes(kv, pages->n_blocks);
+  const uintptr_t a0 = (uintptr_t)before, b0 = (uintptr_t)weights;
+  if (a0 != b0 && a0 < b0 + bytes && b0 < a0 + bytes)
+    return fail(kv, LAR_E_ARG, "before and weights must be the same or lie apart");
+  if (lar_status st = check_grid(kv, std::max<int64_t>(kv->blocks, kv->n_seq) * kv->g.hkv)) return st;
+  KvWeighArgs a{};
+  a.plan = plan_id(kv);
+  a.g = kv->g;
+  a.pool = pool;
+  a.q = qr;
+  a.table = table;
+  a.cols = table_cols;
+  a.scale = std::max((float)(scale * 1.4426950408889634074), FLT_TRUE_MIN);
+  a.window = kv->window;
+  a.sinks = kv->sinks;
+  a.lse = lse;
+  a.before = before;
+  a.after = weights;
+  a.narrow = (const KvSeg*)(kv->dev + kv->lay.narrow);
+  a.narrow_at = (const int32_t*)(kv->dev + kv->lay.narrow_at);
+  a.n_narrow = kv->n_narrow;
+  a.n_wide = (int32_t)kv->blocks;
+  a.spans = (const KvSpan*)(kv->dev + kv->lay.spans);
+  a.n_seq = kv->n_seq;
+  a.err = kv->err;
+  return launch(kv, launch_kv_weigh, a);
+}
+
+lar_status lar_kv_select(lar_kv* kv, const float* weights, int64_t n_blocks, const int32_t* table, int32_t table_cols,
+                         int32_t budget, int32_t first, int32_t last, int32_t* rows) {
+  if (lar_status st = ready(kv)) return st;
+  if (budget < 1 || first < 0 || last < 0 || first > budget || last > budget - first)
+    return fail(kv, LAR_E_ARG, "a budget of %d rows, the first %d and the last %d among them", budget, first, last);
+  if (!kv->n_seq) return LAR_OK;
+  if (!weights || !rows) return fail(kv, LAR_E_ARG, "null weights or rows");
+  if (n_blocks < 1 || n_blocks > ((((int64_t)1 << 32) - 1) >> kv->g.sh) / kv->g.hkv)
+    return fail(kv, LAR_E_ARG, "n_blocks must be in 1 .. (2^32 - 1) / (block_size * n_kv_heads)");
+  if (lar_status st = check_table(kv, table, table_cols, kv->all_pages, "block table")) return st;
+  if (lar_status st = check_grid(kv, (int64_t)kv->n_seq * kv->g.hkv)) return st;
+  KvSelectArgs a{};
+  a.plan = plan_id(kv);
+  a.g = kv->g;
+  a.weights = weights;
+  a.n_blocks = (uint32_t)n_blocks;
+  a.table = table;
+  a.cols = table_cols;
+  a.n_seq = kv->n_seq;
+  a.spans = (const KvSpan*)(kv->dev + kv->lay.spans);
+  a.budget = budget;
+  a.first = first;
+  a.last = last;
+  a.rows = rows;
+  a.err = kv->err;
+  return launch(kv, launch_kv_select, a);
+}
+
+lar_status lar_kv_keep(lar_kv* kv, const lar_kv_pages* pages, const int32_t* table, int32_t table_cols,
+                       const int32_t* to_table, int32_t to_cols, const int32_t* rows, int32_t n_rows, int32_t per_head,
+                       int32_t fresh, float* weights) {
+  if (lar_status st = ready(kv)) return st;
+  if (n_rows < 0 || (per_head & ~1) || (fresh & ~1)) return fail(kv, LAR_E_ARG, "n_rows >= 0, per_head and fresh 0 or 1");
+  if (!kv->n_seq || !n_rows) return LAR_OK;
+  KvPool pool;
+  if (!rows) return fail(kv, LAR_E_ARG, "null rows");
+  if (lar_status st = check(kv, pages, table, table_cols, &pool)) return st;
+  if (lar_status st = check_table(kv, table, table_cols, kv->all_pages, "block table")) return st;
+  if (!to_table) {
+    to_table = table;
+    to_cols = table_cols;
+  }
+  // a list has no more rows than the context, and of the new tokens none goes up
+  const int64_t places = fresh ? kv->longest : std::min(n_rows, kv->longest);
+  if (lar_status st = check_table(kv, to_table, to_cols, ceil_div(places, (int64_t)1 << kv->g.sh), "table of the places"))
+    return st;
+  if (lar_status st = check_grid(kv, (int64_t)kv->n_seq * kv->g.hkv * 64)) return st;
+  KvKeepArgs a{};
+  a.plan = plan_id(kv);
+  a.g = kv->g;
+  a.pool = pool;
+  a.weights = weights;
+  a.table = table;
+  a.to = to_table;
+  a.cols = table_cols;
+  a.to_cols = to_cols;
+  a.n_seq = kv->n_seq;
+  a.spans = (const KvSpan*)(kv->dev + kv->lay.spans);
+  a.rows = rows;
+  a.heads = per_head ? kv->g.hkv : 1;
+  a.n_rows = n_rows;
+  a.fresh = fresh;
+  a.err = kv->err;
+  return launch(kv, launch_kv_keep, a);
+}
+
+}  // extern "C"

@@ -1,6 +1,6 @@
 """Python binding of the paged key/value cache (lar_kv_* in include/lar.h): a token batch's
-K and V rows into and out of the pages, and its attention over them.  Argument marshalling
-only, as in ``lar``; every step runs in the HIP kernels behind the C ABI.
+K and V rows into and out of the pages, its attention over them, with trees of drafted tokens,
+and which rows stay within a budget.  Argument marshalling only, as in ``lar``; every step runs in the HIP kernels behind the C ABI.
 """
 
 from __future__ import annotations
@@ -204,6 +204,15 @@ class PagedKV:
             _on(self._index, table, self._int32, "table")
         return table.data_ptr(), shape[1]
 
+    def _weights(self, t, name, n_blocks=None):
+        p = _on(self._index, t, self._torch.float32, name)
+        if t.dim() != 3 or t.shape[1:] != (self.n_kv, self.block_size) or n_blocks not in (None, t.shape[0]):
+            n = "n_blocks" if n_blocks is None else n_blocks
+            raise ValueError(f"{name} must be [{n}][{self.n_kv}][{self.block_size}]")
+        if t.requires_grad:
+            self._no_gradient(name)
+        return p
+
     def _call(self, f, pages, tensors, *args):
         """f(handle, *args) in order with the current stream."""
         if _raw_stream(self._index) == self._sid:
@@ -219,7 +228,7 @@ class PagedKV:
         try:
             self._check(f(self._h, *args))
         finally:
-            for t in (*tensors, *pages.tensors()):
+            for t in (*tensors, *(pages.tensors() if pages else ())):
                 if t is not None:
                     t.record_stream(self.stream)
             now.wait_stream(self.stream)
@@ -239,9 +248,16 @@ class PagedKV:
             kv += [torch.empty(shape[:3], dtype=torch.uint8, device=self.device) for _ in range(2)]
         return KvPages(*kv)
 
-    def plan(self, q_len, ctx_len, window: int = 0, sinks: int = 0):
+    def new_weights(self, n_blocks: int):
+        """Weights of the rows of one layer's pages (weigh), all 0."""
+        return self._torch.zeros((int(n_blocks), self.n_kv, self.block_size), dtype=self._torch.float32,
+                                 device=self.device)
+
+    def plan(self, q_len, ctx_len, window: int = 0, sinks: int = 0, parents=None):
         """The token batch of the calls that follow: new tokens per sequence and context
-        with them (host integers)."""
+        with them (host integers).  parents, for sequences whose new tokens are a tree of drafted
+        ones: of each new token of the batch the number of its parent among the sequence's new
+        tokens, or -1 for the context."""
         q, c = _int32s(q_len, "q_len"), _int32s(ctx_len, "ctx_len")
         if q.shape != c.shape:
             raise ValueError("q_len and ctx_len must be of one length")
@@ -250,7 +266,15 @@ class PagedKV:
             with self._torch.cuda.device(self.device):
                 if self._torch.cuda.is_current_stream_capturing():
                     raise LarError(LAR_E_STATE, "no plan under stream capture")
-        self._check(self._L.lar_kv_plan(self._h, len(q), q.ctypes.data, c.ctypes.data, int(window), int(sinks)))
+        if parents is None:
+            st = self._L.lar_kv_plan(self._h, len(q), q.ctypes.data, c.ctypes.data, int(window), int(sinks))
+        else:
+            up = _int32s(parents, "parents")
+            if (q < 0).any() or len(up) != q.sum(dtype=np.int64):
+                raise ValueError("parents must be one for each new token")
+            st = self._L.lar_kv_plan_tree(self._h, len(q), q.ctypes.data, c.ctypes.data, up.ctypes.data,
+                                          int(window), int(sinks))
+        self._check(st)
         self._batch(len(q), int(q.sum()))
 
     def append(self, pages: KvPages, k, v, table):
@@ -289,6 +313,57 @@ class PagedKV:
                    self._scale if scale is None else float(scale), to,
                    None if lse is None else _on(self._index, lse, self._torch.float32, "lse", n))
         return out
+
+    def weigh(self, pages: KvPages, q, lse, table, weights, before=None, scale=None):
+        """Adds to the weights of the cache's rows what each gets of the attention of the batch's
+        queries [T][n_q][head_dim], whose log-sums attend() gave as lse.  weights is a float32
+        tensor [n_blocks][n_kv][block_size] (new_weights), updated in place, or made of `before`;
+        the batch's new tokens start with 0."""
+        pg, qa = self._pages(pages), self._rows(q, self._q_shape, "q")
+        if lse.requires_grad:
+            self._no_gradient("lse")
+        z = _on(self._index, lse, self._torch.float32, "lse", self._n_tok * self.n_q)
+        w = self._weights(weights, "weights", pages.k.shape[0])
+        b = w if before is None else self._weights(before, "before", pages.k.shape[0])
+        t, cols = self._table(table)
+        self._call(self._L.lar_kv_weigh, pages, (q, lse, table, weights, before), pg, qa, t, cols,
+                   self._scale if scale is None else float(scale), z, b, w)
+        return weights
+
+    def select(self, weights, table, budget: int, first: int = 0, last: int = 0, rows=None):
+        """Which rows of each planned context stay within a budget: the first and last ones and
+        those of the largest weights.  Returns rows, int32 [n_seqs][n_kv][budget], the positions
+        in ascending order, then -1."""
+        torch = self._torch
+        budget, first, last = _int32(budget, "budget"), _int32(first, "first"), _int32(last, "last")
+        w = self._weights(weights, "weights")
+        shape = (self._n_seq, self.n_kv, budget)
+        if budget < 1:
+            raise ValueError("budget must be positive")
+        if rows is None:
+            rows = torch.empty(shape, dtype=torch.int32, device=self.device)
+        elif rows.shape != shape:
+            raise ValueError(f"rows must be [{shape[0]}][{shape[1]}][{shape[2]}]")
+        to = _on(self._index, rows, torch.int32, "rows")
+        t, cols = self._table(table)
+        self._call(self._L.lar_kv_select, None, (weights, table, rows), w, weights.shape[0], t, cols, budget, first,
+                   last, to)
+        return rows
+
+    def keep(self, pages: KvPages, table, rows, *, new: bool = False, to=None, weights=None):
+        """Moves the rows that lists name, int32 [n_seqs][n_kv][n] or for all heads [n_seqs][n] (in
+        ascending order, ended by -1), to the front of each planned context, with `new` to where
+        its new tokens start, from which the lists count then: an accepted path of a tree.  Into
+        the pages of the table `to`, if given.  weights go along."""
+        pg = self._pages(pages)
+        if rows.dim() not in (2, 3) or rows.shape[0] != self._n_seq or (rows.dim() == 3 and rows.shape[1] != self.n_kv):
+            raise ValueError(f"rows must be [{self._n_seq}][{self.n_kv}][n] or [{self._n_seq}][n]")
+        r = _on(self._index, rows, self._torch.int32, "rows")
+        w = None if weights is None else self._weights(weights, "weights", pages.k.shape[0])
+        t, cols = self._table(table)
+        t2, cols2 = (None, 0) if to is None else self._table(to)
+        self._call(self._L.lar_kv_keep, pages, (table, rows, to, weights), pg, t, cols, t2, cols2, r,
+                   _int32(rows.shape[-1], "n"), int(rows.dim() == 3), int(bool(new)), w)
 
     def sync(self):
         """Synchronise; raises the sticky device error, if any."""

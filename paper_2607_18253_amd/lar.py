@@ -26,7 +26,8 @@ EXPORTED = ("lar_create", "lar_destroy", "lar_error_string", "lar_load_state", "
             "lar_board_destroy", "lar_board_publish", "lar_board_collect",
             "lar_whatif_noalloc", "lar_noalloc_error_string", "lar_estimate_lps",
             "lar_kv_create", "lar_kv_destroy", "lar_kv_error_string", "lar_kv_plan", "lar_kv_append",
-            "lar_kv_read", "lar_kv_attend", "lar_kv_sync")
+            "lar_kv_read", "lar_kv_attend", "lar_kv_sync", "lar_kv_plan_tree", "lar_kv_weigh", "lar_kv_select",
+            "lar_kv_keep")
 LPS_POISSON, LPS_VARIABILITY = 0, 1
 
 
@@ -153,6 +154,14 @@ def load_library(path: str = LIB_PATH):
     L.lar_kv_read.argtypes = [vp, vp, vp, i32, vp, vp]
     L.lar_kv_attend.restype = i32
     L.lar_kv_attend.argtypes = [vp, vp, vp, vp, i32, dbl, vp, vp]
+    L.lar_kv_plan_tree.restype = i32
+    L.lar_kv_plan_tree.argtypes = [vp, i32, vp, vp, vp, i32, i32]
+    L.lar_kv_weigh.restype = i32
+    L.lar_kv_weigh.argtypes = [vp, vp, vp, vp, i32, dbl, vp, vp, vp]
+    L.lar_kv_select.restype = i32
+    L.lar_kv_select.argtypes = [vp, vp, i64, vp, i32, i32, i32, i32, vp]
+    L.lar_kv_keep.restype = i32
+    L.lar_kv_keep.argtypes = [vp, vp, vp, i32, vp, i32, vp, i32, i32, i32, vp]
     L.lar_kv_sync.restype = i32
     L.lar_kv_sync.argtypes = [vp]
     _lib = L
