@@ -559,7 +559,7 @@ lar_status plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t*
   KvTok* tok = (KvTok*)(p + KvLayout().tok);
   int32_t n_narrow = 0, n_wide = 0, n_join = 0, join_rows = 0, most_parts = 0;
   int32_t n_tree = 0, n_tree_waves = 0, n_tree_join = 0, tree_join_rows = 0, tree_most_parts = 0;
-  int64_t blocks = 0;
+  int64_t blocks = 0, cuts = 0;
   kv->planned = false;
   try {
     std::vector<Tile> narrow, wide, none, tree;
@@ -620,7 +620,9 @@ lar_status plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t*
     int64_t rec = 0;
     q0 = 0;
     for (int s = 0; s < n_seqs; q0 += q_len[s], ++s) {
-      KvSpan x{(int32_t)q0, q_len[s], ctx_len[s], -1, 0, (int32_t)std::min<int64_t>(blocks, INT32_MAX)};
+      KvSpan x{(int32_t)q0, q_len[s], ctx_len[s], -1, 0, (int32_t)std::min<int64_t>(blocks, INT32_MAX),
+               (int32_t)std::min<int64_t>(cuts, INT32_MAX)};
+      cuts += kv_select_cuts(ctx_len[s]);
       if (q_len[s] > nt) blocks += ceil_div(ctx_len[s], kWeighKeys);
       if (trees.most && trees.words[s]) {
         x.tree = (int32_t)rec;
@@ -656,6 +658,7 @@ lar_status plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t*
   kv->tree_join_rows = tree_join_rows;
   kv->tree_most_parts = tree_most_parts;
   kv->blocks = blocks;
+  kv->cuts = cuts;
   kv->window = window;
   kv->sinks = sinks;
   kv->plan = id.x;

@@ -44,8 +44,17 @@ struct KvSpan {
   int32_t q0, q_len, ctx;
   int32_t tree, words;
   int32_t blocks;  // blocks of kWeighKeys keys of the sequences before it that take wide tiles
+  int32_t cuts;    // stretches of kSelectStretch rows of those before it
 };
-constexpr int kWeighKeys = 128;
+constexpr int kWeighKeys = 256;
+
+// Contexts that are cut for the selection: stretches of one, one at least, and the working memory, in
+// words, of `contexts` sequences and heads with `cuts` of them.
+constexpr int kSelectStretch = 4096, kSelectDigits = 4, kSelectBins = 512;
+constexpr int kv_select_cuts(int32_t ctx) { return ctx > kSelectStretch ? (ctx + (kSelectStretch - 1)) / kSelectStretch : 1; }
+constexpr int64_t kv_select_words(int64_t contexts, int64_t cuts) {
+  return contexts * 2 * kSelectDigits + (cuts + 3) / 4 * 4 + cuts * kSelectDigits * kSelectBins;
+}
 
 // A stretch of key tiles of one query tile, the work of one wave or workgroup.  Tiles
 // are counted over what the tile's rows can see: ns tiles of first tokens (sinks), then
@@ -162,10 +171,12 @@ struct KvSelectArgs {
   const float* weights;  // [n_blocks][hkv][S]
   uint32_t n_blocks;
   const int32_t* table;
-  int32_t cols, n_seq;
+  int32_t cols, n_seq, longest;  // longest: context of any
   const KvSpan* spans;
   int32_t budget, first, last;
   int32_t* rows;         // [n_seq][hkv][budget]
+  int32_t* work;         // where contexts are cut, else null
+  int32_t cuts;          // of all sequences and heads
   int32_t* err;
 };
 

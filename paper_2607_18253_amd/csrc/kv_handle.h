@@ -64,6 +64,7 @@ struct lar_kv {
   int32_t max_pages = 0, all_pages = 0;  // of a context with new tokens, of any
   int32_t longest = 0;                   // context of any
   int64_t blocks = 0;                    // of kWeighKeys keys of the sequences that take wide tiles
+  int64_t cuts = 0;                      // of kSelectStretch rows of all
   int32_t n_narrow = 0, n_wide = 0, n_join = 0, join_rows = 0, most_parts = 0;
   int32_t n_tree = 0, tree_waves = 0, n_tree_join = 0, tree_join_rows = 0, tree_most_parts = 0;
   lar_status sticky = LAR_OK;

@@ -67,20 +67,27 @@ __device__ __forceinline__ void read(uint4 (&x)[U]) {
 template <int THREADS, int U>
 __device__ __forceinline__ void move_rows(List& list, char* pool, int row_bytes, int col, int cols) {
   const int c = col + threadIdx.x % cols, r = threadIdx.x / cols, step = THREADS / cols;
-  for (int i0 = 0; i0 < list.A.n_rows; i0 += step * U) {
-    if (i0 && list.rows[i0] == -1) break;            // the same for all
-    uint4 x[U] = {};
-    Move m[U];
+  Move m[U], next[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) m[u] = list.move(i0 + u * step + r);
+  for (int u = 0; u < U; ++u) m[u] = list.move(u * step + r);
+  for (int i0 = 0; i0 < list.A.n_rows; i0 += step * U) {
+    uint4 x[U] = {};
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (m[u].on) x[u] = *(const uint4*)(pool + (uint64_t)m[u].from * row_bytes + c * 16);
+    // the rows after these are looked up while these are on their way
+    const int i1 = i0 + step * U;
+    const bool more = i1 < list.A.n_rows && list.rows[i1] != -1;  // the same for all
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = more ? list.move(i1 + u * step + r) : Move{0, 0, false};
     read(x);
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (m[u].on) *(uint4*)(pool + (uint64_t)m[u].to * row_bytes + c * 16) = x[u];
+    if (!more) break;
+#pragma unroll
+    for (int u = 0; u < U; ++u) m[u] = next[u];
   }
 }
 
@@ -108,6 +115,8 @@ __device__ __forceinline__ void move_marks(List& list) {
   }
 }
 
+constexpr int kFewGroups = 1024;
+
 // Jobs of a sequence and head: the shares of K, those of V, the marks.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void k_kv_keep(KvKeepArgs A, int shares, int jobs) {
@@ -131,8 +140,16 @@ __global__ __launch_bounds__(THREADS) void k_kv_keep(KvKeepArgs A, int shares, i
 
 hipError_t launch_kv_keep(const KvKeepArgs& a, hipStream_t stream) {
   const bool marks = a.g.cache == kKvE4m3 || a.weights;
-  const int shares = 1, jobs = 2 * shares + marks;
-  k_kv_keep<256><<<a.n_seq * a.g.hkv * jobs, 256, 0, stream>>>(a, shares, jobs);
+  const int cols = a.g.D * (a.g.cache == kKvE4m3 ? 1 : 2) / 16;  // 16 bytes each
+  const int64_t lists = (int64_t)a.n_seq * a.g.hkv;
+  // few lists: a share of the columns for each workgroup, 64 bytes of a row at least
+  int shares = 1;
+  while (2 * lists * shares < kFewGroups && cols / shares > 4) shares *= 2;
+  const int jobs = 2 * shares + marks;
+  if (2 * lists * shares < kFewGroups && a.n_rows * (cols / shares) > 1024)
+    k_kv_keep<1024><<<lists * jobs, 1024, 0, stream>>>(a, shares, jobs);
+  else
+    k_kv_keep<256><<<lists * jobs, 256, 0, stream>>>(a, shares, jobs);
   return hipGetLastError();
 }
 

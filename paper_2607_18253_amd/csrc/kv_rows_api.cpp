@@ -29,6 +29,15 @@ lar_status check_table(lar_kv* kv, const int32_t* table, int32_t cols, int64_t n
   return LAR_OK;
 }
 
+// Working memory for a selection whose contexts are cut, or null where a workgroup takes a whole one.
+constexpr int kSelectWhole = 32768, kSelectCuts = 64;
+int32_t* select_work(const lar_kv* kv) {
+  const int64_t room = (int64_t)2 * kv->waves * kNarrowRows * kv->g.D;  // of narrow_o, in words
+  const bool cut = kv->longest > kSelectWhole && kv_select_cuts(kv->longest) <= kSelectCuts &&
+                   kv_select_words((int64_t)kv->n_seq * kv->g.hkv, kv->cuts * kv->g.hkv) <= room;
+  return cut ? (int32_t*)kv->narrow_o : nullptr;
+}
+
 }  // namespace
 
 extern "C" {
@@ -91,11 +100,14 @@ lar_status lar_kv_select(lar_kv* kv, const float* weights, int64_t n_blocks, con
   a.table = table;
   a.cols = table_cols;
   a.n_seq = kv->n_seq;
+  a.longest = kv->longest;
   a.spans = (const KvSpan*)(kv->dev + kv->lay.spans);
   a.budget = budget;
   a.first = first;
   a.last = last;
   a.rows = rows;
+  a.work = select_work(kv);
+  a.cuts = a.work ? (int32_t)(kv->cuts * kv->g.hkv) : 0;
   a.err = kv->err;
   return launch(kv, launch_kv_select, a);
 }

@@ -2,17 +2,19 @@
 //
 // Of a sequence's n rows and a kv head, the first F and the last L stay, and of those between the
 // ones of the largest weights, of equal ones the lowest positions; all in ascending order.  A weight
-// is taken as a 32-bit number that orders as it does (-0 as 0, NaN above all), and the smallest one
-// to stay is found byte by byte from the top, by counting the values of a byte among the weights
-// that agree with it so far.  The positions then come out in one more pass, by prefix sums over
-// ballots.  One workgroup for each sequence and kv head.
+// is taken as a 32-bit number that orders as it does (-0 as 0, NaN above all).  The smallest number
+// to stay is found digit by digit from the top: counts of a digit's values among the numbers that
+// agree with it so far, in LDS, and a prefix sum over them from the largest value down.  The first
+// digit is sign, exponent and one more bit: of weights that lie close together a shorter one is the
+// same for most, and their counts would wait for one another.  The positions then come out in one
+// more pass, by prefix sums over ballots.
+//
+// Bound by latency: a few dependent steps between barriers for some 10 KB of weights.
 #include "../../include/lar.h"
 #include "kv_device.h"
 
 namespace lar {
 namespace {
-
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
 
 // A number that orders as the weight does.
 __device__ __forceinline__ uint32_t order(float w) {
@@ -20,99 +22,400 @@ __device__ __forceinline__ uint32_t order(float w) {
   return w != w ? 0xffffffffu : b >> 31 ? ~b : b | 0x80000000u;
 }
 
-__global__ __launch_bounds__(kThreads) void k_kv_select(KvSelectArgs A) {
-  const int seq = blockIdx.x / A.g.hkv, head = blockIdx.x % A.g.hkv;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  __shared__ int count[256];
-  __shared__ int found[2];            // the byte, and how many of it are wanted
-  __shared__ int above[kWaves], same[kWaves];
-  if (*A.plan.now != A.plan.id) {
-    if (tid == 0) *A.err = kKvOtherPlan;
-    return;
-  }
-  const KvSpan s = A.spans[seq];
-  const int n = s.ctx, S = 1 << A.g.sh;
-  int32_t* rows = A.rows + ((int64_t)seq * A.g.hkv + head) * A.budget;
-  if (n <= A.budget) {
-    for (int i = tid; i < A.budget; i += kThreads) rows[i] = i < n ? i : -1;
-    return;
-  }
-  const int32_t* table = A.table + (int64_t)seq * A.cols;
+// A sequence and kv head: its context, its budget, its weights.
+struct Context {
+  const KvSelectArgs& A;
+  int n, end, head;      // end: first row of the last ones
+  const int32_t* table;
+  int32_t* rows;
   bool lost = false;
-  const auto weight = [&](int j) {
+  __device__ __forceinline__ Context(const KvSelectArgs& a, int x) : Context(a, x / a.g.hkv, x % a.g.hkv) {}
+  __device__ __forceinline__ Context(const KvSelectArgs& a, int seq, int h) : A(a), head(h) {
+    n = A.spans[seq].ctx;
+    end = n - A.last;
+    table = A.table + (int64_t)seq * A.cols;
+    rows = A.rows + ((int64_t)seq * A.g.hkv + head) * A.budget;
+  }
+  __device__ __forceinline__ uint32_t weight(int j) {
     const int32_t page = table[j >> A.g.sh];
     if ((uint32_t)page >= A.n_blocks) {
       lost = true;
       return 0u;
     }
-    return order(A.weights[((int64_t)page * A.g.hkv + head) * S + (j & (S - 1))]);
+    return order(A.weights[(((int64_t)page * A.g.hkv + head) << A.g.sh) + (j & ((1 << A.g.sh) - 1))]);
+  }
+  __device__ __forceinline__ bool between(int j) const { return j >= A.first && j < end; }
+};
+
+// Inclusive prefix sum over a wave.
+__device__ __forceinline__ int wave_sums(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);   // row_shr:2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);   // row_shr:4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);   // row_shr:8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31
+  return x;
+}
+
+// The value of a digit at which `want` is reached, counting from the largest one down, and how many
+// of that value itself are wanted then.  count[v]: of value BINS - 1 - v.  All threads get them.
+template <int BINS, int THREADS>
+__device__ __forceinline__ void reach(const int* count, int* part, int* found, int& want, uint32_t& digit) {
+  constexpr int kEach = (BINS + THREADS - 1) / THREADS;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int c[kEach], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int v = tid * kEach + i;
+    c[i] = v < BINS ? count[v] : 0;
+    sum += c[i];
+  }
+  int upto = wave_sums(sum);
+  if (lane == 63) part[wave] = upto;
+  __syncthreads();
+  for (int w = 0; w < THREADS / 64; ++w) upto += w < wave ? part[w] : 0;
+  int before = upto - sum;
+  if (before < want && want <= upto) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (before < want && want <= before + c[i]) {
+        found[0] = BINS - 1 - (tid * kEach + i);
+        found[1] = want - before;
+      }
+      before += c[i];
+    }
+  }
+  __syncthreads();
+  digit = (uint32_t)found[0];
+  want = found[1];
+}
+
+// One workgroup for each sequence and kv head, R numbers for a thread in registers; contexts of
+// more rows are read again in every pass.
+template <int THREADS, int R>
+__global__ __launch_bounds__(THREADS, 4) void k_kv_select(KvSelectArgs A) {
+  constexpr int kBins = 2048, kWaves = THREADS / 64, kRows = THREADS * R;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ int count[kBins];
+  __shared__ int part[kWaves], found[2];
+  __shared__ int2 sums[R * kWaves];  // above the least, and equal to it
+  if (*A.plan.now != A.plan.id) {
+    if (tid == 0) *A.err = kKvOtherPlan;
+    return;
+  }
+  Context c(A, blockIdx.x);
+  if (c.n <= A.budget) {
+    for (int i = tid; i < A.budget; i += THREADS) c.rows[i] = i < c.n ? i : -1;
+    return;
+  }
+  uint32_t x[R];
+  const auto load = [&](int j0) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (j0 + r * THREADS >= c.n) break;  // the same for all threads, here and below
+      const int j = j0 + r * THREADS + tid;
+      x[r] = j < c.n ? c.weight(j) : 0;
+    }
   };
-  const int end = n - A.last;                          // first row of the last ones
-  int want = A.budget - A.first - A.last;              // rows of those between
+  load(0);
+  int want = A.budget - A.first - A.last;  // rows of those between
+  const bool some = want > 0;
   uint32_t least = 0;
-  for (int shift = 24; shift >= 0 && want; shift -= 8) {
-    if (tid < 256) count[tid] = 0;
-    __syncthreads();
-    for (int j = A.first + tid; j < end; j += kThreads) {
-      const uint32_t x = weight(j);
-      if (shift == 24 || (x ^ least) >> (shift + 8) == 0) atomicAdd(&count[x >> shift & 255], 1);
+  if (some) {
+#pragma unroll 1
+    for (int shift = 22; shift >= 0; shift -= 11) {
+      for (int i = tid; i < kBins; i += THREADS) count[i] = 0;
+      __syncthreads();
+      for (int j0 = 0; j0 < c.n; j0 += kRows) {
+        if (c.n > kRows) load(j0);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          if (j0 + r * THREADS >= c.n) break;
+          const int j = j0 + r * THREADS + tid;
+          const bool on = c.between(j) && (shift == 22 || (x[r] ^ least) >> (shift + 11) == 0);
+          if (on) atomicAdd(&count[kBins - 1 - (x[r] >> shift & (kBins - 1))], 1);
+        }
+      }
+      __syncthreads();
+      uint32_t digit;
+      reach<kBins, THREADS>(count, part, found, want, digit);
+      least |= digit << shift;
     }
-    __syncthreads();
-    if (tid == 0) {
-      int left = want, b = 255;
-      while (count[b] < left) left -= count[b--];
-      found[0] = b;
-      found[1] = left;
-    }
-    __syncthreads();
-    least |= (uint32_t)found[0] << shift;
-    want = found[1];                                   // of those that are equal so far
   }
   // rows above the least, and of the equal ones the first `want`
   int out = 0, equal = 0;
-  const bool some = A.budget > A.first + A.last;
-  for (int j0 = 0; j0 < n; j0 += kThreads) {
-    const int j = j0 + tid;
-    bool is_above = false, is_same = false;
-    if (j < n) {
-      if (j < A.first || j >= end) {
-        is_above = true;
-      } else if (some) {
-        const uint32_t x = weight(j);
-        is_above = x > least;
-        is_same = x == least;
-      }
-    }
-    const uint64_t ma = __ballot(is_above), ms = __ballot(is_same);
-    if (lane == 0) {
-      above[wave] = __popcll(ma);
-      same[wave] = __popcll(ms);
+  for (int j0 = 0; j0 < c.n; j0 += kRows) {
+    if (c.n > kRows) load(j0);
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (j0 + r * THREADS >= c.n) break;
+      const int j = j0 + r * THREADS + tid;
+      const bool mid = c.between(j);
+      const int a = __popcll(__ballot(j < c.n && (!mid || (some && x[r] > least))));
+      const int e = __popcll(__ballot(mid && some && x[r] == least));
+      if (lane == 0) sums[r * kWaves + wave] = make_int2(a, e);
     }
     __syncthreads();
-    int a = out, e = equal, all_a = 0, all_e = 0;
-    for (int w = 0; w < kWaves; ++w) {
-      if (w < wave) {
-        a += above[w];
-        e += same[w];
+    if (wave == 0) {  // to what is before each
+      int a = out, e = equal;
+      for (int i0 = 0; i0 < R * kWaves && j0 + i0 / kWaves * THREADS < c.n; i0 += 64) {
+        const int i = i0 + lane;
+        const int2 s = i < R * kWaves && j0 + i / kWaves * THREADS < c.n ? sums[i] : make_int2(0, 0);
+        const int2 u = make_int2(wave_sums(s.x), wave_sums(s.y));
+        if (i < R * kWaves) sums[i] = make_int2(a + u.x - s.x, e + u.y - s.y);
+        a += __builtin_amdgcn_readlane(u.x, 63);
+        e += __builtin_amdgcn_readlane(u.y, 63);
       }
-      all_a += above[w];
-      all_e += same[w];
+      if (lane == 0) {
+        found[0] = a;
+        found[1] = e;
+      }
     }
+    __syncthreads();
+    out = found[0];
+    equal = found[1];
     const uint64_t below = ((uint64_t)1 << lane) - 1;
-    a += __popcll(ma & below);                         // rows above the least before this one
-    e += __popcll(ms & below);                         // equal ones
-    if (is_above || (is_same && e < want)) rows[a + (e < want ? e : want)] = j;
-    out += all_a;
-    equal += all_e;
-    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (j0 + r * THREADS >= c.n) break;
+      const int j = j0 + r * THREADS + tid;
+      const bool mid = c.between(j), above = j < c.n && (!mid || (some && x[r] > least));
+      const bool same = mid && some && x[r] == least;
+      const uint64_t ma = __ballot(above), ms = __ballot(same);
+      const int2 s = sums[r * kWaves + wave];
+      const int a = s.x + __popcll(ma & below), e = s.y + __popcll(ms & below);
+      if (above || (same && e < want)) c.rows[a + (e < want ? e : want)] = j;
+    }
   }
-  if (lost) *A.err = kKvLostPage;
+  if (c.lost) *A.err = kKvLostPage;
+}
+
+// ------------------------------------------------------------------ long contexts
+// Each context is cut into stretches of kStretch rows with a workgroup each; a launch for each digit
+// writes a stretch's counts, and starts with the digit before it from the sum of all stretches'.
+constexpr int kStretch = kSelectStretch, kCut = 256, kEach = kStretch / kCut;
+constexpr int kDigits = kSelectDigits, kBins = kSelectBins;
+constexpr int shift_of(int d) { return d == 0 ? 23 : d == 1 ? 15 : d == 2 ? 7 : 0; }
+constexpr int bins_of(int d) { return d == 0 ? 512 : d == 3 ? 128 : 256; }
+
+// Stretch k of a sequence's and head's `cuts`, and what they have in the working memory.
+struct Cut {
+  int seq, head, k, cuts;
+  const KvSelectArgs& A;
+  int64_t first;  // of the head's stretches among all
+  __device__ __forceinline__ explicit Cut(const KvSelectArgs& a) : A(a) {
+    const int b = blockIdx.x, hkv = A.g.hkv;
+    int lo = 0, hi = A.n_seq;  // the last sequence whose stretches start at or before this one
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (A.spans[mid].cuts * hkv <= b) lo = mid; else hi = mid;
+    }
+    const KvSpan s = A.spans[lo];
+    seq = lo;
+    cuts = kv_select_cuts(s.ctx);
+    const int at = b - s.cuts * hkv;
+    head = at / cuts;
+    k = at - head * cuts;
+    first = (int64_t)s.cuts * hkv + (int64_t)head * cuts;
+  }
+  // the least number so far and what is wanted of those that agree with it, before digit d
+  __device__ __forceinline__ int* state(int d) const {
+    return A.work + ((int64_t)seq * A.g.hkv + head) * (2 * kDigits) + 2 * d;
+  }
+  // rows of the stretch above the digits so far
+  __device__ __forceinline__ int* above() const {
+    return A.work + (int64_t)A.n_seq * A.g.hkv * (2 * kDigits) + first;
+  }
+  // counts of a stretch, aligned to 16 bytes
+  __device__ __forceinline__ int* counts(int d, int k) const {
+    return A.work + (int64_t)A.n_seq * A.g.hkv * (2 * kDigits) + (A.cuts + 3) / 4 * 4 + ((first + k) * kDigits + d) * kBins;
+  }
+};
+
+// Calls f(bin, count) for the four bins of this thread's share of each of the stretches [0, cuts) of
+// digit d, eight loads on their way at a time.
+template <int D, class F>
+__device__ __forceinline__ void each_count(const Cut& w, int cuts, F f) {
+  constexpr int kQuads = bins_of(D) / 4, kSide = kCut / kQuads;
+  const int quad = threadIdx.x % kQuads;
+  for (int k0 = threadIdx.x / kQuads; k0 < cuts; k0 += 8 * kSide) {
+    int4 x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[i] = make_int4(0, 0, 0, 0);
+      if (k0 + i * kSide < cuts) x[i] = *(const int4*)(w.counts(D, k0 + i * kSide) + 4 * quad);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      f(4 * quad, x[i].x);
+      f(4 * quad + 1, x[i].y);
+      f(4 * quad + 2, x[i].z);
+      f(4 * quad + 3, x[i].w);
+    }
+  }
+}
+
+// Takes digit D of the least number from all stretches' counts.
+template <int D>
+__device__ __forceinline__ void settle(const Cut& w, int* count, int* part, int* found, int& want, uint32_t& least,
+                                       uint32_t& digit) {
+  for (int i = threadIdx.x; i < bins_of(D); i += kCut) count[i] = 0;
+  int sum[4] = {0, 0, 0, 0};
+  each_count<D>(w, w.cuts, [&](int bin, int n) { sum[bin & 3] += n; });
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) atomicAdd(&count[4 * (threadIdx.x % (bins_of(D) / 4)) + i], sum[i]);
+  __syncthreads();
+  reach<bins_of(D), kCut>(count, part, found, want, digit);
+  least |= digit << shift_of(D);
+}
+
+template <int DIGIT>
+__global__ __launch_bounds__(kCut) void k_kv_select_count(KvSelectArgs A) {
+  const int tid = threadIdx.x;
+  __shared__ int count[kBins], part[kCut / 64], found[2], more;
+  if (*A.plan.now != A.plan.id) {
+    if (tid == 0) *A.err = kKvOtherPlan;
+    return;
+  }
+  const Cut w(A);
+  const int k = w.k;
+  Context c(A, w.seq, w.head);
+  int want = A.budget - A.first - A.last;
+  if (c.n <= A.budget || want == 0) return;
+  uint32_t v[kEach];
+#pragma unroll
+  for (int r = 0; r < kEach; ++r) {
+    const int j = k * kStretch + r * kCut + tid;
+    v[r] = c.between(j) ? c.weight(j) : 0;
+  }
+  uint32_t least = 0;
+  if constexpr (DIGIT > 0) {
+    constexpr int kPast = DIGIT - 1;
+    uint32_t digit;
+    if (DIGIT > 1) {
+      least = (uint32_t)w.state(kPast)[0];
+      want = w.state(kPast)[1];
+    }
+    if (tid == 0) more = 0;
+    settle<kPast>(w, count, part, found, want, least, digit);
+    if (k == 0 && tid == 0) {
+      w.state(DIGIT)[0] = (int)least;
+      w.state(DIGIT)[1] = want;
+    }
+    int sum = 0;  // of this stretch's rows with larger values of it
+    for (int i = tid; i < bins_of(kPast) - 1 - (int)digit; i += kCut) sum += w.counts(kPast, k)[i];
+    if (sum) atomicAdd(&more, sum);
+    __syncthreads();
+    if (tid == 0) w.above()[k] = (DIGIT > 1 ? w.above()[k] : 0) + more;
+  }
+  constexpr int kShift = shift_of(DIGIT), kValues = bins_of(DIGIT);
+  for (int i = tid; i < kValues; i += kCut) count[i] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < kEach; ++r) {
+    const int j = k * kStretch + r * kCut + tid;
+    if (c.between(j) && (DIGIT == 0 || (v[r] ^ least) >> shift_of(DIGIT ? DIGIT - 1 : 0) == 0))
+      atomicAdd(&count[kValues - 1 - (int)(v[r] >> kShift & (kValues - 1))], 1);
+  }
+  __syncthreads();
+  for (int i = tid; i < kValues; i += kCut) w.counts(DIGIT, k)[i] = count[i];
+  if (c.lost) *A.err = kKvLostPage;
+}
+
+// The positions, after all digits.
+__global__ __launch_bounds__(kCut) void k_kv_select_write(KvSelectArgs A) {
+  constexpr int kWaves = kCut / 64, D = kDigits - 1;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ int count[kBins], part[kWaves], found[2], before[2];
+  __shared__ int2 sums[kEach * kWaves];
+  if (*A.plan.now != A.plan.id) {
+    if (tid == 0) *A.err = kKvOtherPlan;
+    return;
+  }
+  const Cut w(A);
+  const int k = w.k;
+  Context c(A, w.seq, w.head);
+  if (c.n <= A.budget) {
+    for (int i = k * kCut + tid; i < A.budget; i += w.cuts * kCut) c.rows[i] = i < c.n ? i : -1;
+    return;
+  }
+  int want = A.budget - A.first - A.last;
+  const bool some = want > 0;
+  const int j0 = k * kStretch;
+  uint32_t v[kEach];
+#pragma unroll
+  for (int r = 0; r < kEach; ++r) {
+    const int j = j0 + r * kCut + tid;
+    v[r] = c.between(j) && some ? c.weight(j) : 0;
+  }
+  uint32_t least = 0, digit = 0;
+  if (tid < 2) before[tid] = 0;
+  if (some) {
+    least = (uint32_t)w.state(D)[0];
+    want = w.state(D)[1];
+    settle<D>(w, count, part, found, want, least, digit);
+    // rows above the least, and equal ones, of the stretches before this one
+    const int bin = bins_of(D) - 1 - (int)digit;
+    int a = 0, e = 0;
+    each_count<D>(w, k, [&](int i, int n) {
+      a += i < bin ? n : 0;
+      e += i == bin ? n : 0;
+    });
+    if (tid < k) a += w.above()[tid];
+    if (a) atomicAdd(&before[0], a);
+    if (e) atomicAdd(&before[1], e);
+  }
+  __syncthreads();
+  // the first and last rows before this stretch
+  int out = before[0] + min(j0, A.first) + max(0, j0 - c.end), equal = before[1];
+  uint32_t is = 0;  // bits: above, and equal
+#pragma unroll
+  for (int r = 0; r < kEach; ++r) {
+    const int j = j0 + r * kCut + tid;
+    const bool mid = c.between(j);
+    const bool above = j < c.n && (!mid || (some && v[r] > least)), same = mid && some && v[r] == least;
+    is |= (above ? 1u : 0u) << r | (same ? 1u : 0u) << (16 + r);
+    const int a = __popcll(__ballot(above)), e = __popcll(__ballot(same));
+    if (lane == 0) sums[r * kWaves + wave] = make_int2(a, e);
+  }
+  __syncthreads();
+  if (wave == 0) {
+    static_assert(kEach * kWaves == 64);
+    const int2 s = sums[lane];
+    sums[lane] = make_int2(out + wave_sums(s.x) - s.x, equal + wave_sums(s.y) - s.y);
+  }
+  __syncthreads();
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+#pragma unroll
+  for (int r = 0; r < kEach; ++r) {
+    const bool above = is >> r & 1, same = is >> (16 + r) & 1;
+    const uint64_t ma = __ballot(above), ms = __ballot(same);
+    const int2 s = sums[r * kWaves + wave];
+    const int a = s.x + __popcll(ma & below), e = s.y + __popcll(ms & below);
+    if (above || (same && e < want)) c.rows[a + (e < want ? e : want)] = j0 + r * kCut + tid;
+  }
 }
 
 }  // namespace
 
 hipError_t launch_kv_select(const KvSelectArgs& a, hipStream_t stream) {
-  k_kv_select<<<a.n_seq * a.g.hkv, kThreads, 0, stream>>>(a);
+  const int n = a.n_seq * a.g.hkv;
+  if (a.work) {
+    k_kv_select_count<0><<<a.cuts, kCut, 0, stream>>>(a);
+    k_kv_select_count<1><<<a.cuts, kCut, 0, stream>>>(a);
+    k_kv_select_count<2><<<a.cuts, kCut, 0, stream>>>(a);
+    k_kv_select_count<3><<<a.cuts, kCut, 0, stream>>>(a);
+    k_kv_select_write<<<a.cuts, kCut, 0, stream>>>(a);
+  } else if (a.longest <= 4096) {
+    k_kv_select<256, 16><<<n, 256, 0, stream>>>(a);
+  } else if (a.longest <= 16384) {
+    k_kv_select<512, 32><<<n, 512, 0, stream>>>(a);
+  } else {
+    k_kv_select<1024, 32><<<n, 1024, 0, stream>>>(a);
+  }
   return hipGetLastError();
 }
 

@@ -59,63 +59,35 @@ struct Keys {
   }
 };
 
-// 32 query rows: their values, and of the 16 that a lane sums over the log of the sums (log2 units)
-// and whether they count.
-template <bool F8, int D>
-struct Rows {
-  s16x8 q[D / 16];
-  float l[16];
-  uint32_t on;
-  // rows `at` .. of the `n` of a kv head (token * G + head of the group), the first token q0
-  __device__ __forceinline__ void load(const KvWeighArgs& A, int q0, int head, int at, int n, int lane) {
-    const int r = at + (lane & 31), h = lane >> 5, G = A.g.G;
-    const int t = r / G, g = r - t * G;
-    const int16_t* p = (const int16_t*)A.q.p + (int64_t)(q0 + t) * A.q.tok + (int64_t)(head * G + g) * A.q.head;
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) {
-      s16x8 z = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (r < n) z = *(const s16x8*)(p + part_of<F8>(i, h));
-      q[i] = z;
-    }
-    on = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int y = at + key_of(i, h), u = y / G;
-      const float z = y < n ? A.lse[(int64_t)(q0 + u) * A.g.hq + head * G + y - u * G] : -__builtin_inff();
-      on |= (z != -__builtin_inff() ? 1u : 0u) << i;
-      l[i] = z * kLog2e;
-    }
-  }
-};
-
-// Bits of a lane's 16 rows from row `at` on that see key j; rows are tokens from position p0 on.
-__device__ __forceinline__ uint32_t seeing(const KvWeighArgs& A, int p0, int at, int h, int j) {
+// Bits of a lane's 16 rows that see key j; row i's token is at position pos(i).
+template <class Pos>
+__device__ __forceinline__ uint32_t seeing(const KvWeighArgs& A, int j, Pos pos) {
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const int pos = p0 + (at + key_of(i, h)) / A.g.G;
-    const bool in = j <= pos && (!A.window || j > pos - A.window || j < A.sinks);
+    const int p = pos(i);
+    const bool in = j <= p && (!A.window || j > p - A.window || j < A.sinks);
     m |= (in ? 1u : 0u) << i;
   }
   return m;
 }
 
-// The weights of a lane's key over the 16 rows in `on`.
-template <bool BF, bool F8, int D>
-__device__ __forceinline__ float add_up(const Keys<BF, F8, D>& k, const Rows<F8, D>& r, uint32_t on, float c) {
-  f32x16 s;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) s[i] = 0.0f;
-#pragma unroll
-  for (int t = 0; t < D / 16; ++t) s = Elem<BF>::mma(r.q[t], k.part(t), s);
+// Whether rows at positions p .. q may not see all the 32 keys from kb on.
+__device__ __forceinline__ bool cuts(const KvWeighArgs& A, int p, int q, int kb) {
+  return kb + 31 > p || (A.window && kb <= q - A.window && kb + 32 > A.sinks);
+}
+
+// The weights of a lane's key over 16 rows: scores s, the logs of the rows' sums (log2 units,
+// negated), those of the rows that are `on`.
+__device__ __forceinline__ float add_up(const f32x16& s, const float (&l)[16], uint32_t on, float c) {
   float sum = 0.0f;
   if (__all(on == 0xffffu)) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -r.l[i]));
+    for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, l[i]));
   } else {
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      sum += on >> i & 1 ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -r.l[i])) : 0.0f;
+      sum += on >> i & 1 ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, l[i])) : 0.0f;
   }
   return sum;
 }
@@ -125,89 +97,286 @@ __device__ __forceinline__ void put(const KvWeighArgs& A, uint32_t row, bool fre
   A.after[row] = (fresh ? 0.0f : A.before[row]) + x;
 }
 
+// Two waves take the key tiles of a run in turn: more of them, with one tile on its way each, keep more
+// bytes on their way than one with two, and start their stretches beside one another.
+constexpr int kSides = 2;
+
 template <bool BF, bool F8, int D>
-__global__ __launch_bounds__(64, 2) void k_kv_weigh_narrow(KvWeighArgs A) {
-  const int lane = threadIdx.x, n = lane & 31, h = lane >> 5;
-  const int run = run_of(blockIdx.x, A.n_narrow);
+__global__ __launch_bounds__(64, 3) void k_kv_weigh_narrow(KvWeighArgs A) {
+  const int lane = threadIdx.x, n = lane & 31, h = lane >> 5, G = A.g.G;
+  const int wave = run_of(blockIdx.x, A.n_narrow * kSides), run = wave / kSides, side = wave % kSides;
   int e = plan_at(A.narrow_at, run + 1), x = plan_at(A.narrow_at, run);
   if (other(A)) e = x;  // nothing to do
   bool any = false;     // a page outside the pool
   for (; x < e; ++x) {
     const KvSeg s = plan_at(A.narrow, x);
-    if (s.t0 >= s.t1) continue;
+    const int first = s.t0 + side;
+    if (first >= s.t1) continue;
     const int last = s.p0 + s.ntok - 1;  // a narrow tile has all new tokens of its sequence
     const int32_t* table = A.table + (int64_t)s.seq * A.cols;
+    const auto key = [&](int t) { return tile_key<kNarrowKeys>(s, t < s.t1 ? t : s.t1 - 1) + n; };
     const auto look = [&](int t) {
-      const int j = tile_key<kNarrowKeys>(s, t) + n;
+      const int j = key(t);
       return table[(j < last ? j : last) >> A.g.sh];
     };
-    Rows<F8, D> rows;
-    rows.load(A, s.q0, s.head, 0, s.ntok * A.g.G, lane);
-    Keys<BF, F8, D> next;
+    Keys<BF, F8, D> k;
     bool lost;
-    uint32_t row = pool_row(A, look(s.t0), s.head, tile_key<kNarrowKeys>(s, s.t0) + n, lost);
-    next.load(A, row, h);
-    int32_t page = look(s.t0 + 1 < s.t1 ? s.t0 + 1 : s.t0);
-    for (int t = s.t0; t < s.t1; ++t) {
-      const Keys<BF, F8, D> k = next;
-      const uint32_t at = row;
-      const bool gone = lost;
-      const int kb = tile_key<kNarrowKeys>(s, t), j = kb + n;
-      if (t + 1 < s.t1) {
-        row = pool_row(A, page, s.head, tile_key<kNarrowKeys>(s, t + 1) + n, lost);
-        next.load(A, row, h);
-        if (t + 2 < s.t1) page = look(t + 2);
+    uint32_t row = pool_row(A, look(first), s.head, key(first), lost);
+    int32_t page = look(first + kSides);
+    k.load(A, row, h);
+    s16x8 q[D / 16];
+    float l[16];
+    uint32_t rows = 0;
+    {
+      const int t = n / G, g = n - t * G;
+      const int16_t* p = (const int16_t*)A.q.p + (int64_t)(s.q0 + t) * A.q.tok + (int64_t)(s.head * G + g) * A.q.head;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        s16x8 z = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (t < s.ntok) z = *(const s16x8*)(p + part_of<F8>(i, h));
+        q[i] = z;
       }
-      const bool masked = kb + kNarrowKeys - 1 > s.p0 || (A.window && kb <= last - A.window && kb + kNarrowKeys > A.sinks);
-      const uint32_t on = masked ? rows.on & seeing(A, s.p0, 0, h, j) : rows.on;
-      const float sum = add_halves(add_up<BF, F8, D>(k, rows, on, A.scale));
+      float z = -__builtin_inff();
+      if (t < s.ntok) z = A.lse[(int64_t)(s.q0 + t) * A.g.hq + s.head * G + g];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float y = __shfl(z, key_of(i, h));
+        rows |= (y != -__builtin_inff() ? 1u : 0u) << i;
+        l[i] = -y * kLog2e;
+      }
+    }
+    for (int t = first; t < s.t1; t += kSides) {
+      const int kb = tile_key<kNarrowKeys>(s, t), j = kb + n;
+      const uint32_t at = row;
+      const bool gone = lost, fresh = j >= s.p0, mine = h == 0 && j <= last && !gone;
+      const float old = mine && !fresh ? A.before[at] : 0.0f;
+      f32x16 sc;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) sc = Elem<BF>::mma(q[i], k.part(i), sc);
+      row = pool_row(A, page, s.head, key(t + kSides), lost);
+      k.load(A, row, h);  // past the last tile: that one again
+      page = look(t + 2 * kSides);
+      uint32_t on = rows;
+      if (cuts(A, s.p0, last, kb)) {
+        const int half = here(h);  // nothing of this is made before: registers
+        on &= seeing(A, j, [&](int i) { return s.p0 + key_of(i, half) / G; });
+      }
+      const float sum = add_halves(add_up(sc, l, on, A.scale));
       any |= gone && j <= last;
-      if (h == 0 && j <= last && !gone) put(A, at, j >= s.p0, sum);
+      if (mine) A.after[at] = old + sum;
     }
   }
   if (any) *A.err = kKvLostPage;
 }
 
-// One workgroup per kWeighKeys keys of a sequence and kv head, a wave per 32 of them.
-template <bool BF, bool F8, int D>
-__global__ __launch_bounds__(2 * kWeighKeys, 2) void k_kv_weigh_wide(KvWeighArgs A) {
-  const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int head = blockIdx.x % A.g.hkv, block = blockIdx.x / A.g.hkv;
+// A row of a kv head as token and head of the group, and the row 32 further on.
+struct Place {
+  int t, g;
+  static __device__ __forceinline__ Place of(int row, int G) { return Place{row / G, row % G}; }
+  __device__ __forceinline__ void next(int G, int step, int rest) {
+    t += step;
+    g += rest;
+    if (g >= G) {
+      g -= G;
+      ++t;
+    }
+  }
+};
+
+// One workgroup per kWeighKeys keys of a sequence and kv head, KF * 32 of them for a wave, whose
+// part of K stays in its registers; 32 rows of Q at a time are in LDS for all waves.  Bound by the
+// exponentials: one for a weight, at a quarter of the vector unit's rate.
+template <bool BF, bool F8, int D, int KF>
+__global__ __launch_bounds__(2 * kWeighKeys / KF, 2) void k_kv_weigh_wide(KvWeighArgs A) {
+  constexpr int kThreads = 2 * kWeighKeys / KF, kChunks = D / 8, kStep = kThreads / kChunks;
+  constexpr int I = (32 + kStep - 1) / kStep;  // loads of a thread for 32 rows
+  struct alignas(16) Block {
+    char q[32 * kRowK<D>];
+    float l[32];
+    int tok[32];
+    uint32_t on;
+  };
+  __shared__ Block block[3];
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5, G = A.g.G;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int head = blockIdx.x % A.g.hkv, b = blockIdx.x / A.g.hkv;
   if (other(A)) return;
   // the last sequence that starts at or before this block: those of its start before it have none
   int lo = 0, hi = A.n_seq;
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
-    if (plan_at(A.spans, mid).blocks <= block) lo = mid; else hi = mid;
+    if (plan_at(A.spans, mid).blocks <= b) lo = mid; else hi = mid;
   }
   const KvSpan s = plan_at(A.spans, lo);
-  const int kb = (block - s.blocks) * kWeighKeys + wave * 32, base = s.ctx - s.q_len, G = A.g.G;
-  if (kb >= s.ctx) return;
-  const int j = kb + n, last = s.ctx - 1;
-  bool lost;
-  const uint32_t row = pool_row(A, A.table[(int64_t)lo * A.cols + ((j < last ? j : last) >> A.g.sh)], head, j, lost);
-  Keys<BF, F8, D> k;
-  k.load(A, row, h);
-  // tokens that see some of the keys, from the first one's on
-  int t0 = kb > base ? kb - base : 0, t1 = s.q_len;
+  const int kb0 = (b - s.blocks) * kWeighKeys, base = s.ctx - s.q_len, last = s.ctx - 1;
+  const int kb = kb0 + wave * 32 * KF;
+  // tokens that see some of the workgroup's keys
+  int t0 = kb0 > base ? kb0 - base : 0, t1 = s.q_len;
   if (base + t0 < 0) t0 = -base;
-  if (A.window && kb >= A.sinks) t1 = min(t1, A.window + (kb - base + 31));
-  float sum = 0.0f;
-  for (int at = t0 * G; at < t1 * G; at += 32) {
-    Rows<F8, D> rows;
-    rows.load(A, s.q0, head, at, t1 * G, lane);
-    const int p = base + at / G, q = base + (at + 31) / G;
-    const bool masked = kb + 31 > p || (A.window && kb <= q - A.window && kb + 32 > A.sinks);
-    const uint32_t on = masked ? rows.on & seeing(A, base, at, h, j) : rows.on;
-    sum += add_up<BF, F8, D>(k, rows, on, A.scale);
+  if (A.window && kb0 >= A.sinks) t1 = min(t1, A.window + (kb0 - base + kWeighKeys - 1));
+  // rows of Q: this thread's chunks of them, and for the first wave the log of a row's sum
+  const int r0 = tid / kChunks, c = tid % kChunks, step = 32 / G, rest = 32 % G, end = t1 * G;
+  const bool loads = kStep <= 32 || r0 < 32;
+  uint4 x[I];
+  float z = 0.0f;
+  Place at[I], mine = Place::of(t0 * G + n, G);
+  const int16_t* from[I];
+  const int64_t ahead = step * A.q.tok + rest * A.q.head, wrap = A.q.tok - G * A.q.head;
+#pragma unroll
+  for (int i = 0; i < I; ++i) {
+    at[i] = Place::of(t0 * G + r0 + i * kStep, G);
+    from[i] = (const int16_t*)A.q.p + (int64_t)(s.q0 + at[i].t) * A.q.tok + (int64_t)(head * G + at[i].g) * A.q.head + c * 8;
   }
-  sum = add_halves(sum);
-  if (j > last || h) return;
-  if (lost)
-    *A.err = kKvLostPage;
-  else
-    put(A, row, j >= base, sum);
+  int z_tok = 0;
+  const auto fetch = [&]() {
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      x[i] = make_uint4(0, 0, 0, 0);
+      if (loads && at[i].t < t1) x[i] = *(const uint4*)from[i];
+      const bool over = at[i].g + rest >= G;
+      from[i] += ahead + (over ? wrap : 0);
+      at[i].next(G, step, rest);
+    }
+    if (wave == 0) {
+      z = mine.t < t1 ? A.lse[(int64_t)(s.q0 + mine.t) * A.g.hq + head * G + mine.g] : -__builtin_inff();
+      z_tok = mine.t;
+      mine.next(G, step, rest);
+    }
+  };
+  const auto store = [&](Block& to) {
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+      if (loads) *(uint4*)(to.q + (r0 + i * kStep) * kRowK<D> + c * 16) = x[i];
+    if (wave == 0) {
+      const uint64_t on = __ballot(z != -__builtin_inff());
+      if (h == 0) {
+        to.l[n] = -z * kLog2e;
+        to.tok[n] = z_tok;
+      }
+      if (lane == 0) to.on = (uint32_t)on;
+    }
+  };
+  s16x8 k[KF][D / 16];
+  uint32_t row[KF];
+  bool lost[KF];
+  float sum[KF];
+#pragma unroll
+  for (int f = 0; f < KF; ++f) {
+    const int j = kb + 32 * f + n;
+    row[f] = pool_row(A, A.table[(int64_t)lo * A.cols + ((j < last ? j : last) >> A.g.sh)], head, j, lost[f]);
+    Keys<BF, F8, D> y;
+    y.load(A, row[f], h);
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) k[f][t] = y.part(t);
+    sum[f] = 0.0f;
+  }
+  const int blocks = (end - t0 * G + 31) / 32;
+  Place first = Place::of(t0 * G, G), final = Place::of(t0 * G + 31, G);  // rows of a block
+  const auto part = [&](const Block& q, int t) {
+    return *(const s16x8*)(q.q + n * kRowK<D> + part_of<F8>(t, h) * 2);
+  };
+  const auto score = [&](const Block& q, f32x16 (&sc)[KF]) {
+#pragma unroll
+    for (int f = 0; f < KF; ++f)
+#pragma unroll
+      for (int y = 0; y < 16; ++y) sc[f][y] = 0.0f;
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) {
+      const s16x8 p = part(q, t);
+#pragma unroll
+      for (int f = 0; f < KF; ++f) sc[f] = Elem<BF>::mma(p, k[f][t], sc[f]);
+    }
+  };
+  fetch();
+  store(block[0]);
+  fetch();
+  store(block[1]);
+  fetch();
+  lds_barrier();
+  const bool works = kb <= last && blocks > 0;
+  f32x16 sa[KF], sb[KF];
+  if (works) score(block[0], sa);
+  int b0 = 0, b1 = 1, b2 = 2;
+  // one block: the scores of the next rows, `next`, beside the exponentials of these, `sc`
+  const auto go = [&](f32x16 (&sc)[KF], f32x16 (&next)[KF]) {
+    store(block[b2]);
+    fetch();
+    if (works) {
+      const Block &q = block[b0], &qn = block[b1];
+      const int p0 = base + first.t, p1 = base + final.t;
+      float l[16];
+#pragma unroll
+      for (int y = 0; y < 16; y += 4) {
+        const f32x4 v = *(const f32x4*)(q.l + key_of(y, h));
+#pragma unroll
+        for (int w = 0; w < 4; ++w) l[y + w] = v[w];
+      }
+      const uint32_t rows = (uint32_t)__builtin_amdgcn_readfirstlane((int)q.on);
+      if (rows == ~0u && !cuts(A, p0, p1, kb + 32 * (KF - 1)) && !cuts(A, p0, p1, kb)) {
+        float add[KF];
+        s16x8 p[kAhead];
+#pragma unroll
+        for (int t = 0; t < kAhead; ++t) p[t] = part(qn, t);
+#pragma unroll
+        for (int f = 0; f < KF; ++f) {
+          add[f] = 0.0f;
+#pragma unroll
+          for (int y = 0; y < 16; ++y) next[f][y] = 0.0f;
+        }
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) {
+          constexpr int kExps = 16 / (D / 16);
+#pragma unroll
+          for (int f = 0; f < KF; ++f) next[f] = Elem<BF>::mma(p[t % kAhead], k[f][t], next[f]);
+          if (t + kAhead < D / 16) p[t % kAhead] = part(qn, t + kAhead);
+#pragma unroll
+          for (int f = 0; f < KF; ++f) {
+#pragma unroll
+            for (int y = t * kExps; y < (t + 1) * kExps; ++y)
+              add[f] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[f][y], A.scale, l[y]));
+            add[f] = here(add[f]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int f = 0; f < KF; ++f) sum[f] += add[f];
+      } else {
+        const int half = here(h);  // nothing of this is made before
+        uint32_t on = 0;
+#pragma unroll
+        for (int y = 0; y < 16; ++y) on |= (rows >> key_of(y, half) & 1) << y;
+#pragma unroll
+        for (int f = 0; f < KF; ++f) {
+          const uint32_t m = on & seeing(A, kb + 32 * f + n, [&](int y) { return base + q.tok[key_of(y, half)]; });
+          sum[f] += add_up(sc[f], l, m, A.scale);
+        }
+        score(qn, next);
+      }
+    }
+    first.next(G, step, rest);
+    final.next(G, step, rest);
+    const int z = b0;
+    b0 = b1;
+    b1 = b2;
+    b2 = z;
+    lds_barrier();
+  };
+  for (int i = 0; i < blocks; i += 2) {
+    go(sa, sb);
+    if (i + 1 < blocks) go(sb, sa);
+  }
+#pragma unroll
+  for (int f = 0; f < KF; ++f) {
+    const int j = kb + 32 * f + n;
+    const float y = add_halves(sum[f]);
+    if (j > last || h) continue;
+    if (lost[f])
+      *A.err = kKvLostPage;
+    else
+      put(A, row[f], j >= base, y);
+  }
 }
 
 // `before` to `after` for the context of the sequences with new tokens, one workgroup for each
@@ -230,8 +399,12 @@ __global__ __launch_bounds__(256) void k_kv_weigh_copy(KvWeighArgs A) {
 template <bool BF, bool F8, int D>
 hipError_t run(const KvWeighArgs& a, hipStream_t stream) {
   if (a.window && a.before != a.after) k_kv_weigh_copy<<<a.n_seq * a.g.hkv, 256, 0, stream>>>(a);
-  if (a.n_narrow) k_kv_weigh_narrow<BF, F8, D><<<a.n_narrow, 64, 0, stream>>>(a);
-  if (a.n_wide) k_kv_weigh_wide<BF, F8, D><<<a.n_wide * a.g.hkv, 2 * kWeighKeys, 0, stream>>>(a);
+  if (a.n_narrow) k_kv_weigh_narrow<BF, F8, D><<<a.n_narrow * kSides, 64, 0, stream>>>(a);
+  // Few workgroups: eight waves of 32 keys each.
+  if (a.n_wide * a.g.hkv > 256)
+    k_kv_weigh_wide<BF, F8, D, 2><<<a.n_wide * a.g.hkv, kWeighKeys, 0, stream>>>(a);
+  else if (a.n_wide)
+    k_kv_weigh_wide<BF, F8, D, 1><<<a.n_wide * a.g.hkv, 2 * kWeighKeys, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -124,12 +124,12 @@ def test_stretches_of_trees_hold_what_each_token_sees(lib, seed):
     x = Handle(lib, max_seqs=len(q_len), max_tokens=sum(q_len), hq=hkv * G, hkv=hkv, S=S)
     assert x.plan(q_len, ctx, sum(par, []), window, sinks) == 0, lib.lar_kv_error_string(x.h)
     assert x.attend() == 0
-    spans = x.trees(0, 6 * len(q_len)).reshape(-1, 6)
+    spans = x.trees(0, 7 * len(q_len)).reshape(-1, 7)
     waves, _ = x.trees(4)
     segs, at, joins = x.trees(1).reshape(-1, 10), x.trees(2), x.trees(3).reshape(-1, 8)
     K, rows = (32 if waves in (0, 1) else 64), 32 * int(waves)
     eff = window if window < max(c for c, n in zip(ctx, q_len) if n) else 0
-    words = x.trees(5, int(sum(n * (w + 1) for n, (*_, t, w, _) in zip(q_len, spans) if t >= 0)) + 1).view(np.uint32)
+    words = x.trees(5, int(sum(n * (w + 1) for n, (*_, t, w, _, _) in zip(q_len, spans) if t >= 0)) + 1).view(np.uint32)
     assert len(at) == 0 or (at[0] == 0 and at[-1] == len(segs) and (np.diff(at) >= 0).all() and len(at) - 1 <= 2048)
     slots, parts, q0 = set(), {}, 0
     for s, (n, c, p) in enumerate(zip(q_len, ctx, par)):
