@@ -337,15 +337,18 @@ void deal(const std::vector<Tile>& tiles, int groups, const KvGeom& g, KvSeg* se
 // batches end sooner with both at work (mixed batch of 3839 tokens: 387 us one after the other,
 // 293 together).  Where the two bounds of the narrow ones meet they take more than either: a sum
 // of sixth powers (mixed batch: 298 us with the larger of the two).
-int split(const std::vector<Tile>& narrow, const std::vector<Tile>& wide, int groups, const KvGeom& g) {
+int split(const std::vector<Tile>& narrow, const std::vector<Tile>& wide, int groups, const KvGeom& g, bool trees) {
   if (wide.empty()) return 0;
   // microseconds: of a wide key tile and a stretch's start and end, of a narrow one among a
   // CU's eight waves (255 tokens beside 7 chunks of 512 with heads of 64: 161 us, 182 with a time
   // 1.6 times less; 40 tokens beside them: 92 and 103); bytes of a narrow one
   const double wt = g.D == 128 ? 2.1 : 1.35, ws = 8.0, nt = g.D == 128 ? 3.4 : 2.7;
   const double nb = 2.0 * kNarrowKeys * g.D * (g.cache == kKvE4m3 ? 1 : 2), rate = 5.2e6;
-  int64_t w = 0, n = 0;
-  for (const Tile& t : wide) w += t.tiles;
+  int64_t n = 0;
+  // Tiles of trees have fewer rows, and their loads to wait for (125 trees of 5 to 31 tokens over
+  // 1.2k keys each: 168 us, 200 with the time of a full one).
+  double w = 0;
+  for (const Tile& t : wide) w += t.tiles * (trees ? 0.5 + 0.5 * (t.s.ntok * g.G) / kWideRows : 1.0);
   for (const Tile& t : narrow) n += t.tiles;
   int best = groups / 2;
   double least = 1e300;
@@ -422,13 +425,9 @@ void release(lar_kv* kv) {
 int tree_block(int32_t ctx, int32_t n) { return std::max(0, ctx - n) >> 5; }
 int tree_words(int32_t ctx, int32_t n) { return ((ctx - 1) >> 5) - tree_block(ctx, n) + 1; }
 
-// Tokens of trees in a plan at most, the words of their records, and the query tiles: with four
-// waves or more a tree may have several.
+// Tokens of trees in a plan at most, and the words of their records.
 int64_t tree_tokens(const lar_kv_config& cfg) { return std::min(cfg.max_tokens, kTreeTokens); }
 int64_t tree_room(const lar_kv_config& cfg) { return tree_tokens(cfg) * (kMaxTree / 32 + 3); }
-int64_t tree_tiles(const lar_kv_config& cfg, const KvGeom& g) {
-  return (std::min<int64_t>(cfg.max_seqs, tree_tokens(cfg)) + tree_tokens(cfg) / (128 / g.G)) * g.hkv;
-}
 
 // The trees of a batch: which sequences have one, and each token's place.
 struct Trees {
@@ -438,18 +437,6 @@ struct Trees {
   int64_t tokens = 0;          // of all trees
   int32_t most = 0;            // tokens of the largest
 };
-
-// Waves of a workgroup of the tree kernel, each with 32 rows of a query tile: as many as the largest
-// tree has rows for.
-constexpr int kTreeWavesPerCu = 8;
-int tree_waves(const Trees& t, const KvGeom& g) {
-  int w = 1;
-  while (w < 8 && 32 * w < t.most * g.G) w *= 2;
-  return w;
-}
-int tree_keys(int waves) { return waves == 1 ? 32 : 64; }
-
-int tree_least(const std::vector<Tile>&, const KvGeom&) { return 2; }
 
 // Takes the parents in; a sequence whose tokens follow one another has no tree.
 lar_status take_parents(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t* ctx_len, int64_t T,
@@ -558,12 +545,10 @@ lar_status plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t*
   const KvGeom& g = kv->g;
   KvTok* tok = (KvTok*)(p + KvLayout().tok);
   int32_t n_narrow = 0, n_wide = 0, n_join = 0, join_rows = 0, most_parts = 0;
-  int32_t n_tree = 0, n_tree_waves = 0, n_tree_join = 0, tree_join_rows = 0, tree_most_parts = 0;
   int64_t blocks = 0, cuts = 0;
   kv->planned = false;
   try {
-    std::vector<Tile> narrow, wide, none, tree;
-    const int waves = tree_waves(trees, g), runs = kv->cus * kTreeWavesPerCu / waves;
+    std::vector<Tile> narrow, wide, none;
     const int nt = kNarrowRows / g.G, wt = kWideRows / g.G;
     int64_t q0 = 0;
     for (int s = 0; s < n_seqs; ++s) {
@@ -571,8 +556,8 @@ lar_status plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t*
       const int64_t p0 = (int64_t)ctx_len[s] - n;
       for (int r = 0; r < n; ++r) tok[q0 + r] = KvTok{s, (int32_t)(p0 + r)};
       if (!n) continue;
-      const bool has = trees.most && trees.words[s], small = !has && n <= nt;
-      const int per = has ? 32 * waves / g.G : small ? n : wt;
+      const bool has = trees.most && trees.words[s], small = n <= nt;
+      const int per = small ? n : wt;
       for (int h = 0; h < g.hkv; ++h)
         for (int r = 0; r < n; r += per) {
           Tile t{};
@@ -586,9 +571,8 @@ lar_status plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t*
             for (int i = 0; i < t.s.ntok; ++i) low = std::min<int64_t>(low, trees.place[q0 + r + i]);
             low = std::min(low, p0 + window - 1);
           }
-          const int K = has ? tree_keys(waves) : small ? kNarrowKeys : kWideKeys;
-          t.tiles = key_tiles(p0 + r, t.s.ntok, K, window, sinks, low, &t.s.ns, &t.s.fw);
-          (has ? tree : !t.tiles ? none : small ? narrow : wide).push_back(t);
+          t.tiles = key_tiles(p0 + r, t.s.ntok, small ? kNarrowKeys : kWideKeys, window, sinks, low, &t.s.ns, &t.s.fw);
+          (t.tiles ? small ? narrow : wide : none).push_back(t);
         }
       q0 += n;
     }
@@ -597,25 +581,16 @@ lar_status plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t*
     const int64_t nn = (int64_t)narrow.size(), nw = (int64_t)wide.size();
     const KvLayout L(T, nn ? nn + kv->waves : 0, nw ? nw + 2 * kv->groups : 0, kv->waves, kv->groups,
                    std::min<int64_t>(nn, kv->waves) + std::min<int64_t>(nw, kv->groups) * (kWideRows / 32) + kJoins8,
-                   n_seqs, trees.room, tree.empty() ? 0 : (int64_t)tree.size() + runs, tree.empty() ? 0 : runs,
-                   tree.empty() ? 0 : runs * waves + kJoins8);
+                   n_seqs, trees.room);
     if (L.end > kv->cap) return fail(kv, LAR_E_CAPACITY, "plan of %zu bytes, room for %zu", L.end, kv->cap);
     kv->lay = L;
     Joins join{g.G};
-    const int groups = nn ? split(narrow, wide, kv->groups, g) : kv->groups;
+    const int groups = nn ? split(narrow, wide, kv->groups, g, trees.most > 0) : kv->groups;
     cut(narrow, nw ? (kv->groups - groups) * kWideWaves : kv->waves, narrow_least(narrow, g), (KvSeg*)(p + L.narrow),
         (int32_t*)(p + L.narrow_at), &n_narrow, &join);
     deal(wide, groups, g, (KvSeg*)(p + L.wide), (int32_t*)(p + L.wide_at), &n_wide, &join);
     n_join = join.write((KvJoin*)(p + L.join), &join_rows);
     most_parts = join.most;
-    if (!tree.empty()) {
-      Joins parts{g.G};
-      cut(tree, runs, tree_least(tree, g), (KvSeg*)(p + L.tree), (int32_t*)(p + L.tree_at), &n_tree, &parts);
-      for (KvJoin& j : parts.tiles) j.wide = waves > 1;
-      n_tree_join = parts.write((KvJoin*)(p + L.tree_join), &tree_join_rows);
-      tree_most_parts = parts.most;
-      n_tree_waves = waves;
-    }
     KvSpan* span = (KvSpan*)(p + L.spans);
     int64_t rec = 0;
     q0 = 0;
@@ -652,11 +627,7 @@ lar_status plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t*
   kv->max_pages = (int32_t)pages;
   kv->all_pages = (int32_t)all_pages;
   kv->longest = all_longest;
-  kv->n_tree = n_tree;
-  kv->tree_waves = n_tree_waves;
-  kv->n_tree_join = n_tree_join;
-  kv->tree_join_rows = tree_join_rows;
-  kv->tree_most_parts = tree_most_parts;
+  kv->trees = trees.most > 0;
   kv->blocks = blocks;
   kv->cuts = cuts;
   kv->window = window;
@@ -713,8 +684,7 @@ lar_status lar_kv_create(lar_kv** out, const lar_kv_config* cfg) {
   const int64_t wide = (std::min<int64_t>(cfg->max_seqs, cfg->max_tokens / (nt + 1)) + cfg->max_tokens / wt) * g.hkv;
   kv->cap = KvLayout(cfg->max_tokens, narrow + kv->waves, wide + narrow + 2 * kv->groups, kv->waves, kv->groups,
                    std::min<int64_t>(narrow, kv->waves) + std::min<int64_t>(wide + narrow, kv->groups) * (kWideRows / 32) + kJoins8,
-                     cfg->max_seqs, tree_room(*cfg), tree_tiles(*cfg, g) + kv->cus * kTreeWavesPerCu,
-                     kv->cus * kTreeWavesPerCu, kv->cus * kTreeWavesPerCu + kJoins8).end;
+                     cfg->max_seqs, tree_room(*cfg)).end;
   // every wave or workgroup has two stretches at most that are parts of a tile
   bool ok = hipMalloc((void**)&kv->dev, kv->cap) == hipSuccess &&
             hipMalloc((void**)&kv->narrow_o, sizeof(float) * 2 * kv->waves * kNarrowRows * g.D) == hipSuccess &&
@@ -830,17 +800,8 @@ lar_status lar_kv_attend(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_row
   a.narrow_ml = kv->narrow_ml;
   a.wide_ml = kv->wide_ml;
   a.err = kv->err;
-  a.wide_rows = kWideRows;
   a.spans = (const KvSpan*)(kv->dev + kv->lay.spans);
-  a.trees = (const uint32_t*)(kv->dev + kv->lay.trees);
-  a.tree = (const KvSeg*)(kv->dev + kv->lay.tree);
-  a.tree_at = (const int32_t*)(kv->dev + kv->lay.tree_at);
-  a.n_tree = kv->n_tree;
-  a.tree_waves = kv->tree_waves;
-  a.tree_join = (const KvJoin*)(kv->dev + kv->lay.tree_join);
-  a.n_tree_join = kv->n_tree_join;
-  a.tree_join_rows = kv->tree_join_rows;
-  a.tree_most_parts = kv->tree_most_parts;
+  a.trees = kv->trees ? (const uint32_t*)(kv->dev + kv->lay.trees) : nullptr;
   return launch(kv, launch_kv_attend, a);
 }
 

@@ -19,7 +19,8 @@
 //   k_kv_wide    eight waves, 256 rows, 64-key tiles in LDS for all of them: chunks.
 //                Bound by the matrix instructions and the exponentials beside them.
 //   k_kv_join    the partial sums of the tiles whose keys were split over waves.
-// A batch with both kinds of tiles is one launch of k_kv_wide.
+// A batch with both kinds of tiles is one launch of k_kv_wide; one with trees of drafted tokens has
+// kernels of its own (kv_tree.hip) before the join.
 //
 // For the second product P has to be of V's 16-bit type.  Single tokens on a 16-bit cache have
 // matrix instructions to spare: each weight is taken as two such values, 16 bits in all.  (On an
@@ -371,7 +372,7 @@ __global__ __launch_bounds__(THREADS) void k_kv_join(KvAttendArgs A) {
   __shared__ Part parts[THREADS];
   const KvJoin j = plan_at(A.join, blockIdx.x);
   if (other_plan(A)) return;
-  const int rows = j.wide ? A.wide_rows : kNarrowRows, row0 = j.row0;
+  const int rows = j.wide ? kWideRows : kNarrowRows, row0 = j.row0;
   const int have = j.ntok * A.g.G - row0 < A.join_rows ? j.ntok * A.g.G - row0 : A.join_rows;
   const float* po = j.wide ? A.wide_o : A.narrow_o;
   const float4* pml = j.wide ? A.wide_ml : A.narrow_ml;
@@ -429,7 +430,9 @@ __global__ __launch_bounds__(THREADS) void k_kv_join(KvAttendArgs A) {
 
 template <bool BF, bool F8, int D>
 hipError_t run(const KvAttendArgs& a, hipStream_t stream) {
-  if (a.n_wide) {
+  if (a.trees) {
+    if (const hipError_t e = launch_kv_tree(a, stream)) return e;
+  } else if (a.n_wide) {
     const dim3 grid(a.n_wide + (a.n_narrow + kWideWaves - 1) / kWideWaves);
     if (a.lse)
       k_kv_wide<BF, F8, D, true><<<grid, 64 * kWideWaves, 0, stream>>>(a);
@@ -438,7 +441,14 @@ hipError_t run(const KvAttendArgs& a, hipStream_t stream) {
   } else if (a.n_narrow) {
     k_kv_narrow<BF, F8, D><<<a.n_narrow, 64, 0, stream>>>(a);
   }
-  return launch_kv_join(a, stream);
+  // Many parts: more threads to share them out to (40 tokens of 8 heads over 4000 keys, 16
+  // parts of each tile: 15.4 us with 1024 threads, 19.3 with 256); few parts of many tiles:
+  // smaller workgroups (255 decode tokens take 1.5 % more with 1024).
+  if (a.n_join && a.most_parts > 8)
+    k_kv_join<BF, D, 1024><<<a.n_join, 1024, 0, stream>>>(a);
+  else if (a.n_join)
+    k_kv_join<BF, D, 256><<<a.n_join, 256, 0, stream>>>(a);
+  return hipGetLastError();
 }
 
 template <bool BF, bool F8>
@@ -446,37 +456,12 @@ hipError_t run_d(const KvAttendArgs& a, hipStream_t stream) {
   return a.g.D == 128 ? run<BF, F8, 128>(a, stream) : run<BF, F8, 64>(a, stream);
 }
 
-template <bool BF, int D>
-void join(const KvAttendArgs& a, hipStream_t stream) {
-  // Many parts: more threads to share them out to (40 tokens of 8 heads over 4000 keys, 16
-  // parts of each tile: 15.4 us with 1024 threads, 19.3 with 256); few parts of many tiles:
-  // smaller workgroups (255 decode tokens take 1.5 % more with 1024).
-  if (a.most_parts > 8)
-    k_kv_join<BF, D, 1024><<<a.n_join, 1024, 0, stream>>>(a);
-  else
-    k_kv_join<BF, D, 256><<<a.n_join, 256, 0, stream>>>(a);
-}
-
 }  // namespace
 
 hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t stream) {
   const bool f8 = a.g.cache == kKvE4m3;
-  hipError_t e;
-  if (a.g.dtype == kKvBf16)
-    e = f8 ? run_d<true, true>(a, stream) : run_d<true, false>(a, stream);
-  else
-    e = f8 ? run_d<false, true>(a, stream) : run_d<false, false>(a, stream);
-  return e == hipSuccess && a.n_tree ? launch_kv_tree(a, stream) : e;
-}
-
-hipError_t launch_kv_join(const KvAttendArgs& a, hipStream_t stream) {
-  const bool bf = a.g.dtype == kKvBf16;
-  if (!a.n_join) return hipGetLastError();
-  if (a.g.D == 128)
-    bf ? join<true, 128>(a, stream) : join<false, 128>(a, stream);
-  else
-    bf ? join<true, 64>(a, stream) : join<false, 64>(a, stream);
-  return hipGetLastError();
+  if (a.g.dtype == kKvBf16) return f8 ? run_d<true, true>(a, stream) : run_d<true, false>(a, stream);
+  return f8 ? run_d<false, true>(a, stream) : run_d<false, false>(a, stream);
 }
 
 }  // namespace lar

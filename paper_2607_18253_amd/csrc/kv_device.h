@@ -120,16 +120,8 @@ struct KvAttendArgs {
   float *narrow_o, *wide_o;            // partial sums of a slot's rows
   float4 *narrow_ml, *wide_ml;         // [slot][rows]: scale of the weights (log2 units) and sums
   int32_t* err;
-  int32_t wide_rows;                   // rows of a slot of wide_o
-  // The query tiles of sequences with trees, of 32 * tree_waves rows; they have the slots of the
-  // narrow ones once these are joined.
   const KvSpan* spans;                 // [n_seqs]
-  const uint32_t* trees;               // records
-  const KvSeg* tree;
-  const int32_t* tree_at;              // [n_tree + 1] stretches of each workgroup
-  int32_t n_tree, tree_waves;
-  const KvJoin* tree_join;
-  int32_t n_tree_join, tree_join_rows, tree_most_parts;
+  const uint32_t* trees;               // records; null: no sequence has a tree
 };
 
 struct KvCopyArgs {
@@ -197,7 +189,6 @@ struct KvKeepArgs {
 hipError_t launch_kv_append(const KvCopyArgs& a, hipStream_t stream);
 hipError_t launch_kv_read(const KvCopyArgs& a, hipStream_t stream);
 hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t stream);
-hipError_t launch_kv_join(const KvAttendArgs& a, hipStream_t stream);
 hipError_t launch_kv_tree(const KvAttendArgs& a, hipStream_t stream);
 hipError_t launch_kv_weigh(const KvWeighArgs& a, hipStream_t stream);
 hipError_t launch_kv_select(const KvSelectArgs& a, hipStream_t stream);

@@ -21,10 +21,10 @@ inline size_t up(size_t x) { return (x + 255) & ~size_t(255); }
 // Byte offsets of a plan's arrays, the same on the host and on the device, after its number.
 struct KvLayout {
   size_t tok = up(sizeof(uint64_t)), narrow = 0, wide = 0, narrow_at = 0, wide_at = 0, join = 0, spans = 0,
-         trees = 0, tree = 0, tree_at = 0, tree_join = 0, end = 0;
+         trees = 0, end = 0;
   KvLayout() = default;
   KvLayout(int64_t n_tok, int64_t n_narrow, int64_t n_wide, int64_t waves, int64_t groups, int64_t n_join,
-           int64_t n_seq, int64_t tree_words, int64_t n_tree, int64_t tree_runs, int64_t n_tree_join) {
+           int64_t n_seq, int64_t tree_words) {
     narrow = up(tok + sizeof(KvTok) * n_tok);
     wide = up(narrow + sizeof(KvSeg) * n_narrow);
     narrow_at = up(wide + sizeof(KvSeg) * n_wide);
@@ -32,10 +32,7 @@ struct KvLayout {
     join = up(wide_at + sizeof(int32_t) * (groups + 1));
     spans = up(join + sizeof(KvJoin) * n_join);
     trees = up(spans + sizeof(KvSpan) * n_seq);
-    tree = up(trees + sizeof(uint32_t) * tree_words);
-    tree_at = up(tree + sizeof(KvSeg) * n_tree);
-    tree_join = up(tree_at + sizeof(int32_t) * (tree_runs ? tree_runs + 1 : 0));
-    end = up(tree_join + sizeof(KvJoin) * n_tree_join);
+    end = up(trees + sizeof(uint32_t) * tree_words);
   }
 };
 
@@ -66,7 +63,7 @@ struct lar_kv {
   int64_t blocks = 0;                    // of kWeighKeys keys of the sequences that take wide tiles
   int64_t cuts = 0;                      // of kSelectStretch rows of all
   int32_t n_narrow = 0, n_wide = 0, n_join = 0, join_rows = 0, most_parts = 0;
-  int32_t n_tree = 0, tree_waves = 0, n_tree_join = 0, tree_join_rows = 0, tree_most_parts = 0;
+  bool trees = false;
   lar_status sticky = LAR_OK;
   std::string msg;
 };

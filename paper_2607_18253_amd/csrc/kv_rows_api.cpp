@@ -45,7 +45,7 @@ extern "C" {
 lar_status lar_kv_weigh(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_rows* q, const int32_t* table,
                         int32_t table_cols, double scale, const float* lse, const float* before, float* weights) {
   if (lar_status st = ready(kv)) return st;
-  if (kv->n_tree) return fail(kv, LAR_E_STATE, "the planned batch has trees, whose tokens are not weighed");
+  if (kv->trees) return fail(kv, LAR_E_STATE, "the planned batch has trees, whose tokens are not weighed");
   if (!kv->n_tok) return LAR_OK;
   KvPool pool;
   KvRows qr;
