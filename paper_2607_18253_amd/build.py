@@ -27,7 +27,7 @@ SOURCES = [os.path.join(CSRC, "sfs_kernels.hip"), os.path.join(CSRC, "sfs_limits
 HEADERS = [os.path.join(CSRC, "sfs_device.h"), os.path.join(CSRC, "sfs_launch.h"),
            os.path.join(CSRC, "sfs_limits.h"), os.path.join(CSRC, "sfs_route.h"), os.path.join(CSRC, "sfs_walk.h"),
            os.path.join(CSRC, "kv_device.h"), os.path.join(CSRC, "kv_words.h"), os.path.join(CSRC, "kv_attend.h"),
-           os.path.join(CSRC, "kv_handle.h"),
+           os.path.join(CSRC, "kv_handle.h"), os.path.join(CSRC, "kv_cut.h"),
            os.path.join(ROOT, "include", "lar.h")]
 ARCH = "gfx950"
 

@@ -507,12 +507,13 @@ lar_status plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t*
   if (kv->stream) KV_TRY(kv, hipStreamIsCapturing(kv->stream, &capture));
   if (capture != hipStreamCaptureStatusNone) return fail(kv, LAR_E_STATE, "no plan under stream capture");
   int64_t T = 0, pages = 0, all_pages = 0;
-  int32_t longest = 0, all_longest = 0;
+  int32_t longest = 0, all_longest = 0, most_new = 0;
   for (int s = 0; s < n_seqs; ++s) {
     if (q_len[s] < 0 || ctx_len[s] < 0 || ctx_len[s] > 1 << 30)
       return fail(kv, LAR_E_ARG, "sequence %d: %d new tokens, context %d", s, q_len[s], ctx_len[s]);
     T += q_len[s];
     all_longest = std::max(all_longest, ctx_len[s]);
+    most_new = std::max(most_new, q_len[s]);
     if (q_len[s]) longest = std::max(longest, ctx_len[s]);
     if (q_len[s]) pages = std::max<int64_t>(pages, ceil_div(ctx_len[s], (int64_t)1 << kv->g.sh));
   }
@@ -629,6 +630,7 @@ lar_status plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t*
   kv->longest = all_longest;
   kv->trees = trees.most > 0;
   kv->blocks = blocks;
+  kv->most_new = most_new;
   kv->cuts = cuts;
   kv->window = window;
   kv->sinks = sinks;

@@ -153,7 +153,9 @@ struct KvWeighArgs {
   const int32_t* narrow_at;
   int32_t n_narrow, n_wide;
   const KvSpan* spans;
-  int32_t n_seq;
+  int32_t n_seq, cuts;  // cuts: stretches of kSelectStretch rows of all sequences and heads
+  int32_t splits;       // workgroups that share the rows of a block of keys; 1: none do
+  float* parts;         // their sums
   int32_t* err;
 };
 

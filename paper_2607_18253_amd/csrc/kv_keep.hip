@@ -63,6 +63,12 @@ __device__ __forceinline__ void read(uint4 (&x)[U]) {
   for (int u = 0; u < U; ++u) asm volatile("" : "+v"(x[u].x), "+v"(x[u].y), "+v"(x[u].z), "+v"(x[u].w));
 }
 
+// Past the caches: what has been moved is read by a later call.
+__device__ __forceinline__ void put(char* to, const uint4& x) {
+  typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+  __builtin_nontemporal_store(u32x4{x.x, x.y, x.z, x.w}, (u32x4*)to);
+}
+
 // The columns of 16 bytes from `col` on, `cols` of them, of the list's rows.
 template <int THREADS, int U>
 __device__ __forceinline__ void move_rows(List& list, char* pool, int row_bytes, int col, int cols) {
@@ -84,7 +90,7 @@ __device__ __forceinline__ void move_rows(List& list, char* pool, int row_bytes,
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (m[u].on) *(uint4*)(pool + (uint64_t)m[u].to * row_bytes + c * 16) = x[u];
+      if (m[u].on) put(pool + (uint64_t)m[u].to * row_bytes + c * 16, x[u]);
     if (!more) break;
 #pragma unroll
     for (int u = 0; u < U; ++u) m[u] = next[u];
@@ -142,14 +148,20 @@ hipError_t launch_kv_keep(const KvKeepArgs& a, hipStream_t stream) {
   const bool marks = a.g.cache == kKvE4m3 || a.weights;
   const int cols = a.g.D * (a.g.cache == kKvE4m3 ? 1 : 2) / 16;  // 16 bytes each
   const int64_t lists = (int64_t)a.n_seq * a.g.hkv;
-  // few lists: a share of the columns for each workgroup, 64 bytes of a row at least
-  int shares = 1;
+  // One pass of a small workgroup, or many of a larger one, which has fewer barriers for its bytes, and
+  // then a cache line of a long row for each (127 contexts to 777 rows of 256 bytes: 161 us; with 256
+  // threads 176, with whole rows 164).  Few lists: more shares of the columns, 64 bytes at least, and
+  // still more threads (92 lists of 3763 rows: 61 us, 151 with one of 256 threads for a list).
+  const bool small = a.n_rows * (int64_t)cols <= 1024;
+  int shares = !small && cols == 16 ? 2 : 1;
   while (2 * lists * shares < kFewGroups && cols / shares > 4) shares *= 2;
   const int jobs = 2 * shares + marks;
-  if (2 * lists * shares < kFewGroups && a.n_rows * (cols / shares) > 1024)
+  if (small)
+    k_kv_keep<256><<<lists * jobs, 256, 0, stream>>>(a, shares, jobs);
+  else if (2 * lists * shares < kFewGroups)
     k_kv_keep<1024><<<lists * jobs, 1024, 0, stream>>>(a, shares, jobs);
   else
-    k_kv_keep<256><<<lists * jobs, 256, 0, stream>>>(a, shares, jobs);
+    k_kv_keep<512><<<lists * jobs, 512, 0, stream>>>(a, shares, jobs);
   return hipGetLastError();
 }
 

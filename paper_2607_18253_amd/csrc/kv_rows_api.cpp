@@ -29,6 +29,14 @@ lar_status check_table(lar_kv* kv, const int32_t* table, int32_t cols, int64_t n
   return LAR_OK;
 }
 
+// Workgroups that share the rows of a block of keys, where there are few blocks: two for a CU in all, 16
+// blocks of 32 rows at least for each, sums within narrow_o.
+constexpr int kWeighGroups = 512, kWeighSplits = 8, kWeighLeast = 16;
+int32_t weigh_splits(const lar_kv* kv) {
+  const int64_t groups = std::max<int64_t>(1, kv->blocks * kv->g.hkv), rows = (int64_t)kv->most_new * kv->g.G / 32;
+  return (int32_t)std::max<int64_t>(1, std::min({kWeighGroups / groups, rows / kWeighLeast, (int64_t)kWeighSplits}));
+}
+
 // Working memory for a selection whose contexts are cut, or null where a workgroup takes a whole one.
 constexpr int kSelectWhole = 32768, kSelectCuts = 64;
 int32_t* select_work(const lar_kv* kv) {
@@ -57,7 +65,7 @@ lar_status lar_kv_weigh(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_rows
   const uintptr_t a0 = (uintptr_t)before, b0 = (uintptr_t)weights;
   if (a0 != b0 && a0 < b0 + bytes && b0 < a0 + bytes)
     return fail(kv, LAR_E_ARG, "before and weights must be the same or lie apart");
-  if (lar_status st = check_grid(kv, std::max<int64_t>(kv->blocks, kv->n_seq) * kv->g.hkv)) return st;
+  if (lar_status st = check_grid(kv, std::max(kv->blocks, kv->cuts) * kv->g.hkv)) return st;
   KvWeighArgs a{};
   a.plan = plan_id(kv);
   a.g = kv->g;
@@ -77,6 +85,9 @@ lar_status lar_kv_weigh(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_rows
   a.n_wide = (int32_t)kv->blocks;
   a.spans = (const KvSpan*)(kv->dev + kv->lay.spans);
   a.n_seq = kv->n_seq;
+  a.cuts = (int32_t)(kv->cuts * kv->g.hkv);
+  a.splits = weigh_splits(kv);
+  a.parts = kv->narrow_o;
   a.err = kv->err;
   return launch(kv, launch_kv_weigh, a);
 }

@@ -11,7 +11,7 @@
 //
 // Bound by latency: a few dependent steps between barriers for some 10 KB of weights.
 #include "../../include/lar.h"
-#include "kv_device.h"
+#include "kv_cut.h"
 
 namespace lar {
 namespace {
@@ -200,26 +200,10 @@ constexpr int kDigits = kSelectDigits, kBins = kSelectBins;
 constexpr int shift_of(int d) { return d == 0 ? 23 : d == 1 ? 15 : d == 2 ? 7 : 0; }
 constexpr int bins_of(int d) { return d == 0 ? 512 : d == 3 ? 128 : 256; }
 
-// Stretch k of a sequence's and head's `cuts`, and what they have in the working memory.
-struct Cut {
-  int seq, head, k, cuts;
+// A workgroup's stretch, and what it has in the working memory.
+struct Cut : KvCut {
   const KvSelectArgs& A;
-  int64_t first;  // of the head's stretches among all
-  __device__ __forceinline__ explicit Cut(const KvSelectArgs& a) : A(a) {
-    const int b = blockIdx.x, hkv = A.g.hkv;
-    int lo = 0, hi = A.n_seq;  // the last sequence whose stretches start at or before this one
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (A.spans[mid].cuts * hkv <= b) lo = mid; else hi = mid;
-    }
-    const KvSpan s = A.spans[lo];
-    seq = lo;
-    cuts = kv_select_cuts(s.ctx);
-    const int at = b - s.cuts * hkv;
-    head = at / cuts;
-    k = at - head * cuts;
-    first = (int64_t)s.cuts * hkv + (int64_t)head * cuts;
-  }
+  __device__ __forceinline__ explicit Cut(const KvSelectArgs& a) : KvCut(kv_cut(a.spans, a.n_seq, a.g.hkv, blockIdx.x)), A(a) {}
   // the least number so far and what is wanted of those that agree with it, before digit d
   __device__ __forceinline__ int* state(int d) const {
     return A.work + ((int64_t)seq * A.g.hkv + head) * (2 * kDigits) + 2 * d;

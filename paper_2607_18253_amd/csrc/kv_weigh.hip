@@ -14,6 +14,7 @@
 //   k_kv_weigh_copy    the sums that no row of the batch adds to, from `before`.
 #include "../../include/lar.h"
 #include "kv_attend.h"
+#include "kv_cut.h"
 
 namespace lar {
 namespace {
@@ -97,21 +98,23 @@ __device__ __forceinline__ void put(const KvWeighArgs& A, uint32_t row, bool fre
   A.after[row] = (fresh ? 0.0f : A.before[row]) + x;
 }
 
-// Two waves take the key tiles of a run in turn: more of them, with one tile on its way each, keep more
-// bytes on their way than one with two, and start their stretches beside one another.
-constexpr int kSides = 2;
+// Tiles that a wave has on their way: some 190 KB on a CU of eight.
+constexpr int kRing = 3;
 
 template <bool BF, bool F8, int D>
-__global__ __launch_bounds__(64, 3) void k_kv_weigh_narrow(KvWeighArgs A) {
+__global__ __launch_bounds__(64, 2) void k_kv_weigh_narrow(KvWeighArgs A) {
+  __shared__ __align__(16) char kt[kNarrowKeys * kRowK<D>];
+  using St = Stage<BF, F8, D, kNarrowKeys * (F8 ? D / 16 : D / 8) / 64, 64>;
+  constexpr int I = kNarrowKeys / St::kStep;
   const int lane = threadIdx.x, n = lane & 31, h = lane >> 5, G = A.g.G;
-  const int wave = run_of(blockIdx.x, A.n_narrow * kSides), run = wave / kSides, side = wave % kSides;
+  const int r0 = lane / St::kChunks, c = lane % St::kChunks;
+  const int run = run_of(blockIdx.x, A.n_narrow);
   int e = plan_at(A.narrow_at, run + 1), x = plan_at(A.narrow_at, run);
   if (other(A)) e = x;  // nothing to do
   bool any = false;     // a page outside the pool
   for (; x < e; ++x) {
     const KvSeg s = plan_at(A.narrow, x);
-    const int first = s.t0 + side;
-    if (first >= s.t1) continue;
+    if (s.t0 >= s.t1) continue;
     const int last = s.p0 + s.ntok - 1;  // a narrow tile has all new tokens of its sequence
     const int32_t* table = A.table + (int64_t)s.seq * A.cols;
     const auto key = [&](int t) { return tile_key<kNarrowKeys>(s, t < s.t1 ? t : s.t1 - 1) + n; };
@@ -119,11 +122,6 @@ __global__ __launch_bounds__(64, 3) void k_kv_weigh_narrow(KvWeighArgs A) {
       const int j = key(t);
       return table[(j < last ? j : last) >> A.g.sh];
     };
-    Keys<BF, F8, D> k;
-    bool lost;
-    uint32_t row = pool_row(A, look(first), s.head, key(first), lost);
-    int32_t page = look(first + kSides);
-    k.load(A, row, h);
     s16x8 q[D / 16];
     float l[16];
     uint32_t rows = 0;
@@ -133,7 +131,7 @@ __global__ __launch_bounds__(64, 3) void k_kv_weigh_narrow(KvWeighArgs A) {
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
         s16x8 z = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (t < s.ntok) z = *(const s16x8*)(p + part_of<F8>(i, h));
+        if (t < s.ntok) z = *(const s16x8*)(p + 16 * i + 8 * h);
         q[i] = z;
       }
       float z = -__builtin_inff();
@@ -145,27 +143,56 @@ __global__ __launch_bounds__(64, 3) void k_kv_weigh_narrow(KvWeighArgs A) {
         l[i] = -y * kLog2e;
       }
     }
-    for (int t = first; t < s.t1; t += kSides) {
-      const int kb = tile_key<kNarrowKeys>(s, t), j = kb + n;
-      const uint32_t at = row;
-      const bool gone = lost, fresh = j >= s.p0, mine = h == 0 && j <= last && !gone;
-      const float old = mine && !fresh ? A.before[at] : 0.0f;
-      f32x16 sc;
+    St st[kRing];
+    uint32_t row[kRing], ex[kRing];  // pool row and exponent of this lane's key n
+    bool lost[kRing];
+    int32_t page[kRing];
+    float old[kRing];                // asked for with the tile: a later load would wait for all tiles
+    const auto fetch = [&](int u, int t) {  // past the last tile: that one again
+      row[u] = pool_row(A, page[u], s.head, key(t), lost[u]);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
+      for (int i = 0; i < I; ++i)
+        st[u].k[i] = St::load((const char*)A.pool.k, (uint32_t)__shfl((int)row[u], i * St::kStep + r0), c * 16);
+      ex[u] = F8 ? A.pool.ke[row[u]] : 0;
+      old[u] = A.before[row[u]];
+    };
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) sc = Elem<BF>::mma(q[i], k.part(i), sc);
-      row = pool_row(A, page, s.head, key(t + kSides), lost);
-      k.load(A, row, h);  // past the last tile: that one again
-      page = look(t + 2 * kSides);
-      uint32_t on = rows;
-      if (cuts(A, s.p0, last, kb)) {
-        const int half = here(h);  // nothing of this is made before: registers
-        on &= seeing(A, j, [&](int i) { return s.p0 + key_of(i, half) / G; });
+    for (int u = 0; u < kRing; ++u) page[u] = look(s.t0 + u);
+#pragma unroll
+    for (int u = 0; u < kRing; ++u) {
+      fetch(u, s.t0 + u);
+      page[u] = look(s.t0 + kRing + u);
+    }
+    for (int t0 = s.t0; t0 < s.t1; t0 += kRing) {
+#pragma unroll
+      for (int u = 0; u < kRing; ++u) {
+        const int t = t0 + u;
+        if (t >= s.t1) break;
+        const int kb = tile_key<kNarrowKeys>(s, t), j = kb + n;
+        const uint32_t at = row[u];
+        const bool gone = lost[u];
+        const float before = j < s.p0 ? old[u] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+          st[u].put_k(kt, i, i * St::kStep + r0, c, F8 ? scale_of((uint32_t)__shfl((int)ex[u], i * St::kStep + r0)) : 0.0f);
+        fetch(u, t + kRing);
+        page[u] = look(t + 2 * kRing);
+        wave_order();
+        f32x16 sc;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) sc = Elem<BF>::mma(q[i], k_part<D>(kt, i, lane), sc);
+        uint32_t on = rows;
+        if (cuts(A, s.p0, last, kb)) {
+          const int half = here(h);  // nothing of this is made before: registers
+          on &= seeing(A, j, [&](int i) { return s.p0 + key_of(i, half) / G; });
+        }
+        const float sum = add_halves(add_up(sc, l, on, A.scale));
+        any |= gone && j <= last;
+        if (h == 0 && j <= last && !gone) A.after[at] = before + sum;
+        wave_order();
       }
-      const float sum = add_halves(add_up(sc, l, on, A.scale));
-      any |= gone && j <= last;
-      if (mine) A.after[at] = old + sum;
     }
   }
   if (any) *A.err = kKvLostPage;
@@ -185,6 +212,21 @@ struct Place {
   }
 };
 
+// The sequence of block b of keys: the last that starts at or before it, for those of its start before it
+// have no blocks.
+__device__ __forceinline__ int wide_seq(const KvWeighArgs& A, int b) {
+  int lo = 0, hi = A.n_seq;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (plan_at(A.spans, mid).blocks <= b) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// Token of a row that adds nothing: less any key, with any base, it is a negative number of 32 bits (the
+// base less a key is -2^26 - kWeighKeys to 2^30).
+constexpr int kNoToken = -(3 << 29);
+
 // One workgroup per kWeighKeys keys of a sequence and kv head, KF * 32 of them for a wave, whose
 // part of K stays in its registers; 32 rows of Q at a time are in LDS for all waves.  Bound by the
 // exponentials: one for a weight, at a quarter of the vector unit's rate.
@@ -195,20 +237,15 @@ __global__ __launch_bounds__(2 * kWeighKeys / KF, 2) void k_kv_weigh_wide(KvWeig
   struct alignas(16) Block {
     char q[32 * kRowK<D>];
     float l[32];
-    int tok[32];
-    uint32_t on;
+    int tok[32];  // kNoToken: the row adds nothing
+    int all;      // no row is that
   };
   __shared__ Block block[3];
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5, G = A.g.G;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int head = blockIdx.x % A.g.hkv, b = blockIdx.x / A.g.hkv;
+  const int head = blockIdx.x % A.g.hkv, bs = blockIdx.x / A.g.hkv, b = bs % A.n_wide, split = bs / A.n_wide;
   if (other(A)) return;
-  // the last sequence that starts at or before this block: those of its start before it have none
-  int lo = 0, hi = A.n_seq;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (plan_at(A.spans, mid).blocks <= b) lo = mid; else hi = mid;
-  }
+  const int lo = wide_seq(A, b);
   const KvSpan s = plan_at(A.spans, lo);
   const int kb0 = (b - s.blocks) * kWeighKeys, base = s.ctx - s.q_len, last = s.ctx - 1;
   const int kb = kb0 + wave * 32 * KF;
@@ -216,17 +253,21 @@ __global__ __launch_bounds__(2 * kWeighKeys / KF, 2) void k_kv_weigh_wide(KvWeig
   int t0 = kb0 > base ? kb0 - base : 0, t1 = s.q_len;
   if (base + t0 < 0) t0 = -base;
   if (A.window && kb0 >= A.sinks) t1 = min(t1, A.window + (kb0 - base + kWeighKeys - 1));
+  // this workgroup's rows, from row `start` on in `blocks` blocks of 32
+  const int step = 32 / G, rest = 32 % G, all_blocks = max(0, (t1 - t0) * G + 31) / 32;
+  const int start = t0 * G + 32 * (int)((int64_t)all_blocks * split / A.splits);
+  const int blocks = (int)((int64_t)all_blocks * (split + 1) / A.splits) - (int)((int64_t)all_blocks * split / A.splits);
   // rows of Q: this thread's chunks of them, and for the first wave the log of a row's sum
-  const int r0 = tid / kChunks, c = tid % kChunks, step = 32 / G, rest = 32 % G, end = t1 * G;
+  const int r0 = tid / kChunks, c = tid % kChunks;
   const bool loads = kStep <= 32 || r0 < 32;
   uint4 x[I];
   float z = 0.0f;
-  Place at[I], mine = Place::of(t0 * G + n, G);
+  Place at[I], mine = Place::of(start + n, G);
   const int16_t* from[I];
   const int64_t ahead = step * A.q.tok + rest * A.q.head, wrap = A.q.tok - G * A.q.head;
 #pragma unroll
   for (int i = 0; i < I; ++i) {
-    at[i] = Place::of(t0 * G + r0 + i * kStep, G);
+    at[i] = Place::of(start + r0 + i * kStep, G);
     from[i] = (const int16_t*)A.q.p + (int64_t)(s.q0 + at[i].t) * A.q.tok + (int64_t)(head * G + at[i].g) * A.q.head + c * 8;
   }
   int z_tok = 0;
@@ -250,12 +291,13 @@ __global__ __launch_bounds__(2 * kWeighKeys / KF, 2) void k_kv_weigh_wide(KvWeig
     for (int i = 0; i < I; ++i)
       if (loads) *(uint4*)(to.q + (r0 + i * kStep) * kRowK<D> + c * 16) = x[i];
     if (wave == 0) {
-      const uint64_t on = __ballot(z != -__builtin_inff());
+      const bool on = z != -__builtin_inff();
+      const int all = __all(on);
       if (h == 0) {
         to.l[n] = -z * kLog2e;
-        to.tok[n] = z_tok;
+        to.tok[n] = on ? z_tok : kNoToken;
       }
-      if (lane == 0) to.on = (uint32_t)on;
+      if (lane == 0) to.all = all;
     }
   };
   s16x8 k[KF][D / 16];
@@ -272,8 +314,7 @@ __global__ __launch_bounds__(2 * kWeighKeys / KF, 2) void k_kv_weigh_wide(KvWeig
     for (int t = 0; t < D / 16; ++t) k[f][t] = y.part(t);
     sum[f] = 0.0f;
   }
-  const int blocks = (end - t0 * G + 31) / 32;
-  Place first = Place::of(t0 * G, G), final = Place::of(t0 * G + 31, G);  // rows of a block
+  Place first = Place::of(start, G), final = Place::of(start + 31, G);  // rows of a block
   const auto part = [&](const Block& q, int t) {
     return *(const s16x8*)(q.q + n * kRowK<D> + part_of<F8>(t, h) * 2);
   };
@@ -313,8 +354,8 @@ __global__ __launch_bounds__(2 * kWeighKeys / KF, 2) void k_kv_weigh_wide(KvWeig
 #pragma unroll
         for (int w = 0; w < 4; ++w) l[y + w] = v[w];
       }
-      const uint32_t rows = (uint32_t)__builtin_amdgcn_readfirstlane((int)q.on);
-      if (rows == ~0u && !cuts(A, p0, p1, kb + 32 * (KF - 1)) && !cuts(A, p0, p1, kb)) {
+      const bool all = __builtin_amdgcn_readfirstlane(q.all);
+      if (all && !cuts(A, p0, p1, kb + 32 * (KF - 1)) && !cuts(A, p0, p1, kb)) {
         float add[KF];
         s16x8 p[kAhead];
 #pragma unroll
@@ -343,14 +384,23 @@ __global__ __launch_bounds__(2 * kWeighKeys / KF, 2) void k_kv_weigh_wide(KvWeig
 #pragma unroll
         for (int f = 0; f < KF; ++f) sum[f] += add[f];
       } else {
-        const int half = here(h);  // nothing of this is made before
-        uint32_t on = 0;
-#pragma unroll
-        for (int y = 0; y < 16; ++y) on |= (rows >> key_of(y, half) & 1) << y;
+        // a row sees key j if its position less j is in 0 .. the window: as unsigned numbers, one
+        // comparison
 #pragma unroll
         for (int f = 0; f < KF; ++f) {
-          const uint32_t m = on & seeing(A, kb + 32 * f + n, [&](int y) { return base + q.tok[key_of(y, half)]; });
-          sum[f] += add_up(sc[f], l, m, A.scale);
+          const int j = kb + 32 * f + n;
+          const uint32_t most = A.window && j >= A.sinks ? (uint32_t)A.window : 0x80000000u;
+          float add = 0.0f;
+#pragma unroll
+          for (int y = 0; y < 16; y += 4) {
+            const auto tok = *(const __attribute__((ext_vector_type(4))) int*)(q.tok + key_of(y, h));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[f][y + i], A.scale, l[y + i]));
+              add += (uint32_t)(base + tok[i] - j) < most ? v : 0.0f;
+            }
+          }
+          sum[f] += add;
         }
         score(qn, next);
       }
@@ -372,23 +422,45 @@ __global__ __launch_bounds__(2 * kWeighKeys / KF, 2) void k_kv_weigh_wide(KvWeig
     const int j = kb + 32 * f + n;
     const float y = add_halves(sum[f]);
     if (j > last || h) continue;
-    if (lost[f])
+    if (A.splits > 1)
+      A.parts[(int64_t)blockIdx.x * kWeighKeys + j - kb0] = y;
+    else if (lost[f])
       *A.err = kKvLostPage;
     else
       put(A, row[f], j >= base, y);
   }
 }
 
-// `before` to `after` for the context of the sequences with new tokens, one workgroup for each
-// sequence and kv head.
-__global__ __launch_bounds__(256) void k_kv_weigh_copy(KvWeighArgs A) {
-  const int seq = blockIdx.x / A.g.hkv, head = blockIdx.x % A.g.hkv;
+// The sums of a block's keys over the workgroups that shared its rows, in their order.
+__global__ __launch_bounds__(kWeighKeys) void k_kv_weigh_sum(KvWeighArgs A) {
+  const int head = blockIdx.x % A.g.hkv, b = blockIdx.x / A.g.hkv;
   if (other(A)) return;
+  const int seq = wide_seq(A, b);
   const KvSpan s = plan_at(A.spans, seq);
+  const int j = (b - s.blocks) * kWeighKeys + threadIdx.x;
+  if (j >= s.ctx) return;
+  float y = 0.0f;
+  for (int i = 0; i < A.splits; ++i) y += A.parts[((int64_t)i * gridDim.x + blockIdx.x) * kWeighKeys + threadIdx.x];
+  bool lost;
+  const uint32_t row = pool_row(A, A.table[(int64_t)seq * A.cols + (j >> A.g.sh)], head, j, lost);
+  if (lost)
+    *A.err = kKvLostPage;
+  else
+    put(A, row, j >= s.ctx - s.q_len, y);
+}
+
+// `before` to `after` for the context of the sequences with new tokens, a workgroup for a stretch.
+__global__ __launch_bounds__(256) void k_kv_weigh_copy(KvWeighArgs A) {
+  if (other(A)) return;
+  const KvCut c = kv_cut(A.spans, A.n_seq, A.g.hkv, blockIdx.x);
+  const KvSpan s = A.spans[c.seq];
   if (s.q_len == 0) return;
-  for (int j = threadIdx.x; j < s.ctx - s.q_len; j += 256) {
+#pragma unroll 4
+  for (int i = 0; i < kSelectStretch; i += 256) {
+    const int j = c.k * kSelectStretch + i + threadIdx.x;
+    if (j >= s.ctx - s.q_len) break;
     bool lost;
-    const uint32_t row = pool_row(A, A.table[(int64_t)seq * A.cols + (j >> A.g.sh)], head, j, lost);
+    const uint32_t row = pool_row(A, A.table[(int64_t)c.seq * A.cols + (j >> A.g.sh)], c.head, j, lost);
     if (lost)
       *A.err = kKvLostPage;
     else
@@ -398,13 +470,17 @@ __global__ __launch_bounds__(256) void k_kv_weigh_copy(KvWeighArgs A) {
 
 template <bool BF, bool F8, int D>
 hipError_t run(const KvWeighArgs& a, hipStream_t stream) {
-  if (a.window && a.before != a.after) k_kv_weigh_copy<<<a.n_seq * a.g.hkv, 256, 0, stream>>>(a);
-  if (a.n_narrow) k_kv_weigh_narrow<BF, F8, D><<<a.n_narrow * kSides, 64, 0, stream>>>(a);
-  // Few workgroups: eight waves of 32 keys each.
-  if (a.n_wide * a.g.hkv > 256)
-    k_kv_weigh_wide<BF, F8, D, 2><<<a.n_wide * a.g.hkv, kWeighKeys, 0, stream>>>(a);
-  else if (a.n_wide)
-    k_kv_weigh_wide<BF, F8, D, 1><<<a.n_wide * a.g.hkv, 2 * kWeighKeys, 0, stream>>>(a);
+  if (a.window && a.before != a.after) k_kv_weigh_copy<<<a.cuts, 256, 0, stream>>>(a);
+  if (a.n_narrow) k_kv_weigh_narrow<BF, F8, D><<<a.n_narrow, 64, 0, stream>>>(a);
+  if (a.n_wide) {
+    const int n = a.n_wide * a.g.hkv;
+    // few workgroups: eight waves of 32 keys each
+    if (n * a.splits > 256)
+      k_kv_weigh_wide<BF, F8, D, 2><<<n * a.splits, kWeighKeys, 0, stream>>>(a);
+    else
+      k_kv_weigh_wide<BF, F8, D, 1><<<n * a.splits, 2 * kWeighKeys, 0, stream>>>(a);
+    if (a.splits > 1) k_kv_weigh_sum<<<n, kWeighKeys, 0, stream>>>(a);
+  }
   return hipGetLastError();
 }
 
