@@ -506,7 +506,7 @@ lar_status plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t*
   hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
   if (kv->stream) KV_TRY(kv, hipStreamIsCapturing(kv->stream, &capture));
   if (capture != hipStreamCaptureStatusNone) return fail(kv, LAR_E_STATE, "no plan under stream capture");
-  int64_t T = 0, pages = 0, all_pages = 0;
+  int64_t T = 0, pages = 0, all_pages = 0, all_rows = 0;
   int32_t longest = 0, all_longest = 0, most_new = 0;
   for (int s = 0; s < n_seqs; ++s) {
     if (q_len[s] < 0 || ctx_len[s] < 0 || ctx_len[s] > 1 << 30)
@@ -514,6 +514,7 @@ lar_status plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t*
     T += q_len[s];
     all_longest = std::max(all_longest, ctx_len[s]);
     most_new = std::max(most_new, q_len[s]);
+    all_rows += ctx_len[s];
     if (q_len[s]) longest = std::max(longest, ctx_len[s]);
     if (q_len[s]) pages = std::max<int64_t>(pages, ceil_div(ctx_len[s], (int64_t)1 << kv->g.sh));
   }
@@ -632,6 +633,7 @@ lar_status plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t*
   kv->blocks = blocks;
   kv->most_new = most_new;
   kv->cuts = cuts;
+  kv->rows = all_rows;
   kv->window = window;
   kv->sinks = sinks;
   kv->plan = id.x;

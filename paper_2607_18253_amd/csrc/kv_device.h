@@ -170,6 +170,7 @@ struct KvSelectArgs {
   int32_t budget, first, last;
   int32_t* rows;         // [n_seq][hkv][budget]
   int32_t* work;         // where contexts are cut, else null
+  uint32_t* numbers;     // their weights as numbers that order so, by stretches
   int32_t cuts;          // of all sequences and heads
   int32_t* err;
 };

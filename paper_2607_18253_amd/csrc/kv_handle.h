@@ -62,7 +62,7 @@ struct lar_kv {
   int32_t longest = 0;                   // context of any
   int64_t blocks = 0;                    // of kWeighKeys keys of the sequences that take wide tiles
   int32_t most_new = 0;                  // new tokens of a sequence at most
-  int64_t cuts = 0;                      // of kSelectStretch rows of all
+  int64_t cuts = 0, rows = 0;            // stretches of kSelectStretch rows of all contexts; rows
   int32_t n_narrow = 0, n_wide = 0, n_join = 0, join_rows = 0, most_parts = 0;
   bool trees = false;
   lar_status sticky = LAR_OK;

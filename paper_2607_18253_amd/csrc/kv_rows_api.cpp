@@ -38,12 +38,19 @@ int32_t weigh_splits(const lar_kv* kv) {
 }
 
 // Working memory for a selection whose contexts are cut, or null where a workgroup takes a whole one.
+// Five launches over all rows take 28 us and one for 165k rows; a workgroup 10 us and one for 1000 rows
+// in its registers, 1.9 for 1000 of more that it reads again for every digit, and all of them one for 200k
+// and 67k rows.  (8 contexts of 64k rows: 30 us cut, 129 whole; 256 of 64k: 129 and 243, of 32k: 78 and 51.)
 constexpr int kSelectWhole = 32768, kSelectCuts = 64;
 int32_t* select_work(const lar_kv* kv) {
-  const int64_t room = (int64_t)2 * kv->waves * kNarrowRows * kv->g.D;  // of narrow_o, in words
-  const bool cut = kv->longest > kSelectWhole && kv_select_cuts(kv->longest) <= kSelectCuts &&
-                   kv_select_words((int64_t)kv->n_seq * kv->g.hkv, kv->cuts * kv->g.hkv) <= room;
-  return cut ? (int32_t*)kv->narrow_o : nullptr;
+  const int64_t narrow = (int64_t)2 * kv->waves * kNarrowRows * kv->g.D;  // words of narrow_o and wide_o
+  const int64_t wide = (int64_t)2 * kv->groups * kWideRows * kv->g.D, cuts = kv->cuts * kv->g.hkv;
+  if (kv_select_cuts(kv->longest) > kSelectCuts || kv_select_words((int64_t)kv->n_seq * kv->g.hkv, cuts) > narrow ||
+      cuts * kSelectStretch > wide)
+    return nullptr;
+  const double n = kv->longest, all = (double)kv->rows * kv->g.hkv;
+  const double whole = n <= kSelectWhole ? std::max(10 + 1e-3 * n, all / 200e3) : std::max(1.9e-3 * n, all / 67e3);
+  return 28 + all / 165e3 < whole ? (int32_t*)kv->narrow_o : nullptr;
 }
 
 }  // namespace
@@ -118,6 +125,7 @@ lar_status lar_kv_select(lar_kv* kv, const float* weights, int64_t n_blocks, con
   a.last = last;
   a.rows = rows;
   a.work = select_work(kv);
+  a.numbers = (uint32_t*)kv->wide_o;
   a.cuts = a.work ? (int32_t)(kv->cuts * kv->g.hkv) : 0;
   a.err = kv->err;
   return launch(kv, launch_kv_select, a);

@@ -216,6 +216,8 @@ struct Cut : KvCut {
   __device__ __forceinline__ int* counts(int d, int k) const {
     return A.work + (int64_t)A.n_seq * A.g.hkv * (2 * kDigits) + (A.cuts + 3) / 4 * 4 + ((first + k) * kDigits + d) * kBins;
   }
+  // its rows' numbers, from the first pass on: they need not be gathered again
+  __device__ __forceinline__ uint32_t* numbers() const { return A.numbers + (first + k) * kStretch; }
 };
 
 // Calls f(bin, count) for the four bins of this thread's share of each of the stretches [0, cuts) of
@@ -272,9 +274,16 @@ __global__ __launch_bounds__(kCut) void k_kv_select_count(KvSelectArgs A) {
   uint32_t v[kEach];
 #pragma unroll
   for (int r = 0; r < kEach; ++r) {
-    const int j = k * kStretch + r * kCut + tid;
-    v[r] = c.between(j) ? c.weight(j) : 0;
+    if (DIGIT == 0) {
+      const int j = k * kStretch + r * kCut + tid;
+      v[r] = c.between(j) ? c.weight(j) : 0;
+    } else {
+      v[r] = w.numbers()[r * kCut + tid];
+    }
   }
+  if (DIGIT == 0)
+#pragma unroll
+    for (int r = 0; r < kEach; ++r) w.numbers()[r * kCut + tid] = v[r];
   uint32_t least = 0;
   if constexpr (DIGIT > 0) {
     constexpr int kPast = DIGIT - 1;
@@ -332,8 +341,7 @@ __global__ __launch_bounds__(kCut) void k_kv_select_write(KvSelectArgs A) {
   uint32_t v[kEach];
 #pragma unroll
   for (int r = 0; r < kEach; ++r) {
-    const int j = j0 + r * kCut + tid;
-    v[r] = c.between(j) && some ? c.weight(j) : 0;
+    v[r] = some ? w.numbers()[r * kCut + tid] : 0;
   }
   uint32_t least = 0, digit = 0;
   if (tid < 2) before[tid] = 0;

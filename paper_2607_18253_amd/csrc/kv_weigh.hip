@@ -215,12 +215,7 @@ struct Place {
 // The sequence of block b of keys: the last that starts at or before it, for those of its start before it
 // have no blocks.
 __device__ __forceinline__ int wide_seq(const KvWeighArgs& A, int b) {
-  int lo = 0, hi = A.n_seq;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (plan_at(A.spans, mid).blocks <= b) lo = mid; else hi = mid;
-  }
-  return lo;
+  return last_to(A.n_seq, b, [&](int i) { return A.spans[i].blocks; });
 }
 
 // Token of a row that adds nothing: less any key, with any base, it is a negative number of 32 bits (the
@@ -271,15 +266,26 @@ __global__ __launch_bounds__(2 * kWeighKeys / KF, 2) void k_kv_weigh_wide(KvWeig
     from[i] = (const int16_t*)A.q.p + (int64_t)(s.q0 + at[i].t) * A.q.tok + (int64_t)(head * G + at[i].g) * A.q.head + c * 8;
   }
   int z_tok = 0;
+  int left = t1 * G - start;  // rows from the next block's first on
   const auto fetch = [&]() {
+    if (rest == 0 && left >= 32) {  // whole blocks, of the same heads
 #pragma unroll
-    for (int i = 0; i < I; ++i) {
-      x[i] = make_uint4(0, 0, 0, 0);
-      if (loads && at[i].t < t1) x[i] = *(const uint4*)from[i];
-      const bool over = at[i].g + rest >= G;
-      from[i] += ahead + (over ? wrap : 0);
-      at[i].next(G, step, rest);
+      for (int i = 0; i < I; ++i) {
+        if (kStep <= 32 || loads) x[i] = *(const uint4*)from[i];
+        from[i] += ahead;
+        at[i].t += step;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (loads && at[i].t < t1) x[i] = *(const uint4*)from[i];
+        const bool over = at[i].g + rest >= G;
+        from[i] += ahead + (over ? wrap : 0);
+        at[i].next(G, step, rest);
+      }
     }
+    left -= 32;
     if (wave == 0) {
       z = mine.t < t1 ? A.lse[(int64_t)(s.q0 + mine.t) * A.g.hq + head * G + mine.g] : -__builtin_inff();
       z_tok = mine.t;
