@@ -634,18 +634,20 @@ typedef struct {
  * lar_kv_weigh: q and scale as for lar_kv_attend, and lse what it gave.  before: the
  *   weights so far, weights itself or memory apart from it; the rows of the sequences with
  *   new tokens are written, all others stay as they are.  Two sequences with new tokens may not
- *   share pages here.  Not for a plan with trees (LAR_E_STATE).
+ *   share pages here.  Not for a plan with trees (LAR_E_STATE), nor for more than 2^30 / (n_q_heads /
+ *   n_kv_heads) new tokens of a sequence (LAR_E_CAPACITY).
  * lar_kv_select: first + last <= budget.  rows dev [n_seqs][n_kv_heads][budget]: the positions
  *   to keep in ascending order, then -1.  n_blocks: of the weights.
  * lar_kv_keep: rows dev [n_seqs][n_kv_heads][n_rows], or with per_head 0 [n_seqs][n_rows] for all
- *   heads: positions in ascending order, the first -1 ends a list.  Row rows[i] goes to place i;
- *   with `fresh` both count from the sequence's first new token.  K and V, the exponents of an
- *   e4m3 cache and, if given, the weights go along.  The place is that of to_table, dev
- *   [n_seqs][to_cols], or of table itself (NULL); a page of to_table is either the one that
- *   table has in that column or one that table has in no sequence of the batch, and no page that
- *   is written to belongs to two sequences.  What is at the places past a list stays.  Lists that
- *   do not ascend or leave the context set the sticky LAR_E_STATE; nothing is moved for an entry
- *   that does, and what the places of such a list hold is undefined.
+ *   heads: positions in ascending order, then -1 to the end.  Row rows[i] goes to place i; with
+ *   `fresh` both count from the sequence's first new token (of a context shorter than its new
+ *   tokens the first one that is no padding row has the first place, and its own number).  K and V,
+ *   the exponents of an e4m3 cache and, if given, the weights go along.  The place is that of
+ *   to_table, dev [n_seqs][to_cols], or of table itself (NULL); a page of to_table is either the
+ *   one that table has in that column or one that table has in no sequence of the batch, and no page
+ *   that is written to belongs to two sequences.  What is at the places past a list stays.  Lists
+ *   that do not ascend or leave the context set the sticky LAR_E_STATE; nothing is moved for an
+ *   entry that does, and what the other places of such a list hold is undefined.
  * lar_kv_sync: synchronise the stream; the sticky device error, if any.
  * Each call works on the handle's stream, allocates nothing (but create) and does not
  * wait (but plan, as said, and sync).  A handle is not thread-safe; calls of one handle

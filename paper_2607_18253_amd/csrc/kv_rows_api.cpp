@@ -72,6 +72,8 @@ lar_status lar_kv_weigh(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_rows
   const uintptr_t a0 = (uintptr_t)before, b0 = (uintptr_t)weights;
   if (a0 != b0 && a0 < b0 + bytes && b0 < a0 + bytes)
     return fail(kv, LAR_E_ARG, "before and weights must be the same or lie apart");
+  if ((int64_t)kv->most_new * kv->g.G > 1 << 30)  // rows of a sequence and head are counted in 32 bits
+    return fail(kv, LAR_E_CAPACITY, "%d new tokens of %d heads", kv->most_new, kv->g.G);
   if (lar_status st = check_grid(kv, std::max(kv->blocks, kv->cuts) * kv->g.hkv)) return st;
   KvWeighArgs a{};
   a.plan = plan_id(kv);

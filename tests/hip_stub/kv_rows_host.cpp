@@ -41,6 +41,8 @@ int stub_weigh(int32_t* to) {
   weigh.after = nullptr;
   return was;
 }
+// The number of the plan that the last call of a kind was made for: weights, selection, move.
+uint64_t stub_rows_plan(int what) { return what == 0 ? weigh.plan.id : what == 1 ? select_.plan.id : keep.plan.id; }
 int stub_keep(int32_t* to) {
   to[0] = keep.heads;
   to[1] = keep.n_rows;

@@ -525,6 +525,102 @@ def test_pages_outside_the_pool_are_reported():
             x.kv.sync()
 
 
+# ------------------------------------------------------------------ far, strided, shared out
+def test_past_32_bits():
+    """Pages whose bytes and values lie past 2^32: a tree's attention, weights, selection, moves."""
+    S, hkv, d = 16, 8, 128
+    n_blocks = 2 ** 32 // (S * hkv * d) + 700
+    kv = PagedKV(16, hkv, d, block_size=S, dtype=BF, cache_dtype=E4, max_seqs=2, max_tokens=300)
+    pages, w = kv.new_pages(n_blocks), kv.new_weights(n_blocks)
+    tab = torch.arange(n_blocks - 20, n_blocks, dtype=torch.int32, device=DEV).view(2, 10).flip(1).contiguous()
+    g = torch.Generator().manual_seed(2)
+    k, v = (torch.randn((300, hkv, d), generator=g).to(BF) for _ in range(2))
+    kv.plan([150, 150], [150, 150])
+    kv.append(pages, k.to(DEV), v.to(DEV), tab)
+    q = torch.randn((47, 16, d), generator=g).to(BF)
+    par = [tree(7, np.random.RandomState(1)), tree(40, np.random.RandomState(2))]
+    kv.plan([7, 40], [150, 150], parents=sum(par, []))
+    out = kv.attend(pages, q.to(DEV), tab).cpu().double()
+    held = [[R.quantise(x[150 * s:150 * s + 150], BF)[0] for x in (k, v)] for s in range(2)]
+    for s, (a, n) in enumerate(((0, 7), (7, 40))):
+        mask = torch.zeros((n, 150), dtype=torch.bool)
+        for i, see in enumerate(seen(par[s], n, 150)[0]):
+            mask[i, list(see)] = True
+        want, wz, mag, big = R.attend_fast(q[a:a + n].double(), *held[s], mask, d ** -0.5)
+        Batch.near(out[a:a + n], want, R.bounds(BF, mag, big, wz, d, 150, 8.0)[0], s)
+    kv.plan([7, 40], [150, 150])
+    lse = torch.empty((47, 16), device=DEV)
+    kv.attend(pages, q.to(DEV), tab, lse=lse)
+    kv.weigh(pages, q.to(DEV), lse, tab, w)
+    rows = kv.select(w, tab, 60, 2, 5)
+    to = torch.arange(n_blocks - 40, n_blocks - 20, dtype=torch.int32, device=DEV).view(2, 10).contiguous()
+    kv.keep(pages, tab, rows, to=to, weights=w)
+    kv.plan([60, 60], [60, 60])
+    ko, vo = kv.read(pages, to)
+    kv.sync()
+    j = torch.arange(60)
+    for s in range(2):
+        total = 0.0
+        for h in range(hkv):
+            x = rows[s, h].cpu().long()
+            assert (x[1:] > x[:-1]).all() and x[:2].tolist() == [0, 1] and x[-5:].tolist() == list(range(145, 150))
+            for y, i in ((ko, 0), (vo, 1)):
+                assert torch.equal(y[60 * s:60 * s + 60, h].cpu().double(), held[s][i][x, h])
+            at = tab[s].cpu().long()
+            mine = w[at[x // S].to(DEV), h, (x % S).to(DEV)]
+            assert torch.equal(w[to[s].long()[j // S], h, j % S], mine)
+            total += float(w[at.to(DEV), h].flatten()[:150].double().sum())
+        assert abs(total / ((7, 40)[s] * 16) - 1) < 2.0 ** -16
+
+
+def test_weigh_strided_queries_and_scales():
+    """Queries as a slice of a fused projection, for single tokens and chunks; other scales."""
+    b = Batch([1, 150, 3], [96, 300, 41], hq=8, hkv=2, d=128, S=16, dtype=BF, cache=BF)
+    fused = torch.randn((154, 12, 128)).to(BF).to(DEV)
+    q = fused[:, 2:10]
+    b.q = q.cpu()
+    for scale in (128 ** -0.5, 0.011, 1.0):
+        _, lse = b.attend(scale=scale, q=q)
+        w, w2 = (b.k.new_weights(b.pages.k.shape[0]) for _ in range(2))
+        b.k.weigh(b.pages, q, lse.to(DEV), b.table, w, scale=scale)
+        b.k.weigh(b.pages, q.contiguous(), lse.to(DEV), b.table, w2, scale=scale)
+        b.k.sync()
+        assert torch.equal(w, w2)
+        at = 0
+        for s, (n, c) in enumerate(zip(b.q_len, b.ctx)):
+            j = torch.arange(c)
+            got = w.cpu()[b.table[s].cpu().long()[j // 16], :, j % 16].double()
+            want, bound = weigh_ref(b, s, at, R.sees(n, c), lse[at:at + n], scale, torch.zeros(c, 2, dtype=torch.float64))
+            assert ((got - want).abs() <= bound).all(), (scale, s)
+            at += n
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(4, 1, 128), (5, 1, 64), (64, 1, 64), (14, 2, 128)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (300, 5)])
+def test_weigh_rows_shared_out(hq, hkv, d, window, sinks):
+    """Chunks over few keys, whose rows are shared out over workgroups, heads that divide 32 and that do
+    not; the same again bit for bit."""
+    for q_len, ctx in (([600], [700]), ([1100, 1, 40], [1000, 200, 77])):
+        b = run_weigh(q_len, ctx, hq=hq, hkv=hkv, d=d, window=window, sinks=sinks, place=False)
+        _, lse = b.attend(window, sinks)
+        got = []
+        for _ in range(3):
+            w = b.k.new_weights(b.pages.k.shape[0])
+            b.k.weigh(b.pages, b.q.to(DEV), lse.to(DEV), b.table, w)
+            got.append(w)
+        b.k.sync()
+        assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+
+
+def test_select_cut_and_whole_agree():
+    """Long contexts cut over workgroups and taken whole, beside short and empty ones, ties everywhere."""
+    make = lambda r, s: r.randint(0, 50, s).astype(np.float32)  # noqa: E731
+    check_select([70000, 0, 3, 4096, 4097, 300], 500, 4, 60, hkv=2, make=make, seed=1, q_len=[1, 0, 1, 1, 0, 0])
+    check_select([262144], 1000, 0, 0, hkv=1, make=make, seed=2)
+    check_select([262145], 1000, 0, 0, hkv=1, make=make, seed=3)      # more stretches than are cut
+    check_select([20000] * 3, 8192, 16, 16, hkv=1, make=make, seed=4, S=128)
+
+
 # ------------------------------------------------------------------ together
 @pytest.mark.parametrize("cache", [BF, E4])
 def test_drafts_are_verified_and_kept(cache):

@@ -12,6 +12,7 @@ import numpy as np
 import pytest
 
 from paper_2607_18253_amd.kv import KvConfig, KvPagesArg, KvRowsArg
+from test_kv_calls_host import Tensor, binding  # noqa: F401  (the fixture)
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(os.path.dirname(HERE), "paper_2607_18253_amd", "csrc")
@@ -271,3 +272,115 @@ def test_rows_calls_check_their_arguments(lib):
     assert x.weigh() == 0 and x.select() == 0 and x.keep() == 0
     assert lib.stub_weigh(g) == 0 and lib.stub_keep(g) == 0
     x.close()
+
+
+def test_long_chunks_of_many_heads_are_refused(lib):
+    """Rows of a sequence are counted in 32 bits."""
+    x = Handle(lib, max_seqs=1, max_tokens=1 << 24, hq=64, hkv=1)
+    assert x.plan([1 << 24], [1 << 24]) == 0 and x.weigh(cols=1 << 21) == 0
+    x.close()
+    x = Handle(lib, max_seqs=1, max_tokens=(1 << 24) + 1, hq=64, hkv=1)
+    assert x.plan([(1 << 24) + 1], [(1 << 24) + 1]) == 0 and x.weigh(cols=1 << 21) == E_CAPACITY
+    x.close()
+
+
+@pytest.mark.parametrize("current", [0, 1])
+def test_calls_go_to_the_handles_device(lib, current):
+    """A handle made on device 1 works on it whichever device is current, and leaves that one current."""
+    lib.stub_use(1)
+    x = Handle(lib)
+    lib.stub_use(current)
+    lib.stub_calls(0)
+    for call in (lambda: x.plan([1, 5], [40, 100]), x.weigh, x.select, x.keep,
+                 lambda: x.plan([3], [100], [-1, 0, 0]), x.attend, lambda: x.keep(fresh=1)):
+        lib.stub_calls(1)
+        assert call() == 0
+        assert lib.stub_device() == current
+        assert lib.stub_calls(0) == 0 and lib.stub_calls(1) > 0
+    x.close()
+    lib.stub_use(0)
+
+
+def test_launches_carry_their_plan(lib):
+    lib.stub_device_plan.restype = lib.stub_rows_plan.restype = C.c_uint64
+    x = Handle(lib)
+    ids = set()
+    for i, (call, plan) in enumerate(((x.weigh, {}), (x.select, {}), (x.keep, {}), (lambda: x.keep(fresh=1), dict(parents=[-1, 0, 0])))):
+        assert x.plan([3], [50 + i], **plan) == 0 and x.attend() == 0 and call() == 0
+        assert lib.stub_rows_plan(min(i, 2)) == lib.stub_device_plan()
+        ids.add(lib.stub_device_plan())
+    assert len(ids) == 4
+    # a batch without new tokens is a plan too
+    assert x.plan([0, 0], [50, 60]) == 0 and x.select() == 0 and lib.stub_rows_plan(1) not in ids
+    x.close()
+
+
+def test_plans_without_new_tokens_reach_the_device(lib):
+    x = Handle(lib)
+    assert x.plan([3], [50]) == 0 and x.attend() == 0
+    lib.stub_device_plan.restype = lib.stub_rows_plan.restype = C.c_uint64
+    before = lib.stub_device_plan()
+    assert x.plan([0], [50]) == 0 and x.keep() == 0
+    assert lib.stub_device_plan() == lib.stub_rows_plan(2) != before
+    x.close()
+
+
+# ------------------------------------------------------------------ the binding's checks
+def test_tensors_of_another_device_are_refused(binding):  # noqa: F811
+    import torch
+    from paper_2607_18253_amd import KvPages
+    B, F, I = torch.bfloat16, torch.float32, torch.int32
+    pages = KvPages(*(Tensor((9, 2, 16, 64), B) for _ in range(2)))
+    q, tab, lse, w = Tensor((3, 8, 64), B), Tensor((1, 4), I), Tensor((3, 8), F), Tensor((9, 2, 16), F)
+    rows = Tensor((1, 2, 5), I)
+    binding.weigh(pages, q, lse, tab, w, before=Tensor((9, 2, 16), F, at=1 << 20))
+    binding.select(w, tab, 5, rows=rows)
+    binding.keep(pages, tab, rows, to=tab, weights=w)
+    binding.keep(pages, tab, Tensor((1, 5), I), new=True)
+    assert [n for n, _ in binding._L.calls] == ["lar_kv_weigh", "lar_kv_select", "lar_kv_keep", "lar_kv_keep"]
+    far = lambda t: Tensor(t.shape, t.dtype, device=1)  # noqa: E731
+    for call in (lambda: binding.weigh(pages, far(q), lse, tab, w), lambda: binding.weigh(pages, q, far(lse), tab, w),
+                 lambda: binding.weigh(pages, q, lse, far(tab), w), lambda: binding.weigh(pages, q, lse, tab, far(w)),
+                 lambda: binding.weigh(pages, q, lse, tab, w, before=far(w)), lambda: binding.select(far(w), tab, 5, rows=rows),
+                 lambda: binding.select(w, far(tab), 5, rows=rows), lambda: binding.select(w, tab, 5, rows=far(rows)),
+                 lambda: binding.keep(pages, far(tab), rows), lambda: binding.keep(pages, tab, far(rows)),
+                 lambda: binding.keep(pages, tab, rows, to=far(tab)), lambda: binding.keep(pages, tab, rows, weights=far(w))):
+        with pytest.raises(ValueError, match="cuda:0"):
+            call()
+    assert len(binding._L.calls) == 4
+    name, args = binding._L.calls[2]
+    assert args[4] == tab.at and args[7:10] == (5, 1, 0)
+    name, args = binding._L.calls[3]
+    assert args[4] is None and args[7:10] == (5, 0, 1) and args[10] is None
+
+
+def test_shapes_are_refused(binding):  # noqa: F811
+    import torch
+    from paper_2607_18253_amd import KvPages
+    B, F, I = torch.bfloat16, torch.float32, torch.int32
+    pages = KvPages(*(Tensor((9, 2, 16, 64), B) for _ in range(2)))
+    q, tab, lse, w = Tensor((3, 8, 64), B), Tensor((1, 4), I), Tensor((3, 8), F), Tensor((9, 2, 16), F)
+    for call in (lambda: binding.weigh(pages, Tensor((2, 8, 64), B), lse, tab, w),
+                 lambda: binding.weigh(pages, q, Tensor((3, 7), F), tab, w),
+                 lambda: binding.weigh(pages, q, lse, tab, Tensor((8, 2, 16), F)),
+                 lambda: binding.weigh(pages, q, lse, tab, Tensor((9, 16, 2), F)),
+                 lambda: binding.weigh(pages, q, lse, tab, w, before=Tensor((10, 2, 16), F)),
+                 lambda: binding.weigh(pages, q, lse, Tensor((0, 4), I), w),
+                 lambda: binding.select(Tensor((9, 2, 8), F), tab, 5),
+                 lambda: binding.select(w, tab, 5, rows=Tensor((2, 2, 5), I)),
+                 lambda: binding.select(w, tab, 0), lambda: binding.select(w, tab, -5),
+                 lambda: binding.keep(pages, tab, Tensor((1, 3, 5), I)), lambda: binding.keep(pages, tab, Tensor((2, 5), I)),
+                 lambda: binding.keep(pages, tab, Tensor((5,), I)), lambda: binding.keep(pages, tab, Tensor((1, 2, 5), torch.int64)),
+                 lambda: binding.keep(pages, tab, Tensor((1, 2, 5), I), weights=Tensor((8, 2, 16), F))):
+        with pytest.raises(ValueError):
+            call()
+    assert not binding._L.calls
+
+
+def test_parents_are_not_cut(binding):  # noqa: F811
+    for bad in ([-1, 0], [-1, 0, 0, 0], [-1, 0, 0.5], [-1, 0, 2 ** 31], [[-1, 0, 0]], 3):
+        with pytest.raises(ValueError):
+            binding.plan([3], [50], parents=bad)
+    assert not binding._L.calls
+    binding.plan([3], [50], parents=(-1, 0, 0))
+    assert binding._L.calls[0][0] == "lar_kv_plan_tree"
