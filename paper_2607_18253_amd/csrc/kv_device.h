@@ -49,8 +49,8 @@ struct KvSpan {
 constexpr int kWeighKeys = 256;
 
 // Contexts that are cut for the selection: stretches of one, one at least, and the working memory, in
-// words, of `contexts` sequences and heads with `cuts` of them.
-constexpr int kSelectStretch = 4096, kSelectDigits = 4, kSelectBins = 512;
+// words, of `contexts` sequences and heads with `cuts` of them.  kSelectCuts: the most of one context.
+constexpr int kSelectStretch = 4096, kSelectCuts = 256, kSelectDigits = 4, kSelectBins = 512;
 constexpr int kv_select_cuts(int32_t ctx) { return ctx > kSelectStretch ? (ctx + (kSelectStretch - 1)) / kSelectStretch : 1; }
 constexpr int64_t kv_select_words(int64_t contexts, int64_t cuts) {
   return contexts * 2 * kSelectDigits + (cuts + 3) / 4 * 4 + cuts * kSelectDigits * kSelectBins;

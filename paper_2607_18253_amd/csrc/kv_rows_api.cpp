@@ -41,7 +41,8 @@ int32_t weigh_splits(const lar_kv* kv) {
 // Five launches over all rows take 28 us and one for 165k rows; a workgroup 10 us and one for 1000 rows
 // in its registers, 1.9 for 1000 of more that it reads again for every digit, and all of them one for 200k
 // and 67k rows.  (8 contexts of 64k rows: 30 us cut, 129 whole; 256 of 64k: 129 and 243, of 32k: 78 and 51.)
-constexpr int kSelectWhole = 32768, kSelectCuts = 64;
+// Cut, 8 contexts of 260k, 500k and 1M rows take 46, 72 and 151 us; whole, the two longer ones 1.45 and 3.27 ms.
+constexpr int kSelectWhole = 32768;
 int32_t* select_work(const lar_kv* kv) {
   const int64_t narrow = (int64_t)2 * kv->waves * kNarrowRows * kv->g.D;  // words of narrow_o and wide_o
   const int64_t wide = (int64_t)2 * kv->groups * kWideRows * kv->g.D, cuts = kv->cuts * kv->g.hkv;

@@ -356,6 +356,7 @@ __global__ __launch_bounds__(kCut) void k_kv_select_write(KvSelectArgs A) {
       a += i < bin ? n : 0;
       e += i == bin ? n : 0;
     });
+    static_assert(kSelectCuts <= kCut);
     if (tid < k) a += w.above()[tid];
     if (a) atomicAdd(&before[0], a);
     if (e) atomicAdd(&before[1], e);

@@ -621,6 +621,14 @@ def test_select_cut_and_whole_agree():
     check_select([20000] * 3, 8192, 16, 16, hkv=1, make=make, seed=4, S=128)
 
 
+@pytest.mark.parametrize("c,budget,hkv", [(300001, 4096, 2), (1 << 20, 1000000, 1), ((1 << 20) + 1, 9000, 1)])
+def test_select_of_many_stretches(c, budget, hkv):
+    """Up to as many stretches as are cut, and one more row, with many equal weights."""
+    def make(rng, shape):
+        return rng.randint(0, 5000, size=shape).astype(np.float32)
+    check_select([c, 9, 5000], budget, 4, 100, hkv=hkv, make=make, seed=5)
+
+
 # ------------------------------------------------------------------ together
 @pytest.mark.parametrize("cache", [BF, E4])
 def test_drafts_are_verified_and_kept(cache):
