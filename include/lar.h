@@ -565,7 +565,8 @@ lar_status lar_estimate_lps(lar_ctx *ctx, const lar_lps_params *params, int32_t 
  * weights, dev [n_blocks][n_kv_heads][block_size] float32, the caller's, for each layer:
  *     weights_j = before_j + sum_r exp(s_rj - lse_r)
  * over the batch's tokens r that see j and the heads of the group, with before_j = 0 for the
- * batch's new tokens.  A row r whose lse is -infinity adds nothing.
+ * batch's new tokens.  A row r whose lse is -infinity adds nothing.  Of a tree the accepted tokens
+ * are weighed, once they are in their places, as a batch of those alone.
  *
  * Budgets.  lar_kv_select names, for every sequence of the plan (also those without new tokens)
  * and kv head, the rows of its context to keep: all ctx_len if these are within the budget, else

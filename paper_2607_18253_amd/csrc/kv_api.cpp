@@ -342,11 +342,13 @@ int split(const std::vector<Tile>& narrow, const std::vector<Tile>& wide, int gr
   // microseconds: of a wide key tile and a stretch's start and end, of a narrow one among a
   // CU's eight waves (255 tokens beside 7 chunks of 512 with heads of 64: 161 us, 182 with a time
   // 1.6 times less; 40 tokens beside them: 92 and 103); bytes of a narrow one
-  const double wt = g.D == 128 ? 2.1 : 1.35, ws = 8.0, nt = g.D == 128 ? 3.4 : 2.7;
+  const double wt = g.D == 128 ? 2.1 : 1.35, ws = 8.0, nt = g.D == 64 ? 2.7 : trees && g.cache != kKvE4m3 ? 4.8 : 3.4;
   const double nb = 2.0 * kNarrowKeys * g.D * (g.cache == kKvE4m3 ? 1 : 2), rate = 5.2e6;
   int64_t n = 0;
   // Tiles of trees have fewer rows, and their loads to wait for (125 trees of 5 to 31 tokens over
-  // 1.2k keys each: 168 us, 200 with the time of a full one).
+  // 1.2k keys each: 168 us, 200 with the time of a full one).  Narrow tiles of 16 KB wait beside them too
+  // (those trees, 60 of 3 to 40 tokens beside 60 single ones, 100 of 8 to 32 beside 150: 150, 134 and 256 us, with
+  // the time of other batches 168, 144 and 278; tiles of 8 KB, with 8-bit rows or heads of 64, do not).
   double w = 0;
   for (const Tile& t : wide) w += t.tiles * (trees ? 0.5 + 0.5 * (t.s.ntok * g.G) / kWideRows : 1.0);
   for (const Tile& t : narrow) n += t.tiles;

@@ -1,6 +1,6 @@
-// kv_device.h -- what the host (kv_api.cpp, kv_rows_api.cpp) and the kernels (kv_pages.hip,
-// kv_attend.hip, kv_tree.hip, kv_weigh.hip, kv_select.hip, kv_keep.hip) of the paged key/value
-// cache share: the geometry, the plan of a token batch and the launches.
+// kv_device.h -- what the host (kv_api.cpp, kv_rows_api.cpp, kv_handle.h) and the kernels (kv_pages.hip,
+// kv_attend.hip, kv_tree.hip, kv_weigh.hip, kv_select.hip, kv_keep.hip; kv_attend.h, kv_cut.h) of the
+// paged key/value cache share: the geometry, the plan of a token batch and the launches.
 //
 // Cache of one layer: pages of S = 2^sh tokens, [page][kv head][S][D] for K and for V, as
 // 16-bit values or as e4m3 codes with one byte per (page, kv head, row): the exponent k of

@@ -122,7 +122,7 @@ inline lar_status ready(lar_kv* kv) {
   return LAR_OK;
 }
 
-// The arguments that append, read and attend share.
+// The arguments that the calls on pages share.
 inline lar_status check(lar_kv* kv, const lar_kv_pages* pages, const int32_t* table, int32_t cols, KvPool* pool) {
   if (lar_status st = ready(kv)) return st;
   if (!pages || !pages->k || !pages->v) return fail(kv, LAR_E_ARG, "null pages");

@@ -1,6 +1,7 @@
 """Python binding of the paged key/value cache (lar_kv_* in include/lar.h): a token batch's
 K and V rows into and out of the pages, its attention over them, with trees of drafted tokens,
-and which rows stay within a budget.  Argument marshalling only, as in ``lar``; every step runs in the HIP kernels behind the C ABI.
+the weights that it gives to the rows, and which rows stay within a budget.  Argument marshalling
+only, as in ``lar``; every step runs in the HIP kernels behind the C ABI.
 """
 
 from __future__ import annotations
@@ -320,9 +321,9 @@ class PagedKV:
         tensor [n_blocks][n_kv][block_size] (new_weights), updated in place, or made of `before`;
         the batch's new tokens start with 0."""
         pg, qa = self._pages(pages), self._rows(q, self._q_shape, "q")
-        if lse.requires_grad:
-            self._no_gradient("lse")
         z = _on(self._index, lse, self._torch.float32, "lse", self._n_tok * self.n_q)
+        if lse is not None and lse.requires_grad:
+            self._no_gradient("lse")
         w = self._weights(weights, "weights", pages.k.shape[0])
         b = w if before is None else self._weights(before, "before", pages.k.shape[0])
         t, cols = self._table(table)
