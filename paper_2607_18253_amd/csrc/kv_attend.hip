@@ -444,7 +444,10 @@ hipError_t run(const KvAttendArgs& a, hipStream_t stream) {
   // Many parts: more threads to share them out to (40 tokens of 8 heads over 4000 keys, 16
   // parts of each tile: 15.4 us with 1024 threads, 19.3 with 256); few parts of many tiles:
   // smaller workgroups (255 decode tokens take 1.5 % more with 1024).
-  if (a.n_join && a.most_parts > 8)
+  // Few tiles of trees, 1024 quads of values each: 6.7 us, 10.1 with 256 (125 trees of 5 to 31 tokens); with half
+  // as many, of heads of 64, they take the same.
+  const bool large = a.trees && a.n_join < 512 && a.join_rows * D >= 4096;
+  if (a.n_join && (a.most_parts > 8 || large))
     k_kv_join<BF, D, 1024><<<a.n_join, 1024, 0, stream>>>(a);
   else if (a.n_join)
     k_kv_join<BF, D, 256><<<a.n_join, 256, 0, stream>>>(a);
