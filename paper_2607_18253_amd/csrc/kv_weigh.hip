@@ -6,8 +6,7 @@
 // with the lse of the attention, so that one pass over K will do; new tokens have before_j = 0.
 //
 // S = Q K^T by 32x32x16 matrix instructions: a key is a column, held by lanes n and n + 32, and its
-// sum over 32 rows is a lane's own, in 32 bits.  Each key's sum has one order, whatever the launch, so
-// results repeat bit for bit.
+// sum over 32 rows is a lane's own, in 32 bits, in an order that the plan fixes: results repeat bit for bit.
 //
 //   k_kv_weigh_narrow  the plan's narrow stretches (single tokens, short chunks): a wave has its keys
 //                      to itself.
@@ -104,9 +103,9 @@ __device__ __forceinline__ void put(const KvWeighArgs& A, uint32_t row, bool fre
 constexpr int kRing = 3;
 
 // A wave takes its tiles through LDS, where whole rows of a page arrive in wide loads (straight from the
-// pages into the instructions' registers each load takes 32 bytes of 32 rows), the keys' sums so far along
-// with them.  Bound by the bytes of K: 255 tokens over 600 MB of it take 151 us, 4.5 TB/s; one, two or
-// four tiles on their way 163, 154 and 152.
+// pages into the instructions' registers each load takes 32 bytes of 32 rows: 154 us), the keys' sums so
+// far along with them.  Bound by the bytes of K: 255 tokens over 680 MB of it take 151 us, 4.5 TB/s; larger
+// batches come to 5.0, with any number of tiles or waves.
 
 template <bool BF, bool F8, int D>
 __global__ __launch_bounds__(64, 2) void k_kv_weigh_narrow(KvWeighArgs A) {
@@ -230,8 +229,10 @@ __device__ __forceinline__ int wide_seq(const KvWeighArgs& A, int b) {
 constexpr int kNoToken = -(3 << 29);
 
 // One workgroup per kWeighKeys keys of a sequence and kv head, KF * 32 of them for a wave, whose
-// part of K stays in its registers; 32 rows of Q at a time are in LDS for all waves.  Bound by the
-// exponentials: one for a weight, at a quarter of the vector unit's rate.
+// part of K stays in its registers; 32 rows of Q at a time are in LDS for all waves.  The scores of the
+// next rows run beside the exponentials of these, one for a weight at a quarter of the vector unit's rate;
+// matrix and vector instructions fill the cycles between them.  2048 tokens of 32 heads over 49k keys of an e4m3
+// cache: 793 us, 1020 TFLOP/s (one after the other 1273; 32 keys for a wave 1079).
 template <bool BF, bool F8, int D, int KF>
 __global__ __launch_bounds__(2 * kWeighKeys / KF, 2) void k_kv_weigh_wide(KvWeighArgs A) {
   constexpr int kThreads = 2 * kWeighKeys / KF, kChunks = D / 8, kStep = kThreads / kChunks;
