@@ -22,12 +22,14 @@ struct List {
   const KvKeepArgs& A;
   const int32_t *rows, *table, *to;
   int head, base, skip, limit;  // skip: padding rows before the first new token
+  int n;                        // entries to look at: as many as can be right, and one that cannot
   bool bad = false, lost = false;
   __device__ __forceinline__ List(const KvKeepArgs& a, int seq, int h) : A(a), head(h) {
     const KvSpan s = A.spans[seq];
     base = A.fresh ? s.ctx - s.q_len : 0;
     skip = base < 0 ? -base : 0;
     limit = A.fresh ? s.q_len : s.ctx;
+    n = min(A.n_rows, max(0, limit - skip) + 1);
     rows = A.rows + ((int64_t)seq * A.heads + (A.heads > 1 ? h : 0)) * A.n_rows;
     table = A.table + (int64_t)seq * A.cols;
     to = A.to + (int64_t)seq * A.to_cols;
@@ -41,7 +43,7 @@ struct List {
   }
   __device__ __forceinline__ Move move(int i) {
     Move m{0, 0, false};
-    if (i >= A.n_rows) return m;
+    if (i >= n) return m;
     const int r = rows[i], before = i ? rows[i - 1] : skip - 1;
     if (r == -1) return m;                           // the list has ended
     if (r >= limit || r < skip + i || r <= before || (i && before < 0)) {
@@ -76,14 +78,14 @@ __device__ __forceinline__ void move_rows(List& list, char* pool, int row_bytes,
   Move m[U], next[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) m[u] = list.move(u * step + r);
-  for (int i0 = 0; i0 < list.A.n_rows; i0 += step * U) {
+  for (int i0 = 0; i0 < list.n; i0 += step * U) {
     uint4 x[U] = {};
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (m[u].on) x[u] = *(const uint4*)(pool + (uint64_t)m[u].from * row_bytes + c * 16);
     // the rows after these are looked up while these are on their way
     const int i1 = i0 + step * U;
-    const bool more = i1 < list.A.n_rows && list.rows[i1] != -1;  // the same for all
+    const bool more = i1 < list.n && list.rows[i1] != -1;  // the same for all
 #pragma unroll
     for (int u = 0; u < U; ++u) next[u] = more ? list.move(i1 + u * step + r) : Move{0, 0, false};
     read(x);
@@ -102,7 +104,7 @@ __device__ __forceinline__ void move_marks(List& list) {
   const KvKeepArgs& A = list.A;
   const bool f8 = A.g.cache == kKvE4m3;
   uint8_t *ke = (uint8_t*)A.pool.ke, *ve = (uint8_t*)A.pool.ve;
-  for (int i0 = 0; i0 < A.n_rows; i0 += THREADS) {
+  for (int i0 = 0; i0 < list.n; i0 += THREADS) {
     if (i0 && list.rows[i0] == -1) break;
     const Move m = list.move(i0 + threadIdx.x);
     uint8_t a = 0, b = 0;

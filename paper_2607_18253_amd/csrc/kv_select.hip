@@ -49,6 +49,11 @@ struct Context {
   __device__ __forceinline__ bool between(int j) const { return j >= A.first && j < end; }
 };
 
+// All rows of a context within its budget: entries from i on, every step-th.  A budget may end at 2^31 - 1.
+__device__ __forceinline__ void fill(const KvSelectArgs& A, const Context& c, uint32_t i, uint32_t step) {
+  for (; i < (uint32_t)A.budget; i += step) c.rows[i] = i < (uint32_t)c.n ? (int)i : -1;
+}
+
 // Inclusive prefix sum over a wave.
 __device__ __forceinline__ int wave_sums(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr:1
@@ -108,7 +113,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_kv_select(KvSelectArgs A) {
   }
   Context c(A, blockIdx.x);
   if (c.n <= A.budget) {
-    for (int i = tid; i < A.budget; i += THREADS) c.rows[i] = i < c.n ? i : -1;
+    fill(A, c, tid, THREADS);
     return;
   }
   uint32_t x[R];
@@ -334,7 +339,7 @@ __global__ __launch_bounds__(kCut) void k_kv_select_write(KvSelectArgs A) {
   const int k = w.k;
   Context c(A, w.seq, w.head);
   if (c.n <= A.budget) {
-    for (int i = k * kCut + tid; i < A.budget; i += w.cuts * kCut) c.rows[i] = i < c.n ? i : -1;
+    fill(A, c, k * kCut + tid, w.cuts * kCut);
     return;
   }
   int want = A.budget - A.first - A.last;

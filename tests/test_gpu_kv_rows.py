@@ -500,6 +500,35 @@ def test_keep_bad_lists(rows):
         assert torch.equal(t[~mine], b[~mine])
 
 
+def test_lists_and_budgets_of_2_to_the_31_less_1():
+    n = 2 ** 31 - 1
+    x = Cache([1], [40], hkv=1)
+    tab = x.tab.to(DEV)
+    before = [t.clone() for t in x.tensors(True)]
+    r = torch.zeros((1, 1, n), dtype=torch.int32, device=DEV)  # does not ascend, and never ends
+    x.kv.keep(x.pages, tab, r, weights=x.w)
+    refused(L.LAR_E_STATE, x.kv.sync)
+    x.kv.plan([1], [40])
+    for t, b in zip(x.tensors(True), before):
+        t.copy_(b)
+    r.fill_(-1)
+    want = sorted(x.rng.permutation(40)[:17].tolist())
+    r[0, 0, :17] = torch.tensor(want, dtype=torch.int32)
+    x.kv.keep(x.pages, tab, r, weights=x.w)
+    x.kv.sync()
+    at = lambda j: (x.tab[0, j // 16], 0, j % 16)  # noqa: E731
+    for i, j in enumerate(want):
+        assert x.w[at(i)] == before[-1][at(j)]
+    for c in (40, 70000):  # whole, and cut
+        y = Cache([1], [c], hkv=1)
+        r.fill_(7)
+        y.kv.select(y.w, y.tab.to(DEV), n, rows=r)
+        y.kv.sync()
+        assert torch.equal(r[0, 0, :c].cpu(), torch.arange(c, dtype=torch.int32))
+        for i in range(c, n, 1 << 28):
+            assert bool((r[0, 0, i:i + (1 << 28)] == -1).all()), i
+
+
 def test_pages_outside_the_pool_are_reported():
     for bad in (-1, 1000, 2 ** 31 - 1):
         x = Cache([1, 30], [40, 60], cache=E4)
