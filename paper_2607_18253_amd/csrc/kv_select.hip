@@ -38,13 +38,13 @@ struct Context {
     table = A.table + (int64_t)seq * A.cols;
     rows = A.rows + ((int64_t)seq * A.g.hkv + head) * A.budget;
   }
-  __device__ __forceinline__ uint32_t weight(int j) {
-    const int32_t page = table[j >> A.g.sh];
-    if ((uint32_t)page >= A.n_blocks) {
-      lost = true;
-      return 0u;
-    }
-    return order(A.weights[(((int64_t)page * A.g.hkv + head) << A.g.sh) + (j & ((1 << A.g.sh) - 1))]);
+  __device__ __forceinline__ int32_t page(int j) const { return table[j >> A.g.sh]; }
+  __device__ __forceinline__ uint32_t weight(int32_t page, int j) {
+    const bool in = (uint32_t)page < A.n_blocks;  // else page 0's: no branch between the loads
+    lost |= !in;
+    const uint32_t row = (in ? (uint32_t)page : 0u) * ((uint32_t)A.g.hkv << A.g.sh) + ((uint32_t)head << A.g.sh);
+    const float w = A.weights[row + (uint32_t)(j & ((1 << A.g.sh) - 1))];
+    return in ? order(w) : 0u;
   }
   __device__ __forceinline__ bool between(int j) const { return j >= A.first && j < end; }
 };
@@ -117,12 +117,16 @@ __global__ __launch_bounds__(THREADS, 4) void k_kv_select(KvSelectArgs A) {
     return;
   }
   uint32_t x[R];
-  const auto load = [&](int j0) {
+  const auto load = [&](int j0) {  // past the context the last row's, without a branch of threads
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       if (j0 + r * THREADS >= c.n) break;  // the same for all threads, here and below
-      const int j = j0 + r * THREADS + tid;
-      x[r] = j < c.n ? c.weight(j) : 0;
+      x[r] = (uint32_t)c.page(min(j0 + r * THREADS + tid, c.n - 1));
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (j0 + r * THREADS >= c.n) break;
+      x[r] = c.weight((int32_t)x[r], min(j0 + r * THREADS + tid, c.n - 1));
     }
   };
   load(0);
@@ -281,13 +285,14 @@ __global__ __launch_bounds__(kCut) void k_kv_select_count(KvSelectArgs A) {
   uint32_t v[kEach];
 #pragma unroll
   for (int r = 0; r < kEach; ++r) {
-    if (DIGIT == 0) {
-      const int j = k * kStretch + r * kCut + tid;
-      v[r] = c.between(j) ? c.weight(j) : 0;
-    } else {
+    if (DIGIT == 0)
+      v[r] = (uint32_t)c.page(min(k * kStretch + r * kCut + tid, c.n - 1));
+    else
       v[r] = w.numbers()[r * kCut + tid];
-    }
   }
+  if (DIGIT == 0)
+#pragma unroll
+    for (int r = 0; r < kEach; ++r) v[r] = c.weight((int32_t)v[r], min(k * kStretch + r * kCut + tid, c.n - 1));
   if (DIGIT == 0)
 #pragma unroll
     for (int r = 0; r < kEach; ++r) w.numbers()[r * kCut + tid] = v[r];
