@@ -41,20 +41,40 @@ struct List {
     }
     return (((uint32_t)page * (uint32_t)A.g.hkv + head) << A.g.sh) + (uint32_t)(pos & ((1 << A.g.sh) - 1));
   }
-  __device__ __forceinline__ Move move(int i) {
-    Move m{0, 0, false};
-    if (i >= n) return m;
-    const int r = rows[i], before = i ? rows[i - 1] : skip - 1;
-    if (r == -1) return m;                           // the list has ended
-    if (r >= limit || r < skip + i || r <= before || (i && before < 0)) {
-      bad = true;
-      return m;
+  // Rows i + k, i + step + k, .. of the list, `i` the same for all threads: all entries are asked for first,
+  // then all pages.
+  template <int U>
+  __device__ __forceinline__ void moves(int i, int k, int step, Move (&m)[U]) {
+    int r[U], before[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      r[u] = -1;
+      if (i + u * step >= n) continue;
+      const int at = min(i + u * step + k, n - 1);
+      r[u] = rows[at];
+      before[u] = rows[max(at - 1, 0)];
     }
-    const int src = base + r, dst = base + skip + i;
-    m.from = row(table[src >> A.g.sh], src);
-    m.to = row(to[dst >> A.g.sh], dst);
-    m.on = m.from != ~0u && m.to != ~0u && m.from != m.to;
-    return m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      m[u].on = false;
+      if (i + u * step >= n) continue;
+      const int at = i + u * step + k;
+      if (at >= n || r[u] == -1) continue;  // the list has ended
+      if (r[u] >= limit || r[u] < skip + at || (at && (r[u] <= before[u] || before[u] < 0))) {
+        bad = true;
+        continue;
+      }
+      m[u].from = (uint32_t)table[(base + r[u]) >> A.g.sh];
+      m[u].to = (uint32_t)to[(base + skip + at) >> A.g.sh];
+      m[u].on = true;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (!m[u].on) continue;
+      m[u].from = row((int32_t)m[u].from, base + r[u]);
+      m[u].to = row((int32_t)m[u].to, base + skip + i + u * step + k);
+      m[u].on = m[u].from != ~0u && m[u].to != ~0u && m[u].from != m[u].to;
+    }
   }
 };
 
@@ -76,8 +96,7 @@ template <int THREADS, int U>
 __device__ __forceinline__ void move_rows(List& list, char* pool, int row_bytes, int col, int cols) {
   const int c = col + threadIdx.x % cols, r = threadIdx.x / cols, step = THREADS / cols;
   Move m[U], next[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) m[u] = list.move(u * step + r);
+  list.moves(0, r, step, m);
   for (int i0 = 0; i0 < list.n; i0 += step * U) {
     uint4 x[U] = {};
 #pragma unroll
@@ -86,8 +105,7 @@ __device__ __forceinline__ void move_rows(List& list, char* pool, int row_bytes,
     // the rows after these are looked up while these are on their way
     const int i1 = i0 + step * U;
     const bool more = i1 < list.n && list.rows[i1] != -1;  // the same for all
-#pragma unroll
-    for (int u = 0; u < U; ++u) next[u] = more ? list.move(i1 + u * step + r) : Move{0, 0, false};
+    if (more) list.moves(i1, r, step, next);
     read(x);
     __syncthreads();
 #pragma unroll
@@ -106,7 +124,9 @@ __device__ __forceinline__ void move_marks(List& list) {
   uint8_t *ke = (uint8_t*)A.pool.ke, *ve = (uint8_t*)A.pool.ve;
   for (int i0 = 0; i0 < list.n; i0 += THREADS) {
     if (i0 && list.rows[i0] == -1) break;
-    const Move m = list.move(i0 + threadIdx.x);
+    Move one[1];
+    list.moves(i0, threadIdx.x, THREADS, one);
+    const Move m = one[0];
     uint8_t a = 0, b = 0;
     float w = 0.0f;
     if (m.on) {
