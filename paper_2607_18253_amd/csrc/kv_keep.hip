@@ -5,7 +5,7 @@
 // moved one after the other none is written over before it is read, and of those that are moved at
 // the same time all are read before one is written.  A workgroup walks over the list of one sequence
 // and head in that order, with its share of the columns of K, or of V, or with the rows' exponents
-// and weights.  Bound by the rows' bytes, read and written: 674 MB in 164 us, 4.1 TB/s, for 127 contexts.
+// and weights.  Bound by the rows' bytes, read and written: 674 MB in 146 us, 4.6 TB/s, for 127 contexts.
 #include "../../include/lar.h"
 #include "kv_device.h"
 
@@ -143,7 +143,7 @@ __device__ __forceinline__ void move_marks(List& list) {
   }
 }
 
-constexpr int kFewGroups = 1024;
+constexpr int kFewGroups = 128;  // half the CUs
 
 // Jobs of a sequence and head: the shares of K, those of V, the marks.
 template <int THREADS>
@@ -170,20 +170,18 @@ hipError_t launch_kv_keep(const KvKeepArgs& a, hipStream_t stream) {
   const bool marks = a.g.cache == kKvE4m3 || a.weights;
   const int cols = a.g.D * (a.g.cache == kKvE4m3 ? 1 : 2) / 16;  // 16 bytes each
   const int64_t lists = (int64_t)a.n_seq * a.g.hkv;
-  // One pass of a small workgroup, or many of a larger one, which has fewer barriers for its bytes, and
-  // then a cache line of a long row for each (127 contexts to 777 rows of 256 bytes: 161 us; with 256
-  // threads 176, with whole rows 164).  Few lists: more shares of the columns, 64 bytes at least, and
-  // still more threads (92 lists of 3763 rows: 61 us, 151 with one of 256 threads for a list).
-  const bool small = a.n_rows * (int64_t)cols <= 1024;
+  // A few passes of a small workgroup, or as many threads as there are, which have fewer barriers for their
+  // bytes, and then a cache line of a long row for each workgroup (127 contexts to 777 rows of 256 bytes in
+  // the kernel: 137 us; with 256 threads 141, with whole rows 144, with half lines 166).  Half lines only while
+  // lists leave CUs over (8 lists of 5000 such rows: 27 us, 39 with lines; 32 of them: 56 and 46).
+  const bool small = a.n_rows * (int64_t)cols <= 2048;
   int shares = !small && cols == 16 ? 2 : 1;
-  while (2 * lists * shares < kFewGroups && cols / shares > 4) shares *= 2;
+  while (!small && 2 * lists * shares < kFewGroups && cols / shares > 4) shares *= 2;
   const int jobs = 2 * shares + marks;
   if (small)
     k_kv_keep<256><<<lists * jobs, 256, 0, stream>>>(a, shares, jobs);
-  else if (2 * lists * shares < kFewGroups)
-    k_kv_keep<1024><<<lists * jobs, 1024, 0, stream>>>(a, shares, jobs);
   else
-    k_kv_keep<512><<<lists * jobs, 512, 0, stream>>>(a, shares, jobs);
+    k_kv_keep<1024><<<lists * jobs, 1024, 0, stream>>>(a, shares, jobs);
   return hipGetLastError();
 }
 

@@ -9,9 +9,9 @@
 // same for most, and their counts would wait for one another.  The positions then come out in one
 // more pass, by prefix sums over ballots.
 //
-// Bound by latency: a few dependent steps between barriers for some 10 KB of weights, 25 us for 2040 contexts
+// Bound by latency: a few dependent steps between barriers for some 10 KB of weights, 24 us for 2040 contexts
 // of 1.3k rows on the mean (read again for every digit 67); and a context that is cut takes five launches,
-// 37 us for 8 of 130k rows (349 with a workgroup each).
+// 33.5 us for 8 of 130k rows (349 with a workgroup each).
 #include "../../include/lar.h"
 #include "kv_cut.h"
 
