@@ -38,10 +38,10 @@ int32_t weigh_splits(const lar_kv* kv) {
 }
 
 // Working memory for a selection whose contexts are cut, or null where a workgroup takes a whole one.
-// Five launches over all rows take 28 us and one for 165k rows; a workgroup 8 us and 0.85 for 1000 rows
-// in its registers, 1.9 for 1000 of more that it reads again for every digit, and all of them one for 200k
-// and 67k rows.  (8 contexts of 64k rows: 30 us cut, 129 whole; 256 of 64k: 129 and 243, of 32k: 78 and 51.)
-// Cut, 8 contexts of 260k, 500k and 1M rows take 46, 72 and 151 us; whole, the two longer ones 1.45 and 3.27 ms.
+// Five launches over all rows take 28 us and one for 165k rows; a workgroup 7 us and 0.87 for 1000 rows
+// in its registers, 1.5 for 1000 that it reads again for every digit, and all of them one for 200k and 98k rows.
+// Cut and whole: 8 contexts of 24k rows 28 and 28 us, of 64k 29 and 105, of 1M 154 and 2124; 256 of 32k 78 and
+// 42, of 64k 126 and 167.
 constexpr int kSelectWhole = 32768;
 int32_t* select_work(const lar_kv* kv) {
   const int64_t narrow = (int64_t)2 * kv->waves * kNarrowRows * kv->g.D;  // words of narrow_o and wide_o
@@ -50,7 +50,7 @@ int32_t* select_work(const lar_kv* kv) {
       cuts * kSelectStretch > wide)
     return nullptr;
   const double n = kv->longest, all = (double)kv->rows * kv->g.hkv;
-  const double whole = n <= kSelectWhole ? std::max(8 + 0.85e-3 * n, all / 200e3) : std::max(1.9e-3 * n, all / 67e3);
+  const double whole = n <= kSelectWhole ? std::max(7 + 0.87e-3 * n, all / 200e3) : std::max(1.5e-3 * n, all / 98e3);
   return 28 + all / 165e3 < whole ? (int32_t*)kv->narrow_o : nullptr;
 }
 
