@@ -708,6 +708,60 @@ def test_drafts_are_verified_and_kept(cache):
 
 
 @pytest.mark.parametrize("cache", [BF, E4])
+def test_accepted_tokens_are_weighed(cache):
+    """Of a tree the accepted tokens, once in their places, with the log-sums that the tree's attention gave: as
+    if they alone had been appended.  Their rows start with 0, whatever the pages' weights held there.
+
+    The scores are the same; the two log-sums are chains of at most 150 additions in 32 bits each, with a
+    logarithm of a few units at 2^-22: together off by 2 * (150 * 2^-24 + 8 * 2^-22) < 2^-14."""
+    hq, hkv, d, S = 8, 2, 64, 16
+    rng, g = np.random.RandomState(3), torch.Generator().manual_seed(3)
+    ctx, n = [101, 30, 5], [20, 3, 40]
+    par = [tree(m, rng) for m in n]
+    kv = PagedKV(hq, hkv, d, block_size=S, dtype=BF, cache_dtype=cache, max_seqs=3, max_tokens=200)
+    pages = kv.new_pages(30)
+    tab = torch.from_numpy(rng.permutation(30)[:24].reshape(3, 8).astype(np.int32)).to(DEV)
+    draw = lambda n, h: torch.randn((n, h, d), generator=g).to(BF).to(DEV)  # noqa: E731
+    kv.plan(ctx, ctx)
+    kv.append(pages, draw(sum(ctx), hkv), draw(sum(ctx), hkv), tab)
+    k, v, q = draw(sum(n), hkv), draw(sum(n), hkv), draw(sum(n), hq)
+    both = [c + m for c, m in zip(ctx, n)]
+    kv.plan(n, both, parents=sum(par, []))
+    kv.append(pages, k, v, tab)
+    lse = torch.empty((sum(n), hq), dtype=torch.float32, device=DEV)
+    kv.attend(pages, q, tab, lse=lse)
+    paths, start = [], np.cumsum([0] + n)
+    for m, p in zip(n, par):
+        a, line = m - 1, []
+        while a >= 0:
+            line.append(a)
+            a = p[a]
+        paths.append(line[::-1])
+    most = max(map(len, paths))
+    kv.keep(pages, tab, torch.tensor([x + [-1] * (most - len(x)) for x in paths], dtype=torch.int32, device=DEV), new=True)
+    pick = torch.tensor([start[s] + a for s, x in enumerate(paths) for a in x], device=DEV)
+    now = [c + len(x) for c, x in zip(ctx, paths)]
+    before = torch.full((30, hkv, S), math.nan, device=DEV)
+    for s, c in enumerate(ctx):
+        for j in range(c):
+            before[tab[s, j // S], :, j % S] = float(j)
+    got, want = before.clone(), before.clone()
+    kv.plan([len(x) for x in paths], now)
+    kv.weigh(pages, q[pick], lse[pick], tab, got)
+    kv.append(pages, k[pick], v[pick], tab)
+    own = torch.empty((len(pick), hq), dtype=torch.float32, device=DEV)
+    kv.attend(pages, q[pick], tab, lse=own)
+    kv.weigh(pages, q[pick], own, tab, want)
+    kv.sync()
+    for s, c in enumerate(now):
+        for j in range(c):
+            x, y = got[tab[s, j // S], :, j % S], want[tab[s, j // S], :, j % S]
+            added = y - (j if j < ctx[s] else 0)
+            # the sum so far, j, is rounded with what is added
+            assert ((x - y).abs() <= 2.0 ** -14 * added + 2.0 ** -23 * (j + 1)).all(), (s, j)
+
+
+@pytest.mark.parametrize("cache", [BF, E4])
 def test_contexts_are_held_to_a_budget(cache):
     """Steps of a decoding sequence whose cache is cut when it outgrows a budget: what stays is what the
     weights of all steps say, and later tokens attend over it, head by head."""
