@@ -489,10 +489,12 @@ void write_tree(const int32_t* parents, const int32_t* place, int32_t n, int32_t
       for (int64_t j = first; j < base; ++j) set(j);
     set(base + r);
     if (!window) continue;
-    for (int w = 0; w < words; ++w)
-      for (uint32_t x = to[1 + w]; x; x &= x - 1) {
+    bool out = true;  // places ascend with the keys: what is behind the window ends once
+    for (int w = 0; out && w < words; ++w)
+      for (uint32_t x = to[1 + w]; out && x; x &= x - 1) {
         const int64_t j = first + 32 * w + __builtin_ctz(x), p = j < base ? j : place[j - base];
-        if (p <= place[r] - window && p >= sinks) to[1 + w] &= ~(x & -x);
+        out = p <= place[r] - window;
+        if (out && p >= sinks) to[1 + w] &= ~(x & -x);
       }
   }
 }
