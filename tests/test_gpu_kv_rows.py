@@ -453,6 +453,17 @@ def test_keep_long(S):
     x.check([[some(x.rng, c, c // 2)] for c in ctx])
 
 
+@pytest.mark.parametrize("d,cache,n", [(128, BF, 6), (128, BF, 30), (128, E4, 12), (128, E4, 30), (64, BF, 30), (64, E4, 30)])
+def test_keep_many_lists(d, cache, n):
+    """From a few lists to as many as have a workgroup for whole cache lines of their rows, in place; the small
+    workgroups' lists and longer ones."""
+    ctx = [int(c) for c in np.random.RandomState(n).randint(1, 900, size=n)]
+    for short in (False, True):
+        x = Cache([1] * n, ctx, hkv=4, d=d, cache=cache)
+        x.check([[some(x.rng, c, min(c, 60) if short else c - c // 5) for _ in range(4)] for c in ctx])
+        x.check([[list(range(c // 3, c))[:60 if short else c] for _ in range(4)] for c in ctx])
+
+
 @pytest.mark.parametrize("cache", [BF, E4])
 def test_keep_into_other_pages(cache):
     """A table of fresh pages, one that begins with the old pages, and places that go on."""
