@@ -11,7 +11,7 @@
 //
 // Bound by latency: a few dependent steps between barriers for some 10 KB of weights, 24 us for 2040 contexts
 // of 1.3k rows on the mean (read again for every digit 67); and a context that is cut takes five launches,
-// 33.5 us for 8 of 130k rows (349 with a workgroup each).
+// 33 us for 8 of 130k rows (349 with a workgroup each).
 #include "../../include/lar.h"
 #include "kv_cut.h"
 
@@ -231,39 +231,35 @@ struct Cut : KvCut {
   __device__ __forceinline__ uint32_t* numbers() const { return A.numbers + (first + k) * kStretch; }
 };
 
-// Calls f(bin, count) for the four bins of this thread's share of each of the stretches [0, cuts) of
-// digit d, eight loads on their way at a time.
-template <int D, class F>
-__device__ __forceinline__ void each_count(const Cut& w, int cuts, F f) {
+// Takes digit D of the least number from all stretches' counts: a thread has four bins of some stretches,
+// eight loads on their way at a time.  `prior`: its counts of those before this one.
+template <int D>
+__device__ __forceinline__ void settle(const Cut& w, int* count, int* part, int* found, int& want, uint32_t& least,
+                                       uint32_t& digit, int (&prior)[4]) {
   constexpr int kQuads = bins_of(D) / 4, kSide = kCut / kQuads;
   const int quad = threadIdx.x % kQuads;
-  for (int k0 = threadIdx.x / kQuads; k0 < cuts; k0 += 8 * kSide) {
+  for (int i = threadIdx.x; i < bins_of(D); i += kCut) count[i] = 0;
+  int sum[4] = {0, 0, 0, 0};
+  for (int k0 = threadIdx.x / kQuads; k0 < w.cuts; k0 += 8 * kSide) {
     int4 x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       x[i] = make_int4(0, 0, 0, 0);
-      if (k0 + i * kSide < cuts) x[i] = *(const int4*)(w.counts(D, k0 + i * kSide) + 4 * quad);
+      if (k0 + i * kSide < w.cuts) x[i] = *(const int4*)(w.counts(D, k0 + i * kSide) + 4 * quad);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      f(4 * quad, x[i].x);
-      f(4 * quad + 1, x[i].y);
-      f(4 * quad + 2, x[i].z);
-      f(4 * quad + 3, x[i].w);
+      const int n[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        sum[b] += n[b];
+        prior[b] += k0 + i * kSide < w.k ? n[b] : 0;
+      }
     }
   }
-}
-
-// Takes digit D of the least number from all stretches' counts.
-template <int D>
-__device__ __forceinline__ void settle(const Cut& w, int* count, int* part, int* found, int& want, uint32_t& least,
-                                       uint32_t& digit) {
-  for (int i = threadIdx.x; i < bins_of(D); i += kCut) count[i] = 0;
-  int sum[4] = {0, 0, 0, 0};
-  each_count<D>(w, w.cuts, [&](int bin, int n) { sum[bin & 3] += n; });
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 4; ++i) atomicAdd(&count[4 * (threadIdx.x % (bins_of(D) / 4)) + i], sum[i]);
+  for (int b = 0; b < 4; ++b) atomicAdd(&count[4 * quad + b], sum[b]);
   __syncthreads();
   reach<bins_of(D), kCut>(count, part, found, want, digit);
   least |= digit << shift_of(D);
@@ -304,17 +300,25 @@ __global__ __launch_bounds__(kCut) void k_kv_select_count(KvSelectArgs A) {
       least = (uint32_t)w.state(kPast)[0];
       want = w.state(kPast)[1];
     }
+    // this stretch's own, asked for before the digit is known
+    constexpr int kOwn = (bins_of(kPast) + kCut - 1) / kCut;
+    int own[kOwn];
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) own[i] = w.counts(kPast, k)[tid + i * kCut];
+    const int above = DIGIT > 1 ? w.above()[k] : 0;
     if (tid == 0) more = 0;
-    settle<kPast>(w, count, part, found, want, least, digit);
+    int prior[4] = {};
+    settle<kPast>(w, count, part, found, want, least, digit, prior);
     if (k == 0 && tid == 0) {
       w.state(DIGIT)[0] = (int)least;
       w.state(DIGIT)[1] = want;
     }
     int sum = 0;  // of this stretch's rows with larger values of it
-    for (int i = tid; i < bins_of(kPast) - 1 - (int)digit; i += kCut) sum += w.counts(kPast, k)[i];
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) sum += tid + i * kCut < bins_of(kPast) - 1 - (int)digit ? own[i] : 0;
     if (sum) atomicAdd(&more, sum);
     __syncthreads();
-    if (tid == 0) w.above()[k] = (DIGIT > 1 ? w.above()[k] : 0) + more;
+    if (tid == 0) w.above()[k] = above + more;
   }
   constexpr int kShift = shift_of(DIGIT), kValues = bins_of(DIGIT);
   for (int i = tid; i < kValues; i += kCut) count[i] = 0;
@@ -360,16 +364,19 @@ __global__ __launch_bounds__(kCut) void k_kv_select_write(KvSelectArgs A) {
   if (some) {
     least = (uint32_t)w.state(D)[0];
     want = w.state(D)[1];
-    settle<D>(w, count, part, found, want, least, digit);
+    const int past = tid < k ? w.above()[tid] : 0;
+    int prior[4] = {};
+    settle<D>(w, count, part, found, want, least, digit, prior);
     // rows above the least, and equal ones, of the stretches before this one
     const int bin = bins_of(D) - 1 - (int)digit;
-    int a = 0, e = 0;
-    each_count<D>(w, k, [&](int i, int n) {
-      a += i < bin ? n : 0;
-      e += i == bin ? n : 0;
-    });
+    int a = past, e = 0;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const int at = 4 * (tid % (bins_of(D) / 4)) + b;
+      a += at < bin ? prior[b] : 0;
+      e += at == bin ? prior[b] : 0;
+    }
     static_assert(kSelectCuts <= kCut);
-    if (tid < k) a += w.above()[tid];
     if (a) atomicAdd(&before[0], a);
     if (e) atomicAdd(&before[1], e);
   }
