@@ -454,6 +454,7 @@ __global__ __launch_bounds__(kWeighKeys) void k_kv_weigh_sum(KvWeighArgs A) {
   const int j = (b - s.blocks) * kWeighKeys + threadIdx.x;
   if (j >= s.ctx) return;
   float y = 0.0f;
+#pragma unroll 8
   for (int i = 0; i < A.splits; ++i) y += A.parts[((int64_t)i * gridDim.x + blockIdx.x) * kWeighKeys + threadIdx.x];
   bool lost;
   const uint32_t row = pool_row(A, A.table[(int64_t)seq * A.cols + (j >> A.g.sh)], head, j, lost);
@@ -469,17 +470,29 @@ __global__ __launch_bounds__(256) void k_kv_weigh_copy(KvWeighArgs A) {
   const KvCut c = kv_cut(A.spans, A.n_seq, A.g.hkv, blockIdx.x);
   const KvSpan s = A.spans[c.seq];
   if (s.q_len == 0) return;
-#pragma unroll 4
-  for (int i = 0; i < kSelectStretch; i += 256) {
-    const int j = c.k * kSelectStretch + i + threadIdx.x;
-    if (j >= s.ctx - s.q_len) break;
+  const int end = s.ctx - s.q_len, j0 = c.k * kSelectStretch;
+  if (j0 >= end) return;
+  // all pages are looked up first, of rows past the end the last one's
+  constexpr int kRows = kSelectStretch / 256;
+  const auto key = [&](int i) { return min(j0 + i * 256 + (int)threadIdx.x, end - 1); };
+  const int32_t* table = A.table + (int64_t)c.seq * A.cols;
+  uint32_t row[kRows];
+  float x[kRows];
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) row[i] = (uint32_t)table[key(i) >> A.g.sh];
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) {
     bool lost;
-    const uint32_t row = pool_row(A, A.table[(int64_t)c.seq * A.cols + (j >> A.g.sh)], c.head, j, lost);
-    if (lost)
-      *A.err = kKvLostPage;
-    else
-      A.after[row] = A.before[row];
+    row[i] = pool_row(A, (int32_t)row[i], c.head, key(i), lost);
+    x[i] = A.before[row[i]];
+    any |= lost;
+    if (lost || j0 + i * 256 + (int)threadIdx.x >= end) row[i] = ~0u;  // no row of a pool
   }
+#pragma unroll
+  for (int i = 0; i < kRows; ++i)
+    if (row[i] != ~0u) A.after[row[i]] = x[i];
+  if (any) *A.err = kKvLostPage;
 }
 
 template <bool BF, bool F8, int D>
