@@ -604,7 +604,7 @@ lar_status plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t*
       KvSpan x{(int32_t)q0, q_len[s], ctx_len[s], -1, 0, (int32_t)std::min<int64_t>(blocks, INT32_MAX),
                (int32_t)std::min<int64_t>(cuts, INT32_MAX)};
       cuts += kv_select_cuts(ctx_len[s]);
-      if (q_len[s] > nt) blocks += ceil_div(ctx_len[s], kWeighKeys);
+      if (q_len[s] > nt) blocks += KvSeenBlocks(ctx_len[s] - q_len[s], window, sinks).count(ctx_len[s]);
       if (trees.most && trees.words[s]) {
         x.tree = (int32_t)rec;
         x.words = trees.words[s];

@@ -43,10 +43,36 @@ struct KvTok {
 struct KvSpan {
   int32_t q0, q_len, ctx;
   int32_t tree, words;
-  int32_t blocks;  // blocks of kWeighKeys keys of the sequences before it that take wide tiles
+  int32_t blocks;  // blocks of kWeighKeys keys that are seen, of the sequences before it that take wide tiles
   int32_t cuts;    // stretches of kSelectStretch rows of those before it
 };
 constexpr int kWeighKeys = 256;
+
+// The blocks of keys that some new token sees, of a sequence whose first one is at position `base` (< 0: a
+// padding row, and token 0 comes first): `sinks` of the first keys, then from `first` on.
+struct KvSeenBlocks {
+  int32_t sinks, first;
+  constexpr KvSeenBlocks(int32_t base, int32_t window, int32_t n_sinks)
+      : sinks(n_sinks / kWeighKeys + (n_sinks % kWeighKeys != 0)),
+        first(window && base >= window ? (base - window + 1) / kWeighKeys : 0) {
+    if (sinks > first) sinks = first;
+  }
+  constexpr int32_t count(int32_t ctx) const {
+    return sinks + (ctx / kWeighKeys + (ctx % kWeighKeys != 0)) - first;
+  }
+  // the first key of block i
+  constexpr int32_t key(int32_t i) const { return (i < sinks ? i : first - sinks + i) * kWeighKeys; }
+};
+
+// Of those tokens, by number, the first and the one past the last that see some of the block from key kb on.
+struct KvSeers {
+  int32_t t0, t1;
+  constexpr KvSeers(int32_t base, int32_t q_len, int32_t window, int32_t n_sinks, int32_t kb) : t0(0), t1(q_len) {
+    if (kb > base) t0 = kb - base;
+    if (base + t0 < 0) t0 = -base;
+    if (window && kb >= n_sinks && kb - base < q_len - window - kWeighKeys + 1) t1 = kb - base + window + kWeighKeys - 1;
+  }
+};
 
 // Contexts that are cut for the selection: stretches of one, one at least, and the working memory, in
 // words, of `contexts` sequences and heads with `cuts` of them.  kSelectCuts: the most of one context.

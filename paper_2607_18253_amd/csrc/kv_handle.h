@@ -60,7 +60,7 @@ struct lar_kv {
   int32_t n_seq = 0, n_tok = 0, window = 0, sinks = 0;
   int32_t max_pages = 0, all_pages = 0;  // of a context with new tokens, of any
   int32_t longest = 0;                   // context of any
-  int64_t blocks = 0;                    // of kWeighKeys keys of the sequences that take wide tiles
+  int64_t blocks = 0;                    // of kWeighKeys keys that are seen, of the sequences that take wide tiles
   int32_t most_new = 0;                  // new tokens of a sequence at most
   int64_t cuts = 0, rows = 0;            // stretches of kSelectStretch rows of all contexts; rows
   int32_t n_narrow = 0, n_wide = 0, n_join = 0, join_rows = 0, most_parts = 0;

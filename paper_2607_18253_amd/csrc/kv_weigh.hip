@@ -10,7 +10,7 @@
 //
 //   k_kv_weigh_narrow  the plan's narrow stretches (single tokens, short chunks): a wave has its keys
 //                      to itself.
-//   k_kv_weigh_wide    chunks: a wave keeps 32 or 64 keys and walks over the rows.
+//   k_kv_weigh_wide    chunks: a wave keeps 32 or 64 keys that some row sees and walks over the rows.
 //   k_kv_weigh_sum     the sums of workgroups that share the rows of a block of keys.
 //   k_kv_weigh_copy    under a window, the sums that no row of the batch adds to, from `before`.
 #include "../../include/lar.h"
@@ -250,14 +250,13 @@ __global__ __launch_bounds__(2 * kWeighKeys / KF, 2) void k_kv_weigh_wide(KvWeig
   if (other(A)) return;
   const int lo = wide_seq(A, b);
   const KvSpan s = plan_at(A.spans, lo);
-  const int kb0 = (b - s.blocks) * kWeighKeys, base = s.ctx - s.q_len, last = s.ctx - 1;
-  const int kb = kb0 + wave * 32 * KF;
-  // tokens that see some of the workgroup's keys
-  int t0 = kb0 > base ? kb0 - base : 0, t1 = s.q_len;
-  if (base + t0 < 0) t0 = -base;
-  if (A.window && kb0 >= A.sinks) t1 = min(t1, A.window + (kb0 - base + kWeighKeys - 1));
+  const int base = s.ctx - s.q_len, last = s.ctx - 1;
+  const int kb0 = KvSeenBlocks(base, A.window, A.sinks).key(b - s.blocks), kb = kb0 + wave * 32 * KF;
+  // tokens that see some of the workgroup's keys; there is one, so t0 < t1 <= q_len, whose rows 32 bits count
+  const KvSeers seers(base, s.q_len, A.window, A.sinks, kb0);
+  const int t0 = seers.t0, t1 = seers.t1;
   // this workgroup's rows, from row `start` on in `blocks` blocks of 32
-  const int step = 32 / G, rest = 32 % G, all_blocks = max(0, (t1 - t0) * G + 31) / 32;
+  const int step = 32 / G, rest = 32 % G, all_blocks = ((t1 - t0) * G + 31) / 32;
   const int start = t0 * G + 32 * (int)((int64_t)all_blocks * split / A.splits);
   const int blocks = (int)((int64_t)all_blocks * (split + 1) / A.splits) - (int)((int64_t)all_blocks * split / A.splits);
   // rows of Q: this thread's chunks of them, and for the first wave the log of a row's sum
@@ -451,7 +450,8 @@ __global__ __launch_bounds__(kWeighKeys) void k_kv_weigh_sum(KvWeighArgs A) {
   if (other(A)) return;
   const int seq = wide_seq(A, b);
   const KvSpan s = plan_at(A.spans, seq);
-  const int j = (b - s.blocks) * kWeighKeys + threadIdx.x;
+  const int base = s.ctx - s.q_len;
+  const int j = KvSeenBlocks(base, A.window, A.sinks).key(b - s.blocks) + (int)threadIdx.x;
   if (j >= s.ctx) return;
   float y = 0.0f;
 #pragma unroll 8
@@ -461,7 +461,7 @@ __global__ __launch_bounds__(kWeighKeys) void k_kv_weigh_sum(KvWeighArgs A) {
   if (lost)
     *A.err = kKvLostPage;
   else
-    put(A, row, j >= s.ctx - s.q_len, y);
+    put(A, row, j >= base, y);
 }
 
 // `before` to `after` for the context of the sequences with new tokens, a workgroup for a stretch.

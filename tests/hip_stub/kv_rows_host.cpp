@@ -41,6 +41,15 @@ int stub_weigh(int32_t* to) {
   weigh.after = nullptr;
   return was;
 }
+// Blocks of keys that a sequence's new tokens see; of block i the first key, and the tokens that see it.
+int stub_seen_blocks(int32_t ctx, int32_t q_len, int32_t window, int32_t sinks, int32_t i, int32_t* to) {
+  const lar::KvSeenBlocks b(ctx - q_len, window, sinks);
+  to[0] = b.key(i);
+  const lar::KvSeers s(ctx - q_len, q_len, window, sinks, to[0]);
+  to[1] = s.t0;
+  to[2] = s.t1;
+  return b.count(ctx);
+}
 // The number of the plan that the last call of a kind was made for: weights, selection, move.
 uint64_t stub_rows_plan(int what) { return what == 0 ? weigh.plan.id : what == 1 ? select_.plan.id : keep.plan.id; }
 int stub_keep(int32_t* to) {

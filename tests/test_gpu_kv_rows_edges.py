@@ -1,0 +1,61 @@
+"""Weights, selections and moves on the paged cache where batches leave the ordinary sizes: pages that a
+window hides, contexts at the limit, many contexts, lists that go on behind their end."""
+
+from __future__ import annotations
+
+from types import SimpleNamespace
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from gpu_util import DEV  # noqa: E402
+from paper_2607_18253_amd import PagedKV  # noqa: E402
+from paper_2607_18253_amd import lar as L  # noqa: E402
+from test_gpu_kv import BF, E4, F16, Batch, refused  # noqa: E402
+from test_gpu_kv_rows import KINDS, KINDS_OF_WEIGHTS, Cache, check_select, run_weigh, weigh_ref  # noqa: E402
+
+
+# ------------------------------------------------------------------ contexts at the limit
+@pytest.mark.parametrize("ctx", [40000000, (1 << 29) + 77, 1 << 30])
+@pytest.mark.parametrize("G,q_len", [(64, 40), (64, 1), (8, 3), (8, 90)])
+@pytest.mark.parametrize("place", [True])
+def test_weigh_far_from_the_sinks(ctx, G, q_len, place):
+    """The longest contexts under a window: only the pages of sinks and window are there."""
+    window, sinks, S, d = 300, 5, 65536, 64
+    cols, low = -(-ctx // S), ctx - q_len - window + 1
+    kv = PagedKV(G, 1, d, block_size=S, dtype=BF, max_seqs=1, max_tokens=1000)
+    pages = kv.new_pages(4)
+    tab = torch.full((1, cols), -1, dtype=torch.int32)
+    tab[0, 0], tab[0, low // S], tab[0, cols - 1] = 2, 0, 0 if low // S == cols - 1 else 3
+    g = torch.Generator().manual_seed(G)
+    for t in pages.tensors():
+        t.zero_()
+    rows = []
+    for n, end in ((sinks, sinks), (ctx - low, ctx)):
+        k = torch.randn((n, 1, d), generator=g).to(BF)
+        kv.plan([n], [end])
+        kv.append(pages, k.to(DEV), k.to(DEV), tab.to(DEV))
+        rows.append(k)
+    k = torch.cat(rows).double()
+    at = torch.cat([torch.arange(sinks), torch.arange(low, ctx)])
+    q = torch.randn((q_len, G, d), generator=g).to(BF)
+    p = torch.arange(ctx - q_len, ctx)[:, None]
+    mask = (at <= p) & ((at > p - window) | (at < sinks))
+    s = torch.einsum("thd,jd->htj", q.double(), k[:, 0]) * d ** -0.5
+    lse = torch.logsumexp(torch.where(mask, s, -torch.inf), 2).T.float().contiguous()
+    old = torch.rand((4, 1, S), generator=g)
+    want, bound = weigh_ref(SimpleNamespace(q_len=[q_len], ctx=[ctx], d=d, held=[[k]], q=q), 0, 0, mask, lse, d ** -0.5,
+                            torch.where(at < ctx - q_len, old[tab[0].long()[at // S], 0, at % S].double(), 0.0)[:, None])
+    kv.plan([q_len], [ctx], window=window, sinks=sinks)
+    w = old.to(DEV)
+    new = w if place else torch.full_like(w, 9.0)
+    kv.weigh(pages, q.to(DEV), lse.to(DEV), tab.to(DEV), new, before=None if place else w)
+    kv.sync()
+    got = new.cpu()[tab[0].long()[at // S], 0, at % S].double()[:, None]
+    assert ((got - want).abs() <= bound).all(), float(((got - want).abs() / bound).max())
+    # page 0 past the sinks is carried over as it was; page 1 is no one's
+    assert torch.equal(new.cpu()[2, 0, sinks:], old[2, 0, sinks:])
+    assert torch.equal(new.cpu()[1], old[1] if place else torch.full_like(old[1], 9.0))

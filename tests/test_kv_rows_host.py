@@ -274,6 +274,58 @@ def test_rows_calls_check_their_arguments(lib):
     x.close()
 
 
+def test_weights_have_the_key_blocks_that_are_seen(lib):
+    """Chunks under a window: blocks of 256 keys with one that some token sees, no others, and of each the
+    tokens that see one of it."""
+    rng, got = np.random.RandomState(0), np.zeros(3, np.int32)
+    g = got.ctypes.data_as(C.c_void_p)
+    for _ in range(400):
+        n = int(rng.randint(1, 1200))
+        c = max(0, n + int(rng.choice([-n, -7, 0, 1, 255, 256, 257, 900, 4000])))
+        window, sinks = int(rng.choice([0, 1, 2, 255, 256, 257, 600, 5000])), int(rng.choice([0, 1, 256, 300, 2 ** 31 - 1]))
+        p = np.arange(c - n, c)[:, None]
+        j = np.arange(c)[None]
+        mask = (j <= p) & ((window == 0) | (j > p - window) | (j < sinks))
+        want = [kb for kb in range(0, c, 256) if mask[:, kb:kb + 256].any()]
+        assert lib.stub_seen_blocks(c, n, window, sinks, 0, g) == len(want)
+        for i, kb in enumerate(want):
+            lib.stub_seen_blocks(c, n, window, sinks, i, g)
+            t = np.flatnonzero(mask[:, kb:kb + 256].any(1))
+            assert got[0] == kb and got[1] == t[0] and t[-1] < got[2] <= n, (c, n, window, sinks, kb)
+            # a last block ends with the context: its tokens are counted as if it went on
+            assert got[2] == t[-1] + 1 or kb + 256 > c, (c, n, window, sinks, kb)
+    x = Handle(lib, max_seqs=4, max_tokens=4096)
+    assert x.plan([512, 1, 40], [100000, 5000, 90], window=4096, sinks=4) == 0 and x.weigh() == 0
+    lib.stub_weigh(g)
+    first = (100000 - 512 - 4095) // 256
+    assert got[0] == 1 + (391 - first) + 1
+    x.close()
+
+
+@pytest.mark.parametrize("ctx", [1 << 26, (1 << 29) + 77, 1 << 30])
+def test_rows_of_far_key_blocks_are_counted_in_32_bits(lib, ctx):
+    """64 heads for a kv head and a chunk far from the sinks: the tokens of every block are within the chunk."""
+    got = np.zeros(3, np.int32)
+    for n, window, sinks in ((40, 300, 5), (5000, 4096, 0), (1 << 24, 1, 1000), (1, 1 << 20, 0)):
+        for i in range(lib.stub_seen_blocks(ctx, n, window, sinks, 0, got.ctypes.data_as(C.c_void_p))):
+            lib.stub_seen_blocks(ctx, n, window, sinks, i, got.ctypes.data_as(C.c_void_p))
+            kb, t0, t1 = (int(x) for x in got)
+            assert 0 <= kb < ctx and 0 <= t0 < t1 <= n and t1 * 64 < 2 ** 31
+            if i > 64:
+                break
+        assert x_blocks(lib, ctx, n, window, sinks) == lib.stub_seen_blocks(ctx, n, window, sinks, 0, got.ctypes.data_as(C.c_void_p))
+
+
+def x_blocks(lib, ctx, n, window, sinks):
+    """Blocks of one chunk that a call hands on."""
+    got = np.zeros(4, np.int32)
+    x = Handle(lib, max_seqs=1, max_tokens=n, hq=64, hkv=1, S=65536)
+    assert x.plan([n], [ctx], window=window, sinks=sinks) == 0 and x.weigh() == 0
+    lib.stub_weigh(got.ctypes.data_as(C.c_void_p))
+    x.close()
+    return int(got[0])
+
+
 def test_long_chunks_of_many_heads_are_refused(lib):
     """Rows of a sequence are counted in 32 bits."""
     x = Handle(lib, max_seqs=1, max_tokens=1 << 24, hq=64, hkv=1)
