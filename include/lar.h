@@ -634,9 +634,10 @@ typedef struct {
  *   together (LAR_E_ARG, LAR_E_CAPACITY).
  * lar_kv_weigh: q and scale as for lar_kv_attend, and lse what it gave.  before: the
  *   weights so far, weights itself or memory apart from it; the rows of the sequences with
- *   new tokens are written, all others stay as they are.  Two sequences with new tokens may not
- *   share pages here.  Not for a plan with trees (LAR_E_STATE), nor for more than 2^30 / (n_q_heads /
- *   n_kv_heads) new tokens of a sequence (LAR_E_CAPACITY).
+ *   new tokens are written, all others stay as they are.  Rows that a window hides from all new
+ *   tokens have what `before` has; pages of such rows alone may be gone (outside the pool).  Two
+ *   sequences with new tokens may not share pages here.  Not for a plan with trees (LAR_E_STATE),
+ *   nor for more than 2^30 / (n_q_heads / n_kv_heads) new tokens of a sequence (LAR_E_CAPACITY).
  * lar_kv_select: first + last <= budget.  rows dev [n_seqs][n_kv_heads][budget]: the positions
  *   to keep in ascending order, then -1.  n_blocks: of the weights.
  * lar_kv_keep: rows dev [n_seqs][n_kv_heads][n_rows], or with per_head 0 [n_seqs][n_rows] for all

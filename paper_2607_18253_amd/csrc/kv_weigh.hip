@@ -36,6 +36,12 @@ __device__ __forceinline__ uint32_t pool_row(const KvWeighArgs& A, int32_t page,
          (uint32_t)(j & ((1 << A.g.sh) - 1));
 }
 
+// Whether some token sees key j of the context, the first one being at position `base`.  What none sees is
+// looked at only where it shares a tile with what one does, and then its page may be gone.
+__device__ __forceinline__ bool is_seen(const KvWeighArgs& A, int base, int j) {
+  return !A.window || j > base - A.window || j < A.sinks;
+}
+
 // The values of a step t of 16 that half h of a lane has: in memory's order with 8-bit rows, where
 // 16 bytes are two steps.
 template <bool F8>
@@ -195,7 +201,7 @@ __global__ __launch_bounds__(64, 2) void k_kv_weigh_narrow(KvWeighArgs A) {
           on &= seeing(A, j, [&](int i) { return s.p0 + key_of(i, half) / G; });
         }
         const float sum = add_halves(add_up(sc, l, on, A.scale));
-        any |= gone && j <= last;
+        any |= gone && j <= last && is_seen(A, s.p0, j);
         if (h == 0 && j <= last && !gone) A.after[at] = before + sum;
         wave_order();
       }
@@ -437,10 +443,10 @@ __global__ __launch_bounds__(2 * kWeighKeys / KF, 2) void k_kv_weigh_wide(KvWeig
     if (j > last || h) continue;
     if (A.splits > 1)
       A.parts[(int64_t)blockIdx.x * kWeighKeys + j - kb0] = y;
-    else if (lost[f])
-      *A.err = kKvLostPage;
-    else
+    else if (!lost[f])
       put(A, row[f], j >= base, y);
+    else if (is_seen(A, base, j))
+      *A.err = kKvLostPage;
   }
 }
 
@@ -458,13 +464,14 @@ __global__ __launch_bounds__(kWeighKeys) void k_kv_weigh_sum(KvWeighArgs A) {
   for (int i = 0; i < A.splits; ++i) y += A.parts[((int64_t)i * gridDim.x + blockIdx.x) * kWeighKeys + threadIdx.x];
   bool lost;
   const uint32_t row = pool_row(A, A.table[(int64_t)seq * A.cols + (j >> A.g.sh)], head, j, lost);
-  if (lost)
-    *A.err = kKvLostPage;
-  else
+  if (!lost)
     put(A, row, j >= base, y);
+  else if (is_seen(A, base, j))
+    *A.err = kKvLostPage;
 }
 
-// `before` to `after` for the context of the sequences with new tokens, a workgroup for a stretch.
+// `before` to `after` for the context of the sequences with new tokens, a workgroup for a stretch.  A page
+// outside the pool has no weights to carry over; where a token sees it, the other kernels report it.
 __global__ __launch_bounds__(256) void k_kv_weigh_copy(KvWeighArgs A) {
   if (other(A)) return;
   const KvCut c = kv_cut(A.spans, A.n_seq, A.g.hkv, blockIdx.x);
@@ -478,7 +485,6 @@ __global__ __launch_bounds__(256) void k_kv_weigh_copy(KvWeighArgs A) {
   const int32_t* table = A.table + (int64_t)c.seq * A.cols;
   uint32_t row[kRows];
   float x[kRows];
-  bool any = false;
 #pragma unroll
   for (int i = 0; i < kRows; ++i) row[i] = (uint32_t)table[key(i) >> A.g.sh];
 #pragma unroll
@@ -486,13 +492,11 @@ __global__ __launch_bounds__(256) void k_kv_weigh_copy(KvWeighArgs A) {
     bool lost;
     row[i] = pool_row(A, (int32_t)row[i], c.head, key(i), lost);
     x[i] = A.before[row[i]];
-    any |= lost;
     if (lost || j0 + i * 256 + (int)threadIdx.x >= end) row[i] = ~0u;  // no row of a pool
   }
 #pragma unroll
   for (int i = 0; i < kRows; ++i)
     if (row[i] != ~0u) A.after[row[i]] = x[i];
-  if (any) *A.err = kKvLostPage;
 }
 
 template <bool BF, bool F8, int D>

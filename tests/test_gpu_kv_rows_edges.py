@@ -18,10 +18,81 @@ from test_gpu_kv import BF, E4, F16, Batch, refused  # noqa: E402
 from test_gpu_kv_rows import KINDS, KINDS_OF_WEIGHTS, Cache, check_select, run_weigh, weigh_ref  # noqa: E402
 
 
-# ------------------------------------------------------------------ contexts at the limit
+# ------------------------------------------------------------------ pages that a window hides
+def unseen(table, q_len, ctx, S, window, sinks):
+    """The table without the pages that no new token sees."""
+    out = table.clone()
+    for s, (n, c) in enumerate(zip(q_len, ctx)):
+        low = max(0, c - n) - window + 1
+        for i in range(-(-c // S)):
+            if n and i * S >= sinks and (i + 1) * S <= low:
+                out[s, i] = -1
+    assert (out != table).any()
+    return out
+
+
+HIDDEN = [([70], [5000], 100, 4),          # a chunk
+          ([1], [3001], 64, 0),            # one token
+          ([1, 3, 200, 40, 0], [900, 700, 4000, 2000, 600], 90, 70),
+          ([600, 1], [9000, 5000], 33, 300)]
+
+
+@pytest.mark.parametrize("q_len,ctx,window,sinks", HIDDEN)
+@pytest.mark.parametrize("S", [1, 16, 128])
+@pytest.mark.parametrize("cache", [BF, E4])
+def test_weigh_in_place_without_hidden_pages(q_len, ctx, window, sinks, S, cache):
+    """Pages that a window hides from all new tokens may be gone: they are not looked at, and all other rows
+    get what they get with them."""
+    b = Batch(q_len, ctx, hq=8, hkv=2, d=64, S=S, dtype=BF, cache=cache)
+    _, lse = b.attend(window, sinks)
+    tab = unseen(b.table.cpu(), q_len, ctx, S, window, sinks)
+    old = torch.rand((b.pages.k.shape[0], 2, S), generator=torch.Generator().manual_seed(1)).to(DEV)
+    want, got = old.clone(), old.clone()
+    b.k.weigh(b.pages, b.q.to(DEV), lse.to(DEV), b.table, want)
+    b.k.weigh(b.pages, b.q.to(DEV), lse.to(DEV), tab.to(DEV), got)
+    b.k.sync()
+    assert torch.equal(got, want)
+    gone = torch.unique(b.table.cpu()[tab != b.table.cpu()]).long().to(DEV)
+    assert torch.equal(got[gone], old[gone])
+
+
+@pytest.mark.parametrize("q_len,ctx,window,sinks", HIDDEN)
+@pytest.mark.parametrize("S", [1, 16, 128])
+def test_weigh_from_before_without_hidden_pages(q_len, ctx, window, sinks, S):
+    """The same from weights that lie apart: what has no place is not carried over."""
+    b = Batch(q_len, ctx, hq=8, hkv=2, d=128, S=S, dtype=F16, cache=F16)
+    _, lse = b.attend(window, sinks)
+    tab = unseen(b.table.cpu(), q_len, ctx, S, window, sinks)
+    old = torch.rand((b.pages.k.shape[0], 2, S), generator=torch.Generator().manual_seed(1)).to(DEV)
+    want, got = torch.full_like(old, 9.0), torch.full_like(old, 9.0)
+    b.k.weigh(b.pages, b.q.to(DEV), lse.to(DEV), b.table, want, before=old)
+    b.k.weigh(b.pages, b.q.to(DEV), lse.to(DEV), tab.to(DEV), got, before=old)
+    b.k.sync()
+    gone = torch.unique(b.table.cpu()[tab != b.table.cpu()]).long().to(DEV)
+    assert torch.equal(want[gone], old[gone])
+    want[gone] = 9.0
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("place", [True, False])
+def test_weigh_reports_lost_pages_that_are_seen(place):
+    """Under a window too, for chunks and single tokens, in the window and among the sinks."""
+    q_len, ctx, window, sinks, S = [70, 1], [2000, 900], 100, 20, 16
+    b = Batch(q_len, ctx, hq=8, hkv=2, d=64, S=S, dtype=BF, cache=BF)
+    _, lse = b.attend(window, sinks)
+    for s, i in ((0, 0), (0, (2000 - 70 - 99) // S), (0, 1999 // S), (1, 1), (1, 800 // S), (1, 899 // S)):
+        tab = b.table.clone()
+        tab[s, i] = -1
+        w = b.k.new_weights(b.pages.k.shape[0])
+        b.k.weigh(b.pages, b.q.to(DEV), lse.to(DEV), tab, w if place else torch.empty_like(w), before=None if place else w)
+        refused(L.LAR_E_STATE, b.k.sync)
+        b.k.plan(q_len, ctx, window=window, sinks=sinks)
+        b.k.sync()
+
+
 @pytest.mark.parametrize("ctx", [40000000, (1 << 29) + 77, 1 << 30])
 @pytest.mark.parametrize("G,q_len", [(64, 40), (64, 1), (8, 3), (8, 90)])
-@pytest.mark.parametrize("place", [True])
+@pytest.mark.parametrize("place", [True, False])
 def test_weigh_far_from_the_sinks(ctx, G, q_len, place):
     """The longest contexts under a window: only the pages of sinks and window are there."""
     window, sinks, S, d = 300, 5, 65536, 64
