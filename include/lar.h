@@ -648,8 +648,9 @@ typedef struct {
  *   to_table, dev [n_seqs][to_cols], or of table itself (NULL); a page of to_table is either the
  *   one that table has in that column or one that table has in no sequence of the batch, and no page
  *   that is written to belongs to two sequences.  What is at the places past a list stays.  Lists
- *   that do not ascend or leave the context set the sticky LAR_E_STATE; nothing is moved for an
- *   entry that does, and what the other places of such a list hold is undefined.
+ *   that do not ascend, leave the context or go on behind a -1 set the sticky LAR_E_STATE; no row
+ *   outside the context is touched for them, and what their places hold is undefined.  (Of a list
+ *   with more entries than the context has rows the first one too many is the last looked at.)
  * lar_kv_sync: synchronise the stream; the sticky device error, if any.
  * Each call works on the handle's stream, allocates nothing (but create) and does not
  * wait (but plan, as said, and sync).  A handle is not thread-safe; calls of one handle

@@ -78,6 +78,15 @@ struct List {
   }
 };
 
+// Whether a list goes on behind its end.  Of a list that is moved in one pass moves() sees it; in longer ones
+// a pass that starts behind the end is not made.  (After the moves, where the end is known, this takes the
+// kernel above 64 registers and two workgroups of 1024 on a CU.)
+template <int THREADS>
+__device__ __forceinline__ void look_behind(List& list) {
+  for (int i = threadIdx.x + 1; i < list.n; i += THREADS)
+    list.bad |= list.rows[i] != -1 && list.rows[i - 1] == -1;
+}
+
 // What was loaded has arrived before what follows: a barrier alone waits for no loads.
 template <int U>
 __device__ __forceinline__ void read(uint4 (&x)[U]) {
@@ -144,6 +153,7 @@ __device__ __forceinline__ void move_marks(List& list) {
 }
 
 constexpr int kFewGroups = 128;  // half the CUs
+constexpr int kAtOnce = 4;       // rows that a thread moves at once
 
 // Jobs of a sequence and head: the shares of K, those of V, the marks.
 template <int THREADS>
@@ -156,7 +166,8 @@ __global__ __launch_bounds__(THREADS) void k_kv_keep(KvKeepArgs A, int shares, i
   List list(A, x / A.g.hkv, x % A.g.hkv);
   if (job < 2 * shares) {
     const int bytes = A.g.D * (A.g.cache == kKvE4m3 ? 1 : 2), cols = bytes / 16 / shares;
-    move_rows<THREADS, 4>(list, (char*)(job < shares ? A.pool.k : A.pool.v), bytes, job % shares * cols, cols);
+    if (job == 0 && list.n > THREADS / cols * kAtOnce) look_behind<THREADS>(list);
+    move_rows<THREADS, kAtOnce>(list, (char*)(job < shares ? A.pool.k : A.pool.v), bytes, job % shares * cols, cols);
   } else {
     move_marks<THREADS>(list);
   }

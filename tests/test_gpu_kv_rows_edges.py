@@ -130,3 +130,22 @@ def test_weigh_far_from_the_sinks(ctx, G, q_len, place):
     # page 0 past the sinks is carried over as it was; page 1 is no one's
     assert torch.equal(new.cpu()[2, 0, sinks:], old[2, 0, sinks:])
     assert torch.equal(new.cpu()[1], old[1] if place else torch.full_like(old[1], 9.0))
+
+
+# ------------------------------------------------------------------ lists that go on behind their end
+@pytest.mark.parametrize("end", [32, 64, 128, 256, 512, 1024, 2048])
+@pytest.mark.parametrize("weights", [True, False])
+@pytest.mark.parametrize("cache", [BF, E4])
+def test_entries_behind_a_lists_end_are_reported(end, weights, cache):
+    """Wherever the first -1 is, and however far behind it another entry."""
+    x = Cache([1, 1], [3000, 2600], cache=cache)
+    for more in (1, 7, 400):
+        n = end + more + 1
+        rows = np.full((2, 2, n), -1, np.int32)
+        rows[:, :, :end] = np.arange(end)
+        x.kv.plan([1, 1], [3000, 2600])
+        x.kv.keep(x.pages, x.tab.to(DEV), torch.from_numpy(rows).to(DEV), weights=x.w if weights else None)
+        x.kv.sync()
+        rows[1, 1, n - 1] = 2500
+        x.kv.keep(x.pages, x.tab.to(DEV), torch.from_numpy(rows).to(DEV), weights=x.w if weights else None)
+        refused(L.LAR_E_STATE, x.kv.sync)
