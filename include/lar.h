@@ -651,6 +651,8 @@ typedef struct {
  *   that do not ascend, leave the context or go on behind a -1 set the sticky LAR_E_STATE; no row
  *   outside the context is touched for them, and what their places hold is undefined.  (Of a list
  *   with more entries than the context has rows the first one too many is the last looked at.)
+ * lar_kv_weigh, lar_kv_select, lar_kv_keep: LAR_E_CAPACITY for a batch of so many sequences and
+ *   heads that a launch would have 2^32 threads (some 100,000 sequences of 8 kv heads and more).
  * lar_kv_sync: synchronise the stream; the sticky device error, if any.
  * Each call works on the handle's stream, allocates nothing (but create) and does not
  * wait (but plan, as said, and sync).  A handle is not thread-safe; calls of one handle

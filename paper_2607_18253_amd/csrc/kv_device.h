@@ -215,6 +215,41 @@ struct KvKeepArgs {
   int32_t* err;
 };
 
+// A launch has less than 2^32 threads.
+constexpr bool kv_fits(int64_t groups, int threads) { return groups * threads < (int64_t)1 << 32; }
+
+// Threads for a context: while each has a CU of its own the more the better (256 contexts of 4000 rows: 17, 11
+// and 9.6 us with 256, 512 and 1024; of 16000 153, 40 and 27), then as many as leave room for others (1024 of
+// 4000: 28, 21 and 37; of 16000 225, 63 and 103), and of many short ones fewest (4096 of 600: 24, 29 and 71).
+constexpr int kSelectCus = 256;
+constexpr int kv_select_threads(int64_t contexts, int32_t longest) {
+  if (contexts <= kSelectCus || longest > 16384) return 1024;
+  return contexts <= 4 * kSelectCus || longest > 2048 ? 512 : 256;
+}
+
+// The launch of a move: of each list `jobs` workgroups, `shares` for K, as many for V, and one for the rows'
+// exponents and weights.
+//
+// A few passes of a small workgroup, or as many threads as there are, which have fewer barriers for their
+// bytes, and then a cache line of a long row for each workgroup (127 contexts to 777 rows of 256 bytes in
+// the kernel: 137 us; with 256 threads 141, with whole rows 144, with half lines 166).  Half lines only while
+// lists leave CUs over (8 lists of 5000 such rows: 27 us, 39 with lines; 32 of them: 56 and 46).
+struct KvKeepShape {
+  static constexpr int kFewGroups = 128;  // half the CUs
+  int threads, shares = 1, jobs;
+  int64_t groups;
+  KvKeepShape(const KvGeom& g, int32_t n_seq, int32_t n_rows, bool weights) {
+    const int64_t lists = (int64_t)n_seq * g.hkv;
+    const int cols = g.D * (g.cache == kKvE4m3 ? 1 : 2) / 16;  // 16 bytes each
+    const bool small = n_rows * (int64_t)cols <= 2048;
+    threads = small ? 256 : 1024;
+    if (!small && cols == 16) shares = 2;
+    while (!small && 2 * lists * shares < kFewGroups && cols / shares > 4) shares *= 2;
+    jobs = 2 * shares + (g.cache == kKvE4m3 || weights);
+    groups = lists * jobs;
+  }
+};
+
 hipError_t launch_kv_append(const KvCopyArgs& a, hipStream_t stream);
 hipError_t launch_kv_read(const KvCopyArgs& a, hipStream_t stream);
 hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t stream);

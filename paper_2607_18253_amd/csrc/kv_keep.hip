@@ -152,8 +152,7 @@ __device__ __forceinline__ void move_marks(List& list) {
   }
 }
 
-constexpr int kFewGroups = 128;  // half the CUs
-constexpr int kAtOnce = 4;       // rows that a thread moves at once
+constexpr int kAtOnce = 4;  // rows that a thread moves at once
 
 // Jobs of a sequence and head: the shares of K, those of V, the marks.
 template <int THREADS>
@@ -178,21 +177,11 @@ __global__ __launch_bounds__(THREADS) void k_kv_keep(KvKeepArgs A, int shares, i
 }  // namespace
 
 hipError_t launch_kv_keep(const KvKeepArgs& a, hipStream_t stream) {
-  const bool marks = a.g.cache == kKvE4m3 || a.weights;
-  const int cols = a.g.D * (a.g.cache == kKvE4m3 ? 1 : 2) / 16;  // 16 bytes each
-  const int64_t lists = (int64_t)a.n_seq * a.g.hkv;
-  // A few passes of a small workgroup, or as many threads as there are, which have fewer barriers for their
-  // bytes, and then a cache line of a long row for each workgroup (127 contexts to 777 rows of 256 bytes in
-  // the kernel: 137 us; with 256 threads 141, with whole rows 144, with half lines 166).  Half lines only while
-  // lists leave CUs over (8 lists of 5000 such rows: 27 us, 39 with lines; 32 of them: 56 and 46).
-  const bool small = a.n_rows * (int64_t)cols <= 2048;
-  int shares = !small && cols == 16 ? 2 : 1;
-  while (!small && 2 * lists * shares < kFewGroups && cols / shares > 4) shares *= 2;
-  const int jobs = 2 * shares + marks;
-  if (small)
-    k_kv_keep<256><<<lists * jobs, 256, 0, stream>>>(a, shares, jobs);
+  const KvKeepShape s(a.g, a.n_seq, a.n_rows, a.weights != nullptr);
+  if (s.threads == 256)
+    k_kv_keep<256><<<s.groups, 256, 0, stream>>>(a, s.shares, s.jobs);
   else
-    k_kv_keep<1024><<<lists * jobs, 1024, 0, stream>>>(a, shares, jobs);
+    k_kv_keep<1024><<<s.groups, 1024, 0, stream>>>(a, s.shares, s.jobs);
   return hipGetLastError();
 }
 

@@ -18,9 +18,9 @@ uint64_t weight_bytes(const lar_kv* kv, int64_t n_blocks) {
   return ((uint64_t)n_blocks * kv->g.hkv << kv->g.sh) * sizeof(float);
 }
 
-// Workgroups of a launch, one or more for each sequence and kv head.
-lar_status check_grid(lar_kv* kv, int64_t n) {
-  return n < (int64_t)1 << 31 ? LAR_OK : fail(kv, LAR_E_CAPACITY, "a batch of %lld workgroups", (long long)n);
+lar_status check_grid(lar_kv* kv, int64_t groups, int threads) {
+  if (kv_fits(groups, threads)) return LAR_OK;
+  return fail(kv, LAR_E_CAPACITY, "a batch of %lld workgroups of %d threads", (long long)groups, threads);
 }
 
 lar_status check_table(lar_kv* kv, const int32_t* table, int32_t cols, int64_t need, const char* name) {
@@ -78,7 +78,10 @@ lar_status lar_kv_weigh(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_rows
     return fail(kv, LAR_E_ARG, "before and weights must be the same or lie apart");
   if ((int64_t)kv->most_new * kv->g.G > 1 << 30)  // rows of a sequence and head are counted in 32 bits
     return fail(kv, LAR_E_CAPACITY, "%d new tokens of %d heads", kv->most_new, kv->g.G);
-  if (lar_status st = check_grid(kv, std::max(kv->blocks, kv->cuts) * kv->g.hkv)) return st;
+  const int32_t splits = weigh_splits(kv);
+  if (lar_status st = check_grid(kv, kv->blocks * kv->g.hkv * splits, kWeighKeys)) return st;
+  if (kv->window && a0 != b0)  // which carries rows over, by stretches
+    if (lar_status st = check_grid(kv, kv->cuts * kv->g.hkv, 256)) return st;
   KvWeighArgs a{};
   a.plan = plan_id(kv);
   a.g = kv->g;
@@ -99,7 +102,7 @@ lar_status lar_kv_weigh(lar_kv* kv, const lar_kv_pages* pages, const lar_kv_rows
   a.spans = (const KvSpan*)(kv->dev + kv->lay.spans);
   a.n_seq = kv->n_seq;
   a.cuts = (int32_t)(kv->cuts * kv->g.hkv);
-  a.splits = weigh_splits(kv);
+  a.splits = splits;
   a.parts = kv->narrow_o;
   a.err = kv->err;
   return launch(kv, launch_kv_weigh, a);
@@ -115,7 +118,10 @@ lar_status lar_kv_select(lar_kv* kv, const float* weights, int64_t n_blocks, con
   if (n_blocks < 1 || n_blocks > ((((int64_t)1 << 32) - 1) >> kv->g.sh) / kv->g.hkv)
     return fail(kv, LAR_E_ARG, "n_blocks must be in 1 .. (2^32 - 1) / (block_size * n_kv_heads)");
   if (lar_status st = check_table(kv, table, table_cols, kv->all_pages, "block table")) return st;
-  if (lar_status st = check_grid(kv, (int64_t)kv->n_seq * kv->g.hkv)) return st;
+  const int64_t contexts = (int64_t)kv->n_seq * kv->g.hkv;
+  int32_t* const work = select_work(kv);  // in which there is no room for too many
+  if (!work)
+    if (lar_status st = check_grid(kv, contexts, kv_select_threads(contexts, kv->longest))) return st;
   KvSelectArgs a{};
   a.plan = plan_id(kv);
   a.g = kv->g;
@@ -130,7 +136,7 @@ lar_status lar_kv_select(lar_kv* kv, const float* weights, int64_t n_blocks, con
   a.first = first;
   a.last = last;
   a.rows = rows;
-  a.work = select_work(kv);
+  a.work = work;
   a.numbers = (uint32_t*)kv->wide_o;
   a.cuts = a.work ? (int32_t)(kv->cuts * kv->g.hkv) : 0;
   a.err = kv->err;
@@ -155,7 +161,8 @@ lar_status lar_kv_keep(lar_kv* kv, const lar_kv_pages* pages, const int32_t* tab
   const int64_t places = fresh ? kv->longest : std::min(n_rows, kv->longest);
   if (lar_status st = check_table(kv, to_table, to_cols, ceil_div(places, (int64_t)1 << kv->g.sh), "table of the places"))
     return st;
-  if (lar_status st = check_grid(kv, (int64_t)kv->n_seq * kv->g.hkv * 64)) return st;
+  const KvKeepShape shape(kv->g, kv->n_seq, n_rows, weights != nullptr);
+  if (lar_status st = check_grid(kv, shape.groups, shape.threads)) return st;
   KvKeepArgs a{};
   a.plan = plan_id(kv);
   a.g = kv->g;

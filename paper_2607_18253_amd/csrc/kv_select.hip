@@ -413,22 +413,17 @@ __global__ __launch_bounds__(kCut) void k_kv_select_write(KvSelectArgs A) {
 
 }  // namespace
 
-// Threads for a context: while each has a CU of its own the more the better (256 contexts of 4000 rows: 17, 11
-// and 9.6 us with 256, 512 and 1024; of 16000 153, 40 and 27), then as many as leave room for others (1024 of
-// 4000: 28, 21 and 37; of 16000 225, 63 and 103), and of many short ones fewest (4096 of 600: 24, 29 and 71).
-constexpr int kCus = 256;
-
 hipError_t launch_kv_select(const KvSelectArgs& a, hipStream_t stream) {
-  const int n = a.n_seq * a.g.hkv;
+  const int n = a.n_seq * a.g.hkv, threads = kv_select_threads(n, a.longest);
   if (a.work) {
     k_kv_select_count<0><<<a.cuts, kCut, 0, stream>>>(a);
     k_kv_select_count<1><<<a.cuts, kCut, 0, stream>>>(a);
     k_kv_select_count<2><<<a.cuts, kCut, 0, stream>>>(a);
     k_kv_select_count<3><<<a.cuts, kCut, 0, stream>>>(a);
     k_kv_select_write<<<a.cuts, kCut, 0, stream>>>(a);
-  } else if (n <= kCus || a.longest > 16384) {
+  } else if (threads == 1024) {
     k_kv_select<1024, 32><<<n, 1024, 0, stream>>>(a);
-  } else if (n <= 4 * kCus || a.longest > 2048) {
+  } else if (threads == 512) {
     k_kv_select<512, 32><<<n, 512, 0, stream>>>(a);
   } else {
     k_kv_select<256, 8><<<n, 256, 0, stream>>>(a);

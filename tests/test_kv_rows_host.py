@@ -336,6 +336,43 @@ def test_long_chunks_of_many_heads_are_refused(lib):
     x.close()
 
 
+def test_launches_of_too_many_threads_are_refused(lib):
+    """A launch has less than 2^32 threads: the last batch that fits, and one more sequence.  No call counts
+    workgroups that it does not launch."""
+    most = 1 << 20
+    x = Handle(lib, max_seqs=most, max_tokens=1, hkv=8)
+
+    def plan(n, ctx, first=1, window=0):
+        assert x.plan([1] + [0] * (n - 1), [first] + [ctx] * (n - 1), window=window) == 0
+
+    plan((1 << 18) - 1, 5)
+    assert x.keep(n_rows=4096) == 0                    # 8 heads, K and V: 16 workgroups of 1024
+    assert x.keep(n_rows=4096, weights=4096) == E_CAPACITY
+    plan(1 << 18, 5)
+    assert x.keep(n_rows=4096) == E_CAPACITY
+    assert b"1024 threads" in lib.lar_kv_error_string(x.h)
+    plan(most - 1, 5)
+    assert x.keep(n_rows=4) == 0                       # of 256
+    plan(most, 5)
+    assert x.keep(n_rows=4) == E_CAPACITY
+    assert x.select() == 0                             # 8 heads: 8 workgroups of 256
+    plan(most - 1, 5, first=2049)
+    assert x.select() == 0                             # of 512
+    plan(most, 5, first=2049)
+    assert x.select() == E_CAPACITY
+    x.close()
+    x = Handle(lib, max_seqs=most, max_tokens=1, hq=16, hkv=16)
+    plan(most - 1, 5, first=100, window=7)
+    assert x.weigh() == 0 and x.weigh(before=1 << 40) == 0
+    plan(most, 5, first=100, window=7)
+    assert x.weigh() == 0                              # in place nothing is carried over
+    assert x.weigh(before=1 << 40) == E_CAPACITY
+    assert x.select() == E_CAPACITY
+    plan(most, 5, first=100)
+    assert x.weigh(before=1 << 40) == 0                # without a window neither
+    x.close()
+
+
 @pytest.mark.parametrize("current", [0, 1])
 def test_calls_go_to_the_handles_device(lib, current):
     """A handle made on device 1 works on it whichever device is current, and leaves that one current."""
