@@ -542,7 +542,8 @@ lar_status plan(lar_kv* kv, int32_t n_seqs, const int32_t* q_len, const int32_t*
   if (trees.most) {
     int64_t q0 = 0;
     for (int s = 0; s < n_seqs; q0 += q_len[s], ++s)
-      for (int r = 0; trees.words[s] && r < q_len[s]; ++r) id.add((uint32_t)s, (uint32_t)parents[q0 + r]);
+      for (int r = std::max(0, q_len[s] - ctx_len[s]); trees.words[s] && r < q_len[s]; ++r)  // past the padding
+        id.add((uint32_t)s, (uint32_t)parents[q0 + r]);
   }
   // the copy that last left this buffer is done before it is written again
   const int b = kv->stage;

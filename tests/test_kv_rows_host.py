@@ -219,6 +219,22 @@ def test_chains_are_ordinary_batches(lib):
     x.close()
 
 
+def test_padding_rows_have_no_part_in_a_trees_plan(lib):
+    """Their parents are not looked at: a captured call may be replayed under the same trees whatever they are."""
+    x = Handle(lib)
+    lib.stub_attend_plan.restype = C.c_uint64
+    ids, words = [], []
+    for pad in ([-1, -1], [99, -7], [1, 0]):
+        assert x.plan([3, 5], [50, 3], [-1, 0, 0] + pad + [-1, 2, 2]) == 0, lib.lar_kv_error_string(x.h)
+        assert x.attend() == 0
+        ids.append(lib.stub_attend_plan())
+        words.append(x.trees(1, 3 * 2 + 5 * 2).tolist())
+    assert len(set(ids)) == 1 and words[0] == words[1] == words[2]
+    assert x.plan([3, 5], [50, 3], [-1, 0, 0, -1, -1, -1, 2, -1]) == 0 and x.attend() == 0
+    assert lib.stub_attend_plan() not in ids
+    x.close()
+
+
 def test_bad_trees_are_refused(lib):
     x = Handle(lib, max_tokens=40000, max_seqs=64)
     ok = [-1, 0, 0]
