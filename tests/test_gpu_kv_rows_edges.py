@@ -132,6 +132,53 @@ def test_weigh_far_from_the_sinks(ctx, G, q_len, place):
     assert torch.equal(new.cpu()[1], old[1] if place else torch.full_like(old[1], 9.0))
 
 
+# ------------------------------------------------------------------ kernels by the number of key blocks
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype,cache", KINDS)
+def test_weigh_of_many_key_blocks(dtype, cache, d):
+    """More than 256 blocks of keys and heads: 64 keys for a wave, no rows shared out."""
+    run_weigh([40], [9000], hq=16, hkv=8, d=d, dtype=dtype, cache=cache)
+    run_weigh([40, 33, 1, 70], [5003, 3000, 90, 1000], hq=40, hkv=8, d=d, dtype=dtype, cache=cache, place=False)
+
+
+# ------------------------------------------------------------------ selections by the number of contexts
+def lengths(at, most, n, seed):
+    """n lengths, among them those around multiples of `at`."""
+    rng = np.random.RandomState(seed)
+    near = [k * at + e for k in (1, 2, 3, most // at) for e in (-1, 0, 1) if k * at + e <= most]
+    return near + [int(c) for c in np.exp(rng.uniform(0, np.log(most), n - len(near)))]
+
+
+@pytest.mark.parametrize("budget,first,last", [(1, 0, 0), (64, 4, 16), (513, 0, 0), (1000, 4, 128)])
+def test_select_of_some_hundred_contexts(budget, first, last):
+    """512 threads for a context of up to 16384 rows."""
+    check_select(lengths(512, 16384, 100, budget), budget, first, last, hkv=3, seed=budget)
+
+
+@pytest.mark.parametrize("budget,first,last", [(1, 0, 0), (64, 4, 16), (255, 0, 255), (1000, 4, 128)])
+@pytest.mark.parametrize("most", [2048, 2049])
+def test_select_of_many_contexts(budget, first, last, most):
+    """256 threads for a context of up to 2048 rows, 512 from 2049 on."""
+    check_select(lengths(256, 2048, 359, budget) + [most], budget, first, last, hkv=3, seed=budget)
+
+
+@pytest.mark.parametrize("kind", sorted(KINDS_OF_WEIGHTS))
+@pytest.mark.parametrize("ctx,hkv", [([70000], 1), ([5000, 4097, 2500] * 30, 3), ([1500, 400, 2048, 900] * 90, 3)])
+def test_select_values_in_every_kernel(kind, ctx, hkv):
+    """A context that is cut, and those of 512 and 256 threads."""
+    for budget, first, last in ((50, 3, 20), (333, 0, 1)):
+        check_select(ctx, budget, first, last, hkv=hkv, make=KINDS_OF_WEIGHTS[kind])
+
+
+def test_select_of_more_rows_than_fit():
+    """Contexts that a workgroup reads again for every digit: more rows in all than the working memory of
+    cut ones has, and one of more stretches than are cut."""
+    make = lambda r, s: r.randint(0, 300, s).astype(np.float32)  # noqa: E731
+    check_select([40000] * 110, 777, 4, 60, hkv=2, make=make, S=64)
+    for kind in ("not finite", "neighbours"):
+        check_select([(1 << 20) + 4097], 90000, 4, 60, hkv=1, make=KINDS_OF_WEIGHTS[kind], S=64)
+
+
 # ------------------------------------------------------------------ lists that go on behind their end
 @pytest.mark.parametrize("end", [32, 64, 128, 256, 512, 1024, 2048])
 @pytest.mark.parametrize("weights", [True, False])
