@@ -619,7 +619,8 @@ typedef struct {
  *   Clears a sticky error that was reported.  Not under stream capture.  A captured call
  *   belongs to the handle and to the plan it was captured with: replayed, in the order of
  *   the handle's stream, while another plan is the current one it does nothing and sets the
- *   sticky LAR_E_STATE.  (A plan of the same lengths, window and sinks is the same plan.)
+ *   sticky LAR_E_STATE.  (A plan of the same lengths, window, sinks and trees is the same
+ *   plan.)
  * lar_kv_append: k, v rows [T][n_kv_heads][head_dim] into the pages.
  * lar_kv_read: the rows of the batch's tokens from the pages into k, v, of which no two may
  *   share memory.  A plan with q_len == ctx_len reads whole contexts (swap-out of a

@@ -30,9 +30,10 @@ lar_status check_table(lar_kv* kv, const int32_t* table, int32_t cols, int64_t n
 }
 
 // Workgroups that share the rows of a block of keys, where there are few blocks: two for a CU in all, 2
-// blocks of 32 rows at least for each, sums within narrow_o; where that leaves out enough blocks for the time
-// of the sums' launch, 4 us (2048 tokens alone, of 32 heads of 128: 42 us, 162 with one workgroup for a block of keys;
-// of 4 heads of 64 13 and 158; 100 tokens of 32 heads 11 and 15; 33 of them 11 and 9.4).
+// blocks of 32 rows of the longest chunk at least for each (of which a window's keys see fewer), sums within
+// narrow_o; where that leaves out enough blocks for the time of the sums' launch, 4 us (2048 tokens alone, of 32
+// heads of 128: 42 us, 162 with one workgroup for a block of keys; of 4 heads of 64 13 and 158; 100 tokens
+// of 32 heads 11 and 15; 33 of them 11 and 9.4).
 constexpr int kWeighGroups = 512, kWeighSplits = 32, kWeighLeast = 2, kWeighSaved = 8;
 int32_t weigh_splits(const lar_kv* kv) {
   const int64_t groups = std::max<int64_t>(1, kv->blocks * kv->g.hkv), rows = (int64_t)kv->most_new * kv->g.G / 32;

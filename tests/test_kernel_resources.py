@@ -70,6 +70,20 @@ def test_limits_queues_stay_in_registers(kernels):
         assert k[".private_segment_fixed_size"] <= spilled + 16, n
 
 
+def test_paged_cache_kernels_spill_no_vector_registers(kernels):
+    """Those of attention hold up to 253 of 256: a spill costs them more than anything it makes room for."""
+    names = [n for n in kernels if "k_kv_" in n]
+    assert len(names) >= 90
+    for n in names:
+        assert kernels[n][".vgpr_spill_count"] == 0 and kernels[n].get(".agpr_count", 0) == 0, n
+
+
+def test_moves_share_a_cu(kernels):
+    """Two workgroups of 1024 threads, eight waves for a SIMD of 512 registers per lane."""
+    names = [n for n in kernels if "9k_kv_keepILi1024E" in n]
+    assert len(names) == 1 and kernels[names[0]][".vgpr_count"] <= 64
+
+
 @pytest.mark.parametrize("slots,per_cu", [(1, 4), (2, 4), (4, 3), (8, 2)])
 def test_limits_traces_share_a_cu(kernels, slots, per_cu):
     """4-wave workgroups of the clustered trace under limits that one CU holds: a SIMD has
