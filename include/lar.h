@@ -627,7 +627,8 @@ typedef struct {
  *   preempted sequence).
  * lar_kv_attend: q rows [T][n_q_heads][head_dim]; out dev [T][n_q_heads][head_dim]
  *   contiguous; lse dev [T][n_q_heads] float32 or NULL; scale > 0.  The batch's own K and V
- *   must have been appended.
+ *   must have been appended.  Under a window no page is looked at but those of keys that some
+ *   token sees and of the 64 positions (from a multiple of 64 on) around each.
  * lar_kv_plan_tree: lar_kv_plan with host parents [T], copied: of each new token the number
  *   of its parent among its sequence's new tokens, or -1; a parent comes before its children
  *   and is no padding row (whose own parents are not looked at).  A tree, that is a sequence whose

@@ -11,11 +11,13 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
+import kv_ref as R  # noqa: E402
 from gpu_util import DEV  # noqa: E402
 from paper_2607_18253_amd import PagedKV  # noqa: E402
 from paper_2607_18253_amd import lar as L  # noqa: E402
 from test_gpu_kv import BF, E4, F16, Batch, refused  # noqa: E402
 from test_gpu_kv_rows import KINDS, KINDS_OF_WEIGHTS, Cache, check_select, run_weigh, weigh_ref  # noqa: E402
+from test_kv_rows_host import tree  # noqa: E402
 
 
 # ------------------------------------------------------------------ pages that a window hides
@@ -196,3 +198,49 @@ def test_entries_behind_a_lists_end_are_reported(end, weights, cache):
         rows[1, 1, n - 1] = 2500
         x.kv.keep(x.pages, x.tab.to(DEV), torch.from_numpy(rows).to(DEV), weights=x.w if weights else None)
         refused(L.LAR_E_STATE, x.kv.sync)
+
+
+# ------------------------------------------------------------------ trees at the limit
+@pytest.mark.parametrize("ctx", [(1 << 29) + 77, 1 << 30])
+@pytest.mark.parametrize("G,q_len", [(64, 40), (8, 4), (4, 300)])
+def test_trees_far_from_the_sinks(ctx, G, q_len):
+    """The longest contexts under a window, of which only the pages of sinks and window are there."""
+    window, sinks, S, d = 300, 5, 65536, 64
+    cols, low = -(-ctx // S), ctx - q_len - window + 1
+    kv = PagedKV(G, 1, d, block_size=S, dtype=BF, max_seqs=1, max_tokens=1000)
+    pages = kv.new_pages(4)
+    tab = torch.full((1, cols), -1, dtype=torch.int32)
+    tab[0, 0], tab[0, low // S], tab[0, cols - 1] = 2, 0, 0 if low // S == cols - 1 else 3
+    for t in pages.tensors():
+        t.zero_()
+    g = torch.Generator().manual_seed(G)
+    # keys from the first page of attention's tile of 64 with the window's start on
+    start = low // 64 * 64
+    rows = []
+    for n, end in ((sinks, sinks), (ctx - start, ctx)):
+        kv.plan([n], [end])
+        k, v = (torch.randn((n, 1, d), generator=g).to(BF) for _ in range(2))
+        kv.append(pages, k.to(DEV), v.to(DEV), tab.to(DEV))
+        rows.append((k, v))
+    k, v = (torch.cat([r[i] for r in rows]).double() for i in range(2))
+    at = torch.cat([torch.arange(sinks), torch.arange(start, ctx)])
+    par = tree(q_len, np.random.RandomState(G))
+    places, line = [], []
+    for i, a in enumerate(par):
+        places.append(ctx - q_len + (0 if a < 0 else places[a] - (ctx - q_len) + 1))
+        line.append(([] if a < 0 else line[a]) + [i])
+    mask = torch.zeros((q_len, len(at)), dtype=torch.bool)
+    for i in range(q_len):
+        where = torch.where(at < ctx - q_len, at, -1)
+        for x in line[i]:
+            where[len(at) - q_len + x] = places[x]
+        mask[i] = (where >= 0) & ((where > places[i] - window) | (where < sinks))
+    q = (2.0 * torch.randn((q_len, G, d), generator=g)).to(BF)
+    kv.plan([q_len], [ctx], window=window, sinks=sinks, parents=par)
+    lse = torch.empty((q_len, G), dtype=torch.float32, device=DEV)
+    out = kv.attend(pages, q.to(DEV), tab.to(DEV), lse=lse)
+    kv.sync()
+    want, wz, mag, big = R.attend_fast(q.double(), k, v, mask, d ** -0.5)
+    bo, bz = R.bounds(BF, mag, big, wz, d, len(at), float(v.abs().max()))
+    Batch.near(out.cpu().double(), want, bo, ctx)
+    Batch.near(lse.cpu().double(), wz, bz, (ctx, "lse"))
